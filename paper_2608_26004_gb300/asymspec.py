@@ -46,7 +46,7 @@ DIV_NONE = 1
 DIV_KL = 2
 DIV_LAMBDA = 3
 
-# Every function include/asymspec.h declares.
+# Every function that the headers in include/ declare (asymspec_serving.h: serving.py).
 EXPORTED = (
     "asymspec_default_gate_params",
     "asymspec_workspace_bytes",
@@ -65,6 +65,11 @@ EXPORTED = (
     "asymspec_status_string",
     "asymspec_last_cuda_error",
     "asymspec_version",
+    "asymspec_constrain_logits",
+    "asymspec_cache_plan",
+    "asymspec_cache_write",
+    "asymspec_cache_attend_workspace_bytes",
+    "asymspec_cache_attend",
 )
 
 

@@ -1,7 +1,7 @@
 """Builds the native libraries in place (no cmake, no setuptools).
 
-* ``libasymspec.so``: the sm_103a kernels and the C ABI of include/asymspec.h,
-  compiled with nvcc for ``-gencode arch=compute_103a,code=sm_103a`` only.
+* ``libasymspec.so``: the sm_103a kernels and the C ABI of include/asymspec.h and
+  include/asymspec_serving.h, compiled with nvcc for ``-gencode arch=compute_103a,code=sm_103a`` only.
 * ``libasymspec_synth.so``: the host input generator (plain C, gcc).
 """
 from __future__ import annotations
@@ -20,10 +20,11 @@ CUDA_SRC = [os.path.join(CSRC, f) for f in (
     "asymspec.cu", "k_generic.cu", "k_tma_bf16.cu", "k_tma_f32.cu", "k_tma_bf16_prod.cu",
     "k_tma_f32_prod.cu", "k_tma_bf16_any_s.cu", "k_tma_f32_any_s.cu", "k_row_bf16.cu",
     "k_row_f32.cu", "k_full_bf16.cu", "k_full_f32.cu", "k_xrow_bf16.cu",
-    "k_xrow_f32.cu", "k_draft.cu", "k_xvocab.cu")]
+    "k_xrow_f32.cu", "k_draft.cu", "k_xvocab.cu", "serving.cu")]
 CUDA_HEADERS = [os.path.join(CSRC, f) for f in (
     "device_common.cuh", "kernel_generic.cuh", "kernel_tma.cuh", "kernel_row.cuh",
-    "kernel_full.cuh", "kernel_xrow.cuh", "kernel_draft.cuh", "kernel_xvocab.cuh", "kernels.h")]
+    "kernel_full.cuh", "kernel_xrow.cuh", "kernel_draft.cuh", "kernel_xvocab.cuh", "kernel_constrain.cuh",
+    "kernel_cache.cuh", "kernel_attend.cuh", "kernels.h", "host_common.h")]
 CUDA_LIB = os.path.join(HERE, "libasymspec.so")
 GENCODE = "arch=compute_103a,code=sm_103a"
 
@@ -39,7 +40,8 @@ def _stale(target: str, sources) -> bool:
     if not os.path.exists(target):
         return True
     t = os.path.getmtime(target)
-    deps = list(sources) + CUDA_HEADERS + [os.path.join(INCLUDE, "asymspec.h")]
+    deps = list(sources) + CUDA_HEADERS + [os.path.join(INCLUDE, f) for f in
+                                           ("asymspec.h", "asymspec_serving.h")]
     return any(os.path.getmtime(s) > t for s in deps)
 
 

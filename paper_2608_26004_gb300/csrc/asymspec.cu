@@ -35,17 +35,20 @@
 #include "kernel_xvocab.cuh"
 #include "kernel_xrow.cuh"
 #include "kernels.h"
+#include "host_common.h"
+
+namespace {
+thread_local int g_last_cuda_error = 0;
+}  // namespace
+
+int asymspec_impl::cuda_fail(cudaError_t e) {
+  g_last_cuda_error = static_cast<int>(e);
+  return ASYMSPEC_ERR_CUDA;
+}
 
 namespace {
 
 using namespace asymspec_impl;
-
-thread_local int g_last_cuda_error = 0;
-
-int cuda_fail(cudaError_t e) {
-  g_last_cuda_error = static_cast<int>(e);
-  return ASYMSPEC_ERR_CUDA;
-}
 
 constexpr int kTmaPreferredSmem = 113 * 1024;  // two CTAs per SM
 

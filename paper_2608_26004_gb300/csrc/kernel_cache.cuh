@@ -1,0 +1,209 @@
+// The paged key-value cache: block tables and slot maps (asymspec_cache_plan), and the
+// writing of new keys and values (asymspec_cache_write).
+#pragma once
+
+#include "asymspec_serving.h"
+#include "device_common.cuh"
+
+namespace asymspec_impl {
+
+struct PlanParams {
+  const int32_t *lens, *accepted, *grow, *held, *free_count;
+  int grow_all, B, block_size, num_blocks, table_width;
+  int32_t *tables, *free_list;
+  int64_t table_ld;
+  int32_t *out_start, *out_len, *out_held, *out_free, *out_offsets, *out_positions;
+  int64_t* out_slots;
+  int64_t capacity;
+  uint32_t* err;
+};
+
+constexpr int kPThreads = 1024;
+
+// Shared memory of the plan kernel: a request's tokens that stay, its blocks before (bit 31:
+// not served) and the prefix sums of tokens, blocks taken and blocks given back.
+constexpr size_t plan_smem_bytes(int B) {
+  return static_cast<size_t>(B + 1) * (8 + 4 * 4);
+}
+
+// Largest i in [0, n) with first(i) <= x, for first(0) <= x, ascending.
+template <typename A>
+__device__ __forceinline__ int find_last(const A* first, int n, A x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Inclusive prefix sums over the CTA of three numbers a thread.
+__device__ __forceinline__ void scan3(int64_t& a, int& b, int& c, int64_t* wa, int* wb, int* wc) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t a2 = __shfl_up_sync(~0u, a, d);
+    const int b2 = __shfl_up_sync(~0u, b, d), c2 = __shfl_up_sync(~0u, c, d);
+    if (lane >= d) a += a2, b += b2, c += c2;
+  }
+  if (lane == 31) wa[warp] = a, wb[warp] = b, wc[warp] = c;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) a += wa[w], b += wb[w], c += wc[w];
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams p) {
+  extern __shared__ int64_t p_smem[];
+  __shared__ int64_t wa[32];
+  __shared__ int wb[32], wc[32];
+  __shared__ int s_taken;
+  const int B = p.B, bs = p.block_size, tid = threadIdx.x;
+  int64_t* offs = p_smem;  // [B + 1]
+  int* keep_of = reinterpret_cast<int*>(offs + B + 1);
+  int* held_of = keep_of + B + 1;
+  int* more_of = held_of + B + 1;  // blocks taken by the requests before
+  int* less_of = more_of + B + 1;  // blocks given back by the requests before
+  unsigned err = 0;
+  const int free0 = *p.free_count, free_in = min(max(free0, 0), p.num_blocks);
+  if (free_in != free0) err |= ASYMSPEC_DATA_BAD_LENGTH;
+  if (tid == 0) s_taken = 0;
+  int64_t off = 0;
+  int more_sum = 0, less_sum = 0;
+  const int64_t most = static_cast<int64_t>(p.table_width) * bs;
+  for (int b0 = 0; b0 < B; b0 += kPThreads) {
+    const int b = b0 + tid;
+    int64_t g = 0;
+    int more = 0, less = 0, keep = 0, held = 0;
+    if (b < B) {
+      const int l0 = p.lens[b], a0 = p.accepted ? p.accepted[b] : -1;
+      const int g0 = p.grow ? p.grow[b] : p.grow_all, h0 = p.held[b];
+      int64_t k = static_cast<int64_t>(max(l0, 0)) + max(a0, -1) + 1;
+      g = max(g0, 0);
+      held = min(max(h0, 0), p.table_width);
+      bool bad = l0 < 0 || a0 < -1 || g0 < 0 || held != h0;
+      bool served = true;
+      if (k > most) k = most, bad = true;
+      keep = static_cast<int>(k);
+      int64_t blocks = (k + g + bs - 1) / bs;
+      if (k + g > most) {  // too long for its table: what it has stays
+        bad = true;
+        served = false;
+        blocks = held;
+      }
+      if (bad) err |= ASYMSPEC_DATA_BAD_LENGTH;
+      more = static_cast<int>(max(blocks - held, static_cast<int64_t>(0)));
+      less = static_cast<int>(max(held - blocks, static_cast<int64_t>(0)));
+      keep_of[b] = keep;
+      held_of[b] = served ? held : held | INT_MIN;
+    }
+    const int64_t g1 = g;
+    const int m1 = more, l1 = less;
+    scan3(g, more, less, wa, wb, wc);
+    if (b < B) {
+      offs[b] = off + g - g1;
+      more_of[b] = more_sum + more - m1;
+      less_of[b] = less_sum + less - l1;
+    }
+    if (tid == kPThreads - 1) wa[0] = g, wb[0] = more, wc[0] = less;
+    __syncthreads();
+    off += wa[0];
+    more_sum += wb[0];
+    less_sum += wc[0];
+    __syncthreads();
+  }
+  if (tid == 0) offs[B] = off, more_of[B] = more_sum, less_of[B] = less_sum;
+  __syncthreads();
+  const int top = free_in + less_sum;
+  // who is served; the state of the next call
+  for (int b = tid; b < B; b += kPThreads) {
+    const int m = more_of[b + 1] - more_of[b], l = less_of[b + 1] - less_of[b];
+    const int held = held_of[b] & INT_MAX;
+    bool served = held_of[b] >= 0;
+    if (m > 0 && more_of[b + 1] > top) {
+      served = false;
+      err |= ASYMSPEC_DATA_NO_BLOCKS;
+    } else if (m > 0) {
+      atomicMax(&s_taken, more_of[b + 1]);
+    }
+    if (!served) held_of[b] = held | INT_MIN;
+    const int64_t g = offs[b + 1] - offs[b];
+    p.out_start[b] = keep_of[b];
+    p.out_len[b] = served ? keep_of[b] + static_cast<int>(g) : keep_of[b];
+    p.out_held[b] = held - l + (served ? m : 0);
+  }
+  if (off > p.capacity) err |= ASYMSPEC_DATA_BAD_LENGTH;
+  for (int b = tid; b <= B; b += kPThreads)
+    p.out_offsets[b] = static_cast<int>(min(offs[b], static_cast<int64_t>(INT_MAX)));
+  // blocks given back go on the stack
+  for (int i = tid; i < less_sum; i += kPThreads) {
+    const int b = find_last(less_of, B, i);
+    const int kept = (held_of[b] & INT_MAX) - (less_of[b + 1] - less_of[b]);
+    const int at = free_in + i;
+    if (at < p.num_blocks) p.free_list[at] = p.tables[b * p.table_ld + kept + i - less_of[b]];
+    else err |= ASYMSPEC_DATA_BAD_LENGTH;
+  }
+  __syncthreads();
+  // and blocks are taken off it
+  const int taken = s_taken;
+  for (int i = tid; i < taken; i += kPThreads) {
+    const int b = find_last(more_of, B, i);
+    const int at = top - 1 - i;
+    p.tables[b * p.table_ld + (held_of[b] & INT_MAX) + i - more_of[b]] =
+        at < p.num_blocks ? p.free_list[at] : -1;
+  }
+  if (tid == 0) *p.out_free = min(top - taken, p.num_blocks);
+  __syncthreads();
+  for (int64_t t = tid; t < p.capacity; t += kPThreads) {
+    int64_t slot = -1;
+    int pos = -1;
+    if (t < off) {
+      const int b = find_last(offs, B, t);
+      if (held_of[b] >= 0) {
+        pos = keep_of[b] + static_cast<int>(t - offs[b]);
+        const int page = p.tables[b * p.table_ld + pos / bs];
+        if (static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks))
+          slot = static_cast<int64_t>(page) * bs + pos % bs;
+        else err |= ASYMSPEC_DATA_BAD_INDEX;
+      }
+    }
+    p.out_slots[t] = slot;
+    if (p.out_positions) p.out_positions[t] = pos;
+  }
+  if (err && p.err) atomicOr(p.err, err);
+}
+
+struct WriteParams {
+  const void *k, *v;
+  void *keys, *values;
+  int64_t ks[2], vs[2], cks[3], cvs[3];
+  const int64_t* slots;
+  int T, num_blocks, block_size, kv_heads, head_dim;
+  uint32_t* err;
+};
+
+// U: what is moved at once (16 bytes, or one element where something is not on the
+// 16-byte boundaries); strides and head_dim in elements of U.
+template <typename U>
+__global__ void __launch_bounds__(256) cache_write_kernel(const WriteParams p) {
+  const int per = p.kv_heads * p.head_dim;
+  const int64_t n = static_cast<int64_t>(p.T) * per;
+  for (int64_t i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
+    const int t = static_cast<int>(i / per), e = static_cast<int>(i % per);
+    const int h = e / p.head_dim, d = e % p.head_dim;
+    const int64_t slot = p.slots[t];
+    if (slot < 0) continue;
+    const int64_t block = slot / p.block_size;
+    const int at = static_cast<int>(slot % p.block_size);
+    if (block >= p.num_blocks) {
+      if (p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
+      continue;
+    }
+    static_cast<U*>(p.keys)[block * p.cks[0] + at * p.cks[1] + h * p.cks[2] + d] =
+        static_cast<const U*>(p.k)[t * p.ks[0] + h * p.ks[1] + d];
+    static_cast<U*>(p.values)[block * p.cvs[0] + at * p.cvs[1] + h * p.cvs[2] + d] =
+        static_cast<const U*>(p.v)[t * p.vs[0] + h * p.vs[1] + d];
+  }
+}
+
+}  // namespace asymspec_impl

@@ -1,0 +1,249 @@
+// Host side of the C ABI declared in include/asymspec_serving.h: argument checks and
+// launches of the operators around the verification step.
+//
+//   constrain_kernel    (kernel_constrain.cuh) penalties, biases and masks on logits
+//   cache_plan_kernel   (kernel_cache.cuh) block tables and slot maps
+//   cache_write_kernel  (kernel_cache.cuh) new keys and values into the cache
+//   attend_kernel       (kernel_attend.cuh) attention over the cache
+#include <algorithm>
+#include <cmath>
+
+#include "host_common.h"
+#include "kernel_attend.cuh"
+#include "kernel_cache.cuh"
+#include "kernel_constrain.cuh"
+
+namespace {
+
+using namespace asymspec_impl;
+
+constexpr int64_t kMax32 = INT32_MAX;
+
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+int elt_size(int dtype) { return dtype == ASYMSPEC_FP32 ? 4 : 2; }
+
+bool known_dtype(int dtype) { return dtype == ASYMSPEC_FP32 || dtype == ASYMSPEC_BF16; }
+
+int launch(const void* fn, dim3 grid, dim3 block, size_t smem, void* params, void* stream) {
+  cudaError_t e = cudaSuccess;
+  if (smem > 47 * 1024)
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return cuda_fail(e);
+  void* args[] = {params};
+  e = cudaLaunchKernel(fn, grid, block, args, smem, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
+}
+
+int check_constraints(const asymspec_constraints& c, int B, int P, int V) {
+  if (c.history && (!c.history_len || c.history_ld < 0 || c.history_width < 0))
+    return ASYMSPEC_ERR_INVALID_ARG;
+  if (!c.history && (c.history_len || c.prompt_len)) return ASYMSPEC_ERR_INVALID_ARG;
+  if (c.drafts && c.drafts_ld < 0) return ASYMSPEC_ERR_INVALID_ARG;
+  if (c.bias_offsets && (c.bias_count < 0 || (c.bias_count > 0 && (!c.bias_tokens || !c.bias_values))))
+    return ASYMSPEC_ERR_INVALID_ARG;
+  if (!c.bias_offsets && (c.bias_tokens || c.bias_values)) return ASYMSPEC_ERR_INVALID_ARG;
+  if (c.mask) {
+    if (c.mask_count < 0 || c.mask_ld * 32 < V || !(std::fabs(c.mask_value) <= FLT_MAX))
+      return ASYMSPEC_ERR_INVALID_ARG;
+    if (!c.mask_rows && c.mask_count < static_cast<int64_t>(B) * P) return ASYMSPEC_ERR_INVALID_ARG;
+  } else if (c.mask_rows) {
+    return ASYMSPEC_ERR_INVALID_ARG;
+  }
+  for (const void* q : {static_cast<const void*>(c.history), static_cast<const void*>(c.history_len),
+                        static_cast<const void*>(c.prompt_len), static_cast<const void*>(c.drafts),
+                        static_cast<const void*>(c.repetition), static_cast<const void*>(c.frequency),
+                        static_cast<const void*>(c.presence), static_cast<const void*>(c.bias_offsets),
+                        static_cast<const void*>(c.bias_tokens), static_cast<const void*>(c.bias_values),
+                        static_cast<const void*>(c.mask), static_cast<const void*>(c.mask_rows)})
+    if (!aligned(q, 4)) return ASYMSPEC_ERR_MISALIGNED;
+  return ASYMSPEC_OK;
+}
+
+int check_cache(const asymspec_cache* c) {
+  if (!c || !c->keys || !c->values) return ASYMSPEC_ERR_INVALID_ARG;
+  if (!known_dtype(c->dtype)) return ASYMSPEC_ERR_UNSUPPORTED;
+  if (c->num_blocks < 1 || c->block_size < 1 || c->kv_heads < 1 || c->head_dim < 1)
+    return ASYMSPEC_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (c->key_strides[i] < 0 || c->value_strides[i] < 0) return ASYMSPEC_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(c->num_blocks) * c->block_size > kMax32 ||
+      static_cast<int64_t>(c->kv_heads) * c->head_dim > kMax32)
+    return ASYMSPEC_ERR_TOO_LARGE;
+  const int elt = elt_size(c->dtype);
+  if (!aligned(c->keys, elt) || !aligned(c->values, elt)) return ASYMSPEC_ERR_MISALIGNED;
+  return ASYMSPEC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits, int64_t ld,
+                              void* out, int64_t out_ld, int B, int P, int V, int dtype,
+                              uint32_t* out_error_word, void* stream) {
+  if (!known_dtype(dtype)) return ASYMSPEC_ERR_UNSUPPORTED;
+  if (!c || B < 0 || P < 0 || V < 2 || ld < V || out_ld < V) return ASYMSPEC_ERR_INVALID_ARG;
+  if (P > ASYMSPEC_CONSTRAIN_MAX_P || B > 65535 || V > (1 << 30)) return ASYMSPEC_ERR_TOO_LARGE;
+  const int st = check_constraints(*c, B, P, V);
+  if (st != ASYMSPEC_OK) return st;
+  if (B == 0 || P == 0) return ASYMSPEC_OK;
+  if (!logits || !out || (logits == out && ld != out_ld)) return ASYMSPEC_ERR_INVALID_ARG;
+  const int elt = elt_size(dtype);
+  if (!aligned(logits, elt) || !aligned(out, elt) || !aligned(out_error_word, 4))
+    return ASYMSPEC_ERR_MISALIGNED;
+  CParams p = {*c, logits, out, ld, out_ld, B, P, V, out_error_word};
+  const void* fn = dtype == ASYMSPEC_FP32
+                       ? reinterpret_cast<const void*>(&constrain_kernel<float>)
+                       : reinterpret_cast<const void*>(&constrain_kernel<__nv_bfloat16>);
+  const size_t smem = kCSlice * 4 * (c->bias_offsets ? 2 : 1);
+  return launch(fn, dim3((V + kCSlice - 1) / kCSlice, B), dim3(kCThreads), smem, &p, stream);
+}
+
+int asymspec_cache_plan(const int32_t* lens, const int32_t* accepted, const int32_t* grow,
+                        int grow_all, int B, int block_size, int num_blocks,
+                        int32_t* block_tables, int64_t table_ld, int table_width,
+                        const int32_t* held, int32_t* free_list, const int32_t* free_count,
+                        int32_t* out_start, int32_t* out_len, int32_t* out_held,
+                        int32_t* out_free_count, int32_t* out_offsets, int64_t* out_slots,
+                        int32_t* out_positions, int64_t capacity, uint32_t* out_error_word,
+                        void* stream) {
+  if (B < 0 || block_size < 1 || num_blocks < 1 || table_width < 1 || table_ld < table_width ||
+      capacity < 0 || (!grow && grow_all < 0))
+    return ASYMSPEC_ERR_INVALID_ARG;
+  if (B > ASYMSPEC_CACHE_MAX_B || static_cast<int64_t>(B) * table_width > kMax32 ||
+      static_cast<int64_t>(num_blocks) * block_size > kMax32 ||
+      static_cast<int64_t>(table_width) * block_size > kMax32 || capacity > kMax32)
+    return ASYMSPEC_ERR_TOO_LARGE;
+  if (!free_list || !free_count || !out_free_count || !out_offsets || (capacity > 0 && !out_slots) ||
+      (B > 0 && (!lens || !held || !block_tables || !out_start || !out_len || !out_held)))
+    return ASYMSPEC_ERR_INVALID_ARG;
+  for (const void* q : {static_cast<const void*>(lens), static_cast<const void*>(accepted),
+                        static_cast<const void*>(grow), static_cast<const void*>(block_tables),
+                        static_cast<const void*>(held), static_cast<const void*>(free_list),
+                        static_cast<const void*>(free_count), static_cast<const void*>(out_start),
+                        static_cast<const void*>(out_len), static_cast<const void*>(out_held),
+                        static_cast<const void*>(out_free_count), static_cast<const void*>(out_offsets),
+                        static_cast<const void*>(out_positions), static_cast<const void*>(out_error_word)})
+    if (!aligned(q, 4)) return ASYMSPEC_ERR_MISALIGNED;
+  if (!aligned(out_slots, 8)) return ASYMSPEC_ERR_MISALIGNED;
+  PlanParams p = {lens, accepted, grow, held, free_count, grow_all, B, block_size, num_blocks,
+                  table_width, block_tables, free_list, table_ld, out_start, out_len, out_held,
+                  out_free_count, out_offsets, out_positions, out_slots, capacity, out_error_word};
+  return launch(reinterpret_cast<const void*>(&cache_plan_kernel), dim3(1), dim3(kPThreads),
+                plan_smem_bytes(B), &p, stream);
+}
+
+int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void* v,
+                         const int64_t* k_strides, const int64_t* v_strides, const int64_t* slots,
+                         int T, uint32_t* out_error_word, void* stream) {
+  const int st = check_cache(cache);
+  if (st != ASYMSPEC_OK) return st;
+  if (T < 0 || !k_strides || !v_strides) return ASYMSPEC_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i)
+    if (k_strides[i] < 0 || v_strides[i] < 0) return ASYMSPEC_ERR_INVALID_ARG;
+  if (T == 0) return ASYMSPEC_OK;
+  if (!k || !v || !slots) return ASYMSPEC_ERR_INVALID_ARG;
+  const int elt = elt_size(cache->dtype);
+  if (!aligned(k, elt) || !aligned(v, elt) || !aligned(slots, 8) || !aligned(out_error_word, 4))
+    return ASYMSPEC_ERR_MISALIGNED;
+  const int per = 16 / elt;
+  bool wide = aligned(k, 16) && aligned(v, 16) && aligned(cache->keys, 16) &&
+              aligned(cache->values, 16) && cache->head_dim % per == 0;
+  for (int i = 0; i < 3; ++i)
+    wide = wide && cache->key_strides[i] % per == 0 && cache->value_strides[i] % per == 0;
+  for (int i = 0; i < 2; ++i) wide = wide && k_strides[i] % per == 0 && v_strides[i] % per == 0;
+  const int u = wide ? per : 1;
+  WriteParams p = {};
+  p.k = k;
+  p.v = v;
+  p.keys = cache->keys;
+  p.values = cache->values;
+  for (int i = 0; i < 2; ++i) p.ks[i] = k_strides[i] / u, p.vs[i] = v_strides[i] / u;
+  for (int i = 0; i < 3; ++i)
+    p.cks[i] = cache->key_strides[i] / u, p.cvs[i] = cache->value_strides[i] / u;
+  p.slots = slots;
+  p.T = T;
+  p.num_blocks = cache->num_blocks;
+  p.block_size = cache->block_size;
+  p.kv_heads = cache->kv_heads;
+  p.head_dim = cache->head_dim / u;
+  p.err = out_error_word;
+  const int64_t n = static_cast<int64_t>(T) * p.kv_heads * p.head_dim;
+  const void* fn = wide ? reinterpret_cast<const void*>(&cache_write_kernel<uint4>)
+                   : elt == 4 ? reinterpret_cast<const void*>(&cache_write_kernel<uint32_t>)
+                              : reinterpret_cast<const void*>(&cache_write_kernel<uint16_t>);
+  return launch(fn, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 8 * 152))), dim3(256),
+                0, &p, stream);
+}
+
+size_t asymspec_cache_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim) {
+  if (B < 1 || Q < 1 || heads < 1 || kv_heads < 1 || head_dim < 1 || heads % kv_heads != 0 ||
+      head_dim > ASYMSPEC_CACHE_MAX_D || B > ASYMSPEC_CACHE_MAX_B ||
+      static_cast<int64_t>(Q) * heads > (1 << 20))
+    return 0;
+  return 256;
+}
+
+int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int64_t* q_strides,
+                          int B, int Q, int heads, const int32_t* block_tables, int64_t table_ld,
+                          int table_width, const int32_t* lens, float scale, int window, void* out,
+                          const int64_t* out_strides, float* out_lse, void* workspace,
+                          size_t workspace_bytes, uint32_t* out_error_word, void* stream) {
+  const int st = check_cache(cache);
+  if (st != ASYMSPEC_OK) return st;
+  if (cache->head_dim > ASYMSPEC_CACHE_MAX_D) return ASYMSPEC_ERR_UNSUPPORTED;
+  if (B < 0 || Q < 0 || heads < 1 || heads % cache->kv_heads != 0 || table_width < 1 ||
+      table_ld < table_width || !(std::fabs(scale) <= FLT_MAX) || window < 0 || !q_strides || !out_strides)
+    return ASYMSPEC_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (q_strides[i] < 0 || out_strides[i] < 0) return ASYMSPEC_ERR_INVALID_ARG;
+  if (B > ASYMSPEC_CACHE_MAX_B || static_cast<int64_t>(Q) * heads > (1 << 20) ||
+      static_cast<int64_t>(table_width) * cache->block_size > kMax32)
+    return ASYMSPEC_ERR_TOO_LARGE;
+  if (B == 0 || Q == 0) return ASYMSPEC_OK;
+  if (!q || !block_tables || !lens || !out) return ASYMSPEC_ERR_INVALID_ARG;
+  const int elt = elt_size(cache->dtype), per = 16 / elt;
+  if (!aligned(q, elt) || !aligned(out, elt) || !aligned(block_tables, 4) || !aligned(lens, 4) ||
+      !aligned(out_lse, 4) || !aligned(out_error_word, 4) || !aligned(cache->keys, 16) ||
+      !aligned(cache->values, 16) || cache->head_dim % per != 0)
+    return ASYMSPEC_ERR_MISALIGNED;
+  for (int i = 0; i < 3; ++i)
+    if (cache->key_strides[i] % per != 0 || cache->value_strides[i] % per != 0)
+      return ASYMSPEC_ERR_MISALIGNED;
+  const size_t need =
+      asymspec_cache_attend_workspace_bytes(B, Q, heads, cache->kv_heads, cache->head_dim);
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return ASYMSPEC_ERR_WORKSPACE;
+  AttendParams p = {};
+  p.keys = cache->keys;
+  p.values = cache->values;
+  p.q = q;
+  p.out = out;
+  p.lse = out_lse;
+  for (int i = 0; i < 3; ++i) {
+    p.cks[i] = cache->key_strides[i];
+    p.cvs[i] = cache->value_strides[i];
+    p.qs[i] = q_strides[i];
+    p.os[i] = out_strides[i];
+  }
+  p.tables = block_tables;
+  p.lens = lens;
+  p.table_ld = table_ld;
+  p.B = B;
+  p.Q = Q;
+  p.heads = heads;
+  p.kv_heads = cache->kv_heads;
+  p.D = cache->head_dim;
+  p.num_blocks = cache->num_blocks;
+  p.block_size = cache->block_size;
+  p.table_width = table_width;
+  p.window = window;
+  p.scale = scale;
+  p.err = out_error_word;
+  const void* fn = cache->dtype == ASYMSPEC_FP32
+                       ? reinterpret_cast<const void*>(&attend_kernel<float>)
+                       : reinterpret_cast<const void*>(&attend_kernel<__nv_bfloat16>);
+  return launch(fn, dim3(heads, Q, B), dim3(kAThreads), 0, &p, stream);
+}
+
+}  // extern "C"
