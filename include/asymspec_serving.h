@@ -207,8 +207,8 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
  * ASYMSPEC_ERR_UNSUPPORTED: dtype, head_dim > ASYMSPEC_CACHE_MAX_D.  ASYMSPEC_ERR_MISALIGNED:
  * an unaligned pointer; keys, values, their strides and head_dim must lie on 16-byte
  * boundaries.  ASYMSPEC_ERR_WORKSPACE.  ASYMSPEC_ERR_TOO_LARGE: B >
- * ASYMSPEC_CACHE_MAX_B, Q * heads > 2^20, num_blocks * block_size or table_width *
- * block_size beyond 2^31 - 1. */
+ * ASYMSPEC_CACHE_MAX_B, Q * heads > 2^20, num_blocks * block_size beyond 2^31 - 1 or
+ * table_width * block_size beyond 2^30. */
 #define ASYMSPEC_CACHE_MAX_D 256
 size_t asymspec_cache_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim);
 int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int64_t* q_strides,

@@ -16,76 +16,716 @@ struct AttendParams {
   const int32_t *tables, *lens;
   int64_t table_ld;
   int B, Q, heads, kv_heads, D, num_blocks, block_size, table_width, window;
-  float scale;
+  int group;      // query heads of a kv head
+  int rows;       // queries that share a kv head's keys: Q * group, row = query * group + head
+  int row_tiles;  // tiles of 16 * MT of them
+  float scale2;   // scale * log2(e)
+  bool q_vec, out_vec, same_strides;
+  char* ws;
   uint32_t* err;
 };
 
-constexpr int kAThreads = 256;
+constexpr int kAThreads = 128;
 constexpr int kAWarps = kAThreads / 32;
+constexpr int kAKeys = 16;                 // keys of a warp's step
+constexpr int kATile = kAWarps * kAKeys;   // keys of a CTA's step, the unit of the split
+constexpr int kAMaxCtas = 304;             // CTAs that share the work (two on each of 152 SMs)
+
+// A CTA whose share begins inside an item (a request, kv head and row tile) says which.
+struct AttendInfo {
+  int64_t total;  // tiles of all items
+  int64_t first;  // the item's first tile
+  int b, hr, tiles, pad;
+};
+
+// Workspace: an AttendInfo per CTA; then, for two parts a CTA (one of an item that an
+// earlier CTA began, one of an item that a later CTA goes on with), each row's maximum
+// and sum, and each row's weighted values.
+constexpr size_t kAInfoBytes = (kAMaxCtas * sizeof(AttendInfo) + 255) / 256 * 256;
+__host__ __device__ constexpr size_t attend_ml_bytes(int rows) {
+  return (static_cast<size_t>(2 * kAMaxCtas) * rows * 2 * sizeof(float) + 255) / 256 * 256;
+}
+constexpr size_t attend_ws_bytes(int rows, int DP) {
+  return kAInfoBytes + attend_ml_bytes(rows) + static_cast<size_t>(2 * kAMaxCtas) * rows * DP * sizeof(float);
+}
+
+// Dynamic shared memory: the warps' rings, the queries (fp32: in two pieces), each step's
+// mask of keys that exist, each warp's maxima and sums.
+template <typename T>
+constexpr size_t attend_smem_bytes(int DP, int MT, int ST) {
+  return static_cast<size_t>(kAWarps) * ST * 2 * kAKeys * DP * sizeof(T) +
+         static_cast<size_t>(16) * MT * DP * (sizeof(T) == 4 ? 8 : 2) + kAWarps * ST * 4 +
+         static_cast<size_t>(kAWarps) * 16 * MT * 8;
+}
 
 __device__ __forceinline__ void put(float* p, float y) { *p = y; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float y) { *p = __float2bfloat16_rn(y); }
 
-// One CTA per query and head: its warps take the keys in turn, a lane up to eight elements
-// of a head, each warp with a running maximum and sum of its own; joined at the end.
-template <typename T>
-__global__ void __launch_bounds__(kAThreads) attend_kernel(const AttendParams p) {
-  __shared__ float s_m[kAWarps], s_l[kAWarps], s_o[kAWarps][256];
-  const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int kh = h / (p.heads / p.kv_heads);
-  const int len0 = p.lens[b];
-  const int len = min(max(len0, 0), p.table_width * p.block_size);
-  unsigned err = len != len0 ? ASYMSPEC_DATA_BAD_LENGTH : 0u;
-  const int last = len - p.Q + i;
-  const int first = p.window ? max(0, last - p.window + 1) : 0;
-  const T* q = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
-  float x[8], o[8], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int d = lane + 32 * e;
-    x[e] = d < p.D ? to_f32(q[d]) * p.scale : 0.f;
-    o[e] = 0.f;
+__device__ __forceinline__ int attend_len(const AttendParams& p, int b) {
+  return min(max(p.lens[b], 0), p.table_width * p.block_size);
+}
+// First key that any query of a request of this length sees.
+__device__ __forceinline__ int attend_first(const AttendParams& p, int len) {
+  return p.window ? max(0, len - p.Q - p.window + 1) : 0;
+}
+__device__ __forceinline__ int attend_tiles(const AttendParams& p, int len) {
+  return max(1, (len - attend_first(p, len) + kATile - 1) / kATile);
+}
+__device__ __forceinline__ int64_t share_start(int64_t total, int c, int ctas) { return total * c / ctas; }
+
+// 16 bytes, or zeros where `live` is false (the address is then not read).
+__device__ __forceinline__ void cp_async16_or_zero(unsigned smem, const void* gmem, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(unsigned (&r)[4], unsigned a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
+}
+__device__ __forceinline__ void ldmatrix4_trans(unsigned (&r)[4], unsigned a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x = hi + lo + (2^-22 |x| at most), each with tf32's 11 significant bits.
+__device__ __forceinline__ void split_tf32(float x, unsigned& hi, unsigned& lo) {
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+}
+// (x, y) = hi + lo + (2^-17 of each at most), packed bf16.
+__device__ __forceinline__ void split_bf16(float x, float y, unsigned& hi, unsigned& lo) {
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
+  const float rx = x - __uint_as_float(hi << 16), ry = y - __uint_as_float(hi & 0xFFFF0000u);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(ry), "f"(rx));
+}
+
+// Where 16-byte chunk `c` of row `r` of a tile lies.  bf16: ldmatrix reads eight rows of
+// one chunk.  fp32 keys: eight lanes read four chunks of two neighbouring rows; values:
+// two chunks of four rows of one parity.
+template <typename T, bool VALUES>
+__device__ __forceinline__ int swizzled(int r, int c) {
+  return sizeof(T) == 2 || VALUES ? c ^ (r & 7) : c ^ (((r & 1) << 2) | ((r >> 1) & 3));
+}
+
+// The keys are split evenly over the CTAs, in tiles of 64, whatever the requests' lengths;
+// each warp takes 16 keys of a tile through a ring of its own (cp.async, no barrier
+// between warps) and keeps running maxima, sums and weighted values of the tile's rows;
+// a CTA joins its warps' when its share of an item ends.
+template <typename T, int DP, int MT, int ST>
+__global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16;
+  constexpr int kHalf = kAKeys * DP;  // elements of a step's keys (and of its values)
+  constexpr int kRows = 16 * MT;
+  constexpr int NT = DP / 8;
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  constexpr bool kQRegs = BF && MT * DP <= 128;
+  extern __shared__ __align__(128) unsigned char a_smem[];
+  __shared__ int64_t s_scan[kAThreads];
+  __shared__ int64_t s_v;
+  __shared__ int s_b;
+  T* ring0 = reinterpret_cast<T*>(a_smem);
+  unsigned char* at_q = a_smem + static_cast<size_t>(kAWarps) * ST * 2 * kHalf * sizeof(T);
+  T* qs = reinterpret_cast<T*>(at_q);  // fp32: the high pieces, then the low ones
+  unsigned char* at_mask = at_q + static_cast<size_t>(kRows) * DP * (BF ? 2 : 8);
+  float* s_ml = reinterpret_cast<float*>(at_mask + kAWarps * ST * 4);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  unsigned* masks = reinterpret_cast<unsigned*>(at_mask) + warp * ST;
+  T* ring = ring0 + warp * ST * 2 * kHalf;
+  const int c = blockIdx.x, ctas = gridDim.x;
+  const int HR = p.kv_heads * p.row_tiles;
+  unsigned err = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // this CTA's share of the tiles, and where it begins
+  const int per = (p.B + kAThreads - 1) / kAThreads;
+  int64_t mine = 0;
+  for (int b = tid * per; b < min((tid + 1) * per, p.B); ++b) {
+    const int len = attend_len(p, b);
+    if (len != p.lens[b]) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    mine += attend_tiles(p, len);
   }
-  for (int j = first + warp; j <= last; j += kAWarps) {
-    const int page = p.tables[b * p.table_ld + j / p.block_size], at = j % p.block_size;
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_blocks)) {
-      err |= ASYMSPEC_DATA_BAD_INDEX;
-      continue;
-    }
-    const T* k = static_cast<const T*>(p.keys) + page * p.cks[0] + at * p.cks[1] + kh * p.cks[2];
-    const T* v = static_cast<const T*>(p.values) + page * p.cvs[0] + at * p.cvs[1] + kh * p.cvs[2];
-    float s = 0.f;
+  int64_t upto = mine;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (lane + 32 * e < p.D) s = fmaf(x[e], to_f32(k[lane + 32 * e]), s);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-    const float m2 = fmaxf(m, s), ref = m2 == -INFINITY ? 0.f : m2;
-    const float f = expf(m - ref), w = expf(s - ref);
-    m = m2;
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (lane + 32 * e < p.D) o[e] = fmaf(w, to_f32(v[lane + 32 * e]), o[e] * f);
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += o;
   }
-  if (lane == 0) s_m[warp] = m, s_l[warp] = l;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s_o[warp][lane + 32 * e] = o[e];
+  if (lane == 31) s_scan[warp] = upto;
   __syncthreads();
-  float M = -INFINITY, L = 0.f, O = 0.f;
-  for (int w = 0; w < kAWarps; ++w) M = fmaxf(M, s_m[w]);
+  int64_t total = 0;
   for (int w = 0; w < kAWarps; ++w) {
-    const float f = s_m[w] == -INFINITY ? 0.f : expf(s_m[w] - M);
-    L += f * s_l[w];
-    O += f == 0.f ? 0.f : f * s_o[w][threadIdx.x];
+    if (w < warp) upto += s_scan[w];
+    total += s_scan[w];
   }
-  if (threadIdx.x < p.D)
-    put(static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + threadIdx.x,
-        L > 0.f ? O / L : (L == 0.f ? 0.f : L));
-  if (threadIdx.x == 0 && p.lse)
-    p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = M + logf(L);
+  total *= HR;
+  int64_t u = share_start(total, c, ctas);
+  const int64_t u_end = share_start(total, c + 1, ctas);
+  if (u < u_end && (upto - mine) * HR <= u && u < upto * HR) {
+    int64_t v = u - (upto - mine) * HR;
+    int b = tid * per;
+    for (;; ++b) {
+      const int64_t n = static_cast<int64_t>(attend_tiles(p, attend_len(p, b))) * HR;
+      if (v < n) break;
+      v -= n;
+    }
+    s_b = b;
+    s_v = v;
+  }
+  __syncthreads();
+  AttendInfo* info = reinterpret_cast<AttendInfo*>(p.ws) + c;
+  if (u >= u_end) {
+    if (tid == 0) info->tiles = 0;
+    if (err && p.err) atomicOr(p.err, err);
+    return;
+  }
+  int b = s_b;
+  int len = attend_len(p, b), n_tiles = attend_tiles(p, len);
+  int hr = static_cast<int>(s_v / n_tiles), t0 = static_cast<int>(s_v % n_tiles);
+  if (tid == 0) {
+    info->total = total;
+    info->first = u - t0;
+    info->b = b;
+    info->hr = hr;
+    info->tiles = t0 > 0 ? n_tiles : 0;
+  }
+
+  float O[MT][NT][4], m[MT][2], l[MT][2];
+  unsigned qf[kQRegs ? MT * DP / 16 : 1][4];
+  while (u < u_end) {
+    const int t1 = static_cast<int>(min(static_cast<int64_t>(n_tiles), t0 + (u_end - u)));
+    const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * kRows;
+    const int lo = attend_first(p, len);
+    // the item's queries
+    const int rows = min(kRows, p.rows - R0);
+    for (int e = tid; e < kRows * kChunks; e += kAThreads) {
+      const int r = e / kChunks, ch = e % kChunks;
+      constexpr int PE = 16 / sizeof(T);
+      const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+      const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2] + ch * PE;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r < rows && ch * PE < p.D) {
+        if (p.q_vec) {
+          v = *reinterpret_cast<const uint4*>(src);
+        } else {
+          T x[PE];
+#pragma unroll
+          for (int k = 0; k < PE; ++k) x[k] = src[k];
+          v = *reinterpret_cast<const uint4*>(x);
+        }
+      }
+      const int at = r * DP + swizzled<T, false>(r, ch) * PE;
+      if constexpr (BF) {
+        *reinterpret_cast<uint4*>(qs + at) = v;
+      } else {
+        uint4 hi, lw;
+        split_tf32(__uint_as_float(v.x), hi.x, lw.x);
+        split_tf32(__uint_as_float(v.y), hi.y, lw.y);
+        split_tf32(__uint_as_float(v.z), hi.z, lw.z);
+        split_tf32(__uint_as_float(v.w), hi.w, lw.w);
+        *reinterpret_cast<uint4*>(qs + at) = hi;
+        *reinterpret_cast<uint4*>(qs + kRows * DP + at) = lw;
+      }
+    }
+    const T* keys = static_cast<const T*>(p.keys) + kh * p.cks[2];
+    const T* values = static_cast<const T*>(p.values) + kh * p.cvs[2];
+    const int32_t* table = p.tables + b * p.table_ld;
+    const int k_lane = lo + warp * kAKeys + (lane & 15);  // this lane's key of tile 0
+
+    auto page_of = [&](int t) {
+      const int j = k_lane + t * kATile;
+      return t < t1 && j < len ? __ldg(table + j / p.block_size) : INT_MIN;
+    };
+    auto issue = [&](int t, int stage, int page) {
+      if (t < t1) {
+        const int j = k_lane + t * kATile;
+        const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
+        if (!there && j < len) err |= ASYMSPEC_DATA_BAD_INDEX;
+        const unsigned live = __ballot_sync(~0u, there);
+        const int at = j % p.block_size;
+        const int64_t ok = there ? page * p.cks[0] + at * p.cks[1] : 0;
+        const int64_t ov = there ? page * p.cvs[0] + at * p.cvs[1] : 0;
+        if (lane == 0) masks[stage] = live & 0xFFFFu;
+        const unsigned sk = smem_u32(ring + stage * 2 * kHalf), sv = sk + kHalf * sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kChunks / 2; ++i) {
+          const int e = i * 32 + lane, r = e / kChunks, ch = e % kChunks;
+          const int64_t rk = __shfl_sync(~0u, ok, r);
+          const int64_t rv = p.same_strides ? rk : __shfl_sync(~0u, ov, r);
+          const bool on = ((live >> r) & 1u) && ch * (16 / static_cast<int>(sizeof(T))) < p.D;
+          const int el = on ? ch * (16 / static_cast<int>(sizeof(T))) : 0;
+          cp_async16_or_zero(sk + r * kRowBytes + swizzled<T, false>(r, ch) * 16, keys + rk + el, on);
+          cp_async16_or_zero(sv + r * kRowBytes + swizzled<T, true>(r, ch) * 16, values + rv + el, on);
+        }
+      }
+      cp_async_commit();
+    };
+
+    {
+      int pages[ST > 1 ? ST - 1 : 1];
+#pragma unroll
+      for (int s = 0; s < ST - 1; ++s) pages[s] = page_of(t0 + s);
+#pragma unroll
+      for (int s = 0; s < ST - 1; ++s) issue(t0 + s, s, pages[s]);
+    }
+    int next_page = page_of(t0 + ST - 1);
+
+    // of this thread's rows: the last key seen; the tile's least and the windows' largest first
+    int last[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = mt * 16 + h * 8 + g;
+        last[mt][h] = r < rows ? len - p.Q + (R0 + r) / p.group : -1;
+        m[mt][h] = -INFINITY;
+        l[mt][h] = 0.f;
+      }
+    const int least = len - p.Q + R0 / p.group;
+    const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) O[mt][n][e] = 0.f;
+    __syncthreads();
+    if constexpr (kQRegs) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          const int r = mt * 16 + (lane & 15), ch = k * 2 + (lane >> 4);
+          ldmatrix4(qf[mt * (DP / 16) + k], smem_u32(qs + r * DP) + swizzled<T, false>(r, ch) * 16);
+        }
+    }
+
+    int stage = 0;
+    for (int t = t0; t < t1; ++t) {
+      issue(t + ST - 1, stage == 0 ? ST - 1 : stage - 1, next_page);
+      next_page = page_of(t + ST);
+      cp_async_wait<ST - 1>();
+      __syncwarp();
+      const T* ks = ring + stage * 2 * kHalf;
+      const T* vs = ks + kHalf;
+      const unsigned live = masks[stage];
+      const int k0 = lo + t * kATile + warp * kAKeys;
+      if (live != 0) {
+        // scores of 16 keys: S[mt][keys 0-7, 8-15]
+        float S[MT][2][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[mt][n][e] = 0.f;
+        if constexpr (BF) {
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) {
+            const int r = ((lane >> 4) << 3) + (lane & 7), ch = k * 2 + ((lane >> 3) & 1);
+            unsigned kf[4];
+            ldmatrix4(kf, smem_u32(ks + r * DP) + swizzled<T, false>(r, ch) * 16);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              if constexpr (kQRegs) {
+                mma_bf16(S[mt][0], qf[mt * (DP / 16) + k], kf[0], kf[1]);
+                mma_bf16(S[mt][1], qf[mt * (DP / 16) + k], kf[2], kf[3]);
+              } else {
+                const int qr = mt * 16 + (lane & 15), qc = k * 2 + (lane >> 4);
+                unsigned qv[4];
+                ldmatrix4(qv, smem_u32(qs + qr * DP) + swizzled<T, false>(qr, qc) * 16);
+                mma_bf16(S[mt][0], qv, kf[0], kf[1]);
+                mma_bf16(S[mt][1], qv, kf[2], kf[3]);
+              }
+            }
+          }
+        } else {
+          // the sum over a head's elements in an order of its own: of each 16, lane t4 of a
+          // quad takes elements 4 t4 .. 4 t4 + 3, two for each of two products
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) {
+            unsigned kh4[2][4], kl4[2][4];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const int r = n * 8 + g;
+              const float4 x = *reinterpret_cast<const float4*>(ks + r * DP + swizzled<T, false>(r, 4 * k + t4) * 4);
+              split_tf32(x.x, kh4[n][0], kl4[n][0]);
+              split_tf32(x.y, kh4[n][1], kl4[n][1]);
+              split_tf32(x.z, kh4[n][2], kl4[n][2]);
+              split_tf32(x.w, kh4[n][3], kl4[n][3]);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              const int r0 = mt * 16 + g, r1 = r0 + 8;
+              const int a0 = r0 * DP + swizzled<T, false>(r0, 4 * k + t4) * 4;
+              const int a1 = r1 * DP + swizzled<T, false>(r1, 4 * k + t4) * 4;
+              const uint4 h0 = *reinterpret_cast<const uint4*>(qs + a0);
+              const uint4 h1 = *reinterpret_cast<const uint4*>(qs + a1);
+              const uint4 l0 = *reinterpret_cast<const uint4*>(qs + kRows * DP + a0);
+              const uint4 l1 = *reinterpret_cast<const uint4*>(qs + kRows * DP + a1);
+              const unsigned qh[2][4] = {{h0.x, h1.x, h0.y, h1.y}, {h0.z, h1.z, h0.w, h1.w}};
+              const unsigned ql[2][4] = {{l0.x, l1.x, l0.y, l1.y}, {l0.z, l1.z, l0.w, l1.w}};
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                  mma_tf32(S[mt][n], ql[e], kh4[n][2 * e], kh4[n][2 * e + 1]);
+                  mma_tf32(S[mt][n], qh[e], kl4[n][2 * e], kl4[n][2 * e + 1]);
+                  mma_tf32(S[mt][n], qh[e], kh4[n][2 * e], kh4[n][2 * e + 1]);
+                }
+            }
+          }
+        }
+        const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float& s = S[mt][n][2 * h + e];
+                s *= p.scale2;
+                if (!whole) {
+                  const int kk = n * 8 + 2 * t4 + e, j = k0 + kk;
+                  const bool seen = ((live >> kk) & 1u) && j <= last[mt][h] &&
+                                    (p.window == 0 || j > last[mt][h] - p.window);
+                  s = seen ? s : -INFINITY;
+                }
+                top = fmaxf(top, s);
+              }
+            if (__any_sync(~0u, top > m[mt][h])) {
+              float v = fmaxf(m[mt][h], top);
+              v = fmaxf(v, __shfl_xor_sync(~0u, v, 1));
+              v = fmaxf(v, __shfl_xor_sync(~0u, v, 2));
+              const float f = v == m[mt][h] ? 1.f : ex2(m[mt][h] - v);
+              m[mt][h] = v;
+              l[mt][h] *= f;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                O[mt][n][2 * h] *= f;
+                O[mt][n][2 * h + 1] *= f;
+              }
+            }
+            const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              S[mt][n][2 * h] = ex2(S[mt][n][2 * h] - ref);
+              S[mt][n][2 * h + 1] = ex2(S[mt][n][2 * h + 1] - ref);
+              l[mt][h] += S[mt][n][2 * h] + S[mt][n][2 * h + 1];
+            }
+          }
+        if constexpr (BF) {
+          unsigned ph[MT][4], pl[MT][4];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              split_bf16(S[mt][n][0], S[mt][n][1], ph[mt][2 * n], pl[mt][2 * n]);
+              split_bf16(S[mt][n][2], S[mt][n][3], ph[mt][2 * n + 1], pl[mt][2 * n + 1]);
+            }
+#pragma unroll
+          for (int n = 0; n < NT / 2; ++n) {
+            const int r = lane & 15, ch = n * 2 + (lane >> 4);
+            unsigned vf[4];
+            ldmatrix4_trans(vf, smem_u32(vs + r * DP) + swizzled<T, true>(r, ch) * 16);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              mma_bf16(O[mt][2 * n], pl[mt], vf[0], vf[1]);
+              mma_bf16(O[mt][2 * n + 1], pl[mt], vf[2], vf[3]);
+              mma_bf16(O[mt][2 * n], ph[mt], vf[0], vf[1]);
+              mma_bf16(O[mt][2 * n + 1], ph[mt], vf[2], vf[3]);
+            }
+          }
+        } else {
+          // keys 2 t4 and 2 t4 + 1 of each eight are the products' elements t4 and t4 + 4; of each
+          // 32 elements of a head, lane group g takes 4 g .. 4 g + 3, one for each of four products
+#pragma unroll
+          for (int n8 = 0; n8 < 2; ++n8) {
+            unsigned ph[MT][4], pl[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              split_tf32(S[mt][n8][0], ph[mt][0], pl[mt][0]);
+              split_tf32(S[mt][n8][2], ph[mt][1], pl[mt][1]);
+              split_tf32(S[mt][n8][1], ph[mt][2], pl[mt][2]);
+              split_tf32(S[mt][n8][3], ph[mt][3], pl[mt][3]);
+            }
+            const int r0 = n8 * 8 + 2 * t4, r1 = r0 + 1;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+              const float4 x = *reinterpret_cast<const float4*>(vs + r0 * DP + swizzled<T, true>(r0, 8 * i + g) * 4);
+              const float4 y = *reinterpret_cast<const float4*>(vs + r1 * DP + swizzled<T, true>(r1, 8 * i + g) * 4);
+              const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                unsigned h0, l0, h1, l1;
+                split_tf32(xs[e], h0, l0);
+                split_tf32(ys[e], h1, l1);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                  mma_tf32(O[mt][4 * i + e], pl[mt], h0, h1);
+                  mma_tf32(O[mt][4 * i + e], ph[mt], l0, l1);
+                  mma_tf32(O[mt][4 * i + e], ph[mt], h0, h1);
+                }
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();
+      stage = stage + 1 == ST ? 0 : stage + 1;
+    }
+
+    cp_async_wait<0>();
+    __syncwarp();
+    // Infinities and NaN: a weight of zero times one that its row does not see, or one in
+    // two pieces, is a NaN that the formula does not have.  A warp that ends with any works its
+    // keys again, one product after another, and leaves out what a row does not see.
+    float odd = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (mt * 16 + h * 8 + g < rows) {
+          odd = fmaf(0.f, l[mt][h], odd);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) odd = fmaf(0.f, O[mt][n][2 * h], fmaf(0.f, O[mt][n][2 * h + 1], odd));
+        }
+    if (__any_sync(~0u, odd != 0.f)) {
+      constexpr int PE = 16 / sizeof(T);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          m[mt][h] = -INFINITY;
+          l[mt][h] = 0.f;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) O[mt][n][2 * h] = O[mt][n][2 * h + 1] = 0.f;
+        }
+      for (int t = t0; t < t1; ++t) {
+        issue(t, 0, page_of(t));
+        cp_async_wait<0>();
+        __syncwarp();
+        const unsigned live = masks[0];
+        const T* ks = ring;
+        const T* vs = ks + kHalf;
+        for (int kk = 0; kk < kAKeys; ++kk) {
+          if (!((live >> kk) & 1u)) continue;
+          const int j = lo + t * kATile + warp * kAKeys + kk;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int r = min(mt * 16 + h * 8 + g, rows - 1);
+              const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + (R0 + r) / p.group * p.qs[1] +
+                            (kh * p.group + (R0 + r) % p.group) * p.qs[2];
+              float s = 0.f;
+              for (int d = t4; d < p.D; d += 4)
+                s = fmaf(to_f32(qr[d]), to_f32(ks[kk * DP + swizzled<T, false>(kk, d / PE) * PE + d % PE]), s);
+              s += __shfl_xor_sync(~0u, s, 1);
+              s += __shfl_xor_sync(~0u, s, 2);
+              s *= p.scale2;
+              if (j <= last[mt][h] && (p.window == 0 || j > last[mt][h] - p.window)) {
+                const float v = fmaxf(m[mt][h], s), ref = v == -INFINITY ? 0.f : v;
+                const float f = v == m[mt][h] ? 1.f : ex2(m[mt][h] - v), w = ex2(s - ref);
+                m[mt][h] = v;
+                l[mt][h] = l[mt][h] * f + (t4 == 0 ? w : 0.f);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const int d = BF ? n * 8 + 2 * t4 + e : (n >> 2) * 32 + 8 * t4 + 4 * e + (n & 3);
+                    const float x = to_f32(vs[kk * DP + swizzled<T, true>(kk, d / PE) * PE + d % PE]);
+                    O[mt][n][2 * h + e] = fmaf(w, x, O[mt][n][2 * h + e] * f);
+                  }
+              }
+            }
+        }
+        __syncwarp();
+      }
+    }
+
+    // the warps' parts of the item: each leaves its values in its own ring
+    float* mine_o = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = mt * 16 + h * 8 + g;
+        float s = l[mt][h];
+        s += __shfl_xor_sync(~0u, s, 1);
+        s += __shfl_xor_sync(~0u, s, 2);
+        if (t4 == 0) {
+          s_ml[(warp * kRows + r) * 2] = m[mt][h];
+          s_ml[(warp * kRows + r) * 2 + 1] = s;
+        }
+        float* row = mine_o + r * DP;
+        if constexpr (BF) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<float2*>(row + ((n ^ (r & 7)) * 8 + 2 * t4)) =
+                make_float2(O[mt][n][2 * h], O[mt][n][2 * h + 1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              *reinterpret_cast<float4*>(row + (((4 * i + t4) ^ (r & 7)) * 8 + 4 * e)) =
+                  make_float4(O[mt][4 * i][2 * h + e], O[mt][4 * i + 1][2 * h + e],
+                              O[mt][4 * i + 2][2 * h + e], O[mt][4 * i + 3][2 * h + e]);
+        }
+      }
+    __syncthreads();
+    const bool all = t0 == 0 && t1 == n_tiles;
+    const int part = t0 > 0 ? 2 * c : 2 * c + 1;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * kRows * 2;
+    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) +
+                  static_cast<size_t>(part) * kRows * DP;
+    for (int e = tid; e < rows * (DP / 4); e += kAThreads) {
+      const int r = e / (DP / 4), d = (e % (DP / 4)) * 4;
+      float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kAWarps; ++w) M = fmaxf(M, s_ml[(w * kRows + r) * 2]);
+#pragma unroll
+      for (int w = 0; w < kAWarps; ++w) {
+        const float mw = s_ml[(w * kRows + r) * 2], lw = s_ml[(w * kRows + r) * 2 + 1];
+        const float f = mw == M ? 1.f : ex2(mw - M);
+        const float4 o = *reinterpret_cast<const float4*>(
+            reinterpret_cast<const float*>(ring0 + w * ST * 2 * kHalf) + r * DP +
+            (((d >> 3) ^ (r & 7)) * 8 + (d & 7)));
+        L = fmaf(f, lw, L);
+        x[0] = fmaf(f, o.x, x[0]);
+        x[1] = fmaf(f, o.y, x[1]);
+        x[2] = fmaf(f, o.z, x[2]);
+        x[3] = fmaf(f, o.w, x[3]);
+      }
+      if (all) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+        T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
+        if (d < p.D) {  // (D is a multiple of 4)
+          T y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) put(y + k, x[k] * inv);
+          if (p.out_vec) {
+            if constexpr (BF) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
+            else *reinterpret_cast<float4*>(out) = *reinterpret_cast<const float4*>(y);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] = y[k];
+          }
+        }
+        if (d == 0 && p.lse)
+          p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = M == -INFINITY ? -INFINITY : fmaf(M, kLn2, logf(L));
+      } else {
+        *reinterpret_cast<float4*>(ws_o + r * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
+        if (d == 0) *reinterpret_cast<float2*>(ws_ml + r * 2) = make_float2(M, L);
+      }
+    }
+    __syncthreads();
+    u += t1 - t0;
+    t0 = 0;
+    if (++hr == HR && u < u_end) {
+      hr = 0;
+      ++b;
+      len = attend_len(p, b);
+      n_tiles = attend_tiles(p, len);
+    }
+  }
   if (err && p.err) atomicOr(p.err, err);
+}
+
+// The items whose keys lie in several CTAs' shares: one CTA per row of the first CTA that
+// went on with an item.  The parts join in the order of the CTAs.
+template <typename T, int DP, int MT>
+__global__ void __launch_bounds__(kAThreads) attend_join(const AttendParams p, int ctas) {
+  constexpr int kRows = 16 * MT;
+  constexpr int kCols = DP / 4, kWays = kAThreads / kCols;
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  __shared__ float s_w[kAMaxCtas], s_x[kAThreads * 4], s_red[kAWarps];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int c = blockIdx.x + 1, r = blockIdx.y, tid = threadIdx.x;
+  const AttendInfo in = reinterpret_cast<const AttendInfo*>(p.ws)[c];
+  if (in.tiles == 0) return;
+  const int R0 = (in.hr % p.row_tiles) * kRows, kh = in.hr / p.row_tiles;
+  if (R0 + r >= p.rows) return;
+  // owner of tile x: the last CTA whose share starts at x or before
+  auto owner = [&](int64_t x) { return static_cast<int>(((x + 1) * ctas - 1) / in.total); };
+  const int c0 = owner(in.first), c1 = owner(in.first + in.tiles - 1);
+  if (share_start(in.total, c0 + 1, ctas) != share_start(in.total, c, ctas)) return;
+  const int parts = c1 - c0 + 1;
+  const float* ml = reinterpret_cast<const float*>(p.ws + kAInfoBytes);
+  const float* os = reinterpret_cast<const float*>(p.ws + kAInfoBytes + kMlBytes);
+  auto part_of = [&](int k) { return k == 0 ? 2 * c0 + 1 : 2 * (c0 + k); };
+  auto empty = [&](int k) {
+    return share_start(in.total, c0 + k, ctas) == share_start(in.total, c0 + k + 1, ctas);
+  };
+  float M = -INFINITY;
+  for (int k = tid; k < parts; k += kAThreads) {
+    const float mk = empty(k) ? -INFINITY : ml[(static_cast<size_t>(part_of(k)) * kRows + r) * 2];
+    s_w[k] = mk;
+    M = fmaxf(M, mk);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
+  if ((tid & 31) == 0) s_red[tid >> 5] = M;
+  __syncthreads();
+  M = s_red[0];
+#pragma unroll
+  for (int w = 1; w < kAWarps; ++w) M = fmaxf(M, s_red[w]);
+  const int col = tid % kCols, way = tid / kCols;
+  float x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+  for (int k = way; k < parts; k += kWays) {
+    if (empty(k)) continue;
+    const float f = s_w[k] == M ? 1.f : ex2(s_w[k] - M);
+    const size_t at = static_cast<size_t>(part_of(k)) * kRows + r;
+    const float4 o = *reinterpret_cast<const float4*>(os + at * DP + col * 4);
+    L = fmaf(f, ml[at * 2 + 1], L);
+    x[0] = fmaf(f, o.x, x[0]);
+    x[1] = fmaf(f, o.y, x[1]);
+    x[2] = fmaf(f, o.z, x[2]);
+    x[3] = fmaf(f, o.w, x[3]);
+  }
+  __syncthreads();
+  *reinterpret_cast<float4*>(s_x + tid * 4) = make_float4(x[0], x[1], x[2], x[3]);
+  if (col == 0) s_w[way] = L;
+  __syncthreads();
+  if (way != 0) return;
+  L = s_w[0];
+  for (int w = 1; w < kWays; ++w) {
+    L += s_w[w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += s_x[(w * kCols + col) * 4 + e];
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group, d = col * 4;
+  T* out = static_cast<T*>(p.out) + in.b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
+  if (d < p.D) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) put(out + k, x[k] * inv);
+  }
+  if (d == 0 && p.lse)
+    p.lse[(static_cast<int64_t>(in.b) * p.Q + i) * p.heads + h] = M == -INFINITY ? -INFINITY : fmaf(M, kLn2, logf(L));
 }
 
 }  // namespace asymspec_impl

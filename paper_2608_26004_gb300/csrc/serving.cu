@@ -4,11 +4,14 @@
 //   constrain_kernel    (kernel_constrain.cuh) penalties, biases and masks on logits
 //   cache_plan_kernel   (kernel_cache.cuh) block tables and slot maps
 //   cache_write_kernel  (kernel_cache.cuh) new keys and values into the cache
-//   attend_kernel       (kernel_attend.cuh) attention over the cache
+//   attend_split        (kernel_attend.cuh) attention over the cache, the keys split evenly
+//                       over the chip; attend_join joins the parts of a request's keys
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "host_common.h"
+#include "k_attend.h"
 #include "kernel_attend.cuh"
 #include "kernel_cache.cuh"
 #include "kernel_constrain.cuh"
@@ -24,6 +27,29 @@ bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % 
 int elt_size(int dtype) { return dtype == ASYMSPEC_FP32 ? 4 : 2; }
 
 bool known_dtype(int dtype) { return dtype == ASYMSPEC_FP32 || dtype == ASYMSPEC_BF16; }
+
+// Once per kernel and device: room for its dynamic shared memory.
+struct Prepared {
+  const void* fn;
+  int device;
+};
+std::mutex g_mu;
+Prepared g_prepared[64];
+int g_prepared_count = 0;
+
+cudaError_t prepare(const void* fn, int device, int smem) {
+  if (smem <= 47 * 1024) return cudaSuccess;
+  std::lock_guard<std::mutex> lock(g_mu);
+  for (int i = 0; i < g_prepared_count; ++i)
+    if (g_prepared[i].fn == fn && g_prepared[i].device == device) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess && g_prepared_count < 64) g_prepared[g_prepared_count++] = {fn, device};
+  return e;
+}
+
+AttendKernels attend_kernels(int dtype, int D, int rows) {
+  return dtype == ASYMSPEC_FP32 ? attend_kernels_f32(D, rows) : attend_kernels_bf16(D, rows);
+}
 
 int launch(const void* fn, dim3 grid, dim3 block, size_t smem, void* params, void* stream) {
   cudaError_t e = cudaSuccess;
@@ -182,7 +208,9 @@ size_t asymspec_cache_attend_workspace_bytes(int B, int Q, int heads, int kv_hea
       head_dim > ASYMSPEC_CACHE_MAX_D || B > ASYMSPEC_CACHE_MAX_B ||
       static_cast<int64_t>(Q) * heads > (1 << 20))
     return 0;
-  return 256;
+  const int rows = Q * (heads / kv_heads);
+  const AttendKernels a = attend_kernels_bf16(head_dim, rows), b = attend_kernels_f32(head_dim, rows);
+  return std::max(attend_ws_bytes(a.rows, a.DP), attend_ws_bytes(b.rows, b.DP));
 }
 
 int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int64_t* q_strides,
@@ -199,7 +227,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   for (int i = 0; i < 3; ++i)
     if (q_strides[i] < 0 || out_strides[i] < 0) return ASYMSPEC_ERR_INVALID_ARG;
   if (B > ASYMSPEC_CACHE_MAX_B || static_cast<int64_t>(Q) * heads > (1 << 20) ||
-      static_cast<int64_t>(table_width) * cache->block_size > kMax32)
+      static_cast<int64_t>(table_width) * cache->block_size > (1 << 30))
     return ASYMSPEC_ERR_TOO_LARGE;
   if (B == 0 || Q == 0) return ASYMSPEC_OK;
   if (!q || !block_tables || !lens || !out) return ASYMSPEC_ERR_INVALID_ARG;
@@ -238,12 +266,43 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   p.block_size = cache->block_size;
   p.table_width = table_width;
   p.window = window;
-  p.scale = scale;
+  p.group = heads / cache->kv_heads;
+  p.rows = Q * p.group;
+  const AttendKernels k = attend_kernels(cache->dtype, p.D, p.rows);
+  p.row_tiles = (p.rows + k.rows - 1) / k.rows;
+  p.scale2 = scale * kLog2e;
+  p.q_vec = aligned(q, 16);
+  p.out_vec = aligned(out, 4 * elt);
+  p.same_strides = true;
+  for (int i = 0; i < 3; ++i) {
+    p.q_vec = p.q_vec && q_strides[i] % per == 0;
+    p.out_vec = p.out_vec && out_strides[i] % 4 == 0;
+    p.same_strides = p.same_strides && cache->key_strides[i] == cache->value_strides[i];
+  }
+  p.ws = static_cast<char*>(workspace);
   p.err = out_error_word;
-  const void* fn = cache->dtype == ASYMSPEC_FP32
-                       ? reinterpret_cast<const void*>(&attend_kernel<float>)
-                       : reinterpret_cast<const void*>(&attend_kernel<__nv_bfloat16>);
-  return launch(fn, dim3(heads, Q, B), dim3(kAThreads), 0, &p, stream);
+  int device = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (e == cudaSuccess) e = prepare(k.split, device, k.smem);
+  if (e != cudaSuccess) return cuda_fail(e);
+  int ctas = std::min(kAMaxCtas, sms * k.ctas_per_sm);
+  const cudaStream_t st_ = static_cast<cudaStream_t>(stream);
+  void* args[] = {&p, &ctas};
+  e = cudaLaunchKernel(k.split, dim3(ctas), dim3(kAThreads), args, k.smem, st_);
+  if (e != cudaSuccess) return cuda_fail(e);
+  if (ctas == 1) return ASYMSPEC_OK;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(ctas - 1, std::min(p.rows, k.rows));
+  cfg.blockDim = dim3(kAThreads);
+  cfg.stream = st_;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelExC(&cfg, k.join, args);
+  return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
 }
 
 }  // extern "C"

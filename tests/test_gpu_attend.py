@@ -170,6 +170,22 @@ def test_infinite_scores_follow_the_formula(torch):
     check(torch, x, out, lse, [(0, 0, 0)])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_infinite_values_follow_the_formula(torch, dtype):
+    """A value of +infinity makes that element of every query that sees it +infinity, and no other."""
+    Q, n = 3, 400
+    x = inputs(torch, [n, 30], Q, 8, 4, 64, dtype, 16, 19)
+    want, lse = S.CacheAttend(2, Q, 8, 4, 64)(*x)
+    for at in (100, n - 2):                             # seen by all queries; by the last two
+        x[2][int(x[3][0, at // 16]), at % 16, 1, 5] = math.inf
+        want[0, 0 if at == 100 else 1:, 2:4, 5] = math.inf
+    out, lse2 = S.CacheAttend(2, Q, 8, 4, 64)(*x)
+    assert torch.equal(lse, lse2) or torch.allclose(lse, lse2, rtol=0, atol=1e-5)
+    finite = want.isfinite()
+    assert torch.equal(out.isfinite(), finite) and (out[~finite] == math.inf).all()
+    check(torch, x, out, lse2, [(0, i, h) for i in range(Q) for h in (0, 1, 4, 7)] + [(1, 2, 3)])
+
+
 def test_bad_data(torch):
     q, keys, values, tables, lens = inputs(torch, [100, 60, 40], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.CacheAttend(3, 2, 4, 2, 64)
