@@ -31,10 +31,14 @@ constexpr int kAKeys = 16;                 // keys of a warp's step
 constexpr int kATile = kAWarps * kAKeys;   // keys of a CTA's step, the unit of the split
 constexpr int kAMaxCtas = 304;             // CTAs that share the work (two on each of 152 SMs)
 
-// A CTA whose share begins inside an item (a request, kv head and row tile) says which.
+// The work is split by units: an item (a request, kv head and row tile) has one for each
+// of its tiles, after kAItem for what it costs to begin and end one.
+constexpr int kAItem = 2;
+
+// A CTA whose share begins after the first tile of an item says which.
 struct AttendInfo {
-  int64_t total;  // tiles of all items
-  int64_t first;  // the item's first tile
+  int64_t total;  // units of all items
+  int64_t first;  // the item's first unit
   int b, hr, tiles, pad;
 };
 
@@ -71,7 +75,21 @@ __device__ __forceinline__ int attend_first(const AttendParams& p, int len) {
 __device__ __forceinline__ int attend_tiles(const AttendParams& p, int len) {
   return max(1, (len - attend_first(p, len) + kATile - 1) / kATile);
 }
-__device__ __forceinline__ int64_t share_start(int64_t total, int c, int ctas) { return total * c / ctas; }
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {  // (of numbers >= 0)
+  return (a | b) >> 32 ? a / b : static_cast<int64_t>(static_cast<unsigned>(a) / static_cast<unsigned>(b));
+}
+// CTA c's share: units c * each + min(c, more) on, of `each`, the first `more` CTAs one more.
+struct AttendShares {
+  int64_t each;
+  int more;
+  __device__ __forceinline__ AttendShares(int64_t total, int ctas)
+      : each(div64(total, ctas)), more(static_cast<int>(total - each * ctas)) {}
+  __device__ __forceinline__ int64_t start(int c) const { return c * each + min(c, more); }
+  __device__ __forceinline__ int owner(int64_t unit) const {
+    const int64_t big = (each + 1) * more;
+    return static_cast<int>(unit < big ? div64(unit, each + 1) : more + div64(unit - big, each));
+  }
+};
 
 // 16 bytes, or zeros where `live` is false (the address is then not read).
 __device__ __forceinline__ void cp_async16_or_zero(unsigned smem, const void* gmem, bool live) {
@@ -161,7 +179,7 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
   for (int b = tid * per; b < min((tid + 1) * per, p.B); ++b) {
     const int len = attend_len(p, b);
     if (len != p.lens[b]) err |= ASYMSPEC_DATA_BAD_LENGTH;
-    mine += attend_tiles(p, len);
+    mine += attend_tiles(p, len) + kAItem;
   }
   int64_t upto = mine;
 #pragma unroll
@@ -177,13 +195,14 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
     total += s_scan[w];
   }
   total *= HR;
-  int64_t u = share_start(total, c, ctas);
-  const int64_t u_end = share_start(total, c + 1, ctas);
+  const AttendShares shares(total, ctas);
+  int64_t u = shares.start(c);
+  const int64_t u_end = shares.start(c + 1);
   if (u < u_end && (upto - mine) * HR <= u && u < upto * HR) {
     int64_t v = u - (upto - mine) * HR;
     int b = tid * per;
     for (;; ++b) {
-      const int64_t n = static_cast<int64_t>(attend_tiles(p, attend_len(p, b))) * HR;
+      const int64_t n = static_cast<int64_t>(attend_tiles(p, attend_len(p, b)) + kAItem) * HR;
       if (v < n) break;
       v -= n;
     }
@@ -199,19 +218,31 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
   }
   int b = s_b;
   int len = attend_len(p, b), n_tiles = attend_tiles(p, len);
-  int hr = static_cast<int>(s_v / n_tiles), t0 = static_cast<int>(s_v % n_tiles);
+  int hr = static_cast<int>(div64(s_v, n_tiles + kAItem));
+  int at_unit = static_cast<int>(s_v - static_cast<int64_t>(hr) * (n_tiles + kAItem));
   if (tid == 0) {
     info->total = total;
-    info->first = u - t0;
+    info->first = u - at_unit;
     info->b = b;
     info->hr = hr;
-    info->tiles = t0 > 0 ? n_tiles : 0;
+    info->tiles = at_unit > kAItem ? n_tiles : 0;
   }
 
   float O[MT][NT][4], m[MT][2], l[MT][2];
   unsigned qf[kQRegs ? MT * DP / 16 : 1][4];
-  while (u < u_end) {
-    const int t1 = static_cast<int>(min(static_cast<int64_t>(n_tiles), t0 + (u_end - u)));
+  for (; u < u_end; at_unit = 0) {
+    if (hr == HR) {
+      hr = 0;
+      ++b;
+      len = attend_len(p, b);
+      n_tiles = attend_tiles(p, len);
+    }
+    const int end_unit = static_cast<int>(min(static_cast<int64_t>(n_tiles + kAItem), at_unit + (u_end - u)));
+    const int t0 = max(0, at_unit - kAItem), t1 = end_unit - kAItem;
+    u += end_unit - at_unit;
+    if (t1 <= t0) {  // (the item's first tile is the next CTA's)
+      continue;
+    }
     const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * kRows;
     const int lo = attend_first(p, len);
     // the item's queries
@@ -643,14 +674,7 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
       }
     }
     __syncthreads();
-    u += t1 - t0;
-    t0 = 0;
-    if (++hr == HR && u < u_end) {
-      hr = 0;
-      ++b;
-      len = attend_len(p, b);
-      n_tiles = attend_tiles(p, len);
-    }
+    ++hr;
   }
   if (err && p.err) atomicOr(p.err, err);
 }
@@ -669,20 +693,16 @@ __global__ void __launch_bounds__(kAThreads) attend_join(const AttendParams p, i
   if (in.tiles == 0) return;
   const int R0 = (in.hr % p.row_tiles) * kRows, kh = in.hr / p.row_tiles;
   if (R0 + r >= p.rows) return;
-  // owner of tile x: the last CTA whose share starts at x or before
-  auto owner = [&](int64_t x) { return static_cast<int>(((x + 1) * ctas - 1) / in.total); };
-  const int c0 = owner(in.first), c1 = owner(in.first + in.tiles - 1);
-  if (share_start(in.total, c0 + 1, ctas) != share_start(in.total, c, ctas)) return;
+  const AttendShares shares(in.total, ctas);
+  const int c0 = shares.owner(in.first + kAItem), c1 = shares.owner(in.first + kAItem + in.tiles - 1);
+  if (c0 + 1 != c) return;
   const int parts = c1 - c0 + 1;
   const float* ml = reinterpret_cast<const float*>(p.ws + kAInfoBytes);
   const float* os = reinterpret_cast<const float*>(p.ws + kAInfoBytes + kMlBytes);
   auto part_of = [&](int k) { return k == 0 ? 2 * c0 + 1 : 2 * (c0 + k); };
-  auto empty = [&](int k) {
-    return share_start(in.total, c0 + k, ctas) == share_start(in.total, c0 + k + 1, ctas);
-  };
   float M = -INFINITY;
   for (int k = tid; k < parts; k += kAThreads) {
-    const float mk = empty(k) ? -INFINITY : ml[(static_cast<size_t>(part_of(k)) * kRows + r) * 2];
+    const float mk = ml[(static_cast<size_t>(part_of(k)) * kRows + r) * 2];
     s_w[k] = mk;
     M = fmaxf(M, mk);
   }
@@ -696,7 +716,6 @@ __global__ void __launch_bounds__(kAThreads) attend_join(const AttendParams p, i
   const int col = tid % kCols, way = tid / kCols;
   float x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
   for (int k = way; k < parts; k += kWays) {
-    if (empty(k)) continue;
     const float f = s_w[k] == M ? 1.f : ex2(s_w[k] - M);
     const size_t at = static_cast<size_t>(part_of(k)) * kRows + r;
     const float4 o = *reinterpret_cast<const float4*>(os + at * DP + col * 4);
