@@ -98,7 +98,7 @@ typedef struct {
  * 2, ld or out_ld < V, mask_ld * 32 < V, a negative width, count or stride, a mask value
  * that is not finite; without mask_rows, mask_count < B * P.  ASYMSPEC_ERR_UNSUPPORTED:
  * dtype.  ASYMSPEC_ERR_MISALIGNED.  ASYMSPEC_ERR_TOO_LARGE: P > ASYMSPEC_CONSTRAIN_MAX_P,
- * B > 65535 or V > 2^30.  B = 0 or P = 0 is a no-op. */
+ * B > 65535 or V > 2^25.  B = 0 or P = 0 is a no-op. */
 #define ASYMSPEC_CONSTRAIN_MAX_P 256
 int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits, int64_t ld,
                               void* out, int64_t out_ld, int B, int P, int V, int dtype,

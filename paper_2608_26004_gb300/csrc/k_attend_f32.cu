@@ -7,7 +7,7 @@ namespace asymspec_impl {
 template <int DP, int MT, int ST>
 AttendKernels attend_pick() {
   constexpr int smem = static_cast<int>(attend_smem_bytes<float>(DP, MT, ST));
-  static_assert(smem <= kMaxSmem - 2048, "the rings fit");
+  static_assert(smem <= kMaxSmem - 8192, "the rings fit");
   return {reinterpret_cast<const void*>(&attend_split<float, DP, MT, ST>),
           reinterpret_cast<const void*>(&attend_join<float, DP, MT>), DP, 16 * MT, smem,
           smem <= 112 * 1024 ? 2 : 1};

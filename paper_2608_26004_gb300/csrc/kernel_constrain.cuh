@@ -14,46 +14,132 @@ struct CParams {
   void* out;
   int64_t ld, out_ld;
   int B, P, V;
+  int W;           // vocabulary entries of a CTA, a power of two from 1024 on
+  int group_rows;  // rows of a CTA (blockIdx.z: which)
+  int batch_rows;  // rows that come into shared memory together
   uint32_t* err;
 };
 
 constexpr int kCThreads = 256;
-constexpr int kCSlice = 4096;           // vocabulary entries of a CTA
-constexpr unsigned kCPrompt = 1u << 31;  // the token is in the prompt; below: its output count
+constexpr int kCUnroll = 4;
+constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
+constexpr int kCMaxCluster = 8;
+constexpr int kCBiases = 512;  // a slice's bias entries that shared memory holds
+// A token's word: in the prompt, among the drafts, biased, and how often in the output.
+constexpr unsigned kCPrompt = 1u << 31, kCDraft = 1u << 30, kCBias = 1u << 29, kCCount = kCBias - 1;
+
+// Dynamic shared memory: the words and the list of those that are not zero; then the rows
+// of the slice at hand, each with room for the 16-byte boundaries around it.
+__host__ __device__ constexpr size_t constrain_list_bytes(int W) { return static_cast<size_t>(W) * 6; }
+__host__ __device__ constexpr int constrain_pitch(int W, int elt) { return W * elt + 32; }
 
 __device__ __forceinline__ float type_max(float) { return FLT_MAX; }
 __device__ __forceinline__ float type_max(__nv_bfloat16) { return __uint_as_float(0x7F7F0000u); }
-__device__ __forceinline__ void store1(float* p, float y) { *p = y; }
-__device__ __forceinline__ void store1(__nv_bfloat16* p, float y) { *p = __float2bfloat16_rn(y); }
+__device__ __forceinline__ float from_f32(float y, float) { return y; }
+__device__ __forceinline__ __nv_bfloat16 from_f32(float y, __nv_bfloat16) { return __float2bfloat16_rn(y); }
 
-// One CTA per slice of the vocabulary and request: the history's counts of its slice in
-// shared memory, then the request's rows in order, each draft counted after its row.
+// 16 bytes of consecutive entries off the 16-byte boundaries.
+__device__ __forceinline__ uint4 gather16(const float* p) {
+  return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+}
+__device__ __forceinline__ uint4 gather16(const __nv_bfloat16* q) {
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(q);
+  return make_uint4(p[0] | static_cast<unsigned>(p[1]) << 16, p[2] | static_cast<unsigned>(p[3]) << 16,
+                    p[4] | static_cast<unsigned>(p[5]) << 16, p[6] | static_cast<unsigned>(p[7]) << 16);
+}
+
+// The entries whose bit is not set become `low` (a word of the type's entries).
 template <typename T>
-__global__ void __launch_bounds__(kCThreads) constrain_kernel(const CParams p) {
-  extern __shared__ unsigned c_smem[];
-  unsigned* cnt = c_smem;
-  int* bias_at = reinterpret_cast<int*>(c_smem + kCSlice);  // 1 + the entry of a biased token
+__device__ __forceinline__ uint4 masked16(uint4 v, unsigned bits, unsigned low) {
+  if constexpr (sizeof(T) == 4)
+    return make_uint4(bits & 1u ? v.x : low, bits & 2u ? v.y : low, bits & 4u ? v.z : low, bits & 8u ? v.w : low);
+  // bf16: a byte permutation a word, its selector from the bits of four entries at once
+  // (each bit to a byte of its own; a half's bytes are numbered 4 less in v than in low)
+  const unsigned a = 0x76547654u - (((bits & 15u) * 0x204081u) & 0x01010101u) * 0x44u;
+  const unsigned b = 0x76547654u - (((bits >> 4) * 0x204081u) & 0x01010101u) * 0x44u;
+  return make_uint4(__byte_perm(v.x, low, a), __byte_perm(v.y, low, a >> 16), __byte_perm(v.z, low, b),
+                    __byte_perm(v.w, low, b >> 16));
+}
+
+// The mask bits of the 16 / sizeof(T) tokens from v on.
+template <typename T>
+__device__ __forceinline__ unsigned mask_bits(const uint32_t* mask, int v) {
+  constexpr int VE = 16 / sizeof(T);
+  const int sh = v & 31;
+  const uint32_t lo = mask[v >> 5], hi = sh + VE > 32 ? mask[(v >> 5) + 1] : 0u;
+  return __funnelshift_r(lo, hi, sh) & ((1u << VE) - 1u);
+}
+
+// Entries of a row's slice before its first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ int entries_before(const T* p) {
+  return static_cast<int>((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / static_cast<int>(sizeof(T));
+}
+
+// What the CTA's slice of the vocabulary needs of the request: words and the list of those
+// that are not zero, and the slice's biases.
+struct Slice {
+  unsigned* words;
+  uint16_t* list;
+  int2* bias;  // [kCBiases]: entry of the slice, entry of the biases
+  int *listed, *biases;
+  int b, v0, n, W;
+};
+
+// The tokens of the history are counted in shared memory: each CTA reads all of it (from
+// the L2) and counts its slice's, or, where histories are long (CLUSTER), the CTAs of a
+// cluster read a share each and count a token where its slice is.  Ends at a barrier; the
+// words are zero at the start, which a barrier before says.
+template <bool CLUSTER>
+__device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s) {
   const asymspec_constraints& c = p.c;
-  const int b = blockIdx.y, v0 = blockIdx.x * kCSlice, n = min(kCSlice, p.V - v0);
-  const int tid = threadIdx.x;
+  const int b = s.b, v0 = s.v0, n = s.n, W = s.W, tid = threadIdx.x;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = CLUSTER ? static_cast<int>(cluster.num_blocks()) : 1;
+  const int rank = CLUSTER ? static_cast<int>(cluster.block_rank()) : 0;
   unsigned err = 0;
-  for (int i = tid; i < kCSlice; i += kCThreads) {
-    cnt[i] = 0;
-    if (c.bias_offsets) bias_at[i] = 0;
-  }
-  __syncthreads();
   if (c.history) {
     const int len0 = c.history_len[b], len = min(max(len0, 0), c.history_width);
     const int pl0 = c.prompt_len ? c.prompt_len[b] : 0, pl = min(max(pl0, 0), len);
     if (len != len0 || pl != pl0) err |= ASYMSPEC_DATA_BAD_LENGTH;
     const int32_t* h = c.history + b * c.history_ld;
-    for (int i = tid; i < len; i += kCThreads) {
-      const int v = h[i];
+    const int first = v0 - rank * W;  // of the cluster's entries
+    auto count = [&](int v, int i) {
       if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (v >= v0 && v < v0 + n) {
-        if (i < pl) atomicOr(&cnt[v - v0], kCPrompt);
-        else atomicAdd(&cnt[v - v0], 1u);
+      else if (static_cast<unsigned>(v - first) < static_cast<unsigned>(C * W)) {
+        unsigned* word = s.words + ((v - first) & (W - 1));
+        if constexpr (CLUSTER) word = cluster.map_shared_rank(word, (v - first) / W);
+        if (i < pl) atomicOr(word, kCPrompt);
+        else atomicAdd(word, 1u);
       }
+    };
+    // four tokens a load from the first 16-byte boundary on
+    const int head = min(entries_before(h), len), fours = (len - head) / 4;
+    const int end = head + fours * 4;
+    if (rank == 0 && tid < head) count(h[tid], tid);
+    if (rank == 0 && tid < len - end) count(h[end + tid], end + tid);
+    const int4* h4 = reinterpret_cast<const int4*>(h + head);
+    for (int i0 = rank * kCThreads * kCUnroll + tid; i0 < fours; i0 += C * kCThreads * kCUnroll) {
+      int4 v[kCUnroll];
+#pragma unroll
+      for (int e = 0; e < kCUnroll; ++e)
+        if (i0 + e * kCThreads < fours) v[e] = h4[i0 + e * kCThreads];
+#pragma unroll
+      for (int e = 0; e < kCUnroll; ++e) {
+        if (i0 + e * kCThreads >= fours) break;
+        const int i = head + (i0 + e * kCThreads) * 4;
+        count(v[e].x, i);
+        count(v[e].y, i + 1);
+        count(v[e].z, i + 2);
+        count(v[e].w, i + 3);
+      }
+    }
+  }
+  if (c.drafts) {
+    for (int j = tid; j < p.P - 1; j += kCThreads) {
+      const int v = c.drafts[b * c.drafts_ld + j];
+      if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
+      else if (v >= v0 && v < v0 + n) atomicOr(&s.words[v - v0], kCDraft);
     }
   }
   if (c.bias_offsets) {
@@ -63,56 +149,314 @@ __global__ void __launch_bounds__(kCThreads) constrain_kernel(const CParams p) {
     for (int i = a + tid; i < e; i += kCThreads) {
       const int v = c.bias_tokens[i];
       if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (v >= v0 && v < v0 + n) atomicMax(&bias_at[v - v0], i + 1);
-    }
-  }
-  float rep = c.repetition ? c.repetition[b] : 1.f, freq = c.frequency ? c.frequency[b] : 0.f,
-        pres = c.presence ? c.presence[b] : 0.f;
-  if (!(rep > 0.f && rep <= FLT_MAX && fabsf(freq) <= FLT_MAX && fabsf(pres) <= FLT_MAX)) {
-    err |= ASYMSPEC_DATA_BAD_PENALTY;
-    rep = 1.f;
-    freq = pres = 0.f;
-  }
-  const float top = type_max(T());
-  const float low = fminf(fmaxf(c.mask_value, -top), top);
-  for (int k = 0; k < p.P; ++k) {
-    __syncthreads();
-    const int64_t r = static_cast<int64_t>(b) * p.P + k;
-    const T* x = static_cast<const T*>(p.logits) + r * p.ld + v0;
-    T* y = static_cast<T*>(p.out) + r * p.out_ld + v0;
-    const uint32_t* mask = nullptr;
-    bool none = false;
-    if (c.mask) {
-      const int at = c.mask_rows ? c.mask_rows[r] : static_cast<int>(r);
-      none = at < -1 || at >= c.mask_count;
-      if (none) err |= ASYMSPEC_DATA_BAD_INDEX;
-      if (!none && at >= 0) mask = c.mask + at * c.mask_ld;
-    }
-    for (int i = tid; i < n; i += kCThreads) {
-      const unsigned w = cnt[i];
-      const int bi = c.bias_offsets ? bias_at[i] : 0;
-      const T raw = x[i];
-      if (none || (mask && !((mask[(v0 + i) >> 5] >> ((v0 + i) & 31)) & 1u))) store1(y + i, low);
-      else if (w == 0 && bi == 0) y[i] = raw;
-      else {
-        const float z = to_f32(raw);
-        float s = z;
-        if (w) {
-          const float m = static_cast<float>(w & ~kCPrompt);
-          s = z > 0.f ? z / rep : z * rep;
-          s -= freq * m;
-          s -= m > 0.f ? pres : 0.f;
-        }
-        if (bi) s += c.bias_values[bi - 1];
-        if (fabsf(z) <= FLT_MAX) s = fminf(fmaxf(s, -top), top);
-        store1(y + i, s);
+      else if (v >= v0 && v < v0 + n) {
+        atomicOr(&s.words[v - v0], kCBias);
+        const int at = atomicAdd(s.biases, 1);
+        if (at < kCBiases) s.bias[at] = make_int2(v - v0, i);
       }
     }
-    if (k + 1 < p.P && c.drafts) {
-      __syncthreads();
-      const int v = c.drafts[b * c.drafts_ld + k];
-      if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (tid == 0 && v >= v0 && v < v0 + n) ++cnt[v - v0];
+  }
+  if constexpr (CLUSTER) cluster.sync();
+  else __syncthreads();
+  return err;
+}
+
+// The list of the words that are not zero (in any order); a barrier has to follow.
+__device__ __forceinline__ void list_slice(const Slice& s) {
+  for (int i0 = threadIdx.x * 8; i0 < s.W; i0 += kCThreads * 8) {
+    const uint4 f = *reinterpret_cast<const uint4*>(s.words + i0);
+    const uint4 g = *reinterpret_cast<const uint4*>(s.words + i0 + 4);
+    if ((f.x | f.y | f.z | f.w | g.x | g.y | g.z | g.w) == 0) continue;
+    const unsigned w[8] = {f.x, f.y, f.z, f.w, g.x, g.y, g.z, g.w};
+    int at = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) at += w[e] != 0;
+    at = atomicAdd(s.listed, at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (w[e] != 0) s.list[at++] = static_cast<uint16_t>(i0 + e);
+  }
+}
+
+struct Penalties {
+  float rep, freq, pres, top;
+  __device__ __forceinline__ Penalties(const CParams& p, int b, float top_, unsigned& err) : top(top_) {
+    const asymspec_constraints& c = p.c;
+    rep = c.repetition ? c.repetition[b] : 1.f;
+    freq = c.frequency ? c.frequency[b] : 0.f;
+    pres = c.presence ? c.presence[b] : 0.f;
+    if (!(rep > 0.f && rep <= FLT_MAX && fabsf(freq) <= FLT_MAX && fabsf(pres) <= FLT_MAX)) {
+      err |= ASYMSPEC_DATA_BAD_PENALTY;
+      rep = 1.f;
+      freq = pres = 0.f;
+    }
+  }
+};
+
+// One entry of the list: its word, bias, and how often its token came up to a row.
+struct Touched {
+  int v;
+  unsigned w, count;
+  float bias;
+  __device__ __forceinline__ Touched(const CParams& p, const Slice& s, int i, int k0)
+      : v(s.v0 + i), w(s.words[i]), count(w & kCCount), bias(0.f) {
+    const asymspec_constraints& c = p.c;
+    if (w & kCBias) {
+      int last = -1;
+      if (*s.biases <= kCBiases) {
+        for (int j = 0; j < *s.biases; ++j)
+          if (s.bias[j].x == i) last = max(last, s.bias[j].y);
+      } else {
+        const int a = min(max(c.bias_offsets[s.b], 0), c.bias_count);
+        const int e = min(max(c.bias_offsets[s.b + 1], a), c.bias_count);
+        for (int j = a; j < e; ++j)
+          if (c.bias_tokens[j] == v) last = j;
+      }
+      bias = c.bias_values[last];
+    }
+    if (w & kCDraft)
+      for (int j = 0; j < k0; ++j) count += c.drafts[s.b * c.drafts_ld + j] == v;
+  }
+  __device__ __forceinline__ float value(const Penalties& r, float z) const {
+    float f = z;
+    if (count != 0 || (w & kCPrompt)) f = f > 0.f ? f / r.rep : f * r.rep;
+    if (count != 0) f = (f - r.freq * static_cast<float>(count)) - r.pres;
+    if (w & kCBias) f += bias;
+    return fabsf(z) <= FLT_MAX ? fminf(fmaxf(f, -r.top), r.top) : f;
+  }
+  // past row k
+  __device__ __forceinline__ void past(const CParams& p, const Slice& s, int k) {
+    if ((w & kCDraft) && k < p.P - 1) count += p.c.drafts[s.b * p.c.drafts_ld + k] == v;
+  }
+};
+
+// The mask of row r: its row of bits, -1: none, -2: it allows nothing.
+__device__ __forceinline__ int mask_of(const CParams& p, int64_t r, unsigned& err) {
+  if (!p.c.mask) return -1;
+  const int at = p.c.mask_rows ? p.c.mask_rows[r] : static_cast<int>(r);
+  if (at >= -1 && at < p.c.mask_count) return at;
+  err |= ASYMSPEC_DATA_BAD_INDEX;
+  return -2;
+}
+__device__ __forceinline__ bool allowed(const CParams& p, int at, int v) {
+  return at == -1 || (at >= 0 && ((p.c.mask[at * p.c.mask_ld + (v >> 5)] >> (v & 31)) & 1u));
+}
+
+// The constrained rows in another place than the logits: one CTA per slice of the
+// vocabulary, request and group of rows.  The rows' slices come into shared memory by
+// cp.async while the history is counted; the entries that a penalty or a bias touches,
+// gathered in a list so that no lane is idle, are computed there (scattered over the
+// rows in global memory they took longer than the rows); then the rows leave under
+// their masks.  A vector that its row's mask leaves nothing of is not read.  The
+// slices of the lowest token ids, which a vocabulary gives to the most frequent tokens,
+// come first in the grid: theirs are the most entries to compute.
+template <typename T, bool EDGES, bool CLUSTER>
+__global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) {
+  extern __shared__ __align__(16) unsigned c_smem[];
+  __shared__ int2 s_bias[kCBiases];
+  __shared__ uint8_t s_bits[EDGES ? 1 : kCSlots][kCThreads];
+  __shared__ int s_listed, s_biases;
+  constexpr int VE = 16 / sizeof(T);
+  constexpr unsigned kAll = (1u << VE) - 1u;
+  const asymspec_constraints& c = p.c;
+  const int W = p.W, b = blockIdx.x, v0 = blockIdx.y * W, n = min(W, p.V - v0), tid = threadIdx.x;
+  const Slice slice = {c_smem, reinterpret_cast<uint16_t*>(c_smem + W), s_bias, &s_listed, &s_biases, b, v0, n, W};
+  const int pitch = constrain_pitch(W, sizeof(T));
+  unsigned char* tile = reinterpret_cast<unsigned char*>(c_smem) + constrain_list_bytes(W);
+  const int k_end = min((static_cast<int>(blockIdx.z) + 1) * p.group_rows, p.P);
+  const int k0 = blockIdx.z * p.group_rows;
+  unsigned err = 0;
+  const T* x = static_cast<const T*>(p.logits) + (static_cast<int64_t>(b) * p.P + k0) * p.ld + v0;
+  T* y = static_cast<T*>(p.out) + (static_cast<int64_t>(b) * p.P + k0) * p.out_ld + v0;
+  auto misplaced = [&](const T* row) {  // bytes from the 16-byte boundary at or before it
+    return EDGES ? static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15u) : 0;
+  };
+
+  // A batch of rows on its way into shared memory.  A thread's vectors of it are slots 0, 1, ..,
+  // row by row; the bits that the masks allow wait in shared memory for the rows to leave.
+  const int batch = p.batch_rows, per_row = W / VE / kCThreads;
+  auto begin = [&](int first_row, int rows) {
+    const T* from = x + static_cast<int64_t>(first_row) * p.ld;
+    if constexpr (!EDGES) {
+#pragma unroll
+      for (int s0 = 0; s0 < kCSlots; s0 += kCUnroll) {
+        if (s0 >= per_row * rows) break;
+        int at[kCUnroll], k[kCUnroll], i[kCUnroll];
+        unsigned got[kCUnroll];
+#pragma unroll
+        for (int s = 0; s < kCUnroll; ++s) {
+          k[s] = (s0 + s) / per_row;
+          i[s] = (s0 + s) % per_row * kCThreads + tid;
+          at[s] = -2;
+          if (k[s] < rows && i[s] * VE < n) at[s] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k[s], err);
+        }
+#pragma unroll
+        for (int s = 0; s < kCUnroll; ++s) {
+          got[s] = at[s] == -1 ? kAll : 0u;
+          if (at[s] >= 0) {
+            const uint8_t* mask = reinterpret_cast<const uint8_t*>(c.mask + at[s] * c.mask_ld + (v0 >> 5));
+            got[s] = VE == 8 ? mask[i[s]] : (mask[i[s] >> 1] >> ((i[s] & 1) * 4)) & kAll;
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < kCUnroll; ++s) {
+          if (got[s] != 0) cp_async16(tile + k[s] * pitch + i[s] * 16, from + k[s] * p.ld + i[s] * VE);
+          s_bits[s0 + s][tid] = static_cast<uint8_t>(got[s]);
+        }
+      }
+    } else {
+      for (int k = 0; k < rows; ++k) {
+        const T* row = from + k * p.ld;
+        const int off = misplaced(row), first = off / static_cast<int>(sizeof(T));
+        for (int j = tid; j * VE - first < n; j += kCThreads) {
+          const int e0 = j * VE - first;
+          if (e0 < 0 || e0 + VE > n) {
+            for (int e = max(e0, 0); e < min(e0 + VE, n); ++e)
+              *reinterpret_cast<T*>(tile + k * pitch + off + e * sizeof(T)) = row[e];
+          } else {
+            cp_async16(tile + k * pitch + j * 16, row + e0);
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  if (tid == 0) s_listed = s_biases = 0;
+  for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
+  begin(0, min(batch, k_end - k0));
+  if constexpr (CLUSTER) cg::this_cluster().sync();
+  else __syncthreads();
+  err |= count_slice<CLUSTER>(p, slice);
+  if (CLUSTER && n <= 0) return;
+  list_slice(slice);
+  const float top = type_max(T());
+  const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());
+  unsigned low_word;
+  if constexpr (sizeof(T) == 4) low_word = __float_as_uint(low);
+  else low_word = __bfloat16_as_ushort(low) * 0x10001u;
+  const Penalties penalties(p, b, top, err);
+  for (int first_row = 0;;) {
+    const int rows = min(batch, k_end - k0 - first_row);
+    const T* xt = x + static_cast<int64_t>(first_row) * p.ld;
+    T* yt = y + static_cast<int64_t>(first_row) * p.out_ld;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    for (int q = tid; q < s_listed; q += kCThreads) {
+      const int i = slice.list[q];
+      Touched u(p, slice, i, k0 + first_row);
+#pragma unroll 4
+      for (int k = 0; k < rows; ++k) {
+        T* cell = reinterpret_cast<T*>(tile + k * pitch + misplaced(xt + k * p.ld)) + i;
+        *cell = from_f32(u.value(penalties, to_f32(*cell)), T());
+        u.past(p, slice, k0 + first_row + k);
+      }
+    }
+    __syncthreads();
+    if constexpr (!EDGES) {
+#pragma unroll 4
+      for (int s = 0; s < per_row * rows; ++s) {
+        const int k = per_row == 1 ? s : s / per_row, i = (per_row == 1 ? 0 : s % per_row) * kCThreads + tid;
+        if (i * VE >= n) continue;
+        const unsigned on = s_bits[s][tid];
+        uint4 v = make_uint4(low_word, low_word, low_word, low_word);
+        if (on != 0) {
+          v = *reinterpret_cast<const uint4*>(tile + k * pitch + i * 16);
+          if (on != kAll) v = masked16<T>(v, on, low_word);
+        }
+        *reinterpret_cast<uint4*>(yt + k * p.out_ld + i * VE) = v;
+      }
+    } else {
+      for (int k = 0; k < rows; ++k) {
+        T* row = yt + k * p.out_ld;
+        const T* from = reinterpret_cast<const T*>(tile + k * pitch + misplaced(xt + k * p.ld));
+        const int first = misplaced(row) / static_cast<int>(sizeof(T));
+        const int at = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k, err);
+        const uint32_t* mask = c.mask + (at > 0 ? at : 0) * c.mask_ld + (v0 >> 5);
+        for (int j = tid; j * VE - first < n; j += kCThreads) {
+          const int e0 = j * VE - first;
+          if (e0 < 0 || e0 + VE > n) {
+            for (int e = max(e0, 0); e < min(e0 + VE, n); ++e) row[e] = allowed(p, at, v0 + e) ? from[e] : low;
+          } else {
+            const unsigned on = at < 0 ? (at == -1 ? kAll : 0u) : mask_bits<T>(mask, e0);
+            uint4 v = reinterpret_cast<uintptr_t>(from + e0) % 16 == 0
+                          ? *reinterpret_cast<const uint4*>(from + e0) : gather16(from + e0);
+            if (on != kAll) v = masked16<T>(v, on, low_word);
+            *reinterpret_cast<uint4*>(row + e0) = v;
+          }
+        }
+      }
+    }
+    first_row += rows;
+    if (k0 + first_row >= k_end) break;
+    __syncthreads();
+    begin(first_row, min(batch, k_end - k0 - first_row));
+  }
+  if (err && p.err) atomicOr(p.err, err);
+}
+
+// The logits constrained where they are: what nothing changes is neither read nor written.
+// The masked entries are overwritten, a row's vectors at a time; then the entries that a
+// penalty or a bias touches are computed, each where it lies.
+template <typename T, bool CLUSTER>
+__global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p) {
+  extern __shared__ __align__(16) unsigned c_smem[];
+  __shared__ int2 s_bias[kCBiases];
+  __shared__ int s_mask[ASYMSPEC_CONSTRAIN_MAX_P];
+  __shared__ int s_listed, s_biases;
+  constexpr int VE = 16 / sizeof(T);
+  constexpr unsigned kAll = (1u << VE) - 1u;
+  const asymspec_constraints& c = p.c;
+  const int W = p.W, b = blockIdx.x, v0 = blockIdx.y * W, n = min(W, p.V - v0), tid = threadIdx.x;
+  const Slice slice = {c_smem, reinterpret_cast<uint16_t*>(c_smem + W), s_bias, &s_listed, &s_biases, b, v0, n, W};
+  const int k0 = blockIdx.z * p.group_rows, rows = min(p.group_rows, p.P - k0);
+  unsigned err = 0;
+  if (tid == 0) s_listed = s_biases = 0;
+  for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
+  for (int k = tid; k < rows; k += kCThreads)
+    s_mask[k] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + k, err);
+  if constexpr (CLUSTER) cg::this_cluster().sync();
+  else __syncthreads();
+  err |= count_slice<CLUSTER>(p, slice);
+  if (CLUSTER && n <= 0) return;
+  list_slice(slice);
+  const float top = type_max(T());
+  const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());
+  unsigned low_word;
+  if constexpr (sizeof(T) == 4) low_word = __float_as_uint(low);
+  else low_word = __bfloat16_as_ushort(low) * 0x10001u;
+  const Penalties penalties(p, b, top, err);
+  T* x = static_cast<T*>(p.out) + (static_cast<int64_t>(b) * p.P + k0) * p.out_ld + v0;
+  for (int k = 0; k < rows; ++k) {
+    const int at = s_mask[k];
+    if (at == -1) continue;
+    T* row = x + k * p.out_ld;
+    const int first = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15u) / static_cast<int>(sizeof(T));
+    for (int j = tid; j * VE - first < n; j += kCThreads) {
+      const int e0 = j * VE - first;
+      if (e0 < 0 || e0 + VE > n) {
+        for (int e = max(e0, 0); e < min(e0 + VE, n); ++e)
+          if (!allowed(p, at, v0 + e)) row[e] = low;
+        continue;
+      }
+      const unsigned on = at < 0 ? 0u : mask_bits<T>(c.mask + at * c.mask_ld + (v0 >> 5), e0);
+      if (on == kAll) continue;
+      uint4 v = make_uint4(low_word, low_word, low_word, low_word);
+      if (on != 0) v = masked16<T>(*reinterpret_cast<const uint4*>(row + e0), on, low_word);
+      *reinterpret_cast<uint4*>(row + e0) = v;
+    }
+  }
+  __syncthreads();  // the list; the masked entries before the others
+  for (int q = tid; q < s_listed; q += kCThreads) {
+    const int i = slice.list[q];
+    Touched t(p, slice, i, k0);
+#pragma unroll 4
+    for (int k = 0; k < rows; ++k) {
+      if (allowed(p, s_mask[k], t.v)) {
+        T* cell = x + k * p.out_ld + i;
+        *cell = from_f32(t.value(penalties, to_f32(*cell)), T());
+      }
+      t.past(p, slice, k0 + k);
     }
   }
   if (err && p.err) atomicOr(p.err, err);

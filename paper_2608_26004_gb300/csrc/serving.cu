@@ -1,7 +1,8 @@
 // Host side of the C ABI declared in include/asymspec_serving.h: argument checks and
 // launches of the operators around the verification step.
 //
-//   constrain_kernel    (kernel_constrain.cuh) penalties, biases and masks on logits
+//   constrain_rows      (kernel_constrain.cuh) penalties, biases and masks on logits;
+//                       constrain_in_place where they are
 //   cache_plan_kernel   (kernel_cache.cuh) block tables and slot maps
 //   cache_write_kernel  (kernel_cache.cuh) new keys and values into the cache
 //   attend_split        (kernel_attend.cuh) attention over the cache, the keys split evenly
@@ -28,7 +29,9 @@ int elt_size(int dtype) { return dtype == ASYMSPEC_FP32 ? 4 : 2; }
 
 bool known_dtype(int dtype) { return dtype == ASYMSPEC_FP32 || dtype == ASYMSPEC_BF16; }
 
-// Once per kernel and device: room for its dynamic shared memory.
+constexpr int kStaticSmem = 8192;  // what a kernel has beside its dynamic shared memory at most
+
+// Once per kernel and device: room for all the dynamic shared memory that it may ask for.
 struct Prepared {
   const void* fn;
   int device;
@@ -38,13 +41,37 @@ Prepared g_prepared[64];
 int g_prepared_count = 0;
 
 cudaError_t prepare(const void* fn, int device, int smem) {
-  if (smem <= 47 * 1024) return cudaSuccess;
+  if (smem <= 48 * 1024 - kStaticSmem) return cudaSuccess;
   std::lock_guard<std::mutex> lock(g_mu);
   for (int i = 0; i < g_prepared_count; ++i)
     if (g_prepared[i].fn == fn && g_prepared[i].device == device) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - kStaticSmem);
   if (e == cudaSuccess && g_prepared_count < 64) g_prepared[g_prepared_count++] = {fn, device};
   return e;
+}
+
+cudaError_t device_sms(int* device, int* sms) {
+  const cudaError_t e = cudaGetDevice(device);
+  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device) : e;
+}
+
+// A CTA's slice of the vocabulary in 16-byte vectors, and the vectors that a thread has at
+// least, of one row or of several.
+constexpr int kVectors = 256;
+constexpr int kThreadVectors = 4;
+// Histories that may be longer than this are counted by clusters.
+constexpr int kLongHistory = 16384;
+
+template <typename T>
+const void* constrain_pick(bool in_place, bool edges, bool clusters) {
+  if (in_place)
+    return clusters ? reinterpret_cast<const void*>(&constrain_in_place<T, true>)
+                    : reinterpret_cast<const void*>(&constrain_in_place<T, false>);
+  if (edges)
+    return clusters ? reinterpret_cast<const void*>(&constrain_rows<T, true, true>)
+                    : reinterpret_cast<const void*>(&constrain_rows<T, true, false>);
+  return clusters ? reinterpret_cast<const void*>(&constrain_rows<T, false, true>)
+                  : reinterpret_cast<const void*>(&constrain_rows<T, false, false>);
 }
 
 AttendKernels attend_kernels(int dtype, int D, int rows) {
@@ -53,9 +80,12 @@ AttendKernels attend_kernels(int dtype, int D, int rows) {
 
 int launch(const void* fn, dim3 grid, dim3 block, size_t smem, void* params, void* stream) {
   cudaError_t e = cudaSuccess;
-  if (smem > 47 * 1024)
-    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  if (e != cudaSuccess) return cuda_fail(e);
+  if (smem > 48 * 1024 - kStaticSmem) {
+    int device = 0;
+    e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = prepare(fn, device, static_cast<int>(smem));
+    if (e != cudaSuccess) return cuda_fail(e);
+  }
   void* args[] = {params};
   e = cudaLaunchKernel(fn, grid, block, args, smem, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
@@ -110,7 +140,7 @@ int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits,
                               uint32_t* out_error_word, void* stream) {
   if (!known_dtype(dtype)) return ASYMSPEC_ERR_UNSUPPORTED;
   if (!c || B < 0 || P < 0 || V < 2 || ld < V || out_ld < V) return ASYMSPEC_ERR_INVALID_ARG;
-  if (P > ASYMSPEC_CONSTRAIN_MAX_P || B > 65535 || V > (1 << 30)) return ASYMSPEC_ERR_TOO_LARGE;
+  if (P > ASYMSPEC_CONSTRAIN_MAX_P || B > 65535 || V > (1 << 25)) return ASYMSPEC_ERR_TOO_LARGE;
   const int st = check_constraints(*c, B, P, V);
   if (st != ASYMSPEC_OK) return st;
   if (B == 0 || P == 0) return ASYMSPEC_OK;
@@ -118,12 +148,48 @@ int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits,
   const int elt = elt_size(dtype);
   if (!aligned(logits, elt) || !aligned(out, elt) || !aligned(out_error_word, 4))
     return ASYMSPEC_ERR_MISALIGNED;
-  CParams p = {*c, logits, out, ld, out_ld, B, P, V, out_error_word};
-  const void* fn = dtype == ASYMSPEC_FP32
-                       ? reinterpret_cast<const void*>(&constrain_kernel<float>)
-                       : reinterpret_cast<const void*>(&constrain_kernel<__nv_bfloat16>);
-  const size_t smem = kCSlice * 4 * (c->bias_offsets ? 2 : 1);
-  return launch(fn, dim3((V + kCSlice - 1) / kCSlice, B), dim3(kCThreads), smem, &p, stream);
+  CParams p = {*c, logits, out, ld, out_ld, B, P, V, 0, P, 0, out_error_word};
+  int device = 0, sms = 0;
+  cudaError_t e = device_sms(&device, &sms);
+  if (e != cudaSuccess) return cuda_fail(e);
+  const int per = 16 / elt;
+  const bool edges = !aligned(logits, 16) || !aligned(out, 16) || ld % per != 0 || out_ld % per != 0 || V % per != 0;
+  // a slice: more of the vocabulary where there are few rows
+  int vectors = kVectors;
+  for (int rows = P; rows < kThreadVectors && vectors < 1024; rows *= 2) vectors *= 2;
+  p.W = vectors * per;
+  const int64_t slices = (V + p.W - 1) / p.W;
+  // enough CTAs for the chip: fewer rows each
+  while (p.group_rows > 1 && slices * B * ((P + p.group_rows - 1) / p.group_rows) < 2 * sms)
+    p.group_rows = (p.group_rows + 1) / 2;
+  const int groups = (P + p.group_rows - 1) / p.group_rows;
+  // batches of one size, kCSlots vectors of a thread at most
+  const int most = kCSlots * kCThreads / vectors, batches = (p.group_rows + most - 1) / most;
+  p.batch_rows = (p.group_rows + batches - 1) / batches;
+  const bool in_place = logits == out;
+  const size_t smem = constrain_list_bytes(p.W) +
+                      (in_place ? 0 : static_cast<size_t>(p.batch_rows) * constrain_pitch(p.W, elt));
+  const bool clusters = c->history && c->history_width > kLongHistory && slices > 1;
+  const int C = clusters ? static_cast<int>(std::min<int64_t>(slices, kCMaxCluster)) : 1;
+  const void* fn = dtype == ASYMSPEC_FP32 ? constrain_pick<float>(in_place, edges, clusters)
+                                          : constrain_pick<__nv_bfloat16>(in_place, edges, clusters);
+  e = prepare(fn, device, static_cast<int>(smem));
+  if (e != cudaSuccess) return cuda_fail(e);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = C;
+  attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(B, static_cast<unsigned>((slices + C - 1) / C * C), groups);
+  cfg.blockDim = dim3(kCThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cfg.attrs = attr;
+  cfg.numAttrs = clusters ? 1 : 0;
+  void* args[] = {&p};
+  e = cudaLaunchKernelExC(&cfg, fn, args);
+  return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
 }
 
 int asymspec_cache_plan(const int32_t* lens, const int32_t* accepted, const int32_t* grow,
@@ -282,8 +348,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   p.ws = static_cast<char*>(workspace);
   p.err = out_error_word;
   int device = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  cudaError_t e = device_sms(&device, &sms);
   if (e == cudaSuccess) e = prepare(k.split, device, k.smem);
   if (e != cudaSuccess) return cuda_fail(e);
   int ctas = std::min(kAMaxCtas, sms * k.ctas_per_sm);
