@@ -19,6 +19,7 @@ struct PlanParams {
 };
 
 constexpr int kPThreads = 1024;
+constexpr int kPCluster = 8;
 
 // Shared memory of the plan kernel: a request's tokens that stay, its blocks before (bit 31:
 // not served) and the prefix sums of tokens, blocks taken and blocks given back.
@@ -53,12 +54,24 @@ __device__ __forceinline__ void scan3(int64_t& a, int& b, int& c, int64_t* wa, i
   __syncthreads();
 }
 
+// One CTA, or (CLUSTER) a cluster of them.  Every CTA goes over all requests by itself (a few
+// numbers each: cheaper than an exchange), then they share the blocks given back, the
+// blocks taken and the slots, each found by a search in the prefix sums, with a barrier
+// between what one part writes and the next reads.
+template <bool CLUSTER>
 __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams p) {
   extern __shared__ int64_t p_smem[];
   __shared__ int64_t wa[32];
   __shared__ int wb[32], wc[32];
   __shared__ int s_taken;
-  const int B = p.B, bs = p.block_size, tid = threadIdx.x;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = CLUSTER ? static_cast<int>(cluster.block_rank()) : 0;
+  const int stride = (CLUSTER ? static_cast<int>(cluster.num_blocks()) : 1) * kPThreads;
+  auto barrier = [&] {
+    if constexpr (CLUSTER) cluster.sync();
+    else __syncthreads();
+  };
+  const int B = p.B, bs = p.block_size, tid = threadIdx.x, at0 = rank * kPThreads + tid;
   int64_t* offs = p_smem;  // [B + 1]
   int* keep_of = reinterpret_cast<int*>(offs + B + 1);
   int* held_of = keep_of + B + 1;
@@ -85,15 +98,17 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
       bool served = true;
       if (k > most) k = most, bad = true;
       keep = static_cast<int>(k);
-      int64_t blocks = (k + g + bs - 1) / bs;
+      int blocks = held;
       if (k + g > most) {  // too long for its table: what it has stays
         bad = true;
         served = false;
-        blocks = held;
+      } else {
+        blocks = static_cast<int>((static_cast<unsigned>(k + g) + static_cast<unsigned>(bs) - 1u) /
+                                  static_cast<unsigned>(bs));
       }
       if (bad) err |= ASYMSPEC_DATA_BAD_LENGTH;
-      more = static_cast<int>(max(blocks - held, static_cast<int64_t>(0)));
-      less = static_cast<int>(max(held - blocks, static_cast<int64_t>(0)));
+      more = max(blocks - held, 0);
+      less = max(held - blocks, 0);
       keep_of[b] = keep;
       held_of[b] = served ? held : held | INT_MIN;
     }
@@ -113,7 +128,7 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
     __syncthreads();
   }
   if (tid == 0) offs[B] = off, more_of[B] = more_sum, less_of[B] = less_sum;
-  __syncthreads();
+  barrier();  // (the inputs are read: outputs may lie over them)
   const int top = free_in + less_sum;
   // who is served; the state of the next call
   for (int b = tid; b < B; b += kPThreads) {
@@ -127,48 +142,91 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
       atomicMax(&s_taken, more_of[b + 1]);
     }
     if (!served) held_of[b] = held | INT_MIN;
+    if (rank != 0) continue;
     const int64_t g = offs[b + 1] - offs[b];
     p.out_start[b] = keep_of[b];
     p.out_len[b] = served ? keep_of[b] + static_cast<int>(g) : keep_of[b];
     p.out_held[b] = held - l + (served ? m : 0);
   }
   if (off > p.capacity) err |= ASYMSPEC_DATA_BAD_LENGTH;
-  for (int b = tid; b <= B; b += kPThreads)
-    p.out_offsets[b] = static_cast<int>(min(offs[b], static_cast<int64_t>(INT_MAX)));
-  // blocks given back go on the stack
-  for (int i = tid; i < less_sum; i += kPThreads) {
-    const int b = find_last(less_of, B, i);
-    const int kept = (held_of[b] & INT_MAX) - (less_of[b + 1] - less_of[b]);
-    const int at = free_in + i;
-    if (at < p.num_blocks) p.free_list[at] = p.tables[b * p.table_ld + kept + i - less_of[b]];
-    else err |= ASYMSPEC_DATA_BAD_LENGTH;
-  }
+  if (rank == 0)
+    for (int b = tid; b <= B; b += kPThreads)
+      p.out_offsets[b] = static_cast<int>(min(offs[b], static_cast<int64_t>(INT_MAX)));
   __syncthreads();
+  // blocks given back go on the stack
+  if (less_sum > 0) {
+    for (int i = at0; i < less_sum; i += stride) {
+      const int b = find_last(less_of, B, i);
+      const int kept = (held_of[b] & INT_MAX) - (less_of[b + 1] - less_of[b]);
+      const int at = free_in + i;
+      if (at < p.num_blocks) p.free_list[at] = p.tables[b * p.table_ld + kept + i - less_of[b]];
+      else err |= ASYMSPEC_DATA_BAD_LENGTH;
+    }
+    barrier();
+  }
   // and blocks are taken off it
   const int taken = s_taken;
-  for (int i = tid; i < taken; i += kPThreads) {
+  for (int i = at0; i < taken; i += stride) {
     const int b = find_last(more_of, B, i);
     const int at = top - 1 - i;
     p.tables[b * p.table_ld + (held_of[b] & INT_MAX) + i - more_of[b]] =
-        at < p.num_blocks ? p.free_list[at] : -1;
+        at < p.num_blocks ? __ldcg(p.free_list + at) : -1;
   }
-  if (tid == 0) *p.out_free = min(top - taken, p.num_blocks);
-  __syncthreads();
-  for (int64_t t = tid; t < p.capacity; t += kPThreads) {
-    int64_t slot = -1;
-    int pos = -1;
-    if (t < off) {
-      const int b = find_last(offs, B, t);
-      if (held_of[b] >= 0) {
-        pos = keep_of[b] + static_cast<int>(t - offs[b]);
-        const int page = p.tables[b * p.table_ld + pos / bs];
-        if (static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks))
-          slot = static_cast<int64_t>(page) * bs + pos % bs;
-        else err |= ASYMSPEC_DATA_BAD_INDEX;
+  if (at0 == 0) *p.out_free = min(top - taken, p.num_blocks);
+  barrier();
+  // kPSlots slots a thread: one search, a division where a block begins
+  constexpr int kPSlots = CLUSTER ? 4 : 1;
+  const bool wide = (reinterpret_cast<uintptr_t>(p.out_slots) & 15u) == 0;
+  const bool wide_pos = (reinterpret_cast<uintptr_t>(p.out_positions) & 15u) == 0;
+  for (int64_t t0 = static_cast<int64_t>(at0) * kPSlots; t0 < p.capacity;
+       t0 += static_cast<int64_t>(stride) * kPSlots) {
+    int64_t slot[kPSlots];
+    __align__(16) int pos[kPSlots];
+    int b = t0 < off ? find_last(offs, B, t0) : 0, left = 0, next = 0;
+    int64_t place = -1;
+#pragma unroll
+    for (int e = 0; e < kPSlots; ++e) {
+      const int64_t t = t0 + e;
+      slot[e] = -1;
+      pos[e] = -1;
+      if (t >= off || t >= p.capacity) continue;
+      if (t >= offs[b + 1]) {
+        do ++b;
+        while (t >= offs[b + 1]);
+        left = 0;
       }
+      if (held_of[b] < 0) continue;
+      if (left == 0) {
+        next = keep_of[b] + static_cast<int>(t - offs[b]);
+        const int page = __ldcg(p.tables + b * p.table_ld + next / bs), at = next % bs;
+        const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
+        if (!there) err |= ASYMSPEC_DATA_BAD_INDEX;
+        place = there ? static_cast<int64_t>(page) * bs + at : -1;
+        left = bs - at;
+      }
+      slot[e] = place;
+      pos[e] = next;
+      if (place >= 0) ++place;
+      ++next;
+      --left;
     }
-    p.out_slots[t] = slot;
-    if (p.out_positions) p.out_positions[t] = pos;
+    if (CLUSTER && wide && t0 + kPSlots <= p.capacity) {
+#pragma unroll
+      for (int e = 0; e + 1 < kPSlots; e += 2)
+        *reinterpret_cast<longlong2*>(p.out_slots + t0 + e) = make_longlong2(slot[e], slot[e + 1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPSlots; ++e)
+        if (t0 + e < p.capacity) p.out_slots[t0 + e] = slot[e];
+    }
+    if (!p.out_positions) continue;
+    if (CLUSTER && wide_pos && t0 + kPSlots <= p.capacity) {
+      *reinterpret_cast<int4*>(p.out_positions + t0) = *reinterpret_cast<const int4*>(pos);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPSlots; ++e)
+        if (t0 + e < p.capacity) p.out_positions[t0 + e] = pos[e];
+    }
   }
   if (err && p.err) atomicOr(p.err, err);
 }

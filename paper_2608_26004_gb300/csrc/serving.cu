@@ -55,6 +55,9 @@ cudaError_t device_sms(int* device, int* sms) {
   return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device) : e;
 }
 
+// Slots above which the plan takes a cluster.
+constexpr int kPlanTokens = 2048;
+
 // A CTA's slice of the vocabulary in 16-byte vectors, and the vectors that a thread has at
 // least, of one row or of several.
 constexpr int kVectors = 256;
@@ -222,8 +225,31 @@ int asymspec_cache_plan(const int32_t* lens, const int32_t* accepted, const int3
   PlanParams p = {lens, accepted, grow, held, free_count, grow_all, B, block_size, num_blocks,
                   table_width, block_tables, free_list, table_ld, out_start, out_len, out_held,
                   out_free_count, out_offsets, out_positions, out_slots, capacity, out_error_word};
-  return launch(reinterpret_cast<const void*>(&cache_plan_kernel), dim3(1), dim3(kPThreads),
-                plan_smem_bytes(B), &p, stream);
+  // a cluster where there is more than a CTA does in one or two goes
+  const bool clusters = capacity > kPlanTokens;
+  const void* fn = clusters ? reinterpret_cast<const void*>(&cache_plan_kernel<true>)
+                            : reinterpret_cast<const void*>(&cache_plan_kernel<false>);
+  const size_t smem = plan_smem_bytes(B);
+  int device = 0;
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024 - kStaticSmem) e = cudaGetDevice(&device);
+  if (e == cudaSuccess) e = prepare(fn, device, static_cast<int>(smem));
+  if (e != cudaSuccess) return cuda_fail(e);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kPCluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(clusters ? kPCluster : 1);
+  cfg.blockDim = dim3(kPThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cfg.attrs = attr;
+  cfg.numAttrs = clusters ? 1 : 0;
+  void* args[] = {&p};
+  e = cudaLaunchKernelExC(&cfg, fn, args);
+  return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
 }
 
 int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void* v,

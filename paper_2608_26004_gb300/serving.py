@@ -11,9 +11,10 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 from . import asymspec as A
-from .asymspec import AsymSpecError, BF16, FP32, OK, _ptr, _stream
+from .asymspec import AsymSpecError, BF16, FP32, OK
 
 DATA_BAD_PENALTY = 0x40
 DATA_BAD_LENGTH = 0x80
@@ -27,10 +28,12 @@ CACHE_MAX_D = 256      # head size that cache_attend takes
 FLT_MAX = 3.4028234663852886e38
 
 _P, _I, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+
 _L2, _L3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
 class Constraints(ctypes.Structure):
+    """asymspec_constraints, for calls by address through lib()."""
     _fields_ = [("history", _P), ("history_ld", _L), ("history_width", ctypes.c_int32),
                 ("history_len", _P), ("prompt_len", _P), ("drafts", _P), ("drafts_ld", _L),
                 ("repetition", _P), ("frequency", _P), ("presence", _P), ("bias_offsets", _P),
@@ -40,10 +43,20 @@ class Constraints(ctypes.Structure):
 
 
 class Cache(ctypes.Structure):
+    """asymspec_cache, for calls by address through lib()."""
     _fields_ = [("keys", _P), ("values", _P), ("key_strides", _L3), ("value_strides", _L3),
                 ("num_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("dtype", ctypes.c_int32)]
+
+
+# The same structs as bytes, filled in one step: field by field took a third of a small
+# call's host time.
+_CONSTRAINTS = struct.Struct("@PqixxxxPPPqPPPPPPixxxxPqixxxxPfxxxx")
+_CACHE = struct.Struct("@PP6q5ixxxx")
+_STRIDES2, _STRIDES3 = struct.Struct("@2q"), struct.Struct("@3q")
+
+torch = None  # imported with the first call: the addresses' side needs no PyTorch
 
 
 _lib = None
@@ -54,19 +67,17 @@ def lib():
     global _lib
     if _lib is None:
         L = A.lib()
-        L.asymspec_constrain_logits.argtypes = [ctypes.POINTER(Constraints), _P, _L, _P, _L, _I, _I,
-                                                _I, _I, _P, _P]
+        L.asymspec_constrain_logits.argtypes = [_P, _P, _L, _P, _L, _I, _I, _I, _I, _P, _P]
         L.asymspec_constrain_logits.restype = _I
         L.asymspec_cache_plan.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P, _L, _I, _P, _P, _P, _P, _P,
                                           _P, _P, _P, _P, _P, _L, _P, _P]
         L.asymspec_cache_plan.restype = _I
-        L.asymspec_cache_write.argtypes = [ctypes.POINTER(Cache), _P, _P, _L2, _L2, _P, _I, _P, _P]
+        L.asymspec_cache_write.argtypes = [_P, _P, _P, _P, _P, _P, _I, _P, _P]
         L.asymspec_cache_write.restype = _I
         L.asymspec_cache_attend_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
         L.asymspec_cache_attend_workspace_bytes.restype = ctypes.c_size_t
-        L.asymspec_cache_attend.argtypes = [ctypes.POINTER(Cache), _P, _L3, _I, _I, _I, _P, _L, _I,
-                                            _P, ctypes.c_float, _I, _P, _L3, _P, _P,
-                                            ctypes.c_size_t, _P, _P]
+        L.asymspec_cache_attend.argtypes = [_P, _P, _P, _I, _I, _I, _P, _L, _I, _P, ctypes.c_float, _I,
+                                            _P, _P, _P, _P, ctypes.c_size_t, _P, _P]
         L.asymspec_cache_attend.restype = _I
         _lib = L
     return _lib
@@ -78,31 +89,52 @@ def cache_attend_workspace_bytes(B: int, Q: int, heads: int, kv_heads: int, head
 
 # ----------------------------------------------------------------- PyTorch
 
-def _dtype(torch, x) -> int:
-    if x.dtype == torch.float32:
-        return FP32
-    if x.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError("tensors must be float32 or bfloat16")
+_DTYPES = {}
 
 
-def _check(name, x, dtype, dev, shape=None):
-    """`x` is None or a contiguous tensor of this type (and shape) on the call's device."""
-    if x is None:
-        return
-    if x.dtype != dtype or x.device != dev or not x.is_contiguous() \
-            or (shape is not None and tuple(x.shape) != shape):
-        want = "x".join(map(str, shape)) + " " if shape is not None else ""
-        raise ValueError(f"{name} must be a contiguous {want}{dtype} tensor on {dev}")
+def _begin():
+    """The library and PyTorch, at the first call on tensors."""
+    global torch
+    import torch as t
+    lib()
+    _DTYPES.update({t.float32: FP32, t.bfloat16: BF16})
+    torch = t
+
+
+def _dtype(x) -> int:
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise TypeError("tensors must be float32 or bfloat16")
+    return dtype
+
+
+def _flat(name, x, dtype, dev, n):
+    """The address of `x`: contiguous, n entries of this type, on device `dev`."""
+    if x.dtype is not dtype or x.get_device() != dev or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on cuda:{dev}")
+    return x.data_ptr()
 
 
 def _rows(name, x, dtype, dev, n):
-    """`x` is None or [n, any] of this type whose rows are contiguous, any distance apart."""
-    if x is None:
-        return
-    if x.dtype != dtype or x.device != dev or x.dim() != 2 or x.shape[0] != n \
-            or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError(f"{name} must be a [{n}, ...] {dtype} tensor with contiguous rows on {dev}")
+    """(address, distance of rows, width) of `x`: [n, width], rows contiguous, any distance apart."""
+    shape, strides = x.shape, x.stride()
+    if x.dtype is not dtype or x.get_device() != dev or len(shape) != 2 or shape[0] != n \
+            or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name} must be a [{n}, ...] {dtype} tensor with contiguous rows on cuda:{dev}")
+    return x.data_ptr(), max(strides[0], shape[1]), shape[1]
+
+
+def _error_word(x, dev):
+    return 0 if x is None else _flat("error_word", x, torch.int32, dev, 1)
+
+
+def _row_distance(name, x, B, P, V):
+    """Elements between the rows of [B, P, V]: contiguous, evenly spaced."""
+    s0, s1, s2 = x.stride()
+    ld = s1 if P > 1 else s0 if B > 1 else V
+    if s2 != 1 or (B > 1 and P > 1 and s0 != P * ld):
+        raise ValueError(f"the rows of {name} must be contiguous and evenly spaced")
+    return ld
 
 
 def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None, drafts=None,
@@ -117,65 +149,69 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
     words] int32, bit v % 32 of word v / 32 set where v is allowed, mask_rows [B, P]
     int32 (-1: none).  A masked logit becomes mask_value (default: the type's lowest).
     Returns `out`, which may be `logits` itself."""
-    import torch
-    if logits.dim() != 3 or not logits.is_cuda:
+    if torch is None:
+        _begin()
+    dev = logits.get_device()
+    if dev < 0 or logits.dim() != 3:
         raise ValueError("logits must be a [B, P, V] CUDA tensor")
     B, P, V = logits.shape
-    dtype, dev, i32, f32 = _dtype(torch, logits), logits.device, torch.int32, torch.float32
+    dtype, i32, f32 = _dtype(logits), torch.int32, torch.float32
+    ld = out_ld = _row_distance("logits", logits, B, P, V)
     if out is None:
-        out = torch.empty(B, P, V, dtype=logits.dtype, device=dev)
-    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
-        raise ValueError("out must have the shape, type and device of logits")
-    lds = []
-    for x in (logits, out):
-        ld = x.stride(1) if P > 1 else x.stride(0) if B > 1 else V
-        if x.stride(2) != 1 or (B > 1 and P > 1 and x.stride(0) != P * ld):
-            raise ValueError("the rows of logits and out must be contiguous and evenly spaced")
-        lds.append(max(ld, V) if B * P <= 1 else ld)
-    _rows("history", history, i32, dev, B)
-    _rows("drafts", drafts, i32, dev, B)
-    if history is not None and history_len is None:
-        raise ValueError("a history needs history_len")
-    if drafts is not None and drafts.shape[1] < P - 1:
-        raise ValueError("drafts must hold P - 1 tokens of each request")
-    for name, x in (("history_len", history_len), ("prompt_len", prompt_len)):
-        _check(name, x, i32, dev, (B,))
-    for name, x in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
-        _check(name, x, f32, dev, (B,))
-    c = Constraints()
+        out = logits.new_empty((B, P, V))
+        out_ld = V
+    elif out is not logits:
+        if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != dev:
+            raise ValueError("out must have the shape, type and device of logits")
+        out_ld = _row_distance("out", out, B, P, V)
+    h = h_ld = h_width = h_len = p_len = d = d_ld = 0
     if history is not None:
-        c.history, c.history_ld, c.history_width = _ptr(history), history.stride(0), history.shape[1]
-    c.history_len, c.prompt_len = _ptr(history_len), _ptr(prompt_len)
-    if drafts is not None and P > 1:
-        c.drafts, c.drafts_ld = _ptr(drafts), drafts.stride(0)
-    c.repetition, c.frequency, c.presence = _ptr(repetition), _ptr(frequency), _ptr(presence)
+        if history_len is None:
+            raise ValueError("a history needs history_len")
+        h, h_ld, h_width = _rows("history", history, i32, dev, B)
+        h_len = _flat("history_len", history_len, i32, dev, B)
+        if prompt_len is not None:
+            p_len = _flat("prompt_len", prompt_len, i32, dev, B)
+    elif history_len is not None or prompt_len is not None:
+        raise ValueError("lengths of no history")
+    if drafts is not None:
+        d, d_ld, width = _rows("drafts", drafts, i32, dev, B)
+        if width < P - 1:
+            raise ValueError("drafts must hold P - 1 tokens of each request")
+    rep = 0 if repetition is None else _flat("repetition", repetition, f32, dev, B)
+    freq = 0 if frequency is None else _flat("frequency", frequency, f32, dev, B)
+    pres = 0 if presence is None else _flat("presence", presence, f32, dev, B)
+    b_at = b_tok = b_val = b_n = m = m_ld = m_n = m_rows = 0
     if bias is not None:
         offsets, tokens, values = bias
-        _check("bias offsets", offsets, i32, dev, (B + 1,))
-        _check("bias tokens", tokens, i32, dev)
-        _check("bias values", values, f32, dev, tuple(tokens.shape))
-        c.bias_offsets, c.bias_tokens, c.bias_values = _ptr(offsets), _ptr(tokens), _ptr(values)
-        c.bias_count = tokens.numel()
+        b_n = tokens.numel()
+        b_at = _flat("bias offsets", offsets, i32, dev, B + 1)
+        b_tok = _flat("bias tokens", tokens, i32, dev, b_n)
+        b_val = _flat("bias values", values, f32, dev, b_n)
     if mask is not None:
-        if mask.dim() != 2:
-            raise ValueError("mask must be [rows, words]")
-        _rows("mask", mask, i32, dev, mask.shape[0])
-        if mask.shape[1] * 32 < V:
+        m_n = mask.shape[0]
+        m, m_ld, width = _rows("mask", mask, i32, dev, m_n)
+        if width * 32 < V:
             raise ValueError("a mask row must hold a bit for every token")
-        c.mask, c.mask_ld, c.mask_count = _ptr(mask), mask.stride(0), mask.shape[0]
-        c.mask_ld = max(c.mask_ld, mask.shape[1])
+        if mask_rows is not None:
+            m_rows = _flat("mask_rows", mask_rows, i32, dev, B * P)
     elif mask_rows is not None:
         raise ValueError("mask_rows without a mask")
-    _check("mask_rows", mask_rows, i32, dev, (B, P))
-    c.mask_rows = _ptr(mask_rows)
-    c.mask_value = -FLT_MAX if mask_value is None else mask_value
-    _check("error_word", error_word, i32, dev, (1,))
-    st = lib().asymspec_constrain_logits(ctypes.byref(c), logits.data_ptr(), lds[0], out.data_ptr(),
-                                         lds[1], B, P, V, dtype, _ptr(error_word),
-                                         _stream(torch, dev))
+    st = _lib.asymspec_constrain_logits(
+        _CONSTRAINTS.pack(h, h_ld, h_width, h_len, p_len, d if P > 1 else 0, d_ld, rep, freq, pres, b_at,
+                          b_tok, b_val, b_n, m, m_ld, m_n, m_rows,
+                          -FLT_MAX if mask_value is None else mask_value),
+        logits.data_ptr(), ld if ld > V else V, out.data_ptr(), out_ld if out_ld > V else V, B, P, V,
+        dtype, 0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
         raise AsymSpecError(st, "asymspec_constrain_logits")
     return out
+
+
+def _stream(dev) -> int:
+    """The handle of device `dev`'s current stream."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw else torch.cuda.current_stream(dev).cuda_stream
 
 
 def cache_plan(lens, tables, held, free_list, free_count, *, block_size, accepted=None, grow=0,
@@ -188,75 +224,79 @@ def cache_plan(lens, tables, held, free_list, free_count, *, block_size, accepte
     Returns a dict of start, len, held [B], free_count [1], offsets [B + 1] int32, slots
     [capacity] int64 and positions [capacity] int32; ``out`` may pass it to fill (with
     start = lens, held = held and free_count = free_count if those need not be kept)."""
-    import torch
-    if not lens.is_cuda or lens.dim() != 1:
+    if torch is None:
+        _begin()
+    dev, i32 = lens.get_device(), torch.int32
+    if dev < 0 or lens.dim() != 1:
         raise ValueError("lens must be a [B] CUDA tensor")
-    B, dev, i32 = lens.shape[0], lens.device, torch.int32
-    each = None if isinstance(grow, int) else grow
-    for name, x in (("lens", lens), ("held", held), ("accepted", accepted), ("grow", each)):
-        _check(name, x, i32, dev, (B,))
-    _rows("tables", tables, i32, dev, B)
-    _check("free_list", free_list, i32, dev)
-    _check("free_count", free_count, i32, dev, (1,))
-    if each is None:
-        capacity = B * grow if capacity is None else capacity
-    elif capacity is None:
-        raise ValueError("grow as a tensor needs a capacity")
+    B = lens.numel()
+    each, all_ = 0, 0
+    if isinstance(grow, int):
+        all_ = grow
+        if capacity is None:
+            capacity = B * grow
+    else:
+        each = _flat("grow", grow, i32, dev, B)
+        if capacity is None:
+            raise ValueError("grow as a tensor needs a capacity")
+    t, t_ld, width = _rows("tables", tables, i32, dev, B)
+    blocks = free_list.numel()
     r = out
     if r is None:
-        ints = torch.empty(4 * B + 2, dtype=i32, device=dev)
-        r = dict(start=ints[:B], len=ints[B:2 * B], held=ints[2 * B:3 * B],
-                 free_count=ints[3 * B:3 * B + 1], offsets=ints[3 * B + 1:],
-                 slots=torch.empty(capacity, dtype=torch.int64, device=dev),
-                 positions=torch.empty(capacity, dtype=i32, device=dev))
+        positions, start, end, kept, left, offsets = lens.new_empty(4 * B + 2 + capacity) \
+            .split_with_sizes((capacity, B, B, B, 1, B + 1))
+        r = {"start": start, "len": end, "held": kept, "free_count": left, "offsets": offsets,
+             "slots": lens.new_empty(capacity, dtype=torch.int64), "positions": positions}
+        at = (start.data_ptr(), end.data_ptr(), kept.data_ptr(), left.data_ptr(), offsets.data_ptr(),
+              r["slots"].data_ptr(), positions.data_ptr())
     else:
-        for name, shape in (("start", (B,)), ("len", (B,)), ("held", (B,)), ("free_count", (1,)),
-                            ("offsets", (B + 1,)), ("positions", (capacity,))):
-            _check(name, r[name], i32, dev, shape)
-        _check("slots", r["slots"], torch.int64, dev, (capacity,))
-    _check("error_word", error_word, i32, dev, (1,))
-    width = tables.shape[1]
-    st = lib().asymspec_cache_plan(
-        lens.data_ptr(), _ptr(accepted), _ptr(each), grow if each is None else 0, B, block_size,
-        free_list.numel(), tables.data_ptr(), max(tables.stride(0), width), width, held.data_ptr(),
-        free_list.data_ptr(), free_count.data_ptr(), _ptr(r["start"]), _ptr(r["len"]),
-        _ptr(r["held"]), _ptr(r["free_count"]), _ptr(r["offsets"]), _ptr(r["slots"]),
-        _ptr(r["positions"]), capacity, _ptr(error_word), _stream(torch, dev))
+        at = (_flat("start", r["start"], i32, dev, B), _flat("len", r["len"], i32, dev, B),
+              _flat("held", r["held"], i32, dev, B), _flat("free_count", r["free_count"], i32, dev, 1),
+              _flat("offsets", r["offsets"], i32, dev, B + 1),
+              _flat("slots", r["slots"], torch.int64, dev, capacity),
+              _flat("positions", r["positions"], i32, dev, capacity))
+    st = _lib.asymspec_cache_plan(
+        _flat("lens", lens, i32, dev, B), 0 if accepted is None else _flat("accepted", accepted, i32, dev, B),
+        each, all_, B, block_size, blocks, t, t_ld, width, _flat("held", held, i32, dev, B),
+        _flat("free_list", free_list, i32, dev, blocks), _flat("free_count", free_count, i32, dev, 1), *at,
+        capacity, 0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
         raise AsymSpecError(st, "asymspec_cache_plan")
     return r
 
 
-def _cache(torch, keys, values):
-    """The C view of a cache: keys and values [blocks, block_size, kv_heads, head_dim], the
-    last axis contiguous, the others in any order in memory."""
-    shape = keys.shape
-    if len(shape) != 4 or values.shape != shape or values.dtype != keys.dtype or not keys.is_cuda \
-            or values.device != keys.device:
+def _cache(keys, values):
+    """(the C view of a cache, its device, its shape): keys and values [blocks, block_size,
+    kv_heads, head_dim], the last axis contiguous, the others in any order in memory."""
+    shape, dev = keys.shape, keys.get_device()
+    if len(shape) != 4 or values.shape != shape or values.dtype is not keys.dtype or dev < 0 \
+            or values.get_device() != dev:
         raise ValueError("keys and values must be CUDA tensors of one shape "
                          "[blocks, block_size, kv_heads, head_dim] and type")
-    ks, vs = keys.stride(), values.stride()
-    if ks[3] != 1 or vs[3] != 1:
+    k0, k1, k2, k3 = keys.stride()
+    v0, v1, v2, v3 = values.stride()
+    if k3 != 1 or v3 != 1:
         raise ValueError("the heads of keys and values must be contiguous")
-    return Cache(keys.data_ptr(), values.data_ptr(), _L3(*ks[:3]), _L3(*vs[:3]), *shape,
-                 _dtype(torch, keys))
+    return _CACHE.pack(keys.data_ptr(), values.data_ptr(), k0, k1, k2, v0, v1, v2, *shape,
+                       _dtype(keys)), dev, shape
 
 
 def cache_write(k, v, key_cache, value_cache, slots, *, error_word=None):
     """Writes k, v [T, kv_heads, head_dim] into a paged cache ([blocks, block_size, kv_heads,
     head_dim], any order in memory) at slots [T] int64; negative slots are skipped."""
-    import torch
-    cache = _cache(torch, key_cache, value_cache)
-    dev, (T, heads, dim) = key_cache.device, k.shape
-    for x in (k, v):
-        if x.dtype != key_cache.dtype or x.device != dev or x.shape != (T,) + key_cache.shape[2:] \
-                or x.stride(2) != 1:
-            raise ValueError("k and v must be [T, kv_heads, head_dim] like the cache, heads contiguous")
-    _check("slots", slots, torch.int64, dev, (T,))
-    _check("error_word", error_word, torch.int32, dev, (1,))
-    st = lib().asymspec_cache_write(ctypes.byref(cache), k.data_ptr(), v.data_ptr(),
-                                    _L2(*k.stride()[:2]), _L2(*v.stride()[:2]), slots.data_ptr(), T,
-                                    _ptr(error_word), _stream(torch, dev))
+    if torch is None:
+        _begin()
+    view, dev, (_, _, heads, dim) = _cache(key_cache, value_cache)
+    kind, shape = key_cache.dtype, k.shape
+    k0, k1, k2 = k.stride() if len(shape) == 3 else (0, 0, 0)
+    v0, v1, v2 = v.stride() if len(shape) == 3 else (0, 0, 0)
+    if k.dtype is not kind or v.dtype is not kind or k.get_device() != dev or v.get_device() != dev \
+            or v.shape != shape or shape[1:] != (heads, dim) or k2 != 1 or v2 != 1:
+        raise ValueError("k and v must be [T, kv_heads, head_dim] like the cache, heads contiguous")
+    T = shape[0]
+    st = _lib.asymspec_cache_write(view, k.data_ptr(), v.data_ptr(), _STRIDES2.pack(k0, k1),
+                                   _STRIDES2.pack(v0, v1), _flat("slots", slots, torch.int64, dev, T), T,
+                                   0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
         raise AsymSpecError(st, "asymspec_cache_write")
 
@@ -271,7 +311,8 @@ class CacheAttend:
     """
 
     def __init__(self, B_max: int, Q_max: int, heads: int, kv_heads: int, head_dim: int, device=None):
-        import torch
+        if torch is None:
+            _begin()
         self.B_max, self.Q_max = B_max, Q_max
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         self.nbytes = cache_attend_workspace_bytes(B_max, Q_max, heads, kv_heads, head_dim)
@@ -279,36 +320,37 @@ class CacheAttend:
             raise ValueError("no attention of this shape")
         self.workspace = torch.empty(self.nbytes, dtype=torch.uint8,
                                      device=torch.device(device or "cuda"))
+        self.scale = 1.0 / math.sqrt(head_dim)
 
     def __call__(self, q, key_cache, value_cache, tables, lens, *, scale=None, window=0, out=None,
                  lse=None, error_word=None):
-        import torch
-        cache = _cache(torch, key_cache, value_cache)
-        B, Q, heads, dim = q.shape
-        dev = q.device
-        if B > self.B_max or Q > self.Q_max or (heads, cache.kv_heads, dim) != (
+        view, dev, (_, _, kv_heads, head_dim) = _cache(key_cache, value_cache)
+        B, Q, heads, dim = shape = q.shape
+        kind = key_cache.dtype
+        if B > self.B_max or Q > self.Q_max or (heads, kv_heads, head_dim) != (
                 self.heads, self.kv_heads, self.head_dim):
             raise ValueError("batch does not fit this workspace")
+        q0, q1, q2, q3 = q.stride()
+        if q.dtype is not kind or q.get_device() != dev or q3 != 1 or dim != head_dim:
+            raise ValueError("q must be [B, Q, heads, head_dim] like the cache, heads contiguous")
         if out is None:
-            out = torch.empty(B, Q, heads, dim, dtype=q.dtype, device=dev)
+            out = q.new_empty(shape)
+            o0, o1, o2 = Q * heads * dim, heads * dim, dim
+        else:
+            o0, o1, o2, o3 = out.stride()
+            if out.dtype is not kind or out.get_device() != dev or out.shape != shape or o3 != 1:
+                raise ValueError("out must be [B, Q, heads, head_dim] like q, heads contiguous")
         if lse is None:
-            lse = torch.empty(B, Q, heads, dtype=torch.float32, device=dev)
-        for x in (q, out):
-            if x.dtype != key_cache.dtype or x.device != key_cache.device or x.shape != q.shape \
-                    or x.stride(3) != 1 or cache.head_dim != dim:
-                raise ValueError("q and out must be [B, Q, heads, head_dim] like the cache, "
-                                 "heads contiguous")
-        _rows("tables", tables, torch.int32, dev, B)
-        _check("lens", lens, torch.int32, dev, (B,))
-        _check("lse", lse, torch.float32, dev, (B, Q, heads))
-        _check("error_word", error_word, torch.int32, dev, (1,))
-        width = tables.shape[1]
-        st = lib().asymspec_cache_attend(
-            ctypes.byref(cache), q.data_ptr(), _L3(*q.stride()[:3]), B, Q, heads, tables.data_ptr(),
-            max(tables.stride(0), width), width, lens.data_ptr(),
-            1.0 / math.sqrt(dim) if scale is None else scale, window, out.data_ptr(),
-            _L3(*out.stride()[:3]), lse.data_ptr(), self.workspace.data_ptr(), self.nbytes,
-            _ptr(error_word), _stream(torch, dev))
+            lse = q.new_empty((B, Q, heads), dtype=torch.float32)
+            l = lse.data_ptr()
+        else:
+            l = _flat("lse", lse, torch.float32, dev, B * Q * heads)
+        t, t_ld, width = _rows("tables", tables, torch.int32, dev, B)
+        st = _lib.asymspec_cache_attend(
+            view, q.data_ptr(), _STRIDES3.pack(q0, q1, q2), B, Q, heads, t, t_ld, width,
+            _flat("lens", lens, torch.int32, dev, B), self.scale if scale is None else scale, window,
+            out.data_ptr(), _STRIDES3.pack(o0, o1, o2), l, self.workspace.data_ptr(), self.nbytes,
+            0 if error_word is None else _error_word(error_word, dev), _stream(dev))
         if st != OK:
             raise AsymSpecError(st, "asymspec_cache_attend")
         return out, lse

@@ -152,3 +152,14 @@ def test_cache_attend_workspace_of_no_shape(lib):
                   (S.CACHE_MAX_B + 1, 1, 4, 2, 64), (1, 1, 4, 0, 64), (1, 1 << 20, 4, 2, 64)):
         assert n(*shape) == 0, shape
     assert n(1, 1, 4, 2, 64) > 0
+
+
+def test_structs_as_bytes_have_the_structures_layout():
+    for packed, structure in ((S._CONSTRAINTS, S.Constraints), (S._CACHE, S.Cache)):
+        assert packed.size == ctypes.sizeof(structure)
+    n = [name for name, _ in S.Constraints._fields_]
+    c = S.Constraints.from_buffer_copy(S._CONSTRAINTS.pack(*range(1, len(n)), 0.5))
+    assert [getattr(c, name) for name in n] == list(range(1, len(n))) + [0.5]
+    x = S.Cache.from_buffer_copy(S._CACHE.pack(*range(1, 14)))
+    assert (x.keys, x.values, list(x.key_strides), list(x.value_strides)) == (1, 2, [3, 4, 5], [6, 7, 8])
+    assert (x.num_blocks, x.block_size, x.kv_heads, x.head_dim, x.dtype) == (9, 10, 11, 12, 13)
