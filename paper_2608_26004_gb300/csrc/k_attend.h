@@ -7,7 +7,7 @@ namespace asymspec_impl {
 
 struct AttendKernels {
   const void *split, *join;
-  int DP, rows, smem, ctas_per_sm;
+  int DP, rows, threads, smem, ctas_per_sm;
 };
 
 // The kernels for heads of D elements and `rows` queries a kv head (k_attend_bf16.cu,

@@ -4,19 +4,21 @@
 
 namespace asymspec_impl {
 
-template <int DP, int MT, int ST>
+template <int DP, int WR, int ST, int PER_SM>
 AttendKernels attend_pick() {
-  constexpr int smem = static_cast<int>(attend_smem_bytes<__nv_bfloat16>(DP, MT, ST));
-  static_assert(smem <= kMaxSmem - 8192, "the rings fit");
-  return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, MT, ST>),
-          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, MT>), DP, 16 * MT, smem,
-          smem <= 112 * 1024 ? 2 : 1};
+  constexpr int smem = static_cast<int>(attend_smem_bytes<__nv_bfloat16>(DP, WR, ST));
+  static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
+  static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
+  return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, WR, ST, PER_SM>),
+          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM};
 }
 
 AttendKernels attend_kernels_bf16(int D, int rows) {
-  if (D <= 64) return rows <= 16 ? attend_pick<64, 1, 6>() : attend_pick<64, 2, 6>();
-  if (D <= 128) return rows <= 16 ? attend_pick<128, 1, 3>() : attend_pick<128, 2, 3>();
-  return attend_pick<256, 1, 3>();
+  if (D <= 64)
+    return rows <= 16 ? attend_pick<64, 1, 5, 2>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();
+  if (D <= 128)
+    return rows <= 16 ? attend_pick<128, 1, 3, 2>() : rows <= 32 ? attend_pick<128, 2, 3, 2>() : attend_pick<128, 4, 6, 1>();
+  return rows <= 16 ? attend_pick<256, 1, 3, 1>() : attend_pick<256, 2, 3, 1>();
 }
 
 }  // namespace asymspec_impl

@@ -18,18 +18,22 @@ struct AttendParams {
   int B, Q, heads, kv_heads, D, num_blocks, block_size, table_width, window;
   int group;      // query heads of a kv head
   int rows;       // queries that share a kv head's keys: Q * group, row = query * group + head
-  int row_tiles;  // tiles of 16 * MT of them
+  int row_tiles;  // tiles of 16 * WR of them
   float scale2;   // scale * log2(e)
-  bool q_vec, out_vec, same_strides;
+  bool q_vec, out_vec;
+  // Blocks of a multiple of 16 tokens (a step's keys lie in one block, in a row), and
+  // strides within a block of fewer than 2^31 bytes:
+  bool whole_steps;
+  int block_bytes[2], token_bytes[2];  // of keys and values
   char* ws;
   uint32_t* err;
 };
 
-constexpr int kAThreads = 128;
-constexpr int kAWarps = kAThreads / 32;
-constexpr int kAKeys = 16;                 // keys of a warp's step
-constexpr int kATile = kAWarps * kAKeys;   // keys of a CTA's step, the unit of the split
-constexpr int kAMaxCtas = 304;             // CTAs that share the work (two on each of 152 SMs)
+constexpr int kAGroups = 4;                 // groups of warps, each with keys of its own
+constexpr int kAKeys = 16;                  // keys of a group's step
+constexpr int kATile = kAGroups * kAKeys;   // keys of a CTA's step, the unit of the split
+constexpr int kAMaxCtas = 456;              // CTAs that share the work (up to three on each of 152 SMs)
+constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each
 // of its tiles, after kAItem for what it costs to begin and end one.
@@ -53,13 +57,14 @@ constexpr size_t attend_ws_bytes(int rows, int DP) {
   return kAInfoBytes + attend_ml_bytes(rows) + static_cast<size_t>(2 * kAMaxCtas) * rows * DP * sizeof(float);
 }
 
-// Dynamic shared memory: the warps' rings, the queries (fp32: in two pieces), each step's
-// mask of keys that exist, each warp's maxima and sums.
+// Dynamic shared memory, from a 1024-byte boundary on: the groups' rings, the queries (fp32:
+// in two pieces), each warp's masks of keys that exist and its maxima and sums, and the
+// numbers that find a CTA's share.
 template <typename T>
-constexpr size_t attend_smem_bytes(int DP, int MT, int ST) {
-  return static_cast<size_t>(kAWarps) * ST * 2 * kAKeys * DP * sizeof(T) +
-         static_cast<size_t>(16) * MT * DP * (sizeof(T) == 4 ? 8 : 2) + kAWarps * ST * 4 +
-         static_cast<size_t>(kAWarps) * 16 * MT * 8;
+constexpr size_t attend_smem_bytes(int DP, int WR, int ST) {
+  return 1024 + static_cast<size_t>(kAGroups) * ST * 2 * kAKeys * DP * sizeof(T) +
+         static_cast<size_t>(16) * WR * DP * (sizeof(T) == 4 ? 8 : 2) + kAGroups * WR * ST * 4 +
+         static_cast<size_t>(kAGroups) * 16 * WR * 8 + kAGroups * WR * 8 + 16;
 }
 
 __device__ __forceinline__ void put(float* p, float y) { *p = y; }
@@ -68,9 +73,9 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float y) { *p = __float2bf
 __device__ __forceinline__ int attend_len(const AttendParams& p, int b) {
   return min(max(p.lens[b], 0), p.table_width * p.block_size);
 }
-// First key that any query of a request of this length sees.
+// Where a request's keys begin: the first that any query sees, or up to 15 before it.
 __device__ __forceinline__ int attend_first(const AttendParams& p, int len) {
-  return p.window ? max(0, len - p.Q - p.window + 1) : 0;
+  return p.window ? max(0, len - p.Q - p.window + 1) & ~(kAKeys - 1) : 0;
 }
 __device__ __forceinline__ int attend_tiles(const AttendParams& p, int len) {
   return max(1, (len - attend_first(p, len) + kATile - 1) / kATile);
@@ -91,10 +96,9 @@ struct AttendShares {
   }
 };
 
-// 16 bytes, or zeros where `live` is false (the address is then not read).
-__device__ __forceinline__ void cp_async16_or_zero(unsigned smem, const void* gmem, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(live ? 16 : 0)
-               : "memory");
+// 16 bytes, or with bytes = 0 zeros (the address is then not read).
+__device__ __forceinline__ void cp_async16_or_zero(unsigned smem, const void* gmem, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -143,38 +147,48 @@ __device__ __forceinline__ int swizzled(int r, int c) {
   return sizeof(T) == 2 || VALUES ? c ^ (r & 7) : c ^ (((r & 1) << 2) | ((r >> 1) & 3));
 }
 
-// The keys are split evenly over the CTAs, in tiles of 64, whatever the requests' lengths;
-// each warp takes 16 keys of a tile through a ring of its own (cp.async, no barrier
-// between warps) and keeps running maxima, sums and weighted values of the tile's rows;
-// a CTA joins its warps' when its share of an item ends.
-template <typename T, int DP, int MT, int ST>
-__global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) {
+__device__ __forceinline__ void group_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// The keys are split evenly over the CTAs, in tiles of 64, whatever the requests' lengths.
+// A CTA has four groups of WR warps: a group takes 16 keys of each tile through a ring of
+// its own (cp.async, its warps load a part each), and each of its warps 16 of the item's
+// rows, with running references, sums and weighted values in registers.  When the CTA's share of
+// an item ends, the groups' parts are joined in shared memory.
+template <typename T, int DP, int WR, int ST, int PER_SM>
+__global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const AttendParams p) {
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16;
-  constexpr int kHalf = kAKeys * DP;  // elements of a step's keys (and of its values)
-  constexpr int kRows = 16 * MT;
+  constexpr int kThreadsN = kAGroups * WR * 32, kWarpsN = kAGroups * WR;
+  constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16, PE = 16 / sizeof(T);
+  constexpr int kHalf = kAKeys * kRowBytes;  // bytes of a step's keys (and of its values)
+  constexpr int kRows = 16 * WR;
   constexpr int NT = DP / 8;
+  constexpr int kLoads = kChunks / 2 / WR;   // vectors that a lane loads of a step's keys
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  constexpr bool kQRegs = BF && MT * DP <= 128;
-  extern __shared__ __align__(128) unsigned char a_smem[];
-  __shared__ int64_t s_scan[kAThreads];
-  __shared__ int64_t s_v;
-  __shared__ int s_b;
-  T* ring0 = reinterpret_cast<T*>(a_smem);
-  unsigned char* at_q = a_smem + static_cast<size_t>(kAWarps) * ST * 2 * kHalf * sizeof(T);
+  constexpr float kSlack = 8.f;
+  constexpr bool kQRegs = BF && DP <= 128 && WR == 1;
+  static_assert(kLoads >= 1 && (BF ? 1 : 2) * ST >= WR, "a warp loads, and the parts fit in the rings");
+  extern __shared__ unsigned char a_smem_raw[];
+  unsigned char* a_smem = a_smem_raw + ((1024u - (smem_u32(a_smem_raw) & 1023u)) & 1023u);
+  unsigned char* at_q = a_smem + static_cast<size_t>(kAGroups) * ST * 2 * kHalf;
   T* qs = reinterpret_cast<T*>(at_q);  // fp32: the high pieces, then the low ones
-  unsigned char* at_mask = at_q + static_cast<size_t>(kRows) * DP * (BF ? 2 : 8);
-  float* s_ml = reinterpret_cast<float*>(at_mask + kAWarps * ST * 4);
+  unsigned* masks0 = reinterpret_cast<unsigned*>(at_q + static_cast<size_t>(kRows) * DP * (BF ? 2 : 8));
+  float* s_ml = reinterpret_cast<float*>(masks0 + kWarpsN * ST);
+  int64_t* s_scan = reinterpret_cast<int64_t*>(s_ml + kWarpsN * 16 * 2);
+  int64_t* s_find = s_scan + kWarpsN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-  unsigned* masks = reinterpret_cast<unsigned*>(at_mask) + warp * ST;
-  T* ring = ring0 + warp * ST * 2 * kHalf;
+  const int group = warp / WR, wr = warp % WR;  // whose keys; which rows
+  unsigned* masks = masks0 + warp * ST;
+  unsigned char* ring = a_smem + group * ST * 2 * kHalf;
+  const unsigned ring_at = smem_u32(ring), q_at = smem_u32(qs) + wr * 16 * kRowBytes;
   const int c = blockIdx.x, ctas = gridDim.x;
   const int HR = p.kv_heads * p.row_tiles;
   unsigned err = 0;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // this CTA's share of the tiles, and where it begins
-  const int per = (p.B + kAThreads - 1) / kAThreads;
+  // this CTA's share of the units, and where it begins
+  const int per = (p.B + kThreadsN - 1) / kThreadsN;
   int64_t mine = 0;
   for (int b = tid * per; b < min((tid + 1) * per, p.B); ++b) {
     const int len = attend_len(p, b);
@@ -190,7 +204,7 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
   if (lane == 31) s_scan[warp] = upto;
   __syncthreads();
   int64_t total = 0;
-  for (int w = 0; w < kAWarps; ++w) {
+  for (int w = 0; w < kWarpsN; ++w) {
     if (w < warp) upto += s_scan[w];
     total += s_scan[w];
   }
@@ -206,8 +220,8 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
       if (v < n) break;
       v -= n;
     }
-    s_b = b;
-    s_v = v;
+    s_find[0] = b;
+    s_find[1] = v;
   }
   __syncthreads();
   AttendInfo* info = reinterpret_cast<AttendInfo*>(p.ws) + c;
@@ -216,10 +230,10 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
     if (err && p.err) atomicOr(p.err, err);
     return;
   }
-  int b = s_b;
+  int b = static_cast<int>(s_find[0]);
   int len = attend_len(p, b), n_tiles = attend_tiles(p, len);
-  int hr = static_cast<int>(div64(s_v, n_tiles + kAItem));
-  int at_unit = static_cast<int>(s_v - static_cast<int64_t>(hr) * (n_tiles + kAItem));
+  int hr = static_cast<int>(div64(s_find[1], n_tiles + kAItem));
+  int at_unit = static_cast<int>(s_find[1] - static_cast<int64_t>(hr) * (n_tiles + kAItem));
   if (tid == 0) {
     info->total = total;
     info->first = u - at_unit;
@@ -228,8 +242,22 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
     info->tiles = at_unit > kAItem ? n_tiles : 0;
   }
 
-  float O[MT][NT][4], m[MT][2], l[MT][2];
-  unsigned qf[kQRegs ? MT * DP / 16 : 1][4];
+  // this lane's vectors of a step: i = 0 .. kLoads - 1
+  const int lane_id = wr * 32 + lane;
+  auto row_of = [&](int i) { return (i * 32 * WR + lane_id) / kChunks; };
+  auto chunk_of = [&](int i) { return (i * 32 * WR + lane_id) % kChunks; };
+  // where a group loads whole rows at once, they are kLaneRows apart: the same chunk
+  constexpr bool kSameChunk = kChunks <= 32 * WR;
+  constexpr int kLaneRows = kSameChunk ? 32 * WR / kChunks : 1;
+  const int row0 = row_of(0), chunk0 = chunk_of(0);
+  const unsigned to_k = row0 * kRowBytes + swizzled<T, false>(row0, chunk0) * 16;
+  const unsigned to_v = kHalf + row0 * kRowBytes + swizzled<T, true>(row0, chunk0) * 16;
+  const int from_k = row0 * p.token_bytes[0] + chunk0 * 16, from_v = row0 * p.token_bytes[1] + chunk0 * 16;
+  const int chunk_bytes = chunk0 * PE < p.D ? 16 : 0;
+  const int step_blocks = kATile / p.block_size, step_rest = kATile % p.block_size;
+
+  float O[NT][4], m[2], l[2];
+  unsigned qf[kQRegs ? DP / 16 : 1][4];
   for (; u < u_end; at_unit = 0) {
     if (hr == HR) {
       hr = 0;
@@ -240,16 +268,78 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
     const int end_unit = static_cast<int>(min(static_cast<int64_t>(n_tiles + kAItem), at_unit + (u_end - u)));
     const int t0 = max(0, at_unit - kAItem), t1 = end_unit - kAItem;
     u += end_unit - at_unit;
-    if (t1 <= t0) {  // (the item's first tile is the next CTA's)
-      continue;
-    }
+    if (t1 <= t0) continue;  // (the item's first tile is the next CTA's)
     const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * kRows;
     const int lo = attend_first(p, len);
+    const int rows = min(kRows, p.rows - R0);  // of the item
+    const T* keys = static_cast<const T*>(p.keys) + kh * p.cks[2];
+    const T* values = static_cast<const T*>(p.values) + kh * p.cvs[2];
+    const int32_t* table = p.tables + b * p.table_ld;
+    const int k_group = lo + group * kAKeys;  // the group's first key of tile 0
+
+    // the next step to load: this lane's key of it (lane % 16), its block and place there
+    int next_key = k_group + t0 * kATile + (lane & 15);
+    int next_block = next_key / p.block_size, next_at = next_key % p.block_size;
+    const int end_key = min(len, lo + t1 * kATile);
+    auto page_of = [&] { return next_key < end_key ? __ldg(table + next_block) : INT_MIN; };
+    auto advance = [&] {
+      next_key += kATile;
+      next_block += step_blocks;
+      next_at += step_rest;
+      if (next_at >= p.block_size) next_at -= p.block_size, ++next_block;
+    };
+    auto issue = [&](int stage, int page, int key, int at) {
+      const unsigned sk = ring_at + stage * 2 * kHalf, sv = sk + kHalf;
+      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
+      const unsigned live = __ballot_sync(~0u, there) & 0xFFFFu;
+      if (lane == 0) masks[stage] = live;
+      if (kSameChunk && p.whole_steps && live == 0xFFFFu) {
+        const int first = at - (lane & 15);
+        const char* fk = reinterpret_cast<const char*>(keys) + from_k +
+                         (static_cast<int64_t>(page) * p.block_bytes[0] + static_cast<int64_t>(first) * p.token_bytes[0]);
+        const char* fv = reinterpret_cast<const char*>(values) + from_v +
+                         (static_cast<int64_t>(page) * p.block_bytes[1] + static_cast<int64_t>(first) * p.token_bytes[1]);
+        const unsigned dk = sk + to_k, dv = sk + to_v;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          constexpr int kStep = kLaneRows * kRowBytes;
+          cp_async16_or_zero((dk ^ (swizzled<T, false>(i * kLaneRows, 0) * 16)) + i * kStep, fk, chunk_bytes);
+          cp_async16_or_zero((dv ^ (swizzled<T, true>(i * kLaneRows, 0) * 16)) + i * kStep, fv, chunk_bytes);
+          fk += kLaneRows * p.token_bytes[0];
+          fv += kLaneRows * p.token_bytes[1];
+        }
+      } else if (live != 0 || __any_sync(~0u, key < end_key)) {
+        if (!there && key < end_key) err |= ASYMSPEC_DATA_BAD_INDEX;
+        const int64_t ok = there ? page * p.cks[0] + at * p.cks[1] : 0;
+        const int64_t ov = there ? page * p.cvs[0] + at * p.cvs[1] : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int r = row_of(i), ch = chunk_of(i);
+          const int64_t rk = __shfl_sync(~0u, ok, r), rv = __shfl_sync(~0u, ov, r);
+          const bool on = ((live >> r) & 1u) && ch * PE < p.D;
+          const int el = on ? ch * PE : 0;
+          cp_async16_or_zero(sk + r * kRowBytes + swizzled<T, false>(r, ch) * 16, keys + rk + el, on ? 16 : 0);
+          cp_async16_or_zero(sv + r * kRowBytes + swizzled<T, true>(r, ch) * 16, values + rv + el, on ? 16 : 0);
+        }
+      }
+      cp_async_commit();
+    };
+    int next_page = page_of();
+    if constexpr (ST > 1) {
+      int pages[ST - 1], keys_of[ST - 1], ats[ST - 1];
+#pragma unroll
+      for (int s = 0; s < ST - 1; ++s) {
+        pages[s] = next_page, keys_of[s] = next_key, ats[s] = next_at;
+        advance();
+        next_page = page_of();
+      }
+#pragma unroll
+      for (int s = 0; s < ST - 1; ++s) issue(s, pages[s], keys_of[s], ats[s]);
+    }
+
     // the item's queries
-    const int rows = min(kRows, p.rows - R0);
-    for (int e = tid; e < kRows * kChunks; e += kAThreads) {
+    for (int e = tid; e < kRows * kChunks; e += kThreadsN) {
       const int r = e / kChunks, ch = e % kChunks;
-      constexpr int PE = 16 / sizeof(T);
       const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
       const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2] + ch * PE;
       uint4 v = make_uint4(0, 0, 0, 0);
@@ -276,374 +366,301 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
         *reinterpret_cast<uint4*>(qs + kRows * DP + at) = lw;
       }
     }
-    const T* keys = static_cast<const T*>(p.keys) + kh * p.cks[2];
-    const T* values = static_cast<const T*>(p.values) + kh * p.cvs[2];
-    const int32_t* table = p.tables + b * p.table_ld;
-    const int k_lane = lo + warp * kAKeys + (lane & 15);  // this lane's key of tile 0
-
-    auto page_of = [&](int t) {
-      const int j = k_lane + t * kATile;
-      return t < t1 && j < len ? __ldg(table + j / p.block_size) : INT_MIN;
-    };
-    auto issue = [&](int t, int stage, int page) {
-      if (t < t1) {
-        const int j = k_lane + t * kATile;
-        const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
-        if (!there && j < len) err |= ASYMSPEC_DATA_BAD_INDEX;
-        const unsigned live = __ballot_sync(~0u, there);
-        const int at = j % p.block_size;
-        const int64_t ok = there ? page * p.cks[0] + at * p.cks[1] : 0;
-        const int64_t ov = there ? page * p.cvs[0] + at * p.cvs[1] : 0;
-        if (lane == 0) masks[stage] = live & 0xFFFFu;
-        const unsigned sk = smem_u32(ring + stage * 2 * kHalf), sv = sk + kHalf * sizeof(T);
+    // of this thread's rows: the last key seen; of the warp's the least, and the windows'
+    // largest first
+    const int R = R0 + wr * 16, warp_rows = rows - wr * 16;  // (may be none)
+    int last[2];
 #pragma unroll
-        for (int i = 0; i < kChunks / 2; ++i) {
-          const int e = i * 32 + lane, r = e / kChunks, ch = e % kChunks;
-          const int64_t rk = __shfl_sync(~0u, ok, r);
-          const int64_t rv = p.same_strides ? rk : __shfl_sync(~0u, ov, r);
-          const bool on = ((live >> r) & 1u) && ch * (16 / static_cast<int>(sizeof(T))) < p.D;
-          const int el = on ? ch * (16 / static_cast<int>(sizeof(T))) : 0;
-          cp_async16_or_zero(sk + r * kRowBytes + swizzled<T, false>(r, ch) * 16, keys + rk + el, on);
-          cp_async16_or_zero(sv + r * kRowBytes + swizzled<T, true>(r, ch) * 16, values + rv + el, on);
-        }
-      }
-      cp_async_commit();
-    };
-
-    {
-      int pages[ST > 1 ? ST - 1 : 1];
-#pragma unroll
-      for (int s = 0; s < ST - 1; ++s) pages[s] = page_of(t0 + s);
-#pragma unroll
-      for (int s = 0; s < ST - 1; ++s) issue(t0 + s, s, pages[s]);
+    for (int h = 0; h < 2; ++h) {
+      last[h] = h * 8 + g < warp_rows ? len - p.Q + (R + h * 8 + g) / p.group : -1;
+      m[h] = -INFINITY;
+      l[h] = 0.f;
     }
-    int next_page = page_of(t0 + ST - 1);
-
-    // of this thread's rows: the last key seen; the tile's least and the windows' largest first
-    int last[MT][2];
+    const int least = len - p.Q + R / p.group;
+    const int from = p.window ? len - p.Q + (R + min(warp_rows, 16) - 1) / p.group - p.window + 1 : 0;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = mt * 16 + h * 8 + g;
-        last[mt][h] = r < rows ? len - p.Q + (R0 + r) / p.group : -1;
-        m[mt][h] = -INFINITY;
-        l[mt][h] = 0.f;
-      }
-    const int least = len - p.Q + R0 / p.group;
-    const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) O[mt][n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) O[n][e] = 0.f;
     __syncthreads();
     if constexpr (kQRegs) {
+      const unsigned at = q_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k) {
-          const int r = mt * 16 + (lane & 15), ch = k * 2 + (lane >> 4);
-          ldmatrix4(qf[mt * (DP / 16) + k], smem_u32(qs + r * DP) + swizzled<T, false>(r, ch) * 16);
-        }
+      for (int k = 0; k < DP / 16; ++k) ldmatrix4(qf[k], at ^ (k * 32));
     }
 
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
-      issue(t + ST - 1, stage == 0 ? ST - 1 : stage - 1, next_page);
-      next_page = page_of(t + ST);
-      cp_async_wait<ST - 1>();
-      __syncwarp();
-      const T* ks = ring + stage * 2 * kHalf;
-      const T* vs = ks + kHalf;
+      cp_async_wait<ST - 1 - (ST > 1)>();
+      // the group's warps have loaded the step, and are done with the one before
+      if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
+      else __syncwarp();
+      if constexpr (ST > 1) {
+        issue(stage == 0 ? ST - 1 : stage - 1, next_page, next_key, next_at);
+        advance();
+        next_page = page_of();
+      } else {
+        issue(0, next_page, next_key, next_at);
+        advance();
+        next_page = page_of();
+        cp_async_wait<0>();
+        if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
+        else __syncwarp();
+      }
+      const unsigned char* ks = ring + stage * 2 * kHalf;
+      const unsigned char* vs = ks + kHalf;
+      const unsigned ks_at = ring_at + stage * 2 * kHalf, vs_at = ks_at + kHalf;
       const unsigned live = masks[stage];
-      const int k0 = lo + t * kATile + warp * kAKeys;
-      if (live != 0) {
-        // scores of 16 keys: S[mt][keys 0-7, 8-15]
-        float S[MT][2][4];
+      const int k0 = k_group + t * kATile;
+      if (live != 0 && warp_rows > 0) {
+        // scores of keys 0-7 and 8-15
+        float S[2][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[mt][n][e] = 0.f;
+          for (int e = 0; e < 4; ++e) S[n][e] = 0.f;
         if constexpr (BF) {
+          // chunk 2k + j of row r lies at (2k + j) ^ (r & 7): the 2k is an exclusive or of its own
+          const unsigned at = ks_at + (((lane >> 4) << 3) + (lane & 7)) * kRowBytes +
+                              ((((lane >> 3) & 1) ^ (lane & 7)) * 16);
+          const unsigned q_lane = q_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
-            const int r = ((lane >> 4) << 3) + (lane & 7), ch = k * 2 + ((lane >> 3) & 1);
             unsigned kf[4];
-            ldmatrix4(kf, smem_u32(ks + r * DP) + swizzled<T, false>(r, ch) * 16);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              if constexpr (kQRegs) {
-                mma_bf16(S[mt][0], qf[mt * (DP / 16) + k], kf[0], kf[1]);
-                mma_bf16(S[mt][1], qf[mt * (DP / 16) + k], kf[2], kf[3]);
-              } else {
-                const int qr = mt * 16 + (lane & 15), qc = k * 2 + (lane >> 4);
-                unsigned qv[4];
-                ldmatrix4(qv, smem_u32(qs + qr * DP) + swizzled<T, false>(qr, qc) * 16);
-                mma_bf16(S[mt][0], qv, kf[0], kf[1]);
-                mma_bf16(S[mt][1], qv, kf[2], kf[3]);
-              }
+            ldmatrix4(kf, at ^ (k * 32));
+            if constexpr (kQRegs) {
+              mma_bf16(S[0], qf[k], kf[0], kf[1]);
+              mma_bf16(S[1], qf[k], kf[2], kf[3]);
+            } else {
+              unsigned qv[4];
+              ldmatrix4(qv, q_lane ^ (k * 32));
+              mma_bf16(S[0], qv, kf[0], kf[1]);
+              mma_bf16(S[1], qv, kf[2], kf[3]);
             }
           }
         } else {
           // the sum over a head's elements in an order of its own: of each 16, lane t4 of a
           // quad takes elements 4 t4 .. 4 t4 + 3, two for each of two products
+          const float* kf = reinterpret_cast<const float*>(ks);
+          const float* qw = reinterpret_cast<const float*>(qs) + wr * 16 * DP;
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
-            unsigned kh4[2][4], kl4[2][4];
+            const int at = g * DP + swizzled<T, false>(g, 4 * k + t4) * 4;  // (row g + 8: the same chunk)
+            const uint4 h0 = *reinterpret_cast<const uint4*>(qw + at);
+            const uint4 h1 = *reinterpret_cast<const uint4*>(qw + at + 8 * DP);
+            const uint4 l0 = *reinterpret_cast<const uint4*>(qw + kRows * DP + at);
+            const uint4 l1 = *reinterpret_cast<const uint4*>(qw + kRows * DP + at + 8 * DP);
+            const unsigned qh[2][4] = {{h0.x, h1.x, h0.y, h1.y}, {h0.z, h1.z, h0.w, h1.w}};
+            const unsigned ql[2][4] = {{l0.x, l1.x, l0.y, l1.y}, {l0.z, l1.z, l0.w, l1.w}};
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-              const int r = n * 8 + g;
-              const float4 x = *reinterpret_cast<const float4*>(ks + r * DP + swizzled<T, false>(r, 4 * k + t4) * 4);
-              split_tf32(x.x, kh4[n][0], kl4[n][0]);
-              split_tf32(x.y, kh4[n][1], kl4[n][1]);
-              split_tf32(x.z, kh4[n][2], kl4[n][2]);
-              split_tf32(x.w, kh4[n][3], kl4[n][3]);
-            }
+              const float4 x = *reinterpret_cast<const float4*>(kf + at + n * 8 * DP);
+              unsigned kh4[4], kl4[4];
+              split_tf32(x.x, kh4[0], kl4[0]);
+              split_tf32(x.y, kh4[1], kl4[1]);
+              split_tf32(x.z, kh4[2], kl4[2]);
+              split_tf32(x.w, kh4[3], kl4[3]);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              const int r0 = mt * 16 + g, r1 = r0 + 8;
-              const int a0 = r0 * DP + swizzled<T, false>(r0, 4 * k + t4) * 4;
-              const int a1 = r1 * DP + swizzled<T, false>(r1, 4 * k + t4) * 4;
-              const uint4 h0 = *reinterpret_cast<const uint4*>(qs + a0);
-              const uint4 h1 = *reinterpret_cast<const uint4*>(qs + a1);
-              const uint4 l0 = *reinterpret_cast<const uint4*>(qs + kRows * DP + a0);
-              const uint4 l1 = *reinterpret_cast<const uint4*>(qs + kRows * DP + a1);
-              const unsigned qh[2][4] = {{h0.x, h1.x, h0.y, h1.y}, {h0.z, h1.z, h0.w, h1.w}};
-              const unsigned ql[2][4] = {{l0.x, l1.x, l0.y, l1.y}, {l0.z, l1.z, l0.w, l1.w}};
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                  mma_tf32(S[mt][n], ql[e], kh4[n][2 * e], kh4[n][2 * e + 1]);
-                  mma_tf32(S[mt][n], qh[e], kl4[n][2 * e], kl4[n][2 * e + 1]);
-                  mma_tf32(S[mt][n], qh[e], kh4[n][2 * e], kh4[n][2 * e + 1]);
-                }
+              for (int e = 0; e < 2; ++e) {
+                mma_tf32(S[n], ql[e], kh4[2 * e], kh4[2 * e + 1]);
+                mma_tf32(S[n], qh[e], kl4[2 * e], kl4[2 * e + 1]);
+                mma_tf32(S[n], qh[e], kh4[2 * e], kh4[2 * e + 1]);
+              }
             }
           }
         }
         const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int h = 0; h < 2; ++h) {
+          float top = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float top = -INFINITY;
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                float& s = S[mt][n][2 * h + e];
-                s *= p.scale2;
-                if (!whole) {
-                  const int kk = n * 8 + 2 * t4 + e, j = k0 + kk;
-                  const bool seen = ((live >> kk) & 1u) && j <= last[mt][h] &&
-                                    (p.window == 0 || j > last[mt][h] - p.window);
-                  s = seen ? s : -INFINITY;
-                }
-                top = fmaxf(top, s);
+            for (int e = 0; e < 2; ++e) {
+              float& s = S[n][2 * h + e];
+              s *= p.scale2;
+              if (!whole) {
+                const int kk = n * 8 + 2 * t4 + e, j = k0 + kk;
+                const bool seen = ((live >> kk) & 1u) && j <= last[h] && (p.window == 0 || j > last[h] - p.window);
+                s = seen ? s : -INFINITY;
               }
-            if (__any_sync(~0u, top > m[mt][h])) {
-              float v = fmaxf(m[mt][h], top);
-              v = fmaxf(v, __shfl_xor_sync(~0u, v, 1));
-              v = fmaxf(v, __shfl_xor_sync(~0u, v, 2));
-              const float f = v == m[mt][h] ? 1.f : ex2(m[mt][h] - v);
-              m[mt][h] = v;
-              l[mt][h] *= f;
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                O[mt][n][2 * h] *= f;
-                O[mt][n][2 * h + 1] *= f;
-              }
+              top = fmaxf(top, s);
             }
-            const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];
+          // (m is a reference that scores exceed by 2^kSlack at most: the maximum itself, kept,
+          // would rescale the values at most steps, for one of the rows or another)
+          if (__any_sync(~0u, top > m[h] + kSlack)) {
+            float v = fmaxf(m[h], top);
+            v = fmaxf(v, __shfl_xor_sync(~0u, v, 1));
+            v = fmaxf(v, __shfl_xor_sync(~0u, v, 2));
+            const float f = v == m[h] ? 1.f : ex2(m[h] - v);
+            m[h] = v;
+            l[h] *= f;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              S[mt][n][2 * h] = ex2(S[mt][n][2 * h] - ref);
-              S[mt][n][2 * h + 1] = ex2(S[mt][n][2 * h + 1] - ref);
-              l[mt][h] += S[mt][n][2 * h] + S[mt][n][2 * h + 1];
+            for (int n = 0; n < NT; ++n) {
+              O[n][2 * h] *= f;
+              O[n][2 * h + 1] *= f;
             }
           }
+          const float ref = m[h] == -INFINITY ? 0.f : m[h];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            S[n][2 * h] = ex2(S[n][2 * h] - ref);
+            S[n][2 * h + 1] = ex2(S[n][2 * h + 1] - ref);
+            l[h] += S[n][2 * h] + S[n][2 * h + 1];
+          }
+        }
         if constexpr (BF) {
-          unsigned ph[MT][4], pl[MT][4];
+          // weights in two bf16 pieces (2^-17): in one (2^-9) they would cost as much as the
+          // output's own rounding
+          unsigned ph[4], pl[4];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              split_bf16(S[mt][n][0], S[mt][n][1], ph[mt][2 * n], pl[mt][2 * n]);
-              split_bf16(S[mt][n][2], S[mt][n][3], ph[mt][2 * n + 1], pl[mt][2 * n + 1]);
-            }
+          for (int n = 0; n < 2; ++n) {
+            split_bf16(S[n][0], S[n][1], ph[2 * n], pl[2 * n]);
+            split_bf16(S[n][2], S[n][3], ph[2 * n + 1], pl[2 * n + 1]);
+          }
+          const unsigned at = vs_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
 #pragma unroll
           for (int n = 0; n < NT / 2; ++n) {
-            const int r = lane & 15, ch = n * 2 + (lane >> 4);
             unsigned vf[4];
-            ldmatrix4_trans(vf, smem_u32(vs + r * DP) + swizzled<T, true>(r, ch) * 16);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma_bf16(O[mt][2 * n], pl[mt], vf[0], vf[1]);
-              mma_bf16(O[mt][2 * n + 1], pl[mt], vf[2], vf[3]);
-              mma_bf16(O[mt][2 * n], ph[mt], vf[0], vf[1]);
-              mma_bf16(O[mt][2 * n + 1], ph[mt], vf[2], vf[3]);
-            }
+            ldmatrix4_trans(vf, at ^ (n * 32));
+            mma_bf16(O[2 * n], pl, vf[0], vf[1]);
+            mma_bf16(O[2 * n + 1], pl, vf[2], vf[3]);
+            mma_bf16(O[2 * n], ph, vf[0], vf[1]);
+            mma_bf16(O[2 * n + 1], ph, vf[2], vf[3]);
           }
         } else {
           // keys 2 t4 and 2 t4 + 1 of each eight are the products' elements t4 and t4 + 4; of each
           // 32 elements of a head, lane group g takes 4 g .. 4 g + 3, one for each of four products
+          const float* vf = reinterpret_cast<const float*>(vs);
 #pragma unroll
           for (int n8 = 0; n8 < 2; ++n8) {
-            unsigned ph[MT][4], pl[MT][4];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              split_tf32(S[mt][n8][0], ph[mt][0], pl[mt][0]);
-              split_tf32(S[mt][n8][2], ph[mt][1], pl[mt][1]);
-              split_tf32(S[mt][n8][1], ph[mt][2], pl[mt][2]);
-              split_tf32(S[mt][n8][3], ph[mt][3], pl[mt][3]);
-            }
+            unsigned ph[4], pl[4];
+            split_tf32(S[n8][0], ph[0], pl[0]);
+            split_tf32(S[n8][2], ph[1], pl[1]);
+            split_tf32(S[n8][1], ph[2], pl[2]);
+            split_tf32(S[n8][3], ph[3], pl[3]);
             const int r0 = n8 * 8 + 2 * t4, r1 = r0 + 1;
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) {
-              const float4 x = *reinterpret_cast<const float4*>(vs + r0 * DP + swizzled<T, true>(r0, 8 * i + g) * 4);
-              const float4 y = *reinterpret_cast<const float4*>(vs + r1 * DP + swizzled<T, true>(r1, 8 * i + g) * 4);
+              const float4 x = *reinterpret_cast<const float4*>(vf + r0 * DP + swizzled<T, true>(r0, 8 * i + g) * 4);
+              const float4 y = *reinterpret_cast<const float4*>(vf + r1 * DP + swizzled<T, true>(r1, 8 * i + g) * 4);
               const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 unsigned h0, l0, h1, l1;
                 split_tf32(xs[e], h0, l0);
                 split_tf32(ys[e], h1, l1);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                  mma_tf32(O[mt][4 * i + e], pl[mt], h0, h1);
-                  mma_tf32(O[mt][4 * i + e], ph[mt], l0, l1);
-                  mma_tf32(O[mt][4 * i + e], ph[mt], h0, h1);
-                }
+                mma_tf32(O[4 * i + e], pl, h0, h1);
+                mma_tf32(O[4 * i + e], ph, l0, l1);
+                mma_tf32(O[4 * i + e], ph, h0, h1);
               }
             }
           }
         }
       }
-      __syncwarp();
       stage = stage + 1 == ST ? 0 : stage + 1;
     }
 
     cp_async_wait<0>();
-    __syncwarp();
     // Infinities and NaN: a weight of zero times one that its row does not see, or one in
     // two pieces, is a NaN that the formula does not have.  A warp that ends with any works its
     // keys again, one product after another, and leaves out what a row does not see.
     float odd = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int h = 0; h < 2; ++h)
+      if (h * 8 + g < warp_rows) {
+        odd = fmaf(0.f, l[h], odd);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (mt * 16 + h * 8 + g < rows) {
-          odd = fmaf(0.f, l[mt][h], odd);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) odd = fmaf(0.f, O[mt][n][2 * h], fmaf(0.f, O[mt][n][2 * h + 1], odd));
-        }
+        for (int n = 0; n < NT; ++n) odd = fmaf(0.f, O[n][2 * h], fmaf(0.f, O[n][2 * h + 1], odd));
+      }
     if (__any_sync(~0u, odd != 0.f)) {
-      constexpr int PE = 16 / sizeof(T);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int h = 0; h < 2; ++h) {
+        m[h] = -INFINITY;
+        l[h] = 0.f;
 #pragma unroll
+        for (int n = 0; n < NT; ++n) O[n][2 * h] = O[n][2 * h + 1] = 0.f;
+      }
+      for (int k = 0; k < (t1 - t0) * kAKeys; ++k) {
+        const int j = k_group + (t0 + k / kAKeys) * kATile + k % kAKeys;
+        if (j >= len) break;
+        const int page = table[j / p.block_size], at = j % p.block_size;
+        if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_blocks)) continue;
+        const T* kr = keys + page * p.cks[0] + at * p.cks[1];
+        const T* vr = values + page * p.cvs[0] + at * p.cvs[1];
+#pragma unroll 1
         for (int h = 0; h < 2; ++h) {
-          m[mt][h] = -INFINITY;
-          l[mt][h] = 0.f;
+          const int r = R + min(h * 8 + g, warp_rows - 1);
+          const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + r / p.group * p.qs[1] +
+                        (kh * p.group + r % p.group) * p.qs[2];
+          float s = 0.f;
+          for (int d = t4; d < p.D; d += 4) s = fmaf(to_f32(qr[d]), to_f32(kr[d]), s);
+          s += __shfl_xor_sync(~0u, s, 1);
+          s += __shfl_xor_sync(~0u, s, 2);
+          s *= p.scale2;
+          const int end = h ? last[1] : last[0];
+          if (j > end || (p.window != 0 && j <= end - p.window)) continue;
+          const float old = h ? m[1] : m[0], v = fmaxf(old, s), ref = v == -INFINITY ? 0.f : v;
+          const float f = v == old ? 1.f : ex2(old - v), w = ex2(s - ref);
+          if (h) m[1] = v, l[1] = l[1] * f + (t4 == 0 ? w : 0.f);
+          else m[0] = v, l[0] = l[0] * f + (t4 == 0 ? w : 0.f);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) O[mt][n][2 * h] = O[mt][n][2 * h + 1] = 0.f;
-        }
-      for (int t = t0; t < t1; ++t) {
-        issue(t, 0, page_of(t));
-        cp_async_wait<0>();
-        __syncwarp();
-        const unsigned live = masks[0];
-        const T* ks = ring;
-        const T* vs = ks + kHalf;
-        for (int kk = 0; kk < kAKeys; ++kk) {
-          if (!((live >> kk) & 1u)) continue;
-          const int j = lo + t * kATile + warp * kAKeys + kk;
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int r = min(mt * 16 + h * 8 + g, rows - 1);
-              const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + (R0 + r) / p.group * p.qs[1] +
-                            (kh * p.group + (R0 + r) % p.group) * p.qs[2];
-              float s = 0.f;
-              for (int d = t4; d < p.D; d += 4)
-                s = fmaf(to_f32(qr[d]), to_f32(ks[kk * DP + swizzled<T, false>(kk, d / PE) * PE + d % PE]), s);
-              s += __shfl_xor_sync(~0u, s, 1);
-              s += __shfl_xor_sync(~0u, s, 2);
-              s *= p.scale2;
-              if (j <= last[mt][h] && (p.window == 0 || j > last[mt][h] - p.window)) {
-                const float v = fmaxf(m[mt][h], s), ref = v == -INFINITY ? 0.f : v;
-                const float f = v == m[mt][h] ? 1.f : ex2(m[mt][h] - v), w = ex2(s - ref);
-                m[mt][h] = v;
-                l[mt][h] = l[mt][h] * f + (t4 == 0 ? w : 0.f);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                  for (int e = 0; e < 2; ++e) {
-                    const int d = BF ? n * 8 + 2 * t4 + e : (n >> 2) * 32 + 8 * t4 + 4 * e + (n & 3);
-                    const float x = to_f32(vs[kk * DP + swizzled<T, true>(kk, d / PE) * PE + d % PE]);
-                    O[mt][n][2 * h + e] = fmaf(w, x, O[mt][n][2 * h + e] * f);
-                  }
-              }
+            for (int e = 0; e < 2; ++e) {
+              const int d = BF ? n * 8 + 2 * t4 + e : (n >> 2) * 32 + 8 * t4 + 4 * e + (n & 3);
+              const float x = d < p.D ? to_f32(vr[d]) : 0.f;
+              if (h) O[n][2 + e] = fmaf(w, x, O[n][2 + e] * f);
+              else O[n][e] = fmaf(w, x, O[n][e] * f);
             }
         }
-        __syncwarp();
       }
     }
 
-    // the warps' parts of the item: each leaves its values in its own ring
-    float* mine_o = reinterpret_cast<float*>(ring);
+    // the groups' parts of the item: each warp leaves its values in its group's ring
+    if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
+    else __syncwarp();
+    float* mine_o = reinterpret_cast<float*>(ring) + wr * 16 * DP;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = mt * 16 + h * 8 + g;
-        float s = l[mt][h];
-        s += __shfl_xor_sync(~0u, s, 1);
-        s += __shfl_xor_sync(~0u, s, 2);
-        if (t4 == 0) {
-          s_ml[(warp * kRows + r) * 2] = m[mt][h];
-          s_ml[(warp * kRows + r) * 2 + 1] = s;
-        }
-        float* row = mine_o + r * DP;
-        if constexpr (BF) {
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            *reinterpret_cast<float2*>(row + ((n ^ (r & 7)) * 8 + 2 * t4)) =
-                make_float2(O[mt][n][2 * h], O[mt][n][2 * h + 1]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              *reinterpret_cast<float4*>(row + (((4 * i + t4) ^ (r & 7)) * 8 + 4 * e)) =
-                  make_float4(O[mt][4 * i][2 * h + e], O[mt][4 * i + 1][2 * h + e],
-                              O[mt][4 * i + 2][2 * h + e], O[mt][4 * i + 3][2 * h + e]);
-        }
+    for (int h = 0; h < 2; ++h) {
+      const int r = h * 8 + g;
+      float s = l[h];
+      s += __shfl_xor_sync(~0u, s, 1);
+      s += __shfl_xor_sync(~0u, s, 2);
+      if (t4 == 0) {
+        s_ml[(group * kRows + wr * 16 + r) * 2] = m[h];
+        s_ml[(group * kRows + wr * 16 + r) * 2 + 1] = s;
       }
+      float* row = mine_o + r * DP;
+      if constexpr (BF) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          *reinterpret_cast<float2*>(row + ((n ^ (r & 7)) * 8 + 2 * t4)) = make_float2(O[n][2 * h], O[n][2 * h + 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            *reinterpret_cast<float4*>(row + (((4 * i + t4) ^ (r & 7)) * 8 + 4 * e)) = make_float4(
+                O[4 * i][2 * h + e], O[4 * i + 1][2 * h + e], O[4 * i + 2][2 * h + e], O[4 * i + 3][2 * h + e]);
+      }
+    }
     __syncthreads();
     const bool all = t0 == 0 && t1 == n_tiles;
     const int part = t0 > 0 ? 2 * c : 2 * c + 1;
     float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * kRows * 2;
-    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) +
-                  static_cast<size_t>(part) * kRows * DP;
-    for (int e = tid; e < rows * (DP / 4); e += kAThreads) {
+    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * kRows * DP;
+    for (int e = tid; e < rows * (DP / 4); e += kThreadsN) {
       const int r = e / (DP / 4), d = (e % (DP / 4)) * 4;
       float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kAWarps; ++w) M = fmaxf(M, s_ml[(w * kRows + r) * 2]);
+      for (int w = 0; w < kAGroups; ++w) M = fmaxf(M, s_ml[(w * kRows + r) * 2]);
 #pragma unroll
-      for (int w = 0; w < kAWarps; ++w) {
+      for (int w = 0; w < kAGroups; ++w) {
         const float mw = s_ml[(w * kRows + r) * 2], lw = s_ml[(w * kRows + r) * 2 + 1];
         const float f = mw == M ? 1.f : ex2(mw - M);
         const float4 o = *reinterpret_cast<const float4*>(
-            reinterpret_cast<const float*>(ring0 + w * ST * 2 * kHalf) + r * DP +
-            (((d >> 3) ^ (r & 7)) * 8 + (d & 7)));
+            reinterpret_cast<const float*>(a_smem + w * ST * 2 * kHalf) + r * DP + (((d >> 3) ^ (r & 7)) * 8 + (d & 7)));
         L = fmaf(f, lw, L);
         x[0] = fmaf(f, o.x, x[0]);
         x[1] = fmaf(f, o.y, x[1]);
@@ -681,12 +698,11 @@ __global__ void __launch_bounds__(kAThreads) attend_split(const AttendParams p) 
 
 // The items whose keys lie in several CTAs' shares: one CTA per row of the first CTA that
 // went on with an item.  The parts join in the order of the CTAs.
-template <typename T, int DP, int MT>
-__global__ void __launch_bounds__(kAThreads) attend_join(const AttendParams p, int ctas) {
-  constexpr int kRows = 16 * MT;
-  constexpr int kCols = DP / 4, kWays = kAThreads / kCols;
+template <typename T, int DP, int kRows>
+__global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams p, int ctas) {
+  constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  __shared__ float s_w[kAMaxCtas], s_x[kAThreads * 4], s_red[kAWarps];
+  __shared__ float s_w[kAMaxCtas], s_x[kAJoinThreads * 4], s_red[kAWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x + 1, r = blockIdx.y, tid = threadIdx.x;
   const AttendInfo in = reinterpret_cast<const AttendInfo*>(p.ws)[c];
@@ -701,7 +717,7 @@ __global__ void __launch_bounds__(kAThreads) attend_join(const AttendParams p, i
   const float* os = reinterpret_cast<const float*>(p.ws + kAInfoBytes + kMlBytes);
   auto part_of = [&](int k) { return k == 0 ? 2 * c0 + 1 : 2 * (c0 + k); };
   float M = -INFINITY;
-  for (int k = tid; k < parts; k += kAThreads) {
+  for (int k = tid; k < parts; k += kAJoinThreads) {
     const float mk = ml[(static_cast<size_t>(part_of(k)) * kRows + r) * 2];
     s_w[k] = mk;
     M = fmaxf(M, mk);

@@ -365,11 +365,16 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   p.scale2 = scale * kLog2e;
   p.q_vec = aligned(q, 16);
   p.out_vec = aligned(out, 4 * elt);
-  p.same_strides = true;
   for (int i = 0; i < 3; ++i) {
     p.q_vec = p.q_vec && q_strides[i] % per == 0;
     p.out_vec = p.out_vec && out_strides[i] % 4 == 0;
-    p.same_strides = p.same_strides && cache->key_strides[i] == cache->value_strides[i];
+  }
+  p.whole_steps = cache->block_size % kAKeys == 0;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t* strides = i == 0 ? cache->key_strides : cache->value_strides;
+    p.whole_steps = p.whole_steps && strides[0] * elt <= kMax32 && strides[1] * elt * kAKeys <= kMax32;
+    p.block_bytes[i] = static_cast<int>(strides[0] * elt);
+    p.token_bytes[i] = static_cast<int>(strides[1] * elt);
   }
   p.ws = static_cast<char*>(workspace);
   p.err = out_error_word;
@@ -380,7 +385,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   int ctas = std::min(kAMaxCtas, sms * k.ctas_per_sm);
   const cudaStream_t st_ = static_cast<cudaStream_t>(stream);
   void* args[] = {&p, &ctas};
-  e = cudaLaunchKernel(k.split, dim3(ctas), dim3(kAThreads), args, k.smem, st_);
+  e = cudaLaunchKernel(k.split, dim3(ctas), dim3(k.threads), args, k.smem, st_);
   if (e != cudaSuccess) return cuda_fail(e);
   if (ctas == 1) return ASYMSPEC_OK;
   cudaLaunchConfig_t cfg = {};
@@ -388,7 +393,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3(ctas - 1, std::min(p.rows, k.rows));
-  cfg.blockDim = dim3(kAThreads);
+  cfg.blockDim = dim3(kAJoinThreads);
   cfg.stream = st_;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
