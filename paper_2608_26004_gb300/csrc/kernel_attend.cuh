@@ -37,7 +37,7 @@ constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each
 // of its tiles, after kAItem for what it costs to begin and end one.
-constexpr int kAItem = 2;
+constexpr int kAItem = 3;
 
 // A CTA whose share begins after the first tile of an item says which.
 struct AttendInfo {

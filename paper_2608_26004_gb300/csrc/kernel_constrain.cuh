@@ -24,7 +24,7 @@ constexpr int kCThreads = 256;
 constexpr int kCUnroll = 4;
 constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
 constexpr int kCMaxCluster = 8;
-constexpr int kCBiases = 512;  // a slice's bias entries that shared memory holds
+constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
 // A token's word: in the prompt, among the drafts, biased, and how often in the output.
 constexpr unsigned kCPrompt = 1u << 31, kCDraft = 1u << 30, kCBias = 1u << 29, kCCount = kCBias - 1;
 
@@ -70,6 +70,12 @@ __device__ __forceinline__ unsigned mask_bits(const uint32_t* mask, int v) {
   return __funnelshift_r(lo, hi, sh) & ((1u << VE) - 1u);
 }
 
+template <int N>
+__device__ __forceinline__ void cp_async_at(unsigned smem, const void* gmem) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem), "l"(gmem) : "memory");
+}
+
 // Entries of a row's slice before its first 16-byte boundary.
 template <typename T>
 __device__ __forceinline__ int entries_before(const T* p) {
@@ -86,12 +92,31 @@ struct Slice {
   int b, v0, n, W;
 };
 
+// A request's numbers, all on their way together before the CTA's first barrier.
+struct Request {
+  int len0, prompt0, bias0, bias1, draft;
+  float rep, freq, pres;
+  __device__ __forceinline__ Request(const CParams& p, int b) {
+    const asymspec_constraints& c = p.c;
+    len0 = c.history ? c.history_len[b] : 0;
+    prompt0 = c.prompt_len ? c.prompt_len[b] : 0;
+    bias0 = c.bias_offsets ? c.bias_offsets[b] : 0;
+    bias1 = c.bias_offsets ? c.bias_offsets[b + 1] : 0;
+    const int tid = threadIdx.x;  // (P - 1 is at most the CTA's threads)
+    draft = c.drafts && tid < p.P - 1 ? c.drafts[b * c.drafts_ld + tid] : 0;
+    rep = c.repetition ? c.repetition[b] : 1.f;
+    freq = c.frequency ? c.frequency[b] : 0.f;
+    pres = c.presence ? c.presence[b] : 0.f;
+  }
+};
+static_assert(ASYMSPEC_CONSTRAIN_MAX_P - 1 <= kCThreads, "a thread per draft");
+
 // The tokens of the history are counted in shared memory: each CTA reads all of it (from
 // the L2) and counts its slice's, or, where histories are long (CLUSTER), the CTAs of a
 // cluster read a share each and count a token where its slice is.  Ends at a barrier; the
 // words are zero at the start, which a barrier before says.
 template <bool CLUSTER>
-__device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s) {
+__device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s, const Request& r) {
   const asymspec_constraints& c = p.c;
   const int b = s.b, v0 = s.v0, n = s.n, W = s.W, tid = threadIdx.x;
   cg::cluster_group cluster = cg::this_cluster();
@@ -99,9 +124,8 @@ __device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s
   const int rank = CLUSTER ? static_cast<int>(cluster.block_rank()) : 0;
   unsigned err = 0;
   if (c.history) {
-    const int len0 = c.history_len[b], len = min(max(len0, 0), c.history_width);
-    const int pl0 = c.prompt_len ? c.prompt_len[b] : 0, pl = min(max(pl0, 0), len);
-    if (len != len0 || pl != pl0) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    const int len = min(max(r.len0, 0), c.history_width), pl = min(max(r.prompt0, 0), len);
+    if (len != r.len0 || pl != r.prompt0) err |= ASYMSPEC_DATA_BAD_LENGTH;
     const int32_t* h = c.history + b * c.history_ld;
     const int first = v0 - rank * W;  // of the cluster's entries
     auto count = [&](int v, int i) {
@@ -135,17 +159,14 @@ __device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s
       }
     }
   }
-  if (c.drafts) {
-    for (int j = tid; j < p.P - 1; j += kCThreads) {
-      const int v = c.drafts[b * c.drafts_ld + j];
-      if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (v >= v0 && v < v0 + n) atomicOr(&s.words[v - v0], kCDraft);
-    }
+  if (c.drafts && tid < p.P - 1) {
+    const int v = r.draft;
+    if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
+    else if (v >= v0 && v < v0 + n) atomicOr(&s.words[v - v0], kCDraft);
   }
   if (c.bias_offsets) {
-    const int a0 = c.bias_offsets[b], e0 = c.bias_offsets[b + 1];
-    const int a = min(max(a0, 0), c.bias_count), e = min(max(e0, a), c.bias_count);
-    if (a != a0 || e != e0) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    const int a = min(max(r.bias0, 0), c.bias_count), e = min(max(r.bias1, a), c.bias_count);
+    if (a != r.bias0 || e != r.bias1) err |= ASYMSPEC_DATA_BAD_LENGTH;
     for (int i = a + tid; i < e; i += kCThreads) {
       const int v = c.bias_tokens[i];
       if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
@@ -180,11 +201,8 @@ __device__ __forceinline__ void list_slice(const Slice& s) {
 
 struct Penalties {
   float rep, freq, pres, top;
-  __device__ __forceinline__ Penalties(const CParams& p, int b, float top_, unsigned& err) : top(top_) {
-    const asymspec_constraints& c = p.c;
-    rep = c.repetition ? c.repetition[b] : 1.f;
-    freq = c.frequency ? c.frequency[b] : 0.f;
-    pres = c.presence ? c.presence[b] : 0.f;
+  __device__ __forceinline__ Penalties(const Request& r, float top_, unsigned& err)
+      : rep(r.rep), freq(r.freq), pres(r.pres), top(top_) {
     if (!(rep > 0.f && rep <= FLT_MAX && fabsf(freq) <= FLT_MAX && fabsf(pres) <= FLT_MAX)) {
       err |= ASYMSPEC_DATA_BAD_PENALTY;
       rep = 1.f;
@@ -247,14 +265,14 @@ __device__ __forceinline__ bool allowed(const CParams& p, int at, int v) {
 // cp.async while the history is counted; the entries that a penalty or a bias touches,
 // gathered in a list so that no lane is idle, are computed there (scattered over the
 // rows in global memory they took longer than the rows); then the rows leave under
-// their masks.  A vector that its row's mask leaves nothing of is not read.  The
-// slices of the lowest token ids, which a vocabulary gives to the most frequent tokens,
+// their masks.  The slices of the lowest token ids, which a vocabulary gives to the most frequent tokens,
 // come first in the grid: theirs are the most entries to compute.
 template <typename T, bool EDGES, bool CLUSTER>
 __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) {
   extern __shared__ __align__(16) unsigned c_smem[];
   __shared__ int2 s_bias[kCBiases];
-  __shared__ uint8_t s_bits[EDGES ? 1 : kCSlots][kCThreads];
+  __shared__ uint32_t s_mask[kCSlots * kCThreads / 4];  // the rows' masks, the slice's words of each
+  __shared__ int s_at[kCSlots];                         // which, -1: none, -2: one that allows nothing
   __shared__ int s_listed, s_biases;
   constexpr int VE = 16 / sizeof(T);
   constexpr unsigned kAll = (1u << VE) - 1u;
@@ -272,36 +290,20 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
     return EDGES ? static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15u) : 0;
   };
 
-  // A batch of rows on its way into shared memory.  A thread's vectors of it are slots 0, 1, ..,
-  // row by row; the bits that the masks allow wait in shared memory for the rows to leave.
-  const int batch = p.batch_rows, per_row = W / VE / kCThreads;
-  auto begin = [&](int first_row, int rows) {
+  // A batch of rows, and their masks' words, on the way into shared memory
+  const int batch = p.batch_rows, row_words = W / 32;
+  const unsigned tile_at = smem_u32(tile);
+  auto load_rows = [&](int first_row, int rows) {
     const T* from = x + static_cast<int64_t>(first_row) * p.ld;
     if constexpr (!EDGES) {
-#pragma unroll
-      for (int s0 = 0; s0 < kCSlots; s0 += kCUnroll) {
-        if (s0 >= per_row * rows) break;
-        int at[kCUnroll], k[kCUnroll], i[kCUnroll];
-        unsigned got[kCUnroll];
-#pragma unroll
-        for (int s = 0; s < kCUnroll; ++s) {
-          k[s] = (s0 + s) / per_row;
-          i[s] = (s0 + s) % per_row * kCThreads + tid;
-          at[s] = -2;
-          if (k[s] < rows && i[s] * VE < n) at[s] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k[s], err);
-        }
-#pragma unroll
-        for (int s = 0; s < kCUnroll; ++s) {
-          got[s] = at[s] == -1 ? kAll : 0u;
-          if (at[s] >= 0) {
-            const uint8_t* mask = reinterpret_cast<const uint8_t*>(c.mask + at[s] * c.mask_ld + (v0 >> 5));
-            got[s] = VE == 8 ? mask[i[s]] : (mask[i[s] >> 1] >> ((i[s] & 1) * 4)) & kAll;
-          }
-        }
-#pragma unroll
-        for (int s = 0; s < kCUnroll; ++s) {
-          if (got[s] != 0) cp_async16(tile + k[s] * pitch + i[s] * 16, from + k[s] * p.ld + i[s] * VE);
-          s_bits[s0 + s][tid] = static_cast<uint8_t>(got[s]);
+      for (int i = tid; i * VE < n; i += kCThreads) {
+        const T* src = from + i * VE;
+        unsigned dst = tile_at + i * 16;
+#pragma unroll 4
+        for (int k = 0; k < rows; ++k) {
+          cp_async_at<16>(dst, src);
+          src += p.ld;
+          dst += pitch;
         }
       }
     } else {
@@ -314,20 +316,34 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
             for (int e = max(e0, 0); e < min(e0 + VE, n); ++e)
               *reinterpret_cast<T*>(tile + k * pitch + off + e * sizeof(T)) = row[e];
           } else {
-            cp_async16(tile + k * pitch + j * 16, row + e0);
+            cp_async_at<16>(tile_at + k * pitch + j * 16, row + e0);
           }
         }
       }
     }
+  };
+  auto load_masks = [&](int first_row, int rows) {
+    if (c.mask) {
+      for (int q = tid; q < rows * row_words; q += kCThreads) {
+        const int k = q / row_words, w = q - k * row_words;
+        const int at = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k, err);
+        if (w == 0) s_at[k] = at;
+        if (at >= 0 && w * 32 < n) cp_async_at<4>(smem_u32(s_mask + q), c.mask + at * c.mask_ld + (v0 >> 5) + w);
+      }
+    } else if (tid < rows) {
+      s_at[tid] = -1;
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
+  load_rows(0, min(batch, k_end - k0));
+  const Request request(p, b);
   if (tid == 0) s_listed = s_biases = 0;
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
-  begin(0, min(batch, k_end - k0));
+  load_masks(0, min(batch, k_end - k0));
   if constexpr (CLUSTER) cg::this_cluster().sync();
   else __syncthreads();
-  err |= count_slice<CLUSTER>(p, slice);
+  err |= count_slice<CLUSTER>(p, slice, request);
   if (CLUSTER && n <= 0) return;
   list_slice(slice);
   const float top = type_max(T());
@@ -335,14 +351,15 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
   unsigned low_word;
   if constexpr (sizeof(T) == 4) low_word = __float_as_uint(low);
   else low_word = __bfloat16_as_ushort(low) * 0x10001u;
-  const Penalties penalties(p, b, top, err);
+  const Penalties penalties(request, top, err);
   for (int first_row = 0;;) {
     const int rows = min(batch, k_end - k0 - first_row);
     const T* xt = x + static_cast<int64_t>(first_row) * p.ld;
     T* yt = y + static_cast<int64_t>(first_row) * p.out_ld;
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
-    for (int q = tid; q < s_listed; q += kCThreads) {
+    const int listed = s_listed;
+    for (int q = tid; q < listed; q += kCThreads) {
       const int i = slice.list[q];
       Touched u(p, slice, i, k0 + first_row);
 #pragma unroll 4
@@ -352,36 +369,40 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
         u.past(p, slice, k0 + first_row + k);
       }
     }
-    __syncthreads();
+    if (listed > 0) __syncthreads();
     if constexpr (!EDGES) {
+      for (int i = tid; i * VE < n; i += kCThreads) {
+        const unsigned char* src = tile + i * 16;
+        T* dst = yt + i * VE;
 #pragma unroll 4
-      for (int s = 0; s < per_row * rows; ++s) {
-        const int k = per_row == 1 ? s : s / per_row, i = (per_row == 1 ? 0 : s % per_row) * kCThreads + tid;
-        if (i * VE >= n) continue;
-        const unsigned on = s_bits[s][tid];
-        uint4 v = make_uint4(low_word, low_word, low_word, low_word);
-        if (on != 0) {
-          v = *reinterpret_cast<const uint4*>(tile + k * pitch + i * 16);
-          if (on != kAll) v = masked16<T>(v, on, low_word);
+        for (int k = 0; k < rows; ++k) {
+          uint4 v = *reinterpret_cast<const uint4*>(src);
+          const int at = s_at[k];
+          if (at != -1) {
+            const uint8_t* mask = reinterpret_cast<const uint8_t*>(s_mask + k * row_words);
+            const unsigned on = at < 0 ? 0u : VE == 8 ? mask[i] : (mask[i >> 1] >> ((i & 1) * 4)) & kAll;
+            v = masked16<T>(v, on, low_word);
+          }
+          *reinterpret_cast<uint4*>(dst) = v;
+          src += pitch;
+          dst += p.out_ld;
         }
-        *reinterpret_cast<uint4*>(yt + k * p.out_ld + i * VE) = v;
       }
     } else {
       for (int k = 0; k < rows; ++k) {
         T* row = yt + k * p.out_ld;
         const T* from = reinterpret_cast<const T*>(tile + k * pitch + misplaced(xt + k * p.ld));
-        const int first = misplaced(row) / static_cast<int>(sizeof(T));
-        const int at = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k, err);
-        const uint32_t* mask = c.mask + (at > 0 ? at : 0) * c.mask_ld + (v0 >> 5);
+        const int first = misplaced(row) / static_cast<int>(sizeof(T)), at = s_at[k];
+        const uint32_t* mask = s_mask + k * row_words;
         for (int j = tid; j * VE - first < n; j += kCThreads) {
           const int e0 = j * VE - first;
           if (e0 < 0 || e0 + VE > n) {
-            for (int e = max(e0, 0); e < min(e0 + VE, n); ++e) row[e] = allowed(p, at, v0 + e) ? from[e] : low;
+            for (int e = max(e0, 0); e < min(e0 + VE, n); ++e)
+              row[e] = at == -1 || (at >= 0 && ((mask[e >> 5] >> (e & 31)) & 1u)) ? from[e] : low;
           } else {
-            const unsigned on = at < 0 ? (at == -1 ? kAll : 0u) : mask_bits<T>(mask, e0);
             uint4 v = reinterpret_cast<uintptr_t>(from + e0) % 16 == 0
                           ? *reinterpret_cast<const uint4*>(from + e0) : gather16(from + e0);
-            if (on != kAll) v = masked16<T>(v, on, low_word);
+            if (at != -1) v = masked16<T>(v, at < 0 ? 0u : mask_bits<T>(mask, e0), low_word);
             *reinterpret_cast<uint4*>(row + e0) = v;
           }
         }
@@ -390,7 +411,8 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
     first_row += rows;
     if (k0 + first_row >= k_end) break;
     __syncthreads();
-    begin(first_row, min(batch, k_end - k0 - first_row));
+    load_rows(first_row, min(batch, k_end - k0 - first_row));
+    load_masks(first_row, min(batch, k_end - k0 - first_row));
   }
   if (err && p.err) atomicOr(p.err, err);
 }
@@ -411,13 +433,14 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   const Slice slice = {c_smem, reinterpret_cast<uint16_t*>(c_smem + W), s_bias, &s_listed, &s_biases, b, v0, n, W};
   const int k0 = blockIdx.z * p.group_rows, rows = min(p.group_rows, p.P - k0);
   unsigned err = 0;
+  const Request request(p, b);
   if (tid == 0) s_listed = s_biases = 0;
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
   for (int k = tid; k < rows; k += kCThreads)
     s_mask[k] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + k, err);
   if constexpr (CLUSTER) cg::this_cluster().sync();
   else __syncthreads();
-  err |= count_slice<CLUSTER>(p, slice);
+  err |= count_slice<CLUSTER>(p, slice, request);
   if (CLUSTER && n <= 0) return;
   list_slice(slice);
   const float top = type_max(T());
@@ -425,7 +448,7 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   unsigned low_word;
   if constexpr (sizeof(T) == 4) low_word = __float_as_uint(low);
   else low_word = __bfloat16_as_ushort(low) * 0x10001u;
-  const Penalties penalties(p, b, top, err);
+  const Penalties penalties(request, top, err);
   T* x = static_cast<T*>(p.out) + (static_cast<int64_t>(b) * p.P + k0) * p.out_ld + v0;
   for (int k = 0; k < rows; ++k) {
     const int at = s_mask[k];

@@ -156,6 +156,15 @@ def test_the_last_bias_of_a_token_counts(torch):
     assert y[0, 0, 5] == 5 and y[0, 0, 7] == 4 and y[0, 0, 5999] == 6 and y.sum() == 15
 
 
+def test_more_biases_than_a_slice_holds(torch):
+    i32 = dict(device="cuda", dtype=torch.int32)
+    g = torch.Generator(device="cuda").manual_seed(77)
+    z = torch.randn(2, 3, 1500, generator=g, device="cuda")
+    tokens = torch.randint(0, 1500, (3000,), generator=g, **i32)
+    x = dict(bias=(torch.tensor([0, 2900, 3000], **i32), tokens, torch.randn(3000, generator=g, device="cuda")))
+    check(torch, z, x, S.constrain_logits(z, **x))
+
+
 def test_bad_data_sets_bits_and_leaves_the_rest(torch):
     i32 = dict(device="cuda", dtype=torch.int32)
     z, x = inputs(torch, 2, 3, 500, torch.float32, 40, 21, 0, None, 0)
