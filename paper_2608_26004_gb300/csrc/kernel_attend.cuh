@@ -439,10 +439,17 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
             }
           }
         } else {
-          // the sum over a head's elements in an order of its own: of each 16, lane t4 of a
-          // quad takes elements 4 t4 .. 4 t4 + 3, two for each of two products
+          // The sum over a head's elements in an order of its own: of each 16, lane t4 of a
+          // quad takes elements 4 t4 .. 4 t4 + 3, two for each of two products.  The matrix
+          // unit's running sums are cut, not rounded: the pieces' products have sums of their
+          // own, the large ones two, added up in fp32 at the end.
           const float* kf = reinterpret_cast<const float*>(ks);
           const float* qw = reinterpret_cast<const float*>(qs) + wr * 16 * DP;
+          float large[2][4], small[2][4];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) large[n][e] = small[n][e] = 0.f;
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
             const int at = g * DP + swizzled<T, false>(g, 4 * k + t4) * 4;  // (row g + 8: the same chunk)
@@ -460,14 +467,19 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
               split_tf32(x.y, kh4[1], kl4[1]);
               split_tf32(x.z, kh4[2], kl4[2]);
               split_tf32(x.w, kh4[3], kl4[3]);
+              mma_tf32(S[n], qh[0], kh4[0], kh4[1]);
+              mma_tf32(large[n], qh[1], kh4[2], kh4[3]);
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                mma_tf32(S[n], ql[e], kh4[2 * e], kh4[2 * e + 1]);
-                mma_tf32(S[n], qh[e], kl4[2 * e], kl4[2 * e + 1]);
-                mma_tf32(S[n], qh[e], kh4[2 * e], kh4[2 * e + 1]);
+                mma_tf32(small[n], ql[e], kh4[2 * e], kh4[2 * e + 1]);
+                mma_tf32(small[n], qh[e], kl4[2 * e], kl4[2 * e + 1]);
               }
             }
           }
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[n][e] += large[n][e] + small[n][e];
         }
         const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
 #pragma unroll
@@ -529,19 +541,29 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
             mma_bf16(O[2 * n + 1], ph, vf[2], vf[3]);
           }
         } else {
-          // keys 2 t4 and 2 t4 + 1 of each eight are the products' elements t4 and t4 + 4; of each
-          // 32 elements of a head, lane group g takes 4 g .. 4 g + 3, one for each of four products
+          // Keys 2 t4 and 2 t4 + 1 of each eight are the products' elements t4 and t4 + 4; of each
+          // 32 elements of a head, lane group g takes 4 g .. 4 g + 3, one for each of four
+          // products.  A step's products are summed by themselves and added to the running
+          // values in fp32, which rounds where the matrix unit would cut.
           const float* vf = reinterpret_cast<const float*>(vs);
+          unsigned ph[2][4], pl[2][4];
 #pragma unroll
           for (int n8 = 0; n8 < 2; ++n8) {
-            unsigned ph[4], pl[4];
-            split_tf32(S[n8][0], ph[0], pl[0]);
-            split_tf32(S[n8][2], ph[1], pl[1]);
-            split_tf32(S[n8][1], ph[2], pl[2]);
-            split_tf32(S[n8][3], ph[3], pl[3]);
-            const int r0 = n8 * 8 + 2 * t4, r1 = r0 + 1;
+            split_tf32(S[n8][0], ph[n8][0], pl[n8][0]);
+            split_tf32(S[n8][2], ph[n8][1], pl[n8][1]);
+            split_tf32(S[n8][1], ph[n8][2], pl[n8][2]);
+            split_tf32(S[n8][3], ph[n8][3], pl[n8][3]);
+          }
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
+          for (int i = 0; i < DP / 32; ++i) {
+            float sum[4][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sum[e][j] = 0.f;
+#pragma unroll
+            for (int n8 = 0; n8 < 2; ++n8) {
+              const int r0 = n8 * 8 + 2 * t4, r1 = r0 + 1;
               const float4 x = *reinterpret_cast<const float4*>(vf + r0 * DP + swizzled<T, true>(r0, 8 * i + g) * 4);
               const float4 y = *reinterpret_cast<const float4*>(vf + r1 * DP + swizzled<T, true>(r1, 8 * i + g) * 4);
               const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
@@ -550,11 +572,15 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
                 unsigned h0, l0, h1, l1;
                 split_tf32(xs[e], h0, l0);
                 split_tf32(ys[e], h1, l1);
-                mma_tf32(O[4 * i + e], pl, h0, h1);
-                mma_tf32(O[4 * i + e], ph, l0, l1);
-                mma_tf32(O[4 * i + e], ph, h0, h1);
+                mma_tf32(sum[e], pl[n8], h0, h1);
+                mma_tf32(sum[e], ph[n8], l0, l1);
+                mma_tf32(sum[e], ph[n8], h0, h1);
               }
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) O[4 * i + e][j] += sum[e][j];
           }
         }
       }

@@ -21,9 +21,8 @@ struct CParams {
 };
 
 constexpr int kCThreads = 256;
-constexpr int kCUnroll = 4;
+constexpr int kCAhead = 4;     // 16-byte loads of the history that a thread has on their way
 constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
-constexpr int kCMaxCluster = 8;
 constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
 // A token's word: in the prompt, among the drafts, biased, and how often in the output.
 constexpr unsigned kCPrompt = 1u << 31, kCDraft = 1u << 30, kCBias = 1u << 29, kCCount = kCBias - 1;
@@ -112,44 +111,38 @@ struct Request {
 static_assert(ASYMSPEC_CONSTRAIN_MAX_P - 1 <= kCThreads, "a thread per draft");
 
 // The tokens of the history are counted in shared memory: each CTA reads all of it (from
-// the L2) and counts its slice's, or, where histories are long (CLUSTER), the CTAs of a
-// cluster read a share each and count a token where its slice is.  Ends at a barrier; the
-// words are zero at the start, which a barrier before says.
-template <bool CLUSTER>
+// the L2) and counts its slice's.  Ends at a barrier; the words are zero at the start,
+// which a barrier before says.  (Clusters whose CTAs read a share each and count a token
+// where its slice is, by remote atomics: 92 us for 32 requests of 65,536 tokens each against
+// 117, but 61 against 47 at 8,000 and 66 against 60 at 20,000.)
 __device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s, const Request& r) {
   const asymspec_constraints& c = p.c;
-  const int b = s.b, v0 = s.v0, n = s.n, W = s.W, tid = threadIdx.x;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int C = CLUSTER ? static_cast<int>(cluster.num_blocks()) : 1;
-  const int rank = CLUSTER ? static_cast<int>(cluster.block_rank()) : 0;
+  const int b = s.b, v0 = s.v0, n = s.n, tid = threadIdx.x;
   unsigned err = 0;
   if (c.history) {
     const int len = min(max(r.len0, 0), c.history_width), pl = min(max(r.prompt0, 0), len);
     if (len != r.len0 || pl != r.prompt0) err |= ASYMSPEC_DATA_BAD_LENGTH;
     const int32_t* h = c.history + b * c.history_ld;
-    const int first = v0 - rank * W;  // of the cluster's entries
     auto count = [&](int v, int i) {
       if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (static_cast<unsigned>(v - first) < static_cast<unsigned>(C * W)) {
-        unsigned* word = s.words + ((v - first) & (W - 1));
-        if constexpr (CLUSTER) word = cluster.map_shared_rank(word, (v - first) / W);
-        if (i < pl) atomicOr(word, kCPrompt);
-        else atomicAdd(word, 1u);
+      else if (static_cast<unsigned>(v - v0) < static_cast<unsigned>(n)) {
+        if (i < pl) atomicOr(&s.words[v - v0], kCPrompt);
+        else atomicAdd(&s.words[v - v0], 1u);
       }
     };
     // four tokens a load from the first 16-byte boundary on
     const int head = min(entries_before(h), len), fours = (len - head) / 4;
     const int end = head + fours * 4;
-    if (rank == 0 && tid < head) count(h[tid], tid);
-    if (rank == 0 && tid < len - end) count(h[end + tid], end + tid);
+    if (tid < head) count(h[tid], tid);
+    if (tid < len - end) count(h[end + tid], end + tid);
     const int4* h4 = reinterpret_cast<const int4*>(h + head);
-    for (int i0 = rank * kCThreads * kCUnroll + tid; i0 < fours; i0 += C * kCThreads * kCUnroll) {
-      int4 v[kCUnroll];
+    for (int i0 = tid; i0 < fours; i0 += kCThreads * kCAhead) {
+      int4 v[kCAhead];
 #pragma unroll
-      for (int e = 0; e < kCUnroll; ++e)
+      for (int e = 0; e < kCAhead; ++e)
         if (i0 + e * kCThreads < fours) v[e] = h4[i0 + e * kCThreads];
 #pragma unroll
-      for (int e = 0; e < kCUnroll; ++e) {
+      for (int e = 0; e < kCAhead; ++e) {
         if (i0 + e * kCThreads >= fours) break;
         const int i = head + (i0 + e * kCThreads) * 4;
         count(v[e].x, i);
@@ -177,8 +170,7 @@ __device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s
       }
     }
   }
-  if constexpr (CLUSTER) cluster.sync();
-  else __syncthreads();
+  __syncthreads();
   return err;
 }
 
@@ -267,7 +259,7 @@ __device__ __forceinline__ bool allowed(const CParams& p, int at, int v) {
 // rows in global memory they took longer than the rows); then the rows leave under
 // their masks.  The slices of the lowest token ids, which a vocabulary gives to the most frequent tokens,
 // come first in the grid: theirs are the most entries to compute.
-template <typename T, bool EDGES, bool CLUSTER>
+template <typename T, bool EDGES>
 __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) {
   extern __shared__ __align__(16) unsigned c_smem[];
   __shared__ int2 s_bias[kCBiases];
@@ -341,10 +333,8 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
   if (tid == 0) s_listed = s_biases = 0;
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
   load_masks(0, min(batch, k_end - k0));
-  if constexpr (CLUSTER) cg::this_cluster().sync();
-  else __syncthreads();
-  err |= count_slice<CLUSTER>(p, slice, request);
-  if (CLUSTER && n <= 0) return;
+  __syncthreads();
+  err |= count_slice(p, slice, request);
   list_slice(slice);
   const float top = type_max(T());
   const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());
@@ -420,7 +410,7 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
 // The logits constrained where they are: what nothing changes is neither read nor written.
 // The masked entries are overwritten, a row's vectors at a time; then the entries that a
 // penalty or a bias touches are computed, each where it lies.
-template <typename T, bool CLUSTER>
+template <typename T>
 __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p) {
   extern __shared__ __align__(16) unsigned c_smem[];
   __shared__ int2 s_bias[kCBiases];
@@ -438,10 +428,8 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
   for (int k = tid; k < rows; k += kCThreads)
     s_mask[k] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + k, err);
-  if constexpr (CLUSTER) cg::this_cluster().sync();
-  else __syncthreads();
-  err |= count_slice<CLUSTER>(p, slice, request);
-  if (CLUSTER && n <= 0) return;
+  __syncthreads();
+  err |= count_slice(p, slice, request);
   list_slice(slice);
   const float top = type_max(T());
   const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());

@@ -62,19 +62,11 @@ constexpr int kPlanTokens = 2048;
 // least, of one row or of several.
 constexpr int kVectors = 256;
 constexpr int kThreadVectors = 4;
-// Histories that may be longer than this are counted by clusters.
-constexpr int kLongHistory = 16384;
-
 template <typename T>
-const void* constrain_pick(bool in_place, bool edges, bool clusters) {
-  if (in_place)
-    return clusters ? reinterpret_cast<const void*>(&constrain_in_place<T, true>)
-                    : reinterpret_cast<const void*>(&constrain_in_place<T, false>);
-  if (edges)
-    return clusters ? reinterpret_cast<const void*>(&constrain_rows<T, true, true>)
-                    : reinterpret_cast<const void*>(&constrain_rows<T, true, false>);
-  return clusters ? reinterpret_cast<const void*>(&constrain_rows<T, false, true>)
-                  : reinterpret_cast<const void*>(&constrain_rows<T, false, false>);
+const void* constrain_pick(bool in_place, bool edges) {
+  if (in_place) return reinterpret_cast<const void*>(&constrain_in_place<T>);
+  return edges ? reinterpret_cast<const void*>(&constrain_rows<T, true>)
+               : reinterpret_cast<const void*>(&constrain_rows<T, false>);
 }
 
 AttendKernels attend_kernels(int dtype, int D, int rows) {
@@ -172,26 +164,13 @@ int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits,
   const bool in_place = logits == out;
   const size_t smem = constrain_list_bytes(p.W) +
                       (in_place ? 0 : static_cast<size_t>(p.batch_rows) * constrain_pitch(p.W, elt));
-  const bool clusters = c->history && c->history_width > kLongHistory && slices > 1;
-  const int C = clusters ? static_cast<int>(std::min<int64_t>(slices, kCMaxCluster)) : 1;
-  const void* fn = dtype == ASYMSPEC_FP32 ? constrain_pick<float>(in_place, edges, clusters)
-                                          : constrain_pick<__nv_bfloat16>(in_place, edges, clusters);
+  const void* fn = dtype == ASYMSPEC_FP32 ? constrain_pick<float>(in_place, edges)
+                                          : constrain_pick<__nv_bfloat16>(in_place, edges);
   e = prepare(fn, device, static_cast<int>(smem));
   if (e != cudaSuccess) return cuda_fail(e);
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 1;
-  attr[0].val.clusterDim.y = C;
-  attr[0].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(B, static_cast<unsigned>((slices + C - 1) / C * C), groups);
-  cfg.blockDim = dim3(kCThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = static_cast<cudaStream_t>(stream);
-  cfg.attrs = attr;
-  cfg.numAttrs = clusters ? 1 : 0;
   void* args[] = {&p};
-  e = cudaLaunchKernelExC(&cfg, fn, args);
+  e = cudaLaunchKernel(fn, dim3(B, static_cast<unsigned>(slices), groups), dim3(kCThreads), args, smem,
+                       static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
 }
 
