@@ -1,0 +1,79 @@
+"""The serving loop of examples/serving_round.py: what is committed keeps the rules, and every
+cache holds exactly the committed tokens' keys and values."""
+import importlib.util
+import os
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def example():
+    import torch
+    assert torch.cuda.is_available(), "the gpu tests need a CUDA device"
+    from paper_2608_26004_gb300 import build
+    build.build_cuda()
+    spec = importlib.util.spec_from_file_location("serving_round", os.path.join(ROOT, "examples", "serving_round.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.parametrize("B,K,rounds", [(6, 4, 10), (1, 1, 6), (17, 7, 5)])
+def test_rounds_commit_what_the_rules_allow(example, B, K, rounds):
+    import torch
+    loop = example.Loop(B=B, K=K, V=1024, prompt=(30, 70), rounds=rounds, seed=B)
+    accepted = 0
+    for _ in range(rounds):
+        error = loop.round()
+        assert int(error) == 0
+        assert (loop.accepted >= 0).all()
+        accepted += int(loop.accepted.sum())
+    assert [int(c.error) for c in loop.contexts] == [0, 0, 0]
+    for b in range(B):
+        said = loop.history[b, int(loop.prompt_len[b]):int(loop.history_len[b])]
+        assert rounds <= said.numel() <= rounds * (K + 1)
+        assert (said != 0).all()
+        if b % 2 == 0:
+            assert (said < 512).all()
+    # cached: the prompt, then the round's first token (the prompt's last, again) and what was
+    # accepted; the last next token is not cached yet
+    for c in loop.contexts:
+        length = c.state["start"] + loop.accepted + 1
+        for b in range(B):
+            n = int(length[b])
+            committed = loop.history[b, int(loop.prompt_len[b]) - 1:int(loop.history_len[b]) - 1]
+            at = torch.arange(n - committed.numel(), n, device="cuda")
+            page = c.tables[b].long()[at // c.block_size]
+            _, _, k, v = c.project(committed)
+            close = dict(rtol=0.02, atol=0.02)  # (another shape of matrix product may round otherwise)
+            assert torch.allclose(c.keys[page, at % c.block_size].float(), k.float(), **close)
+            assert torch.allclose(c.values[page, at % c.block_size].float(), v.float(), **close)
+
+
+def test_attention_of_the_loop_equals_attention_without_a_cache(example):
+    """The verifier's logits of a round against dense attention over the committed tokens."""
+    import torch
+    loop = example.Loop(B=4, K=3, V=512, prompt=(25, 50), rounds=4, seed=9)
+    for _ in range(3):
+        loop.round()
+    c, m = loop.verifier, loop.verifier.model
+    c.plan(loop.K + 1, loop.accepted)
+    tokens = torch.randint(0, 512, (4, loop.K + 1), device="cuda")
+    got = c.logits(tokens).float()
+    start = c.state["start"].tolist()
+    for b in range(4):
+        n = start[b]
+        at = torch.arange(n + loop.K + 1, device="cuda")
+        page = c.tables[b].long()[at // 16]
+        k, v = c.keys[page, at % 16].double(), c.values[page, at % 16].double()
+        x, q, _, _ = c.project(tokens[b])
+        for i in range(loop.K + 1):
+            kk, vv = (t[:n + i + 1].repeat_interleave(m.heads // m.kv_heads, 1) for t in (k, v))
+            s = torch.einsum("hd,nhd->hn", q[i].double(), kk) / m.dim ** 0.5
+            o = torch.einsum("hn,nhd->hd", s.softmax(-1), vv).reshape(-1).bfloat16()
+            want = m.logits(x[i], o).float()
+            assert (got[b, i] - want).abs().max() <= 0.05 * want.abs().max()
