@@ -55,7 +55,10 @@ def test_rounds_commit_what_the_rules_allow(example, B, K, rounds):
 
 
 def test_attention_of_the_loop_equals_attention_without_a_cache(example):
-    """The verifier's logits of a round against dense attention over the committed tokens."""
+    """The verifier's logits of a round against dense attention over the committed tokens.  The
+    attention's output is rounded to bf16 (2^-8) before two bf16 products; a logit sums 128
+    terms of either sign, so 5 % of the largest logit is ample for it and far below what a
+    wrong key or position does."""
     import torch
     loop = example.Loop(B=4, K=3, V=512, prompt=(25, 50), rounds=4, seed=9)
     for _ in range(3):

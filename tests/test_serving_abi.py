@@ -163,3 +163,17 @@ def test_structs_as_bytes_have_the_structures_layout():
     x = S.Cache.from_buffer_copy(S._CACHE.pack(*range(1, 14)))
     assert (x.keys, x.values, list(x.key_strides), list(x.value_strides)) == (1, 2, [3, 4, 5], [6, 7, 8])
     assert (x.num_blocks, x.block_size, x.kv_heads, x.head_dim, x.dtype) == (9, 10, 11, 12, 13)
+
+
+def test_the_joining_kernel_waits_for_the_one_before():
+    # attend_join is a programmatic dependent: resident while attend_split still runs
+    import os
+    import re
+    with open(os.path.join(build.CSRC, "serving.cu")) as f:
+        host = re.sub(r"//[^\n]*", "", f.read())
+    assert host.count("programmaticStreamSerializationAllowed = 1") == 1
+    with open(os.path.join(build.CSRC, "kernel_attend.cuh")) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    body = text[text.index(" attend_join("):]
+    first = re.search(r"griddepcontrol\.wait|\breturn;|p\.ws", body)
+    assert first and first.group().startswith("griddep")
