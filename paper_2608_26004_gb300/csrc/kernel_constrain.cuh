@@ -21,7 +21,7 @@ struct CParams {
 };
 
 constexpr int kCThreads = 256;
-constexpr int kCAhead = 4;     // 16-byte loads of the history that a thread has on their way
+constexpr int kCAhead = 2;     // 16-byte loads of the history that a thread has on their way
 constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
 constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
 // A token's word: in the prompt, among the drafts, biased, and how often in the output.
@@ -110,65 +110,79 @@ struct Request {
 };
 static_assert(ASYMSPEC_CONSTRAIN_MAX_P - 1 <= kCThreads, "a thread per draft");
 
+// A thread's first tokens of the history (four a load from the first 16-byte boundary on, one
+// before and one after them) and its first bias, on their way before that barrier too.
+struct Tokens {
+  const int4* fours;
+  int len, prompt, head, count, end, before, after, bias_first, bias_end, bias;
+  int4 v[kCAhead];
+  __device__ __forceinline__ void load(int4 (&to)[kCAhead], int i0) const {
+#pragma unroll
+    for (int e = 0; e < kCAhead; ++e)
+      if (i0 + e * kCThreads < count) to[e] = fours[i0 + e * kCThreads];
+  }
+  __device__ __forceinline__ Tokens(const CParams& p, const Request& r, int b, unsigned& err) {
+    const asymspec_constraints& c = p.c;
+    const int tid = threadIdx.x;
+    len = min(max(r.len0, 0), c.history_width);
+    prompt = min(max(r.prompt0, 0), len);
+    if (len != r.len0 || prompt != r.prompt0) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    const int32_t* h = c.history + b * c.history_ld;
+    head = min(entries_before(h), len);
+    count = (len - head) / 4;
+    end = head + count * 4;
+    fours = reinterpret_cast<const int4*>(h + head);
+    before = tid < head ? h[tid] : 0;
+    after = tid < len - end ? h[end + tid] : 0;
+    load(v, tid);
+    bias_first = min(max(r.bias0, 0), c.bias_count);
+    bias_end = min(max(r.bias1, bias_first), c.bias_count);
+    if (bias_first != r.bias0 || bias_end != r.bias1) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    bias = bias_first + tid < bias_end ? c.bias_tokens[bias_first + tid] : 0;
+  }
+};
+
 // The tokens of the history are counted in shared memory: each CTA reads all of it (from
 // the L2) and counts its slice's.  Ends at a barrier; the words are zero at the start,
 // which a barrier before says.  (Clusters whose CTAs read a share each and count a token
 // where its slice is, by remote atomics: 92 us for 32 requests of 65,536 tokens each against
 // 117, but 61 against 47 at 8,000 and 66 against 60 at 20,000.)
-__device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s, const Request& r) {
-  const asymspec_constraints& c = p.c;
-  const int b = s.b, v0 = s.v0, n = s.n, tid = threadIdx.x;
+__device__ __forceinline__ unsigned count_slice(const CParams& p, const Slice& s, const Request& r, Tokens& t) {
+  const int v0 = s.v0, n = s.n, tid = threadIdx.x;
   unsigned err = 0;
-  if (c.history) {
-    const int len = min(max(r.len0, 0), c.history_width), pl = min(max(r.prompt0, 0), len);
-    if (len != r.len0 || pl != r.prompt0) err |= ASYMSPEC_DATA_BAD_LENGTH;
-    const int32_t* h = c.history + b * c.history_ld;
-    auto count = [&](int v, int i) {
-      if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (static_cast<unsigned>(v - v0) < static_cast<unsigned>(n)) {
-        if (i < pl) atomicOr(&s.words[v - v0], kCPrompt);
-        else atomicAdd(&s.words[v - v0], 1u);
-      }
-    };
-    // four tokens a load from the first 16-byte boundary on
-    const int head = min(entries_before(h), len), fours = (len - head) / 4;
-    const int end = head + fours * 4;
-    if (tid < head) count(h[tid], tid);
-    if (tid < len - end) count(h[end + tid], end + tid);
-    const int4* h4 = reinterpret_cast<const int4*>(h + head);
-    for (int i0 = tid; i0 < fours; i0 += kCThreads * kCAhead) {
-      int4 v[kCAhead];
-#pragma unroll
-      for (int e = 0; e < kCAhead; ++e)
-        if (i0 + e * kCThreads < fours) v[e] = h4[i0 + e * kCThreads];
-#pragma unroll
-      for (int e = 0; e < kCAhead; ++e) {
-        if (i0 + e * kCThreads >= fours) break;
-        const int i = head + (i0 + e * kCThreads) * 4;
-        count(v[e].x, i);
-        count(v[e].y, i + 1);
-        count(v[e].z, i + 2);
-        count(v[e].w, i + 3);
-      }
-    }
-  }
-  if (c.drafts && tid < p.P - 1) {
-    const int v = r.draft;
+  auto here = [&](int v) {
     if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-    else if (v >= v0 && v < v0 + n) atomicOr(&s.words[v - v0], kCDraft);
-  }
-  if (c.bias_offsets) {
-    const int a = min(max(r.bias0, 0), c.bias_count), e = min(max(r.bias1, a), c.bias_count);
-    if (a != r.bias0 || e != r.bias1) err |= ASYMSPEC_DATA_BAD_LENGTH;
-    for (int i = a + tid; i < e; i += kCThreads) {
-      const int v = c.bias_tokens[i];
-      if (static_cast<unsigned>(v) >= static_cast<unsigned>(p.V)) err |= ASYMSPEC_DATA_BAD_TOKEN;
-      else if (v >= v0 && v < v0 + n) {
-        atomicOr(&s.words[v - v0], kCBias);
-        const int at = atomicAdd(s.biases, 1);
-        if (at < kCBiases) s.bias[at] = make_int2(v - v0, i);
-      }
+    return static_cast<unsigned>(v - v0) < static_cast<unsigned>(n);
+  };
+  auto count = [&](int v, int i) {
+    if (!here(v)) return;
+    if (i < t.prompt) atomicOr(&s.words[v - v0], kCPrompt);
+    else atomicAdd(&s.words[v - v0], 1u);
+  };
+  if (tid < t.head) count(t.before, tid);
+  if (tid < t.len - t.end) count(t.after, t.end + tid);
+  for (int i0 = tid; i0 < t.count; i0 += kCThreads * kCAhead) {
+    int4 next[kCAhead];
+    t.load(next, i0 + kCThreads * kCAhead);
+#pragma unroll
+    for (int e = 0; e < kCAhead; ++e) {
+      if (i0 + e * kCThreads >= t.count) break;
+      const int i = t.head + (i0 + e * kCThreads) * 4;
+      count(t.v[e].x, i);
+      count(t.v[e].y, i + 1);
+      count(t.v[e].z, i + 2);
+      count(t.v[e].w, i + 3);
     }
+#pragma unroll
+    for (int e = 0; e < kCAhead; ++e) t.v[e] = next[e];
+  }
+  if (p.c.drafts && tid < p.P - 1 && here(r.draft)) atomicOr(&s.words[r.draft - v0], kCDraft);
+  for (int i = t.bias_first + tid; i < t.bias_end; i += kCThreads) {
+    const int v = i == t.bias_first + tid ? t.bias : p.c.bias_tokens[i];
+    if (!here(v)) continue;
+    atomicOr(&s.words[v - v0], kCBias);
+    const int at = atomicAdd(s.biases, 1);
+    if (at < kCBiases) s.bias[at] = make_int2(v - v0, i);
   }
   __syncthreads();
   return err;
@@ -333,8 +347,9 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
   if (tid == 0) s_listed = s_biases = 0;
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
   load_masks(0, min(batch, k_end - k0));
+  Tokens tokens(p, request, b, err);
   __syncthreads();
-  err |= count_slice(p, slice, request);
+  err |= count_slice(p, slice, request, tokens);
   list_slice(slice);
   const float top = type_max(T());
   const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());
@@ -349,11 +364,13 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
     const int listed = s_listed;
-    for (int q = tid; q < listed; q += kCThreads) {
-      const int i = slice.list[q];
-      Touched u(p, slice, i, k0 + first_row);
+    // an entry's rows by one thread, or, where entries are fewer than threads, by one each
+    const int each = listed * rows <= 2 * kCThreads ? 1 : rows;
+    for (int q = tid; q < listed * (rows / each); q += kCThreads) {
+      const int i = slice.list[q % listed], first = q / listed;
+      Touched u(p, slice, i, k0 + first_row + first);
 #pragma unroll 4
-      for (int k = 0; k < rows; ++k) {
+      for (int k = first; k < first + each; ++k) {
         T* cell = reinterpret_cast<T*>(tile + k * pitch + misplaced(xt + k * p.ld)) + i;
         *cell = from_f32(u.value(penalties, to_f32(*cell)), T());
         u.past(p, slice, k0 + first_row + k);
@@ -428,8 +445,9 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   for (int i = tid; i < W / 4; i += kCThreads) reinterpret_cast<uint4*>(c_smem)[i] = make_uint4(0, 0, 0, 0);
   for (int k = tid; k < rows; k += kCThreads)
     s_mask[k] = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + k, err);
+  Tokens tokens(p, request, b, err);
   __syncthreads();
-  err |= count_slice(p, slice, request);
+  err |= count_slice(p, slice, request, tokens);
   list_slice(slice);
   const float top = type_max(T());
   const T low = from_f32(fminf(fmaxf(c.mask_value, -top), top), T());
