@@ -237,30 +237,56 @@ struct WriteParams {
   int64_t ks[2], vs[2], cks[3], cvs[3];
   const int64_t* slots;
   int T, num_blocks, block_size, kv_heads, head_dim;
+  int log_lanes;  // 2^log_lanes lanes for a token
   uint32_t* err;
 };
 
+constexpr int kWThreads = 256;
+
 // U: what is moved at once (16 bytes, or one element where something is not on the
-// 16-byte boundaries); strides and head_dim in elements of U.
+// 16-byte boundaries); strides and head_dim in elements of U.  A copy, bound by its bytes: a
+// warp, or part of one where a token has fewer vectors, takes a token, four of its
+// vectors a lane on their way together, so that a slot is looked up and divided once.
 template <typename U>
-__global__ void __launch_bounds__(256) cache_write_kernel(const WriteParams p) {
+__global__ void __launch_bounds__(kWThreads) cache_write_kernel(const WriteParams p) {
+  const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);
   const int per = p.kv_heads * p.head_dim;
-  const int64_t n = static_cast<int64_t>(p.T) * per;
-  for (int64_t i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
-    const int t = static_cast<int>(i / per), e = static_cast<int>(i % per);
-    const int h = e / p.head_dim, d = e % p.head_dim;
+  const unsigned slots = static_cast<unsigned>(p.num_blocks) * static_cast<unsigned>(p.block_size);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * (kWThreads >> p.log_lanes);
+  for (int64_t t = (static_cast<int64_t>(blockIdx.x) * kWThreads + threadIdx.x) >> p.log_lanes; t < p.T; t += stride) {
     const int64_t slot = p.slots[t];
     if (slot < 0) continue;
-    const int64_t block = slot / p.block_size;
-    const int at = static_cast<int>(slot % p.block_size);
-    if (block >= p.num_blocks) {
-      if (p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
+    if (slot >= slots) {
+      if (lane == 0 && p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
       continue;
     }
-    static_cast<U*>(p.keys)[block * p.cks[0] + at * p.cks[1] + h * p.cks[2] + d] =
-        static_cast<const U*>(p.k)[t * p.ks[0] + h * p.ks[1] + d];
-    static_cast<U*>(p.values)[block * p.cvs[0] + at * p.cvs[1] + h * p.cvs[2] + d] =
-        static_cast<const U*>(p.v)[t * p.vs[0] + h * p.vs[1] + d];
+    const unsigned block = static_cast<unsigned>(slot) / static_cast<unsigned>(p.block_size);
+    const unsigned at = static_cast<unsigned>(slot) - block * static_cast<unsigned>(p.block_size);
+    const U* k = static_cast<const U*>(p.k) + t * p.ks[0];
+    const U* v = static_cast<const U*>(p.v) + t * p.vs[0];
+    U* keys = static_cast<U*>(p.keys) + block * p.cks[0] + at * p.cks[1];
+    U* values = static_cast<U*>(p.values) + block * p.cvs[0] + at * p.cvs[1];
+    for (int e0 = lane; e0 < per; e0 += lanes * 4) {
+      U x[4], y[4];
+      int h[4], d[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = e0 + i * lanes;
+        h[i] = e / p.head_dim;
+        d[i] = e - h[i] * p.head_dim;
+        if (e < per) {
+          x[i] = k[h[i] * p.ks[1] + d[i]];
+          y[i] = v[h[i] * p.vs[1] + d[i]];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (e0 + i * lanes < per) {
+          keys[h[i] * p.cks[2] + d[i]] = x[i];
+          values[h[i] * p.cvs[2] + d[i]] = y[i];
+        }
+      }
+    }
   }
 }
 

@@ -55,6 +55,8 @@ cudaError_t device_sms(int* device, int* sms) {
   return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device) : e;
 }
 
+constexpr int kWriteCtas = 1216;  // CTAs of the write at most
+
 // Slots above which the plan takes a cluster.
 constexpr int kPlanTokens = 2048;
 
@@ -266,12 +268,14 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
   p.kv_heads = cache->kv_heads;
   p.head_dim = cache->head_dim / u;
   p.err = out_error_word;
-  const int64_t n = static_cast<int64_t>(T) * p.kv_heads * p.head_dim;
+  const int per_token = p.kv_heads * p.head_dim;
+  while (p.log_lanes < 5 && (1 << p.log_lanes) < per_token) ++p.log_lanes;
+  const int64_t ctas = (static_cast<int64_t>(T) + (kWThreads >> p.log_lanes) - 1) / (kWThreads >> p.log_lanes);
   const void* fn = wide ? reinterpret_cast<const void*>(&cache_write_kernel<uint4>)
                    : elt == 4 ? reinterpret_cast<const void*>(&cache_write_kernel<uint32_t>)
                               : reinterpret_cast<const void*>(&cache_write_kernel<uint16_t>);
-  return launch(fn, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 8 * 152))), dim3(256),
-                0, &p, stream);
+  return launch(fn, dim3(static_cast<unsigned>(std::min<int64_t>(ctas, kWriteCtas))), dim3(kWThreads), 0, &p,
+                stream);
 }
 
 size_t asymspec_cache_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim) {
