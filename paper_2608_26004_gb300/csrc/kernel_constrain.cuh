@@ -329,12 +329,14 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
     }
   };
   auto load_masks = [&](int first_row, int rows) {
-    if (c.mask) {
-      for (int q = tid; q < rows * row_words; q += kCThreads) {
-        const int k = q / row_words, w = q - k * row_words;
+    if (c.mask) {  // a warp a row
+      const int words = min(row_words, (n + 31) / 32);
+      for (int k = tid / 32; k < rows; k += kCThreads / 32) {
         const int at = mask_of(p, static_cast<int64_t>(b) * p.P + k0 + first_row + k, err);
-        if (w == 0) s_at[k] = at;
-        if (at >= 0 && w * 32 < n) cp_async_at<4>(smem_u32(s_mask + q), c.mask + at * c.mask_ld + (v0 >> 5) + w);
+        if (tid % 32 == 0) s_at[k] = at;
+        if (at < 0) continue;
+        const uint32_t* src = c.mask + at * c.mask_ld + (v0 >> 5);
+        for (int w = tid % 32; w < words; w += 32) cp_async_at<4>(smem_u32(s_mask + k * row_words + w), src + w);
       }
     } else if (tid < rows) {
       s_at[tid] = -1;
