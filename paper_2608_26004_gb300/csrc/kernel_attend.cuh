@@ -728,7 +728,7 @@ template <typename T, int DP, int kRows>
 __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams p, int ctas) {
   constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  __shared__ float s_w[kAMaxCtas], s_x[kAJoinThreads * 4], s_red[kAWarps];
+  __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_x[kAJoinThreads * 4], s_red[kAWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x + 1, r = blockIdx.y, tid = threadIdx.x;
   const AttendInfo in = reinterpret_cast<const AttendInfo*>(p.ws)[c];
@@ -744,9 +744,10 @@ __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams 
   auto part_of = [&](int k) { return k == 0 ? 2 * c0 + 1 : 2 * (c0 + k); };
   float M = -INFINITY;
   for (int k = tid; k < parts; k += kAJoinThreads) {
-    const float mk = ml[(static_cast<size_t>(part_of(k)) * kRows + r) * 2];
-    s_w[k] = mk;
-    M = fmaxf(M, mk);
+    const float2 x = *reinterpret_cast<const float2*>(ml + (static_cast<size_t>(part_of(k)) * kRows + r) * 2);
+    s_w[k] = x.x;
+    s_l[k] = x.y;
+    M = fmaxf(M, x.x);
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
@@ -757,11 +758,11 @@ __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams 
   for (int w = 1; w < kAWarps; ++w) M = fmaxf(M, s_red[w]);
   const int col = tid % kCols, way = tid / kCols;
   float x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+#pragma unroll 8
   for (int k = way; k < parts; k += kWays) {
     const float f = s_w[k] == M ? 1.f : ex2(s_w[k] - M);
-    const size_t at = static_cast<size_t>(part_of(k)) * kRows + r;
-    const float4 o = *reinterpret_cast<const float4*>(os + at * DP + col * 4);
-    L = fmaf(f, ml[at * 2 + 1], L);
+    const float4 o = *reinterpret_cast<const float4*>(os + (static_cast<size_t>(part_of(k)) * kRows + r) * DP + col * 4);
+    L = fmaf(f, s_l[k], L);
     x[0] = fmaf(f, o.x, x[0]);
     x[1] = fmaf(f, o.y, x[1]);
     x[2] = fmaf(f, o.z, x[2]);

@@ -2,7 +2,7 @@
 // launches of the operators around the verification step.
 //
 //   constrain_rows      (kernel_constrain.cuh) penalties, biases and masks on logits;
-//                       constrain_in_place where they are
+//                       constrain_in_place where they are (no masks)
 //   cache_plan_kernel   (kernel_cache.cuh) block tables and slot maps
 //   cache_write_kernel  (kernel_cache.cuh) new keys and values into the cache
 //   attend_split        (kernel_attend.cuh) attention over the cache, the keys split evenly
@@ -163,7 +163,7 @@ int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits,
   // batches of one size, kCSlots vectors of a thread at most
   const int most = kCSlots * kCThreads / vectors, batches = (p.group_rows + most - 1) / most;
   p.batch_rows = (p.group_rows + batches - 1) / batches;
-  const bool in_place = logits == out;
+  const bool in_place = logits == out && !c->mask;
   const size_t smem = constrain_list_bytes(p.W) +
                       (in_place ? 0 : static_cast<size_t>(p.batch_rows) * constrain_pitch(p.W, elt));
   const void* fn = dtype == ASYMSPEC_FP32 ? constrain_pick<float>(in_place, edges)
