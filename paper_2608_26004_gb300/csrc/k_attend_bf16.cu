@@ -13,6 +13,10 @@ AttendKernels attend_pick() {
           reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM};
 }
 
+// One, two or four warps for the rows of a group: as many as the rows fill.  us, 8 requests of
+// 4096 to 32768 tokens, 8 kv heads of 128 elements, with row tiles of 16 / 32 / 64:
+//   32 rows 127 / 102 / 164     64 rows 206 / 185 / 179     24 rows 125 / 100 / 163
+// Rings as deep as shared memory allows at two CTAs an SM (one for 64 rows: the registers).
 AttendKernels attend_kernels_bf16(int D, int rows) {
   if (D <= 64)
     return rows <= 16 ? attend_pick<64, 1, 5, 2>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();

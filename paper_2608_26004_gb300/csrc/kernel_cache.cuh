@@ -57,7 +57,8 @@ __device__ __forceinline__ void scan3(int64_t& a, int& b, int& c, int64_t* wa, i
 // One CTA, or (CLUSTER) a cluster of them.  Every CTA goes over all requests by itself (a few
 // numbers each: cheaper than an exchange), then they share the blocks given back, the
 // blocks taken and the slots, each found by a search in the prefix sums, with a barrier
-// between what one part writes and the next reads.
+// between what one part writes and the next reads.  Bound by latency: 64 requests of 8 slots
+// 4.9 us, 256 requests of 115,000 slots in all 17.3 us (8 CTAs; 120 with one).
 template <bool CLUSTER>
 __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams p) {
   extern __shared__ int64_t p_smem[];
@@ -247,6 +248,7 @@ constexpr int kWThreads = 256;
 // 16-byte boundaries); strides and head_dim in elements of U.  A copy, bound by its bytes: a
 // warp, or part of one where a token has fewer vectors, takes a token, four of its
 // vectors a lane on their way together, so that a slot is looked up and divided once.
+// 16384 tokens of 8 heads of 128 bf16: 21.1 us = 6.4 TB/s (a thread per vector: 23.3).
 template <typename U>
 __global__ void __launch_bounds__(kWThreads) cache_write_kernel(const WriteParams p) {
   const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);

@@ -263,13 +263,17 @@ __device__ __forceinline__ int mask_of(const CParams& p, int64_t r, unsigned& er
   return -2;
 }
 
-// The constrained rows, in another place than the logits or (masks) in theirs: one CTA per slice of the
-// vocabulary, request and group of rows.  The rows' slices come into shared memory by
-// cp.async while the history is counted; the entries that a penalty or a bias touches,
-// gathered in a list so that no lane is idle, are computed there (scattered over the
-// rows in global memory they took longer than the rows); then the rows leave under
-// their masks.  The slices of the lowest token ids, which a vocabulary gives to the most frequent tokens,
-// come first in the grid: theirs are the most entries to compute.
+// The constrained rows, in another place than the logits or (masks) in theirs: one CTA per
+// slice of the vocabulary, request and group of rows.  The rows' slices and their masks' words
+// come into shared memory by cp.async while the history is counted; the entries that a penalty
+// or a bias touches, gathered in a list so that no lane is idle, are computed there (in
+// registers on the way of a copy each held up the 255 others of its warp, scattered over the
+// rows in global memory they took longer than the rows); then the rows leave under their
+// masks.  The slices of the lowest token ids, which a vocabulary gives to the most frequent
+// tokens, come first in the grid: theirs are the most entries to compute.
+// Bound by HBM, a row in and out; 64x8 rows of V=128256 bf16, half of them masked, histories to
+// 8192: 47 us = 5.6 TB/s (43 with nothing to do but copy); 32x9 rows of V=151936, histories to
+// 65536: 48 us, issuing instructions for the histories (34 without).
 template <typename T, bool EDGES>
 __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) {
   extern __shared__ __align__(16) unsigned c_smem[];
