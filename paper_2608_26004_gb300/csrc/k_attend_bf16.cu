@@ -19,9 +19,9 @@ AttendKernels attend_pick() {
 // Rings as deep as shared memory allows at two CTAs an SM (one for 64 rows: the registers).
 AttendKernels attend_kernels_bf16(int D, int rows) {
   if (D <= 64)
-    return rows <= 16 ? attend_pick<64, 1, 5, 2>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();
+    return rows <= 16 ? attend_pick<64, 1, 3, 3>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();
   if (D <= 128)
-    return rows <= 16 ? attend_pick<128, 1, 3, 2>() : rows <= 32 ? attend_pick<128, 2, 3, 2>() : attend_pick<128, 4, 6, 1>();
+    return rows <= 16 ? attend_pick<128, 1, 2, 3>() : rows <= 32 ? attend_pick<128, 2, 3, 2>() : attend_pick<128, 4, 6, 1>();
   return rows <= 16 ? attend_pick<256, 1, 3, 1>() : attend_pick<256, 2, 3, 1>();
 }
 

@@ -16,7 +16,7 @@ AttendKernels attend_pick() {
 // As for bf16, with two warps for a group's rows at most (the operands' pieces leave no
 // registers for more); a key of 256 elements leaves room for one step a ring.
 AttendKernels attend_kernels_f32(int D, int rows) {
-  if (D <= 64) return rows <= 16 ? attend_pick<64, 1, 3, 2>() : attend_pick<64, 2, 2, 2>();
+  if (D <= 64) return rows <= 16 ? attend_pick<64, 1, 2, 3>() : attend_pick<64, 2, 2, 2>();
   if (D <= 128) return rows <= 16 ? attend_pick<128, 1, 3, 1>() : attend_pick<128, 2, 2, 1>();
   return attend_pick<256, 1, 1, 1>();
 }

@@ -38,7 +38,7 @@ constexpr int kAJoinThreads = 128;
 // The work is split by units: an item (a request, kv head and row tile) has one for each
 // of its tiles, after kAItem for what it costs to begin and end one (64 requests of 64 to 8192
 // tokens, kAItem = 0, 1, 2, 3, 4: 105, 88, 76, 74, 76 us).
-constexpr int kAItem = 3;
+constexpr int kAItem = 2;
 
 // A CTA whose share begins after the first tile of an item says which.
 struct AttendInfo {
