@@ -15,13 +15,15 @@ AttendKernels attend_pick() {
 
 // One, two or four warps for the rows of a group: as many as the rows fill.  us, 8 requests of
 // 4096 to 32768 tokens, 8 kv heads of 128 elements, with row tiles of 16 / 32 / 64:
-//   32 rows 127 / 102 / 164     64 rows 206 / 185 / 179     24 rows 125 / 100 / 163
-// Rings as deep as shared memory allows at two CTAs an SM (one for 64 rows: the registers).
+//   24 rows 117 / 97 / 151     32 rows 119 / 99 / 152     48 rows 173 / 169 / 160     64 rows 181 / 174 / 167
+// CTAs an SM: as many as the registers allow, with rings as deep as shared memory then does.  Three
+// at 16 rows, where two with deeper rings are as fast for long contexts (64 requests of 64 to 8192
+// tokens 74 both) and slower for short ones (256 of 16 to 300 tokens 39 to 34).
 AttendKernels attend_kernels_bf16(int D, int rows) {
   if (D <= 64)
     return rows <= 16 ? attend_pick<64, 1, 3, 3>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();
   if (D <= 128)
-    return rows <= 16 ? attend_pick<128, 1, 2, 3>() : rows <= 32 ? attend_pick<128, 2, 3, 2>() : attend_pick<128, 4, 6, 1>();
+    return rows <= 16 ? attend_pick<128, 1, 2, 3>() : rows <= 32 ? attend_pick<128, 2, 3, 2>() : attend_pick<128, 4, 5, 1>();
   return rows <= 16 ? attend_pick<256, 1, 3, 1>() : attend_pick<256, 2, 3, 1>();
 }
 

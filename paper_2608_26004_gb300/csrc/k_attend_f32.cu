@@ -13,8 +13,9 @@ AttendKernels attend_pick() {
           reinterpret_cast<const void*>(&attend_join<float, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM};
 }
 
-// As for bf16, with two warps for a group's rows at most (the operands' pieces leave no
-// registers for more); a key of 256 elements leaves room for one step a ring.
+// As for bf16 (three CTAs an SM instead of two at 16 rows of 64: a window of 2000, 32 requests
+// of 5 queries, 49 to 45 us), with two warps for a group's rows at most (the operands' pieces
+// leave no registers for more); a key of 256 elements leaves room for one step a ring.
 AttendKernels attend_kernels_f32(int D, int rows) {
   if (D <= 64) return rows <= 16 ? attend_pick<64, 1, 2, 3>() : attend_pick<64, 2, 2, 2>();
   if (D <= 128) return rows <= 16 ? attend_pick<128, 1, 3, 1>() : attend_pick<128, 2, 2, 1>();

@@ -37,7 +37,7 @@ constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each
 // of its tiles, after kAItem for what it costs to begin and end one (64 requests of 64 to 8192
-// tokens, kAItem = 0, 1, 2, 3, 4: 105, 88, 76, 74, 76 us).
+// tokens, kAItem = 1, 2, 3: 80, 75, 76 us; a window of 2000, fp32: 44, 45, 46.5).
 constexpr int kAItem = 2;
 
 // A CTA whose share begins after the first tile of an item says which.
@@ -58,13 +58,27 @@ constexpr size_t attend_ws_bytes(int rows, int DP) {
   return kAInfoBytes + attend_ml_bytes(rows) + static_cast<size_t>(2 * kAMaxCtas) * rows * DP * sizeof(float);
 }
 
-// Dynamic shared memory, from a 1024-byte boundary on: the groups' rings, the queries (fp32:
-// in two pieces), each warp's masks of keys that exist and its maxima and sums, and the
-// numbers that find a CTA's share.
+// Whether rows of keys, values and queries lie in shared memory 16 bytes further apart than they
+// are long, so that the eight rows that ldmatrix reads meet no bank twice and all addresses are
+// one and an immediate; else their 16-byte chunks are swizzled.  us, swizzled / with such rows:
+// two warps a group (8 requests of 4096 to 32768 tokens, 32 rows a kv head of 128) 102.7 / 99.1,
+// four (64 rows) 179 / 167; one (64 requests of one query) 74.7 / 79.3; heads of 256 167 / 183.
+// fp32 has no room for longer rows.
+template <typename T>
+__host__ __device__ constexpr bool attend_long_rows(int DP, int WR) {
+  return sizeof(T) == 2 && DP <= 128 && WR > 1;
+}
+template <typename T>
+__host__ __device__ constexpr int attend_pitch(int DP, int WR) {
+  return DP * static_cast<int>(sizeof(T)) + (attend_long_rows<T>(DP, WR) ? 16 : 0);
+}
+
+// Dynamic shared memory: the groups' rings, the queries (fp32: in two pieces), each warp's masks
+// of keys that exist and its references and sums, and the numbers that find a CTA's share.
 template <typename T>
 constexpr size_t attend_smem_bytes(int DP, int WR, int ST) {
-  return 1024 + static_cast<size_t>(kAGroups) * ST * 2 * kAKeys * DP * sizeof(T) +
-         static_cast<size_t>(16) * WR * DP * (sizeof(T) == 4 ? 8 : 2) + kAGroups * WR * ST * 4 +
+  return static_cast<size_t>(kAGroups) * ST * 2 * kAKeys * attend_pitch<T>(DP, WR) +
+         static_cast<size_t>(16) * WR * attend_pitch<T>(DP, WR) * (sizeof(T) == 4 ? 2 : 1) + kAGroups * WR * ST * 4 +
          static_cast<size_t>(kAGroups) * 16 * WR * 8 + kAGroups * WR * 8 + 16;
 }
 
@@ -140,12 +154,19 @@ __device__ __forceinline__ void split_bf16(float x, float y, unsigned& hi, unsig
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(ry), "f"(rx));
 }
 
-// Where 16-byte chunk `c` of row `r` of a tile lies.  bf16: ldmatrix reads eight rows of
-// one chunk.  fp32 keys: eight lanes read four chunks of two neighbouring rows; values:
-// two chunks of four rows of one parity.
-template <typename T, bool VALUES>
+// Where 16-byte chunk `c` of row `r` lies in the row, if rows are not longer.  bf16: ldmatrix
+// reads one chunk of eight rows.  fp32 keys: eight lanes read four chunks of two neighbouring
+// rows; values: two chunks of four rows of one parity.
+template <typename T, bool VALUES, bool LONG_ROWS>
 __device__ __forceinline__ int swizzled(int r, int c) {
+  if constexpr (LONG_ROWS) return c;
   return sizeof(T) == 2 || VALUES ? c ^ (r & 7) : c ^ (((r & 1) << 2) | ((r >> 1) & 3));
+}
+
+// Chunks 2 k and 2 k + 1 of a row from the address of its chunks 0 and 1.
+template <bool LONG_ROWS>
+__device__ __forceinline__ unsigned chunk_pair(unsigned at, int k) {
+  return LONG_ROWS ? at + k * 32 : at ^ (k * 32);
 }
 
 __device__ __forceinline__ void group_barrier(int id, int threads) {
@@ -158,16 +179,18 @@ __device__ __forceinline__ void group_barrier(int id, int threads) {
 // rows, with running references, sums and weighted values in registers.  When the CTA's share of
 // an item ends, the groups' parts are joined in shared memory.
 // Bound by the bytes of keys and values at 16 rows: bf16, 64 requests of 64 to 8192 tokens, 32
-// heads on 8 of 128: 73 us = 6.0 TB/s; by issue and latency at 32 (16 requests of 4096 to
-// 131072 tokens, 8 queries each: 452 us = 5.6 TB/s) and by the matrix instructions at 64 (8
-// requests to 32768: 179 us, 103 at 32 rows).  fp32, 32 requests, 5 queries, a window of 2000, 8
-// heads of 64: 49 us = 3.2 TB/s, splitting operands.
+// heads on 8 of 128: 74 us = 5.9 TB/s; by issue and latency at 32 (16 requests of 4096 to
+// 131072 tokens, 8 queries each: 425 us = 6.0 TB/s) and by the matrix instructions at 64 (8
+// requests to 32768: 167 us, 99 at 32 rows).  fp32, 32 requests, 5 queries, a window of 2000, 8
+// heads of 64: 44 us = 3.6 TB/s, splitting operands.
 template <typename T, int DP, int WR, int ST, int PER_SM>
 __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const AttendParams p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int kThreadsN = kAGroups * WR * 32, kWarpsN = kAGroups * WR;
   constexpr int kRowBytes = DP * sizeof(T), kChunks = kRowBytes / 16, PE = 16 / sizeof(T);
-  constexpr int kHalf = kAKeys * kRowBytes;  // bytes of a step's keys (and of its values)
+  constexpr bool kLong = attend_long_rows<T>(DP, WR);
+  constexpr int kPitch = attend_pitch<T>(DP, WR);
+  constexpr int kHalf = kAKeys * kPitch;  // bytes of a step's keys (and of its values)
   constexpr int kRows = 16 * WR;
   constexpr int NT = DP / 8;
   constexpr int kLoads = kChunks / 2 / WR;   // vectors that a lane loads of a step's keys
@@ -175,11 +198,10 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
   constexpr float kSlack = 8.f;
   constexpr bool kQRegs = BF && DP <= 128 && WR == 1;
   static_assert(kLoads >= 1 && (BF ? 1 : 2) * ST >= WR, "a warp loads, and the parts fit in the rings");
-  extern __shared__ unsigned char a_smem_raw[];
-  unsigned char* a_smem = a_smem_raw + ((1024u - (smem_u32(a_smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) unsigned char a_smem[];
   unsigned char* at_q = a_smem + static_cast<size_t>(kAGroups) * ST * 2 * kHalf;
   T* qs = reinterpret_cast<T*>(at_q);  // fp32: the high pieces, then the low ones
-  unsigned* masks0 = reinterpret_cast<unsigned*>(at_q + static_cast<size_t>(kRows) * DP * (BF ? 2 : 8));
+  unsigned* masks0 = reinterpret_cast<unsigned*>(at_q + static_cast<size_t>(kRows) * kPitch * (BF ? 1 : 2));
   float* s_ml = reinterpret_cast<float*>(masks0 + kWarpsN * ST);
   int64_t* s_scan = reinterpret_cast<int64_t*>(s_ml + kWarpsN * 16 * 2);
   int64_t* s_find = s_scan + kWarpsN;
@@ -187,7 +209,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
   const int group = warp / WR, wr = warp % WR;  // whose keys; which rows
   unsigned* masks = masks0 + warp * ST;
   unsigned char* ring = a_smem + group * ST * 2 * kHalf;
-  const unsigned ring_at = smem_u32(ring), q_at = smem_u32(qs) + wr * 16 * kRowBytes;
+  const unsigned ring_at = smem_u32(ring), q_at = smem_u32(qs) + wr * 16 * kPitch;
   const int c = blockIdx.x, ctas = gridDim.x;
   const int HR = p.kv_heads * p.row_tiles;
   unsigned err = 0;
@@ -256,8 +278,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
   constexpr bool kSameChunk = kChunks <= 32 * WR;
   constexpr int kLaneRows = kSameChunk ? 32 * WR / kChunks : 1;
   const int row0 = row_of(0), chunk0 = chunk_of(0);
-  const unsigned to_k = row0 * kRowBytes + swizzled<T, false>(row0, chunk0) * 16;
-  const unsigned to_v = kHalf + row0 * kRowBytes + swizzled<T, true>(row0, chunk0) * 16;
+  const unsigned to_k = row0 * kPitch + swizzled<T, false, kLong>(row0, chunk0) * 16;
+  const unsigned to_v = kHalf + row0 * kPitch + swizzled<T, true, kLong>(row0, chunk0) * 16;
   const int from_k = row0 * p.token_bytes[0] + chunk0 * 16, from_v = row0 * p.token_bytes[1] + chunk0 * 16;
   const int chunk_bytes = chunk0 * PE < p.D ? 16 : 0;
   const int step_blocks = kATile / p.block_size, step_rest = kATile % p.block_size;
@@ -308,9 +330,9 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
         const unsigned dk = sk + to_k, dv = sk + to_v;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          constexpr int kStep = kLaneRows * kRowBytes;
-          cp_async16_or_zero((dk ^ (swizzled<T, false>(i * kLaneRows, 0) * 16)) + i * kStep, fk, chunk_bytes);
-          cp_async16_or_zero((dv ^ (swizzled<T, true>(i * kLaneRows, 0) * 16)) + i * kStep, fv, chunk_bytes);
+          constexpr int kStep = kLaneRows * kPitch;
+          cp_async16_or_zero((dk ^ (swizzled<T, false, kLong>(i * kLaneRows, 0) * 16)) + i * kStep, fk, chunk_bytes);
+          cp_async16_or_zero((dv ^ (swizzled<T, true, kLong>(i * kLaneRows, 0) * 16)) + i * kStep, fv, chunk_bytes);
           fk += kLaneRows * p.token_bytes[0];
           fv += kLaneRows * p.token_bytes[1];
         }
@@ -324,8 +346,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           const int64_t rk = __shfl_sync(~0u, ok, r), rv = __shfl_sync(~0u, ov, r);
           const bool on = ((live >> r) & 1u) && ch * PE < p.D;
           const int el = on ? ch * PE : 0;
-          cp_async16_or_zero(sk + r * kRowBytes + swizzled<T, false>(r, ch) * 16, keys + rk + el, on ? 16 : 0);
-          cp_async16_or_zero(sv + r * kRowBytes + swizzled<T, true>(r, ch) * 16, values + rv + el, on ? 16 : 0);
+          cp_async16_or_zero(sk + r * kPitch + swizzled<T, false, kLong>(r, ch) * 16, keys + rk + el, on ? 16 : 0);
+          cp_async16_or_zero(sv + r * kPitch + swizzled<T, true, kLong>(r, ch) * 16, values + rv + el, on ? 16 : 0);
         }
       }
       cp_async_commit();
@@ -359,7 +381,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           v = *reinterpret_cast<const uint4*>(x);
         }
       }
-      const int at = r * DP + swizzled<T, false>(r, ch) * PE;
+      const int at = r * (kPitch / static_cast<int>(sizeof(T))) + swizzled<T, false, kLong>(r, ch) * PE;
       if constexpr (BF) {
         *reinterpret_cast<uint4*>(qs + at) = v;
       } else {
@@ -390,9 +412,9 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
       for (int e = 0; e < 4; ++e) O[n][e] = 0.f;
     __syncthreads();
     if constexpr (kQRegs) {
-      const unsigned at = q_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
+      const unsigned at = q_at + (lane & 15) * kPitch + swizzled<T, false, kLong>(lane, lane >> 4) * 16;
 #pragma unroll
-      for (int k = 0; k < DP / 16; ++k) ldmatrix4(qf[k], at ^ (k * 32));
+      for (int k = 0; k < DP / 16; ++k) ldmatrix4(qf[k], chunk_pair<kLong>(at, k));
     }
 
     int stage = 0;
@@ -426,20 +448,19 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
 #pragma unroll
           for (int e = 0; e < 4; ++e) S[n][e] = 0.f;
         if constexpr (BF) {
-          // chunk 2k + j of row r lies at (2k + j) ^ (r & 7): the 2k is an exclusive or of its own
-          const unsigned at = ks_at + (((lane >> 4) << 3) + (lane & 7)) * kRowBytes +
-                              ((((lane >> 3) & 1) ^ (lane & 7)) * 16);
-          const unsigned q_lane = q_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
+          const unsigned at = ks_at + (((lane >> 4) << 3) + (lane & 7)) * kPitch +
+                              swizzled<T, false, kLong>(lane, (lane >> 3) & 1) * 16;
+          const unsigned q_lane = q_at + (lane & 15) * kPitch + swizzled<T, false, kLong>(lane, lane >> 4) * 16;
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
             unsigned kf[4];
-            ldmatrix4(kf, at ^ (k * 32));
+            ldmatrix4(kf, chunk_pair<kLong>(at, k));
             if constexpr (kQRegs) {
               mma_bf16(S[0], qf[k], kf[0], kf[1]);
               mma_bf16(S[1], qf[k], kf[2], kf[3]);
             } else {
               unsigned qv[4];
-              ldmatrix4(qv, q_lane ^ (k * 32));
+              ldmatrix4(qv, chunk_pair<kLong>(q_lane, k));
               mma_bf16(S[0], qv, kf[0], kf[1]);
               mma_bf16(S[1], qv, kf[2], kf[3]);
             }
@@ -458,7 +479,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
             for (int e = 0; e < 4; ++e) large[n][e] = small[n][e] = 0.f;
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
-            const int at = g * DP + swizzled<T, false>(g, 4 * k + t4) * 4;  // (row g + 8: the same chunk)
+            const int at = g * DP + swizzled<T, false, kLong>(g, 4 * k + t4) * 4;  // (row g + 8: the same chunk)
             const uint4 h0 = *reinterpret_cast<const uint4*>(qw + at);
             const uint4 h1 = *reinterpret_cast<const uint4*>(qw + at + 8 * DP);
             const uint4 l0 = *reinterpret_cast<const uint4*>(qw + kRows * DP + at);
@@ -536,11 +557,11 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
             split_bf16(S[n][0], S[n][1], ph[2 * n], pl[2 * n]);
             split_bf16(S[n][2], S[n][3], ph[2 * n + 1], pl[2 * n + 1]);
           }
-          const unsigned at = vs_at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) * 16);
+          const unsigned at = vs_at + (lane & 15) * kPitch + swizzled<T, false, kLong>(lane, lane >> 4) * 16;
 #pragma unroll
           for (int n = 0; n < NT / 2; ++n) {
             unsigned vf[4];
-            ldmatrix4_trans(vf, at ^ (n * 32));
+            ldmatrix4_trans(vf, chunk_pair<kLong>(at, n));
             mma_bf16(O[2 * n], pl, vf[0], vf[1]);
             mma_bf16(O[2 * n + 1], pl, vf[2], vf[3]);
             mma_bf16(O[2 * n], ph, vf[0], vf[1]);
@@ -570,8 +591,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
 #pragma unroll
             for (int n8 = 0; n8 < 2; ++n8) {
               const int r0 = n8 * 8 + 2 * t4, r1 = r0 + 1;
-              const float4 x = *reinterpret_cast<const float4*>(vf + r0 * DP + swizzled<T, true>(r0, 8 * i + g) * 4);
-              const float4 y = *reinterpret_cast<const float4*>(vf + r1 * DP + swizzled<T, true>(r1, 8 * i + g) * 4);
+              const float4 x = *reinterpret_cast<const float4*>(vf + r0 * DP + swizzled<T, true, kLong>(r0, 8 * i + g) * 4);
+              const float4 y = *reinterpret_cast<const float4*>(vf + r1 * DP + swizzled<T, true, kLong>(r1, 8 * i + g) * 4);
               const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
