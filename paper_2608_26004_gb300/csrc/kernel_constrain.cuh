@@ -17,12 +17,16 @@ struct CParams {
   int W;           // vocabulary entries of a CTA, a power of two from 1024 on
   int group_rows;  // rows of a CTA (blockIdx.z: which)
   int batch_rows;  // rows that come into shared memory together
+  int ordered_from;  // the slice from which on the longest histories come first
+  int length_bits;   // of the histories' lengths in steps of 2^kCStepBits
   uint32_t* err;
 };
 
 constexpr int kCThreads = 256;
 constexpr int kCAhead = 2;     // 16-byte loads of the history that a thread has on their way
 constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
+constexpr int kCOrdered = 64;     // requests that are taken in the order of their lengths at most
+constexpr int kCStepBits = 8;      // in steps of so many tokens (a power of two)
 constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
 // A token's word: in the prompt, among the drafts, biased, and how often in the output.
 constexpr unsigned kCPrompt = 1u << 31, kCDraft = 1u << 30, kCBias = 1u << 29, kCCount = kCBias - 1;
@@ -90,6 +94,28 @@ struct Slice {
   int *listed, *biases;
   int b, v0, n, W;
 };
+
+// The request that comes `q`-th when the longest histories (in steps of 2^kCStepBits tokens) come
+// first, by bisection of the lengths; for kCOrdered requests at most.  Ends at a barrier.
+__device__ __forceinline__ int ordered_request(const CParams& p, int q, int* found) {
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    const int32_t* len = p.c.history_len;
+    const int a = lane < p.B ? min(max(len[lane], 0), p.c.history_width) >> kCStepBits : -1;
+    const int b = lane + 32 < p.B ? min(max(len[lane + 32], 0), p.c.history_width) >> kCStepBits : -1;
+    int key = 0;  // of the q-th: the largest that more than q have or exceed
+    for (int bit = p.length_bits - 1; bit >= 0; --bit) {
+      const int more = key | 1 << bit;
+      if (__popc(__ballot_sync(~0u, a >= more)) + __popc(__ballot_sync(~0u, b >= more)) > q) key = more;
+    }
+    const unsigned ea = __ballot_sync(~0u, a == key), eb = __ballot_sync(~0u, b == key), below = (1u << lane) - 1u;
+    q -= __popc(__ballot_sync(~0u, a > key)) + __popc(__ballot_sync(~0u, b > key));
+    if (a == key && __popc(ea & below) == q) *found = lane;
+    if (b == key && __popc(ea) + __popc(eb & below) == q) *found = lane + 32;
+  }
+  __syncthreads();
+  return *found;
+}
 
 // A request's numbers, all on their way together before the CTA's first barrier.
 struct Request {
@@ -273,7 +299,7 @@ __device__ __forceinline__ int mask_of(const CParams& p, int64_t r, unsigned& er
 // tokens, come first in the grid: theirs are the most entries to compute.
 // Bound by HBM, a row in and out; 64x8 rows of V=128256 bf16, half of them masked, histories to
 // 8192: 47 us = 5.6 TB/s (43 with nothing to do but copy); 32x9 rows of V=151936, histories to
-// 65536: 48 us, issuing instructions for the histories (34 without).
+// 65536: 45 us, issuing instructions for the histories (34 without).
 template <typename T, bool EDGES>
 __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) {
   extern __shared__ __align__(16) unsigned c_smem[];
@@ -284,7 +310,14 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
   constexpr int VE = 16 / sizeof(T);
   constexpr unsigned kAll = (1u << VE) - 1u;
   const asymspec_constraints& c = p.c;
-  const int W = p.W, b = blockIdx.x, v0 = blockIdx.y * W, n = min(W, p.V - v0), tid = threadIdx.x;
+  __shared__ int s_request;
+  int b = blockIdx.x, at_slice = blockIdx.y;
+  if (at_slice >= p.ordered_from) {
+    const int last = static_cast<int>(gridDim.y) - p.ordered_from, i = (at_slice - p.ordered_from) * p.B + b;
+    at_slice = p.ordered_from + i % last;
+    b = ordered_request(p, i / last, &s_request);
+  }
+  const int W = p.W, v0 = at_slice * W, n = min(W, p.V - v0), tid = threadIdx.x;
   const Slice slice = {c_smem, reinterpret_cast<uint16_t*>(c_smem + W), s_bias, &s_listed, &s_biases, b, v0, n, W};
   const int pitch = constrain_pitch(W, sizeof(T));
   unsigned char* tile = reinterpret_cast<unsigned char*>(c_smem) + constrain_list_bytes(W);
@@ -437,7 +470,14 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   extern __shared__ __align__(16) unsigned c_smem[];
   __shared__ int2 s_bias[kCBiases];
   __shared__ int s_listed, s_biases;
-  const int W = p.W, b = blockIdx.x, v0 = blockIdx.y * W, n = min(W, p.V - v0), tid = threadIdx.x;
+  __shared__ int s_request;
+  int b = blockIdx.x, at_slice = blockIdx.y;
+  if (at_slice >= p.ordered_from) {
+    const int last = static_cast<int>(gridDim.y) - p.ordered_from, i = (at_slice - p.ordered_from) * p.B + b;
+    at_slice = p.ordered_from + i % last;
+    b = ordered_request(p, i / last, &s_request);
+  }
+  const int W = p.W, v0 = at_slice * W, n = min(W, p.V - v0), tid = threadIdx.x;
   const Slice slice = {c_smem, reinterpret_cast<uint16_t*>(c_smem + W), s_bias, &s_listed, &s_biases, b, v0, n, W};
   const int k0 = blockIdx.z * p.group_rows, rows = min(p.group_rows, p.P - k0);
   unsigned err = 0;

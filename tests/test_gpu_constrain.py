@@ -165,6 +165,29 @@ def test_more_biases_than_a_slice_holds(torch):
     check(torch, z, x, S.constrain_logits(z, **x))
 
 
+@pytest.mark.parametrize("B", [2, 33, 64, 65])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_long_histories_of_many_lengths(torch, B, in_place):
+    """Where histories may be long, some CTAs take the requests in the order of their lengths:
+    none is left out or done twice, with equal lengths, empty ones and ones out of range."""
+    V, P, N = 9001, 2, 16385
+    z, x = inputs(torch, B, P, V, torch.float32, N, B, 0, None, 3)
+    some = [0, N, 255, 256, 257, N, 4000, 0]
+    x["history_len"][:min(B, 8)] = torch.tensor(some[:min(B, 8)], dtype=torch.int32)
+    x["prompt_len"] = x["history_len"] // 3
+    sound = x["history_len"].clone()
+    x["history_len"][B - 1] = N + 5 if B % 2 else -3
+    sound[B - 1] = N if B % 2 else 0
+    x["prompt_len"][B - 1] = 0
+    error = torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = S.constrain_logits(z.clone(), **x, error_word=error) if not in_place else None
+    if in_place:
+        y = z.clone()
+        S.constrain_logits(y, **x, out=y, error_word=error)
+    assert int(error) == S.DATA_BAD_LENGTH
+    check(torch, z, dict(x, history_len=sound), y, {(b, b % 2) for b in range(B)})
+
+
 def test_bad_data_sets_bits_and_leaves_the_rest(torch):
     i32 = dict(device="cuda", dtype=torch.int32)
     z, x = inputs(torch, 2, 3, 500, torch.float32, 40, 21, 0, None, 0)
