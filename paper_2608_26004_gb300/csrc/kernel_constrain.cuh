@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
 
 // The logits penalised and biased where they are, without masks: nothing but the entries
 // that something touches is read or written, each where it lies (64x8 rows of V=128256 bf16
-// with histories to 8192: 30 us, 45 through constrain_rows; with masks on half of the rows,
+// with histories to 8192: 24 us, 45 through constrain_rows; with masks on half of the rows,
 // when those were overwritten here too, 64 against 48: a call with masks takes constrain_rows
 // in place).
 template <typename T>
