@@ -121,7 +121,7 @@ def _rows(name, x, dtype, dev, n):
     if x.dtype is not dtype or x.get_device() != dev or len(shape) != 2 or shape[0] != n \
             or (strides[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be a [{n}, ...] {dtype} tensor with contiguous rows on cuda:{dev}")
-    return x.data_ptr(), max(strides[0], shape[1]), shape[1]
+    return x.data_ptr(), strides[0] if n > 1 else shape[1], shape[1]
 
 
 def _error_word(x, dev):
@@ -129,11 +129,11 @@ def _error_word(x, dev):
 
 
 def _row_distance(name, x, B, P, V):
-    """Elements between the rows of [B, P, V]: contiguous, evenly spaced."""
+    """Elements between the rows of [B, P, V]: contiguous, evenly spaced, each its own memory."""
     s0, s1, s2 = x.stride()
     ld = s1 if P > 1 else s0 if B > 1 else V
-    if s2 != 1 or (B > 1 and P > 1 and s0 != P * ld):
-        raise ValueError(f"the rows of {name} must be contiguous and evenly spaced")
+    if s2 != 1 or ld < V or (B > 1 and P > 1 and s0 != P * ld):
+        raise ValueError(f"the rows of {name} must be contiguous, evenly spaced and apart")
     return ld
 
 
@@ -201,7 +201,7 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
         _CONSTRAINTS.pack(h, h_ld, h_width, h_len, p_len, d if P > 1 else 0, d_ld, rep, freq, pres, b_at,
                           b_tok, b_val, b_n, m, m_ld, m_n, m_rows,
                           -FLT_MAX if mask_value is None else mask_value),
-        logits.data_ptr(), ld if ld > V else V, out.data_ptr(), out_ld if out_ld > V else V, B, P, V,
+        logits.data_ptr(), ld, out.data_ptr(), out_ld, B, P, V,
         dtype, 0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
         raise AsymSpecError(st, "asymspec_constrain_logits")
@@ -307,7 +307,8 @@ class CacheAttend:
     ``__call__`` takes q [B, Q, heads, head_dim] (any strides, heads contiguous), a paged
     cache as cache_write does, tables [B, width] int32 and lens [B] int32 (the cached
     tokens of each request, the Q new ones included) and returns (out [B, Q, heads,
-    head_dim], lse [B, Q, heads] float32), enqueued on the current stream.
+    head_dim], lse [B, Q, heads] float32), enqueued on the current stream.  Calls that
+    share the workspace must follow one another: on one stream, or ordered by events.
     """
 
     def __init__(self, B_max: int, Q_max: int, heads: int, kv_heads: int, head_dim: int, device=None):
@@ -320,6 +321,7 @@ class CacheAttend:
             raise ValueError("no attention of this shape")
         self.workspace = torch.empty(self.nbytes, dtype=torch.uint8,
                                      device=torch.device(device or "cuda"))
+        self.device_index = self.workspace.get_device()
         self.scale = 1.0 / math.sqrt(head_dim)
 
     def __call__(self, q, key_cache, value_cache, tables, lens, *, scale=None, window=0, out=None,
@@ -327,6 +329,8 @@ class CacheAttend:
         view, dev, (_, _, kv_heads, head_dim) = _cache(key_cache, value_cache)
         B, Q, heads, dim = shape = q.shape
         kind = key_cache.dtype
+        if dev != self.device_index:
+            raise ValueError("the cache must be on the workspace's device")
         if B > self.B_max or Q > self.Q_max or (heads, kv_heads, head_dim) != (
                 self.heads, self.kv_heads, self.head_dim):
             raise ValueError("batch does not fit this workspace")

@@ -256,3 +256,16 @@ def test_refusals_of_the_binding(torch):
         S.constrain_logits(z.half())
     with pytest.raises(A.AsymSpecError):
         S.constrain_logits(z, mask=torch.zeros(5, 2, **i32))
+
+
+def test_a_history_and_drafts_that_requests_share(torch):
+    z, x = inputs(torch, 4, 3, 1500, torch.float32, 400, 41)
+    x["history"], x["drafts"] = x["history"][:1].expand(4, 400), x["drafts"][1:2].expand(4, 2)
+    error = torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = S.constrain_logits(z, **x, error_word=error)
+    assert int(error) == 0
+    check(torch, z, x, y)
+    with pytest.raises(ValueError):
+        S.constrain_logits(z[:1, :1].expand(4, 3, 1500), **x)
+    with pytest.raises(ValueError):
+        S.constrain_logits(z, **x, out=z[:1].expand(4, 3, 1500))

@@ -177,3 +177,21 @@ def test_the_joining_kernel_waits_for_the_one_before():
     body = text[text.index(" attend_join("):]
     first = re.search(r"griddepcontrol\.wait|\breturn;|p\.ws", body)
     assert first and first.group().startswith("griddep")
+
+
+def test_rows_that_share_memory():
+    """Expanded views: rows that lie over one another are read where they are, never a row's
+    width apart (which would be past the tensor's end); logits' rows must not be."""
+    torch = pytest.importorskip("torch")
+    one = torch.zeros(1, 9, dtype=torch.int32)
+    assert S._rows("x", one.expand(5, 9), torch.int32, -1, 5)[1:] == (0, 9)
+    assert S._rows("x", one, torch.int32, -1, 1)[1:] == (9, 9)
+    assert S._rows("x", torch.zeros(3, 12, dtype=torch.int32)[:, :9], torch.int32, -1, 3)[1:] == (12, 9)
+    z = torch.zeros(1, 1, 8)
+    assert S._row_distance("z", z, 1, 1, 8) == 8
+    assert S._row_distance("z", torch.zeros(2, 3, 10)[..., :8], 2, 3, 8) == 10
+    for B, P in ((4, 1), (1, 4), (2, 3)):
+        with pytest.raises(ValueError):
+            S._row_distance("z", z.expand(B, P, 8), B, P, 8)
+    with pytest.raises(ValueError):
+        S._row_distance("z", torch.zeros(40).as_strided((2, 3, 8), (15, 5, 1)), 2, 3, 8)
