@@ -37,7 +37,7 @@ constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each
 // of its tiles, after kAItem for what it costs to begin and end one (64 requests of 64 to 8192
-// tokens, kAItem = 1, 2, 3: 80, 75, 76 us; a window of 2000, fp32: 44, 45, 46.5).
+// tokens, kAItem = 1, 2, 3: 80, 75, 76 us).
 constexpr int kAItem = 2;
 
 // A CTA whose share begins after the first tile of an item says which.
@@ -142,10 +142,13 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const unsigned (&a)[4], 
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x = hi + lo + (2^-22 |x| at most), each with tf32's 11 significant bits.
+// x = hi + lo + (2^-21 |x| at most, of lo's sign, which is either), each with tf32's 11
+// significant bits: hi rounded, its distance from x (exact) cut.  In integer arithmetic: the
+// conversion instruction is slow (32 requests, a window of 2000: 43.7 us with it, 39.1 so).  An
+// x that is a NaN or infinite makes lo a NaN.
 __device__ __forceinline__ void split_tf32(float x, unsigned& hi, unsigned& lo) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+  hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
+  lo = __float_as_uint(x - __uint_as_float(hi)) & 0xFFFFE000u;
 }
 // (x, y) = hi + lo + (2^-17 of each at most), packed bf16.
 __device__ __forceinline__ void split_bf16(float x, float y, unsigned& hi, unsigned& lo) {
@@ -182,7 +185,7 @@ __device__ __forceinline__ void group_barrier(int id, int threads) {
 // heads on 8 of 128: 74 us = 5.9 TB/s; by issue and latency at 32 (16 requests of 4096 to
 // 131072 tokens, 8 queries each: 425 us = 6.0 TB/s) and by the matrix instructions at 64 (8
 // requests to 32768: 167 us, 99 at 32 rows).  fp32, 32 requests, 5 queries, a window of 2000, 8
-// heads of 64: 44 us = 3.6 TB/s, splitting operands.
+// heads of 64: 39 us = 4.0 TB/s, splitting operands.
 template <typename T, int DP, int WR, int ST, int PER_SM>
 __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const AttendParams p) {
   constexpr bool BF = sizeof(T) == 2;
