@@ -4,12 +4,12 @@
 
 namespace asymspec_impl {
 
-template <int DP, int WR, int ST, int PER_SM>
+template <int DP, int WR, int ST, int PER_SM, int kH = 2>
 AttendKernels attend_pick() {
   constexpr int smem = static_cast<int>(attend_smem_bytes<__nv_bfloat16>(DP, WR, ST));
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
   static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
-  return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, WR, ST, PER_SM>),
+  return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, WR, ST, PER_SM, kH>),
           reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM};
 }
 

@@ -185,8 +185,8 @@ __device__ __forceinline__ void group_barrier(int id, int threads) {
 // heads on 8 of 128: 74 us = 5.9 TB/s; by issue and latency at 32 (16 requests of 4096 to
 // 131072 tokens, 8 queries each: 425 us = 6.0 TB/s) and by the matrix instructions at 64 (8
 // requests to 32768: 167 us, 99 at 32 rows).  fp32, 32 requests, 5 queries, a window of 2000, 8
-// heads of 64: 39 us = 4.0 TB/s, splitting operands.
-template <typename T, int DP, int WR, int ST, int PER_SM>
+// heads of 64: 37 us = 4.2 TB/s, splitting operands.  kH: halves of a warp's 16 rows in use.
+template <typename T, int DP, int WR, int ST, int PER_SM, int kH>
 __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const AttendParams p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int kThreadsN = kAGroups * WR * 32, kWarpsN = kAGroups * WR;
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
   const int chunk_bytes = chunk0 * PE < p.D ? 16 : 0;
   const int step_blocks = kATile / p.block_size, step_rest = kATile % p.block_size;
 
-  float O[NT][4], m[2], l[2];
+  float O[NT][4], m[kH], l[kH];
   unsigned qf[kQRegs ? DP / 16 : 1][4];
   for (; u < u_end; at_unit = 0) {
     if (hr == HR) {
@@ -400,9 +400,9 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
     // of this thread's rows: the last key seen; of the warp's the least, and the windows'
     // largest first
     const int R = R0 + wr * 16, warp_rows = rows - wr * 16;  // (may be none)
-    int last[2];
+    int last[kH];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kH; ++h) {
       last[h] = h * 8 + g < warp_rows ? len - p.Q + (R + h * 8 + g) / p.group : -1;
       m[h] = -INFINITY;
       l[h] = 0.f;
@@ -475,6 +475,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           // own, the large ones two, added up in fp32 at the end.
           const float* kf = reinterpret_cast<const float*>(ks);
           const float* qw = reinterpret_cast<const float*>(qs) + wr * 16 * DP;
+          const uint4 none = make_uint4(0, 0, 0, 0);
           float large[2][4], small[2][4];
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -484,9 +485,9 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           for (int k = 0; k < DP / 16; ++k) {
             const int at = g * DP + swizzled<T, false, kLong>(g, 4 * k + t4) * 4;  // (row g + 8: the same chunk)
             const uint4 h0 = *reinterpret_cast<const uint4*>(qw + at);
-            const uint4 h1 = *reinterpret_cast<const uint4*>(qw + at + 8 * DP);
+            const uint4 h1 = kH == 1 ? none : *reinterpret_cast<const uint4*>(qw + at + 8 * DP);
             const uint4 l0 = *reinterpret_cast<const uint4*>(qw + kRows * DP + at);
-            const uint4 l1 = *reinterpret_cast<const uint4*>(qw + kRows * DP + at + 8 * DP);
+            const uint4 l1 = kH == 1 ? none : *reinterpret_cast<const uint4*>(qw + kRows * DP + at + 8 * DP);
             const unsigned qh[2][4] = {{h0.x, h1.x, h0.y, h1.y}, {h0.z, h1.z, h0.w, h1.w}};
             const unsigned ql[2][4] = {{l0.x, l1.x, l0.y, l1.y}, {l0.z, l1.z, l0.w, l1.w}};
 #pragma unroll
@@ -509,11 +510,11 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[n][e] += large[n][e] + small[n][e];
+            for (int e = 0; e < 2 * kH; ++e) S[n][e] += large[n][e] + small[n][e];
         }
         const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kH; ++h) {
           float top = -INFINITY;
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -557,8 +558,10 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           unsigned ph[4], pl[4];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            split_bf16(S[n][0], S[n][1], ph[2 * n], pl[2 * n]);
-            split_bf16(S[n][2], S[n][3], ph[2 * n + 1], pl[2 * n + 1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (h < kH) split_bf16(S[n][2 * h], S[n][2 * h + 1], ph[2 * n + h], pl[2 * n + h]);
+              else ph[2 * n + h] = pl[2 * n + h] = 0;
           }
           const unsigned at = vs_at + (lane & 15) * kPitch + swizzled<T, false, kLong>(lane, lane >> 4) * 16;
 #pragma unroll
@@ -579,10 +582,13 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           unsigned ph[2][4], pl[2][4];
 #pragma unroll
           for (int n8 = 0; n8 < 2; ++n8) {
-            split_tf32(S[n8][0], ph[n8][0], pl[n8][0]);
-            split_tf32(S[n8][2], ph[n8][1], pl[n8][1]);
-            split_tf32(S[n8][1], ph[n8][2], pl[n8][2]);
-            split_tf32(S[n8][3], ph[n8][3], pl[n8][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ph[n8][e] = pl[n8][e] = 0;
+#pragma unroll
+            for (int h = 0; h < kH; ++h) {
+              split_tf32(S[n8][2 * h], ph[n8][h], pl[n8][h]);
+              split_tf32(S[n8][2 * h + 1], ph[n8][2 + h], pl[n8][2 + h]);
+            }
           }
 #pragma unroll
           for (int i = 0; i < DP / 32; ++i) {
@@ -610,7 +616,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) O[4 * i + e][j] += sum[e][j];
+              for (int j = 0; j < 2 * kH; ++j) O[4 * i + e][j] += sum[e][j];
           }
         }
       }
@@ -623,7 +629,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
     // keys again, one product after another, and leaves out what a row does not see.
     float odd = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kH; ++h)
       if (h * 8 + g < warp_rows) {
         odd = fmaf(0.f, l[h], odd);
 #pragma unroll
@@ -631,7 +637,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
       }
     if (__any_sync(~0u, odd != 0.f)) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < kH; ++h) {
         m[h] = -INFINITY;
         l[h] = 0.f;
 #pragma unroll
@@ -645,7 +651,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
         const T* kr = keys + page * p.cks[0] + at * p.cks[1];
         const T* vr = values + page * p.cvs[0] + at * p.cvs[1];
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kH; ++h) {
           const int r = R + min(h * 8 + g, warp_rows - 1);
           const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + r / p.group * p.qs[1] +
                         (kh * p.group + r % p.group) * p.qs[2];
@@ -654,11 +660,11 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           s += __shfl_xor_sync(~0u, s, 1);
           s += __shfl_xor_sync(~0u, s, 2);
           s *= p.scale2;
-          const int end = h ? last[1] : last[0];
+          const int end = h ? last[kH - 1] : last[0];
           if (j > end || (p.window != 0 && j <= end - p.window)) continue;
-          const float old = h ? m[1] : m[0], v = fmaxf(old, s), ref = v == -INFINITY ? 0.f : v;
+          const float old = h ? m[kH - 1] : m[0], v = fmaxf(old, s), ref = v == -INFINITY ? 0.f : v;
           const float f = v == old ? 1.f : ex2(old - v), w = ex2(s - ref);
-          if (h) m[1] = v, l[1] = l[1] * f + (t4 == 0 ? w : 0.f);
+          if (h) m[kH - 1] = v, l[kH - 1] = l[kH - 1] * f + (t4 == 0 ? w : 0.f);
           else m[0] = v, l[0] = l[0] * f + (t4 == 0 ? w : 0.f);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -678,7 +684,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
     else __syncwarp();
     float* mine_o = reinterpret_cast<float*>(ring) + wr * 16 * DP;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kH; ++h) {
       const int r = h * 8 + g;
       float s = l[h];
       s += __shfl_xor_sync(~0u, s, 1);
