@@ -19,7 +19,14 @@ AttendKernels attend_pick() {
 // CTAs an SM: as many as the registers allow, with rings as deep as shared memory then does.  Three
 // at 16 rows, where two with deeper rings are as fast for long contexts (64 requests of 64 to 8192
 // tokens 74 both) and slower for short ones (256 of 16 to 300 tokens 39 to 34).
+// Up to 8 rows (half of the matrix instructions' 16) the other half's softmax and pieces are left
+// out: those 64 requests 74.3 to 73.7 us (heads of 64 45.0 to 43.9, of 256 163 to 157), those 256
+// 33.6 to 31.3.
 AttendKernels attend_kernels_bf16(int D, int rows) {
+  if (rows <= 8)
+    return D <= 64    ? attend_pick<64, 1, 3, 3, 1>()
+           : D <= 128 ? attend_pick<128, 1, 2, 3, 1>()
+                      : attend_pick<256, 1, 3, 1, 1>();
   if (D <= 64)
     return rows <= 16 ? attend_pick<64, 1, 3, 3>() : rows <= 32 ? attend_pick<64, 2, 5, 2>() : attend_pick<64, 4, 8, 1>();
   if (D <= 128)
