@@ -185,7 +185,7 @@ __device__ __forceinline__ void group_barrier(int id, int threads) {
 // heads on 8 of 128: 74 us = 5.9 TB/s; by issue and latency at 32 (16 requests of 4096 to
 // 131072 tokens, 8 queries each: 425 us = 6.0 TB/s) and by the matrix instructions at 64 (8
 // requests to 32768: 167 us, 99 at 32 rows).  fp32, 32 requests, 5 queries, a window of 2000, 8
-// heads of 64: 37 us = 4.2 TB/s, splitting operands.  kH: halves of a warp's 16 rows in use.
+// heads of 64: 37 us = 4.2 TB/s, waiting for its products.  kH: halves of a warp's 16 rows in use.
 template <typename T, int DP, int WR, int ST, int PER_SM, int kH>
 __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const AttendParams p) {
   constexpr bool BF = sizeof(T) == 2;
