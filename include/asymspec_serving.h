@@ -181,7 +181,7 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
 /* Attention of the last Q of each request's tokens over its cached ones (their own keys and
  * values written before).  For request b, query i and query head h, at position p = lens[b]
  * - Q + i, over the keys j of kv head h / (heads / kv_heads) with max(0, p - window + 1) <= j
- * <= p (window 0: from 0 on):
+ * <= p (window 0, or one that spans the whole table row: from 0 on):
  *
  *   s_j = scale * q . k_j,   lse = ln sum_j exp(s_j),   out = sum_j exp(s_j - lse) v_j
  *

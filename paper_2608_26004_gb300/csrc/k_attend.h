@@ -2,8 +2,16 @@
 #pragma once
 
 #include <cstddef>
+#include <cstdint>
 
 namespace asymspec_impl {
+
+// The window that the kernels work with: 0 (none) where it spans whatever a table row can hold.  A
+// window that is left is below that, 2^30 at most, so that the kernels' 32-bit length - Q - window + 1
+// stays above -2^31 (Q * heads is 2^20 at most).
+inline int attend_window(int window, int table_width, int block_size) {
+  return window >= static_cast<int64_t>(table_width) * block_size ? 0 : window;
+}
 
 struct AttendKernels {
   const void *split, *join;

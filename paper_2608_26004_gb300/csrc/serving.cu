@@ -355,7 +355,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   p.num_blocks = cache->num_blocks;
   p.block_size = cache->block_size;
   p.table_width = table_width;
-  p.window = window;
+  p.window = attend_window(window, table_width, cache->block_size);
   p.group = heads / cache->kv_heads;
   p.rows = Q * p.group;
   const AttendKernels k = attend_kernels(cache->dtype, p.D, p.rows);

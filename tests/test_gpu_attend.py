@@ -124,6 +124,25 @@ def test_rows_against_the_definition(torch, case):
     assert torch.equal(out, again) and torch.equal(lse, lse2)   # the same bits each time
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("lens,Q", [([0, 7, 1, 300], 8), ([0, 0], 3), ([3, 0, 2, 90, 1], 5), ([40], 1)])
+def test_a_window_past_the_table_hides_nothing(torch, dtype, lens, Q):
+    """Windows at and past what a table row holds, up to the largest number, with requests that
+    have ended or are shorter than their queries: the bits of no window."""
+    x = inputs(torch, lens, Q, 8, 4, 64, dtype, 16, 31)
+    attend = S.CacheAttend(len(lens), Q, 8, 4, 64)
+    err = torch.zeros(1, device="cuda", dtype=torch.int32)
+    want, want_lse = attend(*x)
+    span = x[3].shape[1] * 16
+    for window in (span, span + 1, 2 ** 30, 2 ** 31 - Q, 2 ** 31 - 1):
+        out, lse = attend(*x, window=window, error_word=err)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), window
+    check(torch, x, want, want_lse, some_rows(len(lens), Q, 8, 3))
+    out, lse = attend(*x, window=span - 1, error_word=err)
+    check(torch, x, out, lse, some_rows(len(lens), Q, 8, 3), window=span - 1)
+    assert int(err) == 0
+
+
 def test_all_requests_empty(torch):
     x = inputs(torch, [0, 0, 0], 2, 8, 4, 64, "bfloat16", 16, 1)
     out, lse = S.CacheAttend(3, 2, 8, 4, 64)(*x)

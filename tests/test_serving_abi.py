@@ -195,3 +195,40 @@ def test_rows_that_share_memory():
             S._row_distance("z", z.expand(B, P, 8), B, P, 8)
     with pytest.raises(ValueError):
         S._row_distance("z", torch.zeros(40).as_strided((2, 3, 8), (15, 5, 1)), 2, 3, 8)
+
+
+def test_windows_of_any_size_stay_in_32_bits(tmp_path):
+    """The host's bound of the window, compiled as it is, and the kernels' 32-bit sums with it: the
+    first key, in request lengths from none to the table's; a window that spans the table is none."""
+    import subprocess
+    source = tmp_path / "window.cpp"
+    source.write_text('''
+        #include <cstdio>
+        #include "k_attend.h"
+        int main() {
+          int window, width, block;
+          while (std::scanf("%d %d %d", &window, &width, &block) == 3)
+            std::printf("%d\\n", asymspec_impl::attend_window(window, width, block));
+        }''')
+    program = str(tmp_path / "window")
+    subprocess.run(["g++", "-std=c++17", "-I", build.CSRC, str(source), "-o", program], check=True)
+    top = 2 ** 31 - 1
+    tables = [(1, 1), (4, 16), (64, 24), (1 << 26, 16), (1, 1 << 30)]
+    asked = [(w, width, bs) for width, bs in tables
+             for w in {0, 1, 16, width * bs - 1, width * bs, width * bs + 1, 1 << 30, top - 8, top} if w <= top]
+    got = subprocess.run([program], input="\n".join("%d %d %d" % a for a in asked), capture_output=True,
+                         text=True, check=True).stdout.split()
+    assert len(got) == len(asked)
+    for (w, width, bs), g in zip(asked, map(int, got)):
+        assert g == (w if w < width * bs else 0), (w, width, bs)
+        for n in (0, 1, width * bs):
+            for Q in (1, 3, 1 << 20):
+                first = max(0, n - Q - g + 1) if g else 0
+                assert -2 ** 31 <= n - Q - g + 1 and 0 <= first <= n
+                # of the key p that a query is at, with and without the bound: the same first key
+                for p in (0, n - Q, n - 1):
+                    if 0 <= p < width * bs:
+                        assert (max(0, p - w + 1) if w else 0) == (max(0, p - g + 1) if g else 0)
+    import os
+    with open(os.path.join(build.CSRC, "serving.cu")) as f:
+        assert f.read().count("p.window = attend_window(window, table_width, cache->block_size);") == 1
