@@ -198,7 +198,8 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
  *       no zeroing, serves any calls that it is large enough for, and must not be shared by
  *       calls in flight at the same time
  * A length below 0 counts as 0 and one beyond the table as the table's (ASYMSPEC_DATA_BAD_
- * LENGTH); keys in a block outside [0, num_blocks) are not seen (ASYMSPEC_DATA_BAD_INDEX).
+ * LENGTH); keys in a block outside [0, num_blocks) are not seen (ASYMSPEC_DATA_BAD_INDEX; blocks
+ * that lie before every query's window may be gone from the table).
  * B = 0 or Q = 0 is a no-op.  The work is split over the cached tokens of all requests
  * evenly, whatever their lengths, and the parts joined by a second launch; results do
  * not depend on the order in which the parts finish.

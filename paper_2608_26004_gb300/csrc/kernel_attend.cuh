@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           fv += kLaneRows * p.token_bytes[1];
         }
       } else if (live != 0 || __any_sync(~0u, key < end_key)) {
-        if (!there && key < end_key) err |= ASYMSPEC_DATA_BAD_INDEX;
+        // (up to 15 keys are before the window of every query: their block may be gone)
+        if (!there && key < end_key && (p.window == 0 || key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
         const int64_t ok = there ? page * p.cks[0] + at * p.cks[1] : 0;
         const int64_t ov = there ? page * p.cvs[0] + at * p.cvs[1] : 0;
 #pragma unroll

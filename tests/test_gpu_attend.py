@@ -143,6 +143,28 @@ def test_a_window_past_the_table_hides_nothing(torch, dtype, lens, Q):
     assert int(err) == 0
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("bs,n,Q,window", [(8, 155, 2, 50), (24, 400, 3, 55), (1, 60, 1, 7), (5, 90, 4, 30),
+                                           (16, 200, 2, 41)])
+def test_blocks_before_the_window_may_be_gone(torch, dtype, bs, n, Q, window):
+    """What no query sees need not be in the table: no data error for it, but one for the first
+    block that a query does see."""
+    q, keys, values, tables, lens = x = inputs(torch, [n, 3], Q, 4, 2, 64, dtype, bs, 35)
+    attend = S.CacheAttend(2, Q, 4, 2, 64)
+    err = torch.zeros(1, device="cuda", dtype=torch.int32)
+    want, want_lse = attend(*x, window=window)
+    first = n - Q - window + 1
+    tables[0, :first // bs] = -1
+    out, lse = attend(*x, window=window, error_word=err)
+    assert int(err) == 0
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    check(torch, x, out, lse, some_rows(2, Q, 4, 5), window=window)
+    tables[0, first // bs] = -1
+    out, lse = attend(*x, window=window, error_word=err)
+    assert int(err) == S.DATA_BAD_INDEX
+    check(torch, x, out, lse, some_rows(2, Q, 4, 5), window=window)
+
+
 def test_all_requests_empty(torch):
     x = inputs(torch, [0, 0, 0], 2, 8, 4, 64, "bfloat16", 16, 1)
     out, lse = S.CacheAttend(3, 2, 8, 4, 64)(*x)
