@@ -85,6 +85,10 @@ constexpr size_t attend_smem_bytes(int DP, int WR, int ST) {
 __device__ __forceinline__ void put(float* p, float y) { *p = y; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float y) { *p = __float2bfloat16_rn(y); }
 
+// ln of a row's sum, from its reference and the sum of its weights: -infinity where it has no keys;
+// where all of its scores are NaN its reference is -infinity too, and its sum the NaN.
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l)); }
+
 __device__ __forceinline__ int attend_len(const AttendParams& p, int b) {
   return min(max(p.lens[b], 0), p.table_width * p.block_size);
 }
@@ -747,7 +751,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
           }
         }
         if (d == 0 && p.lse)
-          p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = M == -INFINITY ? -INFINITY : fmaf(M, kLn2, logf(L));
+          p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = lse_of(M, L);
       } else {
         *reinterpret_cast<float4*>(ws_o + r * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
         if (d == 0) *reinterpret_cast<float2*>(ws_ml + r * 2) = make_float2(M, L);
@@ -824,7 +828,7 @@ __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams 
     for (int k = 0; k < 4; ++k) put(out + k, x[k] * inv);
   }
   if (d == 0 && p.lse)
-    p.lse[(static_cast<int64_t>(in.b) * p.Q + i) * p.heads + h] = M == -INFINITY ? -INFINITY : fmaf(M, kLn2, logf(L));
+    p.lse[(static_cast<int64_t>(in.b) * p.Q + i) * p.heads + h] = lse_of(M, L);
 }
 
 }  // namespace asymspec_impl

@@ -227,6 +227,24 @@ def test_infinite_values_follow_the_formula(torch, dtype):
     check(torch, x, out, lse2, [(0, i, h) for i in range(Q) for h in (0, 1, 4, 7)] + [(1, 2, 3)])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n", [90, 30000])              # one CTA's share, and joined ones
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_without_numbers_has_no_number(torch, dtype, n, bad):
+    """A NaN in a query makes its out and lse NaN, not -infinity, which says that it has no keys; so
+    does an infinity, whose scores are infinities of both signs."""
+    x = inputs(torch, [n, 0, 40], 3, 4, 2, 64, dtype, 16, 23)
+    attend = S.CacheAttend(3, 3, 4, 2, 64)
+    q = x[0].clone()
+    q[0, 1, 2, 5] = q[2, 0, 3, 63] = bad
+    out, lse = attend(q, *x[1:])
+    hit = torch.zeros(3, 3, 4, device="cuda", dtype=torch.bool)
+    hit[0, 1, 2] = hit[2, 0, 3] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert not out[~hit].isnan().any() and (lse[1] == -math.inf).all()
+    check(torch, x, out, lse, [(b, i, h) for b in range(3) for i in range(3) for h in range(4) if not hit[b, i, h]])
+
+
 def test_bad_data(torch):
     q, keys, values, tables, lens = inputs(torch, [100, 60, 40], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.CacheAttend(3, 2, 4, 2, 64)
