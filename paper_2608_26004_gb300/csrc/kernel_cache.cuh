@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
   }
   if (tid == 0) offs[B] = off, more_of[B] = more_sum, less_of[B] = less_sum;
   barrier();  // (the inputs are read: outputs may lie over them)
-  const int top = free_in + less_sum;
+  const int64_t top = static_cast<int64_t>(free_in) + less_sum;  // (bad data: past num_blocks, and 2^31)
   // who is served; the state of the next call
   for (int b = tid; b < B; b += kPThreads) {
     const int m = more_of[b + 1] - more_of[b], l = less_of[b + 1] - less_of[b];
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
     for (int i = at0; i < less_sum; i += stride) {
       const int b = find_last(less_of, B, i);
       const int kept = (held_of[b] & INT_MAX) - (less_of[b + 1] - less_of[b]);
-      const int at = free_in + i;
+      const int64_t at = static_cast<int64_t>(free_in) + i;
       if (at < p.num_blocks) p.free_list[at] = p.tables[b * p.table_ld + kept + i - less_of[b]];
       else err |= ASYMSPEC_DATA_BAD_LENGTH;
     }
@@ -169,11 +169,11 @@ __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams 
   const int taken = s_taken;
   for (int i = at0; i < taken; i += stride) {
     const int b = find_last(more_of, B, i);
-    const int at = top - 1 - i;
+    const int64_t at = top - 1 - i;
     p.tables[b * p.table_ld + (held_of[b] & INT_MAX) + i - more_of[b]] =
         at < p.num_blocks ? __ldcg(p.free_list + at) : -1;
   }
-  if (at0 == 0) *p.out_free = min(top - taken, p.num_blocks);
+  if (at0 == 0) *p.out_free = static_cast<int>(min(top - taken, static_cast<int64_t>(p.num_blocks)));
   barrier();
   // kPSlots slots a thread: one search, a division where a block begins
   constexpr int kPSlots = CLUSTER ? 4 : 1;

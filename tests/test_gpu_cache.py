@@ -202,6 +202,37 @@ def test_bad_data(torch):
     assert e == S.DATA_BAD_INDEX
 
 
+def test_more_blocks_than_there_are(torch):
+    """Blocks given back to a list that is full already (bad data) go nowhere, in a pool of so many
+    that the place after the list's end does not fit 32 bits either."""
+    i32 = dict(device="cuda", dtype=torch.int32)
+    for blocks in (40, 2 ** 31 - 1):
+        room = torch.empty(blocks + 64, **i32)
+        room[:32] = -77
+        room[32 + blocks:] = -77
+        free = room[32:32 + blocks]
+        free[-40:] = torch.arange(40, **i32)
+        tables = torch.arange(40, **i32).view(2, 20)
+        err = torch.zeros(1, **i32)
+        r = S.cache_plan(torch.tensor([0, 3], **i32), tables, torch.tensor([20, 15], **i32), free,
+                         torch.tensor([blocks], **i32), block_size=1, grow=2, error_word=err)
+        assert int(err) == S.DATA_BAD_LENGTH
+        assert r["held"].tolist() == [2, 5] and r["free_count"].tolist() == [blocks]
+        assert r["slots"].tolist() == [0, 1, 23, 24]
+        assert (room[:32] == -77).all() and (room[32 + blocks:] == -77).all()
+        assert torch.equal(free[-40:], torch.arange(40, **i32))
+        # and requests that need some take none of what was not put there
+        err.zero_()
+        r = S.cache_plan(torch.tensor([0, 3], **i32), tables, torch.tensor([20, 3], **i32), free,
+                         torch.tensor([blocks], **i32), block_size=1, grow=torch.tensor([0, 4], **i32),
+                         capacity=4, error_word=err)
+        assert int(err) == S.DATA_BAD_LENGTH | S.DATA_BAD_INDEX
+        assert r["held"].tolist() == [0, 7] and r["slots"].tolist() == [-1] * 4
+        assert tables[1, 3:7].tolist() == [-1] * 4
+        assert (room[:32] == -77).all() and (room[32 + blocks:] == -77).all()
+        del room, free
+
+
 WRITES = [
     # T, heads, D, block, dtype, layout, offset of k in its allocation
     (1, 1, 64, 16, "bfloat16", "nhd", 0), (513, 8, 128, 16, "bfloat16", "nhd", 0),
