@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
         if (p.q_vec) {
           v = *reinterpret_cast<const uint4*>(src);
         } else {
-          T x[PE];
+          __align__(16) T x[PE];
 #pragma unroll
           for (int k = 0; k < PE; ++k) x[k] = src[k];
           v = *reinterpret_cast<const uint4*>(x);
@@ -739,7 +739,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
         const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
         T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
         if (d < p.D) {  // (D is a multiple of 4)
-          T y[4];
+          __align__(16) T y[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) put(y + k, x[k] * inv);
           if (p.out_vec) {
@@ -769,7 +769,8 @@ template <typename T, int DP, int kRows>
 __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams p, int ctas) {
   constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_x[kAJoinThreads * 4], s_red[kAWarps];
+  __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_red[kAWarps];
+  __shared__ __align__(16) float s_x[kAJoinThreads * 4];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x + 1, r = blockIdx.y, tid = threadIdx.x;
   const AttendInfo in = reinterpret_cast<const AttendInfo*>(p.ws)[c];

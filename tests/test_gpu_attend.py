@@ -308,6 +308,22 @@ def test_other_streams_workspaces_and_a_graph(torch):
     check(torch, big, out, lse, some_rows(8, 8, 16, 2))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("off", [1, 3])
+def test_queries_and_outputs_off_the_16_byte_boundaries(torch, dtype, off):
+    x = inputs(torch, [300, 20, 5000], 3, 8, 2, 64, dtype, 16, 13)
+    attend = S.CacheAttend(3, 3, 8, 2, 64)
+    want, lse = attend(*x)
+    room = torch.zeros(3 * 3 * (8 * 64 + 5) + off, device="cuda", dtype=x[0].dtype)
+    q = room[off:].view(3, 3, 8 * 64 + 5)[..., :512].unflatten(-1, (8, 64))
+    q.copy_(x[0])
+    room = torch.zeros_like(room)
+    out = room[off:].view(3, 3, 8 * 64 + 5)[..., :512].unflatten(-1, (8, 64))
+    _, lse2 = attend(q, *x[1:], out=out)
+    assert torch.equal(out, want) and torch.equal(lse, lse2)
+    assert (room[:off] == 0).all() and (room[off:].view(3, 3, -1)[..., 512:] == 0).all()
+
+
 def test_strided_outputs(torch):
     x = inputs(torch, [300, 20], 3, 8, 2, 64, "bfloat16", 16, 12)
     attend = S.CacheAttend(2, 3, 8, 2, 64)

@@ -179,6 +179,23 @@ def test_the_joining_kernel_waits_for_the_one_before():
     assert first and first.group().startswith("griddep")
 
 
+def test_arrays_that_vectors_read_lie_on_their_boundaries():
+    import os
+    import re
+    for name in ("kernel_attend.cuh", "kernel_cache.cuh", "kernel_constrain.cuh"):
+        with open(os.path.join(build.CSRC, name)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        arrays = set()
+        for m in re.finditer(r"reinterpret_cast<(?:const )?(?:uint2|uint4|int4|float4|longlong2)\*>\((\w+)\b", text):
+            # (the nearest declaration of that name before it, if that is an array)
+            found = re.findall(r"[;{]([^;{}]*\b(?:T|float|int|unsigned)\b\*? [^;{}()]*\b%s\b[^;]*);" % m.group(1), text[:m.start()])
+            if found and re.search(r"\b%s\[" % m.group(1), found[-1]):
+                arrays.add(m.group(1))
+                assert "__align__(16)" in found[-1], (name, found[-1].strip())
+        assert arrays == {"kernel_attend.cuh": {"x", "y", "s_x"}, "kernel_cache.cuh": {"pos"},
+                          "kernel_constrain.cuh": {"c_smem"}}[name]
+
+
 def test_rows_that_share_memory():
     """Expanded views: rows that lie over one another are read where they are, never a row's
     width apart (which would be past the tensor's end); logits' rows must not be."""
