@@ -170,6 +170,9 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
             raise ValueError("a history needs history_len")
         h, h_ld, h_width = _rows("history", history, i32, dev, B)
         h_len = _flat("history_len", history_len, i32, dev, B)
+        # (a tensor without elements has address 0, which would be a group that is absent: any
+        # other does for one that nothing is read from)
+        h = h or h_len
         if prompt_len is not None:
             p_len = _flat("prompt_len", prompt_len, i32, dev, B)
     elif history_len is not None or prompt_len is not None:
@@ -195,6 +198,9 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
             raise ValueError("a mask row must hold a bit for every token")
         if mask_rows is not None:
             m_rows = _flat("mask_rows", mask_rows, i32, dev, B * P)
+            m = m or m_rows
+        elif m_n == 0 and B * P > 0:
+            raise ValueError("a mask without mask_rows must hold a row for every position")
     elif mask_rows is not None:
         raise ValueError("mask_rows without a mask")
     st = _lib.asymspec_constrain_logits(

@@ -269,3 +269,25 @@ def test_a_history_and_drafts_that_requests_share(torch):
         S.constrain_logits(z[:1, :1].expand(4, 3, 1500), **x)
     with pytest.raises(ValueError):
         S.constrain_logits(z, **x, out=z[:1].expand(4, 3, 1500))
+
+
+def test_groups_that_are_empty_this_round(torch):
+    """A history without room for a token and a mask tensor without a row are groups like others:
+    nothing is said, no position has a grammar, and what goes past them is a data error."""
+    i32 = dict(device="cuda", dtype=torch.int32)
+    z, x = inputs(torch, 2, 3, 500, torch.float32, 40, 43, 0, None, 4)
+    x.update(history=torch.zeros(2, 0, **i32), history_len=torch.zeros(2, **i32), prompt_len=torch.zeros(2, **i32),
+             mask=torch.zeros(0, 16, **i32), mask_rows=torch.full((2, 3), -1, **i32))
+    err = torch.zeros(1, **i32)
+    y = S.constrain_logits(z, **x, error_word=err)
+    assert int(err) == 0
+    check(torch, z, x, y)
+    x["history_len"][1], x["mask_rows"][0, 2] = 1, 0
+    y = S.constrain_logits(z, **x, error_word=err)
+    assert int(err) == S.DATA_BAD_LENGTH | S.DATA_BAD_INDEX
+    check(torch, z, x, y)
+    into = z.clone()
+    S.constrain_logits(into, **x, out=into)
+    assert torch.equal(into, y)
+    with pytest.raises(ValueError):
+        S.constrain_logits(z, mask=x["mask"])
