@@ -5,7 +5,8 @@ under penalties, biases and grammar masks; block tables and slot maps of a paged
 key-value cache; the writing of new keys and values; attention over the cache.  The
 functions on tensors below extract addresses, sizes and strides, enqueue on the
 current stream and raise ``AsymSpecError`` on a status other than OK; everything is
-computed in the library's CUDA kernels.  Nothing is read back to the host.
+computed in the library's CUDA kernels.  Nothing is read back to the host.  All tensors
+of a call lie on the current device.
 """
 from __future__ import annotations
 
@@ -215,7 +216,12 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
 
 
 def _stream(dev) -> int:
-    """The handle of device `dev`'s current stream."""
+    """The handle of device `dev`'s current stream.  A launch goes to the current device, whatever the
+    stream (a device's default one has the same handle on all): that has to be `dev`."""
+    current = torch.cuda.current_device()
+    if dev != current:
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{current}: "
+                         f"call under torch.cuda.device({dev})")
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(dev) if raw else torch.cuda.current_stream(dev).cuda_stream
 
@@ -326,7 +332,7 @@ class CacheAttend:
         if self.nbytes == 0:
             raise ValueError("no attention of this shape")
         self.workspace = torch.empty(self.nbytes, dtype=torch.uint8,
-                                     device=torch.device(device or "cuda"))
+                                     device=torch.device("cuda" if device is None else device))
         self.device_index = self.workspace.get_device()
         self.scale = 1.0 / math.sqrt(head_dim)
 

@@ -81,3 +81,52 @@ def test_no_requests(library):
                        mask_rows=ints(0, 3))
     c = constraints(library)
     assert not (c.history or c.history_len or c.mask or c.mask_rows)
+
+
+def every_call(dev_of):
+    """Each operator once, on tensors that claim to be on cuda:`dev_of`."""
+    cache = placed(3, 16, 2, 64)
+    k, slots = placed(4, 2, 64), placed(4, dtype=torch.int64)
+    attend = S.CacheAttend.__new__(S.CacheAttend)
+    attend.B_max, attend.Q_max, attend.heads, attend.kv_heads, attend.head_dim = 2, 3, 4, 2, 64
+    attend.nbytes, attend.workspace, attend.device_index, attend.scale = 256, placed(64), dev_of, 1.0
+    return {
+        "asymspec_constrain_logits": lambda: S.constrain_logits(placed(2, 3, 64)),
+        "asymspec_cache_plan": lambda: S.cache_plan(ints(2), ints(2, 3), ints(2), ints(5), ints(1), block_size=16,
+                                                    grow=3),
+        "asymspec_cache_write": lambda: S.cache_write(k, k, cache, cache, slots),
+        "asymspec_cache_attend": lambda: attend(placed(2, 3, 4, 64), cache, cache, ints(2, 3), ints(2)),
+    }
+
+
+@pytest.mark.parametrize("where", [0, 1])
+@pytest.mark.parametrize("name", [n for n in A.EXPORTED if n in (
+    "asymspec_constrain_logits", "asymspec_cache_plan", "asymspec_cache_write", "asymspec_cache_attend")])
+def test_tensors_on_another_device_than_the_current_one(library, monkeypatch, name, where):
+    """A launch goes to the current device: on tensors of another one it is refused, and goes to
+    their device's stream where that is the current one."""
+    monkeypatch.setattr(Placed, "place", where)
+    call = every_call(where)[name]
+    monkeypatch.setattr(S.torch.cuda, "current_device", lambda: 1 - where)
+    with pytest.raises(ValueError, match="cuda:%d" % where):
+        call()
+    assert not library.calls
+    monkeypatch.setattr(S.torch.cuda, "current_device", lambda: where)
+    call()
+    (got, args), = library.calls
+    assert got == name and args[-1] == 0x5000 + where
+
+
+def test_a_workspace_on_device_0_that_is_not_the_current_one(library, monkeypatch):
+    asked = []
+    library.asymspec_cache_attend_workspace_bytes = lambda *a: 256
+
+    def empty(n, dtype, device):
+        asked.append(torch.device(device))
+        return placed(n, dtype=dtype)
+
+    monkeypatch.setattr(S.torch, "empty", empty)
+    for device in (0, "cuda:0", torch.device("cuda", 0), 1, None):
+        S.CacheAttend(2, 3, 4, 2, 64, device=device)
+    # ("cuda" alone is the current device)
+    assert [d.index for d in asked] == [0, 0, 0, 1, None]
