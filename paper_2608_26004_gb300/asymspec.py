@@ -321,7 +321,12 @@ def _ptr(t):
 def _stream(torch, dev) -> int:
     """The handle of the current stream of a tensor's device.  The raw-handle
     query costs 0.1 us where building torch.cuda.current_stream's object takes
-    2.3 us of a 16 us call (B=1, K=4, V=32000)."""
+    2.3 us of a 16 us call (B=1, K=4, V=32000).  A launch goes to the current
+    device, whatever the stream: that has to be the tensors'."""
+    current = torch.cuda.current_device()
+    if dev.index != current:
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{current}: "
+                         f"call under torch.cuda.device({dev.index})")
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(dev.index) if raw else torch.cuda.current_stream(dev).cuda_stream
 
@@ -352,7 +357,7 @@ class FuseVerify:
         self.V_ws = V
         self.nbytes = workspace_bytes(self.B_max, self.K, V)
         self.workspace = torch.zeros(self.nbytes, dtype=torch.uint8,
-                                     device=torch.device(self.device or "cuda"))
+                                     device=torch.device("cuda" if self.device is None else self.device))
 
     def __call__(self, logits_full, logits_comp, logits_ver, draft_tokens, draft_probs=None,
                  uniforms=None, *, gamma=0.5, beta=1.0, lam=0.1, mode=MODE_GREEDY,

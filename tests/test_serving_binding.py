@@ -130,3 +130,50 @@ def test_a_workspace_on_device_0_that_is_not_the_current_one(library, monkeypatc
         S.CacheAttend(2, 3, 4, 2, 64, device=device)
     # ("cuda" alone is the current device)
     assert [d.index for d in asked] == [0, 0, 0, 1, None]
+
+
+class StepTensor(Placed):
+    is_cuda = True
+
+    @property
+    def device(self):
+        return torch.device("cuda", Placed.place)
+
+
+@pytest.mark.parametrize("where", [0, 1])
+@pytest.mark.parametrize("name", ["asymspec_fuse_verify_ex", "asymspec_draft_sample"])
+def test_the_step_and_the_draw_on_another_device_than_the_current_one(library, monkeypatch, name, where):
+    monkeypatch.setattr(A, "_lib", library)
+    monkeypatch.setattr(Placed, "place", where)
+    z = torch.zeros(2, 3, 64).as_subclass(StepTensor)
+    out = {n: torch.zeros(2, dtype=torch.int32) for n in ("accept_len", "next_token", "error_word")}
+    step = A.FuseVerify(2, 2)
+    step.workspace, step.V_ws, step.nbytes = torch.zeros(64), 64, 256
+
+    def call():
+        if name == "asymspec_draft_sample":
+            A.draft_tokens(z, out=(out["accept_len"], out["next_token"]))
+        else:
+            step(z, z, z, ints(2, 2), out=out)
+
+    def launched():
+        return [c for c in library.calls if c[0] == name]
+
+    monkeypatch.setattr(S.torch.cuda, "current_device", lambda: 1 - where)
+    with pytest.raises(ValueError, match="cuda:%d" % where):
+        call()
+    assert not launched()
+    monkeypatch.setattr(S.torch.cuda, "current_device", lambda: where)
+    call()
+    (_, args), = launched()
+    assert args[-1] == 0x5000 + where
+
+
+def test_the_steps_workspace_on_device_0_that_is_not_the_current_one(library, monkeypatch):
+    asked = []
+    monkeypatch.setattr(A, "_lib", library)
+    monkeypatch.setattr(A, "workspace_bytes", lambda *a: 256)
+    monkeypatch.setattr(S.torch, "zeros", lambda n, dtype, device: asked.append(torch.device(device)))
+    for device in (0, "cuda:0", 1, None):
+        A.FuseVerify(2, 2, device=device, V_max=64)
+    assert [d.index for d in asked] == [0, 0, 1, None]
