@@ -191,7 +191,8 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
  * them (the rest of a block, a later token's).  Sums, maxima and the accumulated values
  * are fp32; out is rounded once.
  *   q [B, Q, heads, head_dim]: strides q_strides (request, query, head), out likewise; the
- *       cache's dtype, element-aligned
+ *       cache's dtype, element-aligned.  out must not overlap q (whose queries are read
+ *       until the call ends) nor anything else that the call reads
  *   block_tables [B, table_width] int32, rows table_ld apart; lens [B] int32
  *   out_lse: [B, Q, heads] fp32 contiguous, or NULL
  *   workspace: asymspec_cache_attend_workspace_bytes(...) bytes, 256-byte aligned; it needs
@@ -204,7 +205,8 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
  * evenly, whatever their lengths, and the parts joined by a second launch; results do
  * not depend on the order in which the parts finish.
  * ASYMSPEC_ERR_INVALID_ARG: a null pointer, a size < 1 (B, Q < 0), heads not a multiple of
- * kv_heads, a scale that is not finite, window < 0, a negative stride.
+ * kv_heads, table_ld < table_width, a scale that is not finite, window < 0, a negative stride,
+ * out = q.
  * ASYMSPEC_ERR_UNSUPPORTED: dtype, head_dim > ASYMSPEC_CACHE_MAX_D.  ASYMSPEC_ERR_MISALIGNED:
  * an unaligned pointer; keys, values, their strides and head_dim must lie on 16-byte
  * boundaries.  ASYMSPEC_ERR_WORKSPACE.  ASYMSPEC_ERR_TOO_LARGE: B >

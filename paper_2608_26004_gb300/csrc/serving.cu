@@ -332,6 +332,7 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
   const size_t need =
       asymspec_cache_attend_workspace_bytes(B, Q, heads, cache->kv_heads, cache->head_dim);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return ASYMSPEC_ERR_WORKSPACE;
+  if (q == out) return ASYMSPEC_ERR_INVALID_ARG;  // (one CTA of a request may read what another has written)
   AttendParams p = {};
   p.keys = cache->keys;
   p.values = cache->values;

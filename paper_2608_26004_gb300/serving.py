@@ -319,7 +319,8 @@ class CacheAttend:
     ``__call__`` takes q [B, Q, heads, head_dim] (any strides, heads contiguous), a paged
     cache as cache_write does, tables [B, width] int32 and lens [B] int32 (the cached
     tokens of each request, the Q new ones included) and returns (out [B, Q, heads,
-    head_dim], lse [B, Q, heads] float32), enqueued on the current stream.  Calls that
+    head_dim], lse [B, Q, heads] float32), enqueued on the current stream; ``out`` may pass a
+    tensor to fill, which must not overlap q or the cache.  Calls that
     share the workspace must follow one another: on one stream, or ordered by events.
     """
 

@@ -351,3 +351,12 @@ def test_refusals_of_the_binding(torch):
     with pytest.raises(A.AsymSpecError):               # rows off the 16-byte boundaries
         room = torch.zeros(keys.numel() + 1, device="cuda", dtype=torch.bfloat16)
         attend(q, room[1:].view(keys.shape), values, tables, lens)
+
+
+def test_attention_in_place_is_refused(torch):
+    q, keys, values, tables, lens = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
+    attend = S.CacheAttend(2, 2, 4, 2, 64)
+    before = q.clone()
+    with pytest.raises(A.AsymSpecError):
+        attend(q, keys, values, tables, lens, out=q)
+    assert torch.equal(q, before)

@@ -146,6 +146,13 @@ def test_cache_attend_validation_codes(lib):
     assert attend(lib, Q=0, q=0) == A.OK
 
 
+def test_cache_attend_refuses_its_queries_as_its_output(lib):
+    """CTAs that share a request read its queries while others write: not in place."""
+    assert attend(lib, q=FAKE, out=FAKE) == A.ERR_INVALID_ARG
+    assert attend(lib, q=FAKE, out=FAKE, head_dim=36) == A.ERR_MISALIGNED    # (after all other checks)
+    assert attend(lib, q=FAKE, out=FAKE, nbytes=0) == A.ERR_WORKSPACE
+
+
 def test_cache_attend_workspace_of_no_shape(lib):
     n = S.cache_attend_workspace_bytes
     for shape in ((0, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 3, 2, 64), (1, 1, 4, 2, 257),
