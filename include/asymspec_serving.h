@@ -205,8 +205,8 @@ int asymspec_cache_write(const asymspec_cache* cache, const void* k, const void*
  * evenly, whatever their lengths, and the parts joined by a second launch; results do
  * not depend on the order in which the parts finish.
  * ASYMSPEC_ERR_INVALID_ARG: a null pointer, a size < 1 (B, Q < 0), heads not a multiple of
- * kv_heads, table_ld < table_width, a scale that is not finite, window < 0, a negative stride,
- * out = q.
+ * kv_heads, table_ld < table_width, a scale that is not finite, window < 0, a negative stride, a
+ * stride of 0 along an axis of out that is longer than 1, out = q.
  * ASYMSPEC_ERR_UNSUPPORTED: dtype, head_dim > ASYMSPEC_CACHE_MAX_D.  ASYMSPEC_ERR_MISALIGNED:
  * an unaligned pointer; keys, values, their strides and head_dim must lie on 16-byte
  * boundaries.  ASYMSPEC_ERR_WORKSPACE.  ASYMSPEC_ERR_TOO_LARGE: B >

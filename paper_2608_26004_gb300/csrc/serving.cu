@@ -316,6 +316,9 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
     return ASYMSPEC_ERR_INVALID_ARG;
   for (int i = 0; i < 3; ++i)
     if (q_strides[i] < 0 || out_strides[i] < 0) return ASYMSPEC_ERR_INVALID_ARG;
+  const int extents[3] = {B, Q, heads};
+  for (int i = 0; i < 3; ++i)
+    if (out_strides[i] == 0 && extents[i] > 1) return ASYMSPEC_ERR_INVALID_ARG;
   if (B > ASYMSPEC_CACHE_MAX_B || static_cast<int64_t>(Q) * heads > (1 << 20) ||
       static_cast<int64_t>(table_width) * cache->block_size > (1 << 30))
     return ASYMSPEC_ERR_TOO_LARGE;

@@ -360,3 +360,14 @@ def test_attention_in_place_is_refused(torch):
     with pytest.raises(A.AsymSpecError):
         attend(q, keys, values, tables, lens, out=q)
     assert torch.equal(q, before)
+
+
+def test_an_expanded_output_is_refused(torch):
+    x = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
+    attend = S.CacheAttend(2, 2, 4, 2, 64)
+    for shape in ((1, 2, 4, 64), (2, 1, 4, 64), (2, 2, 1, 64)):
+        with pytest.raises(A.AsymSpecError):
+            attend(*x, out=torch.zeros(shape, device="cuda", dtype=torch.bfloat16).expand(2, 2, 4, 64))
+    one = inputs(torch, [100], 1, 4, 2, 64, "bfloat16", 16, 5)
+    out = torch.zeros(1, 4, 64, device="cuda", dtype=torch.bfloat16)[None].expand(1, 1, 4, 64)
+    assert torch.equal(attend(*one, out=out)[0], attend(*one)[0])

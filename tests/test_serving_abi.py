@@ -256,3 +256,16 @@ def test_windows_of_any_size_stay_in_32_bits(tmp_path):
     import os
     with open(os.path.join(build.CSRC, "serving.cu")) as f:
         assert f.read().count("p.window = attend_window(window, table_width, cache->block_size);") == 1
+
+
+def test_cache_attend_refuses_outputs_that_lie_over_one_another(lib):
+    def call(os, B=2, Q=3, heads=4):
+        x = cache()
+        return lib.asymspec_cache_attend(ctypes.byref(x), FAKE, S._L3(384, 128, 32), B, Q, heads, FAKE, 4, 4, FAKE,
+                                         1.0, 0, FAKE, S._L3(*os), 0, 0, 0, None, None)
+    for os in ((0, 128, 32), (384, 0, 32), (384, 128, 0)):
+        assert call(os) == A.ERR_INVALID_ARG, os
+    # an axis of one has any stride: what follows is the next check, of the workspace
+    assert call((384, 128, 32)) == A.ERR_WORKSPACE
+    assert call((0, 128, 32), B=1) == A.ERR_WORKSPACE
+    assert call((384, 0, 32), Q=1) == A.ERR_WORKSPACE
