@@ -109,6 +109,12 @@ def _dtype(x) -> int:
     return dtype
 
 
+def _int(n) -> int:
+    """n for a C int, which would take the low bits of a larger number: past its range the range's
+    largest, below zero -1."""
+    return n if -1 <= n <= 0x7FFFFFFF else 0x7FFFFFFF if n > 0 else -1
+
+
 def _flat(name, x, dtype, dev, n):
     """The address of `x`: contiguous, n entries of this type, on device `dev`."""
     if x.dtype is not dtype or x.get_device() != dev or x.numel() != n or not x.is_contiguous():
@@ -269,7 +275,7 @@ def cache_plan(lens, tables, held, free_list, free_count, *, block_size, accepte
               _flat("positions", r["positions"], i32, dev, capacity))
     st = _lib.asymspec_cache_plan(
         _flat("lens", lens, i32, dev, B), 0 if accepted is None else _flat("accepted", accepted, i32, dev, B),
-        each, all_, B, block_size, blocks, t, t_ld, width, _flat("held", held, i32, dev, B),
+        each, _int(all_), B, _int(block_size), blocks, t, t_ld, width, _flat("held", held, i32, dev, B),
         _flat("free_list", free_list, i32, dev, blocks), _flat("free_count", free_count, i32, dev, 1), *at,
         capacity, 0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
@@ -365,7 +371,7 @@ class CacheAttend:
         t, t_ld, width = _rows("tables", tables, torch.int32, dev, B)
         st = _lib.asymspec_cache_attend(
             view, q.data_ptr(), _STRIDES3.pack(q0, q1, q2), B, Q, heads, t, t_ld, width,
-            _flat("lens", lens, torch.int32, dev, B), self.scale if scale is None else scale, window,
+            _flat("lens", lens, torch.int32, dev, B), self.scale if scale is None else scale, _int(window),
             out.data_ptr(), _STRIDES3.pack(o0, o1, o2), l, self.workspace.data_ptr(), self.nbytes,
             0 if error_word is None else _error_word(error_word, dev), _stream(dev))
         if st != OK:

@@ -177,3 +177,21 @@ def test_the_steps_workspace_on_device_0_that_is_not_the_current_one(library, mo
     for device in (0, "cuda:0", 1, None):
         A.FuseVerify(2, 2, device=device, V_max=64)
     assert [d.index for d in asked] == [0, 0, 1, None]
+
+
+TOP = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("given,passed", [(0, 0), (7, 7), (TOP, TOP), (2 ** 31, TOP), (2 ** 32 + 5, TOP),
+                                          (2 ** 63 - 1, TOP), (-1, -1), (-2 ** 32, -1), (-2 ** 31 - 5, -1)])
+def test_numbers_past_32_bits_are_not_cut(library, given, passed):
+    """C integers take the low bits of a larger number: a window of 2^32 + 5 is not one of 5."""
+    cache = placed(3, 16, 2, 64)
+    attend = S.CacheAttend.__new__(S.CacheAttend)
+    attend.B_max, attend.Q_max, attend.heads, attend.kv_heads, attend.head_dim = 2, 3, 4, 2, 64
+    attend.nbytes, attend.workspace, attend.device_index, attend.scale = 256, placed(64), 0, 1.0
+    attend(placed(2, 3, 4, 64), cache, cache, ints(2, 3), ints(2), window=given)
+    assert library.calls[0][1][11] == passed
+    S.cache_plan(ints(2), ints(2, 3), ints(2), ints(5), ints(1), block_size=given, grow=given, capacity=4)
+    args = library.calls[1][1]
+    assert args[3] == passed and args[5] == passed
