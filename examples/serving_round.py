@@ -83,8 +83,9 @@ class Context:
         self.plan(lengths, capacity=prompts.numel())
         _, _, k, v = self.project(prompts)
         S.cache_write(k, v, self.keys, self.values, self.state["slots"], error_word=self.error)
-        # what was just written stays: the next plan keeps it
-        self.state = dict(self.state, start=self.state["len"])
+        # the next plan keeps what was just written, but for the last token: that is the first
+        # round's first, which writes it again, at its place
+        self.state = dict(self.state, start=(self.state["len"] - 1).clamp(min=0))
 
     def logits(self, tokens, first=0):
         """[B, n, V] after each of the round's tokens first .. first + n - 1."""

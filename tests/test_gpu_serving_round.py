@@ -80,3 +80,25 @@ def test_attention_of_the_loop_equals_attention_without_a_cache(example):
             o = torch.einsum("hn,nhd->hd", s.softmax(-1), vv).reshape(-1).bfloat16()
             want = m.logits(x[i], o).float()
             assert (got[b, i] - want).abs().max() <= 0.05 * want.abs().max()
+
+
+@pytest.mark.parametrize("B,K,rounds", [(5, 3, 6), (1, 2, 3)])
+def test_every_token_is_cached_once_at_its_place(example, B, K, rounds):
+    """The prompt's last token is the first round's first: it has one place, like all others."""
+    import torch
+    loop = example.Loop(B=B, K=K, V=1024, prompt=(30, 70), rounds=rounds, seed=B)
+    prompt = [c.state["len"].tolist() for c in loop.contexts]
+    for _ in range(rounds):
+        loop.round()
+    for c, lengths in zip(loop.contexts, prompt):
+        cached = (c.state["start"] + loop.accepted + 1).tolist()
+        for b in range(B):
+            begin, end = int(loop.prompt_len[b]), int(loop.history_len[b])
+            tokens = loop.history[b, begin - lengths[b]:end - 1]  # (the last one waits for the next round)
+            assert cached[b] == tokens.numel() == lengths[b] + (end - begin) - 1
+            at = torch.arange(cached[b], device="cuda")
+            page = c.tables[b].long()[at // c.block_size]
+            _, _, k, v = c.project(tokens)
+            close = dict(rtol=0.02, atol=0.02)
+            assert torch.allclose(c.keys[page, at % c.block_size].float(), k.float(), **close)
+            assert torch.allclose(c.values[page, at % c.block_size].float(), v.float(), **close)
