@@ -93,7 +93,9 @@ class Context:
         x, q, k, v = self.project(tokens)
         slots = self.state["slots"].view(B, -1)[:, first:first + n].contiguous().view(-1)
         S.cache_write(k.flatten(0, 1), v.flatten(0, 1), self.keys, self.values, slots, error_word=self.error)
-        seen = self.state["start"] + (first + n)
+        # (no more than its blocks hold: where the pool had none for a request, the table's entries
+        # from there on are another's)
+        seen = torch.minimum(self.state["start"] + (first + n), self.state["len"])
         o, _ = self.attend(q, self.keys, self.values, self.tables, seen, error_word=self.error)
         return self.model.logits(x, o.flatten(2))
 
@@ -149,6 +151,7 @@ class Loop:
         B, K = self.B, self.K
         for c in self.contexts:
             c.plan(K + 1, self.accepted)
+        served = torch.stack([c.state["len"] > c.state["start"] for c in self.contexts]).all(0)
         # drafting: each token's constraints count the drafts before it as said
         said = self.history.clone()
         rows, drafts, token = [], [], self.last
@@ -171,7 +174,9 @@ class Loop:
         comp = self.constrained(self.drafter_comp.logits(inputs), drafts)
         ver = self.constrained(self.verifier.logits(inputs), drafts)
         r = self.step(full, comp, ver, drafts)
-        self.accepted, next_token = r["accept_len"], r["next_token"]
+        # a request that a context had no blocks for sits the round out: nothing of it is kept
+        self.accepted = torch.where(served, r["accept_len"], -1)
+        next_token = torch.where(served, r["next_token"], self.last)
         # the accepted drafts and the next token join the history
         j = torch.arange(K + 1, device="cuda")
         new = torch.where(j < self.accepted[:, None], torch.cat([drafts, drafts[:, :1]], 1), next_token[:, None])

@@ -123,7 +123,8 @@ int asymspec_constrain_logits(const asymspec_constraints* c, const void* logits,
  * long as they last: a request that needs blocks is served if it and all before it fit, and
  * gets none otherwise (ASYMSPEC_DATA_NO_BLOCKS; out_len tells which).  Outputs:
  *
- *   out_start [B] = keep;  out_len [B] = keep + grow, or keep where not served
+ *   out_start [B] = keep;  out_len [B] = keep + grow, or keep where not served: what may be
+ *       attended over, at most (the table's entries past it may be another request's blocks)
  *   out_held [B], *out_free_count: the state for the next call
  *   block_tables, free_list: updated in place; table entries from out_held[b] on are left
  *       as they are

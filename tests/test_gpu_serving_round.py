@@ -102,3 +102,43 @@ def test_every_token_is_cached_once_at_its_place(example, B, K, rounds):
             close = dict(rtol=0.02, atol=0.02)
             assert torch.allclose(c.keys[page, at % c.block_size].float(), k.float(), **close)
             assert torch.allclose(c.values[page, at % c.block_size].float(), v.float(), **close)
+
+
+def test_requests_that_the_pool_has_no_blocks_for_sit_out(example):
+    """The verifier's pool runs out: what it cannot serve attends over none but its own tokens,
+    commits nothing and stays as it is; the others go on."""
+    import torch
+    from paper_2608_26004_gb300 import serving as S
+    B, K, rounds = 6, 4, 8
+    loop = example.Loop(B=B, K=K, V=1024, prompt=(30, 70), rounds=rounds, seed=2)
+    prompt = [c.state["len"].tolist() for c in loop.contexts]
+    loop.verifier.state["free_count"].fill_(4)
+    calls = []
+    for c in loop.contexts:
+        def recorded(q, keys, values, tables, lens, c=c, call=c.attend, **more):
+            calls.append((lens.clone(), c.state["len"]))
+            return call(q, keys, values, tables, lens, **more)
+        c.attend = recorded
+    sat_out = 0
+    for _ in range(rounds):
+        before = loop.history_len.clone()
+        assert int(loop.round()) == 0
+        v = loop.verifier.state
+        unserved = v["len"] == v["start"]
+        sat_out += int(unserved.sum())
+        assert torch.equal(loop.history_len == before, unserved)
+    assert 0 < sat_out < B * rounds and int(unserved.sum()) < B
+    assert int(loop.verifier.error) == S.DATA_NO_BLOCKS
+    assert [int(c.error) for c in loop.contexts[:2]] == [0, 0]
+    for lens, room in calls:
+        assert (lens <= room).all()
+    for c, lengths in zip(loop.contexts, prompt):
+        cached = (c.state["start"] + loop.accepted + 1).tolist()
+        for b in range(B):
+            begin, end = int(loop.prompt_len[b]), int(loop.history_len[b])
+            tokens = loop.history[b, begin - lengths[b]:end - 1]
+            assert cached[b] == tokens.numel()
+            at = torch.arange(cached[b], device="cuda")
+            page = c.tables[b].long()[at // c.block_size]
+            _, _, k, _ = c.project(tokens)
+            assert torch.allclose(c.keys[page, at % c.block_size].float(), k.float(), rtol=0.02, atol=0.02)
