@@ -49,10 +49,13 @@ class Model:
 
 
 class Context:
-    """A model on one context of every request: its paged cache and the state of its plan."""
+    """A model on one context of every request, of `tokens` tokens at most: its paged cache and the state
+    of its plan."""
 
-    def __init__(self, model, B, most_new, blocks, block_size=16, width=64):
+    def __init__(self, model, B, most_new, tokens, block_size=16):
         i32 = dict(dtype=torch.int32, device="cuda")
+        width = -(-tokens // block_size)
+        blocks = B * width
         shape = (blocks, block_size, model.kv_heads, model.dim)
         self.model, self.B, self.block_size = model, B, block_size
         self.keys = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
@@ -108,10 +111,10 @@ class Loop:
         drafter = Model(V, gen)
         verifier = Model(V, gen, near=drafter)
         full, short = prompt[1], prompt[0]  # tokens of a full context, and of a compressed one
-        blocks = B * (-(-(full + (K + 1) * (rounds + 1)) // 16) + 1)
-        self.drafter_full = Context(drafter, B, 1, blocks)
-        self.drafter_comp = Context(drafter, B, K + 1, blocks)
-        self.verifier = Context(verifier, B, K + 1, blocks)
+        tokens = full + (K + 1) * (rounds + 1)
+        self.drafter_full = Context(drafter, B, 1, tokens)
+        self.drafter_comp = Context(drafter, B, K + 1, tokens)
+        self.verifier = Context(verifier, B, K + 1, tokens)
         self.contexts = (self.drafter_full, self.drafter_comp, self.verifier)
         lengths = torch.randint(short // 2, short + 1, (B,), generator=gen, **i32)
         prompts = torch.randint(0, V, (B, full), generator=gen, **i32)
@@ -138,14 +141,24 @@ class Loop:
         # nobody says token 0
         self.bias = (torch.arange(B + 1, **i32), torch.zeros(B, **i32), torch.full((B,), -1e4, device="cuda"))
         self.step = A.FuseVerify(B, K)
+        self.error = torch.zeros(1, **i32)  # of the constraints
         self.accepted = None
+
+    def raise_errors(self, step):
+        """Raises what the error words of the loop (and `step`, of its steps) hold, if anything."""
+        words = dict(step=step, constraints=self.error, drafter_full=self.drafter_full.error,
+                     drafter_comp=self.drafter_comp.error, verifier=self.verifier.error)
+        bad = {name: hex(int(w)) for name, w in words.items() if int(w)}
+        if bad:
+            raise RuntimeError(f"bad data: {bad}")
 
     def constrained(self, logits, drafts=None, first=0):
         n = logits.shape[1]
         return S.constrain_logits(
             logits, history=self.history, history_len=self.history_len, prompt_len=self.prompt_len,
             drafts=drafts, bias=self.bias, mask=self.mask,
-            mask_rows=self.mask_rows[:, first:first + n].contiguous(), mask_value=-1e4, **self.penalties)
+            mask_rows=self.mask_rows[:, first:first + n].contiguous(), mask_value=-1e4,
+            error_word=self.error, **self.penalties)
 
     def round(self):
         B, K = self.B, self.K
@@ -163,7 +176,7 @@ class Loop:
             row = S.constrain_logits(raw, history=said, history_len=self.history_len + i,
                                      prompt_len=self.prompt_len, bias=self.bias, mask=self.mask,
                                      mask_rows=self.mask_rows[:, i:i + 1].contiguous(), mask_value=-1e4,
-                                     **self.penalties)
+                                     error_word=self.error, **self.penalties)
             rows.append(row)
             if i < K:
                 token, _ = A.draft_tokens(row[:, 0].contiguous())
@@ -195,8 +208,10 @@ def main():
     ap.add_argument("--rounds", type=int, default=16)
     a = ap.parse_args()
     loop = Loop(B=a.requests, K=a.drafts, rounds=a.rounds)
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
     for _ in range(a.rounds):
-        loop.round()
+        step |= loop.round()
+    loop.raise_errors(step)
     said = loop.history_len - loop.prompt_len
     print("tokens committed per request:", said.tolist(), "in", a.rounds, "rounds")
     print("request 0:", loop.history[0, int(loop.prompt_len[0]):int(loop.history_len[0])].tolist())

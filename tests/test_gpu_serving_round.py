@@ -142,3 +142,37 @@ def test_requests_that_the_pool_has_no_blocks_for_sit_out(example):
             page = c.tables[b].long()[at // c.block_size]
             _, _, k, _ = c.project(tokens)
             assert torch.allclose(c.keys[page, at % c.block_size].float(), k.float(), rtol=0.02, atol=0.02)
+
+
+@pytest.mark.parametrize("K,rounds", [(4, 16), (7, 200)])
+def test_tables_hold_all_rounds(example, K, rounds):
+    loop = example.Loop(B=2, K=K, V=1024, rounds=rounds)
+    most = loop.history.shape[1] + K + 1  # everything that may be said, and the last round's drafts
+    for c in loop.contexts:
+        assert c.tables.shape[1] * c.block_size >= most
+        assert c.keys.shape[0] >= 2 * -(-most // c.block_size)
+
+
+def test_the_program_says_when_its_data_was_bad(example, monkeypatch, capsys):
+    monkeypatch.setattr("sys.argv", ["serving_round.py", "--requests", "2", "--rounds", "3"])
+    example.main()
+    assert "tokens committed per request" in capsys.readouterr().out
+
+    class Starved(example.Loop):
+        def __init__(self, **kw):
+            super().__init__(**kw)
+            self.verifier.state["free_count"].zero_()
+
+    monkeypatch.setattr(example, "Loop", Starved)
+    monkeypatch.setattr("sys.argv", ["serving_round.py", "--requests", "2", "--rounds", "12"])
+    with pytest.raises(RuntimeError, match="verifier.*0x200"):
+        example.main()
+
+    class Unseen(example.Loop):
+        def __init__(self, **kw):
+            super().__init__(**kw)
+            self.history[0, 0] = -1  # (no token: what the constraints read)
+
+    monkeypatch.setattr(example, "Loop", Unseen)
+    with pytest.raises(RuntimeError, match="constraints.*0x"):
+        example.main()
