@@ -44,8 +44,8 @@ extern "C" {
  *
  * computed in fp32 and rounded once, to `dtype`.  A finite logit stays finite (a result
  * beyond the type's range becomes its largest or lowest value), so that a logit masked
- * before at the lowest value stays there; a NaN or an infinity stays what it is unless
- * the mask replaces it.  An entry that nothing changes is copied bit for bit.  The same
+ * before at the lowest value stays there; a NaN or an infinity stays what it is, and a NaN
+ * bias makes a NaN, unless the mask replaces it.  An entry that nothing changes is copied bit for bit.  The same
  * constraints belong on the step's three logit tensors and on the drafter's rows.
  * Every group of members may be absent (NULL).
  */

@@ -272,7 +272,7 @@ struct Touched {
     if (count != 0 || (w & kCPrompt)) f = f > 0.f ? f / r.rep : f * r.rep;
     if (count != 0) f = (f - r.freq * static_cast<float>(count)) - r.pres;
     if (w & kCBias) f += bias;
-    return fabsf(z) <= FLT_MAX ? fminf(fmaxf(f, -r.top), r.top) : f;
+    return fabsf(z) <= FLT_MAX && bias == bias ? fminf(fmaxf(f, -r.top), r.top) : f;  // (fmaxf drops a NaN)
   }
   // past row k
   __device__ __forceinline__ void past(const CParams& p, const Slice& s, int k) {

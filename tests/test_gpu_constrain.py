@@ -291,3 +291,23 @@ def test_groups_that_are_empty_this_round(torch):
     assert torch.equal(into, y)
     with pytest.raises(ValueError):
         S.constrain_logits(z, mask=x["mask"])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_biases_that_are_not_numbers(torch, dtype, in_place):
+    """A NaN among the biases makes that entry NaN (it is neither kept nor taken for the lowest
+    value); an infinite one stops at the type's range, also for a token that is penalised."""
+    i32 = dict(device="cuda", dtype=torch.int32)
+    z = torch.randn(1, 3, 3000, device="cuda").to(getattr(torch, dtype))
+    x = dict(history=torch.tensor([[5, 2900, 7]], **i32), history_len=torch.tensor([3], **i32),
+             repetition=torch.tensor([1.5], device="cuda"), presence=torch.tensor([0.5], device="cuda"),
+             bias=(torch.tensor([0, 5], **i32), torch.tensor([5, 9, 7, 2999, 11], **i32),
+                   torch.tensor([math.nan, math.nan, math.inf, -math.inf, 2.0], device="cuda")))
+    z0 = z.clone()
+    y = S.constrain_logits(z, out=z if in_place else None, **x)
+    check(torch, z0, x, y)
+    nan = y.isnan().nonzero()[:, 2].tolist()
+    assert nan == [5, 9] * 3
+    top = torch.finfo(z.dtype).max
+    assert (y[..., 7] == top).all() and (y[..., 2999] == -top).all()
