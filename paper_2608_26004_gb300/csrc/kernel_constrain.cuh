@@ -28,6 +28,7 @@ constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
 constexpr int kCOrdered = 64;     // requests that are taken in the order of their lengths at most
 constexpr int kCStepBits = 8;      // in steps of so many tokens (a power of two)
 constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
+constexpr int kCPart = 2 * kCBiases;  // tokens of a part of a slice with more of them: divides every W
 // A token's word: in the prompt, among the drafts, biased, and how often in the output.
 constexpr unsigned kCPrompt = 1u << 31, kCDraft = 1u << 30, kCBias = 1u << 29, kCCount = kCBias - 1;
 
@@ -90,7 +91,7 @@ __device__ __forceinline__ int entries_before(const T* p) {
 struct Slice {
   unsigned* words;
   uint16_t* list;
-  int2* bias;  // [kCBiases]: entry of the slice, entry of the biases
+  int2* bias;  // [kCBiases]: entry of the slice, entry of the biases (more: last_biases')
   int *listed, *biases;
   int b, v0, n, W;
 };
@@ -231,6 +232,24 @@ __device__ __forceinline__ void list_slice(const Slice& s) {
   }
 }
 
+// Where a slice has more than kCBiases bias entries, its tokens take theirs in parts of kCPart: the
+// last entry of each token of a part, plus one (0: none), by a sweep of the request's list.  (A
+// search of the list for each token would take the square of the biases: 64 requests of 16,000 each
+// 3096 us, 337 so; of all 128,256 180 ms.)  Begins and ends at a barrier.
+__device__ __forceinline__ void last_biases(const asymspec_constraints& c, int b, int first, int n, int* last) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kCPart; i += kCThreads) last[i] = 0;
+  __syncthreads();
+  const int a = min(max(c.bias_offsets[b], 0), c.bias_count);
+  const int e = min(max(c.bias_offsets[b + 1], a), c.bias_count);
+#pragma unroll 4
+  for (int j = a + threadIdx.x; j < e; j += kCThreads) {
+    const unsigned i = static_cast<unsigned>(c.bias_tokens[j]) - static_cast<unsigned>(first);
+    if (i < static_cast<unsigned>(n)) atomicMax(last + i, j + 1);
+  }
+  __syncthreads();
+}
+
 struct Penalties {
   float rep, freq, pres, top;
   __device__ __forceinline__ Penalties(const Request& r, float top_, unsigned& err)
@@ -257,10 +276,7 @@ struct Touched {
         for (int j = 0; j < *s.biases; ++j)
           if (s.bias[j].x == i) last = max(last, s.bias[j].y);
       } else {
-        const int a = min(max(c.bias_offsets[s.b], 0), c.bias_count);
-        const int e = min(max(c.bias_offsets[s.b + 1], a), c.bias_count);
-        for (int j = a; j < e; ++j)
-          if (c.bias_tokens[j] == v) last = j;
+        last = reinterpret_cast<const int*>(s.bias)[i % kCPart] - 1;
       }
       bias = c.bias_values[last];
     }
@@ -402,7 +418,7 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
     const int listed = s_listed;
     // an entry's rows by one thread, or, where entries are fewer than threads, by one each
     const int each = listed * rows <= 2 * kCThreads ? 1 : rows;
-    for (int q = tid; q < listed * (rows / each); q += kCThreads) {
+    auto touch = [&](int q) {
       const int i = slice.list[q % listed], first = q / listed;
       Touched u(p, slice, i, k0 + first_row + first);
 #pragma unroll 4
@@ -410,6 +426,16 @@ __global__ void __launch_bounds__(kCThreads, 4) constrain_rows(const CParams p) 
         T* cell = reinterpret_cast<T*>(tile + k * pitch + misplaced(xt + k * p.ld)) + i;
         *cell = from_f32(u.value(penalties, to_f32(*cell)), T());
         u.past(p, slice, k0 + first_row + k);
+      }
+    };
+    const int touches = listed * (rows / each);
+    if (s_biases <= kCBiases) {
+      for (int q = tid; q < touches; q += kCThreads) touch(q);
+    } else {
+      for (int part = 0; part < n; part += kCPart) {
+        last_biases(c, b, v0 + part, min(kCPart, n - part), reinterpret_cast<int*>(s_bias));
+        for (int q = tid; q < touches; q += kCThreads)
+          if (slice.list[q % listed] / kCPart == part / kCPart) touch(q);
       }
     }
     if (listed > 0) __syncthreads();
@@ -491,14 +517,22 @@ __global__ void __launch_bounds__(kCThreads) constrain_in_place(const CParams p)
   const Penalties penalties(request, type_max(T()), err);
   T* x = static_cast<T*>(p.out) + (static_cast<int64_t>(b) * p.P + k0) * p.out_ld + v0;
   __syncthreads();  // the list
-  for (int q = tid; q < s_listed; q += kCThreads) {
-    const int i = slice.list[q];
+  auto touch = [&](int i) {
     Touched t(p, slice, i, k0);
 #pragma unroll 4
     for (int k = 0; k < rows; ++k) {
       T* cell = x + k * p.out_ld + i;
       *cell = from_f32(t.value(penalties, to_f32(*cell)), T());
       t.past(p, slice, k0 + k);
+    }
+  };
+  if (s_biases <= kCBiases) {
+    for (int q = tid; q < s_listed; q += kCThreads) touch(slice.list[q]);
+  } else {
+    for (int part = 0; part < n; part += kCPart) {
+      last_biases(p.c, b, v0 + part, min(kCPart, n - part), reinterpret_cast<int*>(s_bias));
+      for (int q = tid; q < s_listed; q += kCThreads)
+        if (slice.list[q] / kCPart == part / kCPart) touch(slice.list[q]);
     }
   }
   if (err && p.err) atomicOr(p.err, err);

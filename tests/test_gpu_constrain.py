@@ -311,3 +311,48 @@ def test_biases_that_are_not_numbers(torch, dtype, in_place):
     assert nan == [5, 9] * 3
     top = torch.finfo(z.dtype).max
     assert (y[..., 7] == top).all() and (y[..., 2999] == -top).all()
+
+
+@pytest.mark.parametrize("B,P,V,dtype,pad", [(2, 2, 9001, "bfloat16", 0), (1, 13, 5000, "float32", 3),
+                                             (2, 1, 20000, "float32", 0), (1, 40, 2560, "bfloat16", 0)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_biases_for_all_tokens(torch, B, P, V, dtype, pad, in_place):
+    """Biases for every token, most of them several times, beside the other constraints: the last
+    entry of each counts, in each batch of rows."""
+    i32 = dict(device="cuda", dtype=torch.int32)
+    z, x = inputs(torch, B, P, V, getattr(torch, dtype), 600, 51, pad, None if in_place else 3, 0)
+    g = torch.Generator(device="cuda").manual_seed(52)
+    tokens = torch.cat([torch.randint(-3, V + 3, (2 * V,), generator=g, **i32), torch.randperm(V, generator=g, **i32),
+                        torch.randint(0, V, (V // 3,), generator=g, **i32)])
+    m = tokens.numel()
+    x["bias"] = (torch.tensor([0, m, m + 5][:B + 1], **i32), torch.cat([tokens, tokens[-5:]]),
+                 torch.randn(m + 5, generator=g, device="cuda"))
+    z0, err = z.clone(), torch.zeros(1, **i32)
+    y = S.constrain_logits(z, out=z if in_place else None, error_word=err, **x)
+    assert int(err) == A.DATA_BAD_TOKEN
+    check(torch, z0, x, y, {(b, k) for b in range(B) for k in (0, P // 2, P - 1)})
+
+
+def test_many_biases_take_no_square_of_their_number(torch):
+    """Sixteen times the biases take at most 64 times as long (a search of the list for each token
+    takes 256 times as long)."""
+    B, V = 64, 128256
+    z = torch.randn(B, 1, V, device="cuda").bfloat16()
+    out = torch.empty_like(z)
+
+    def us(m):
+        off = torch.arange(0, B * m + 1, m, device="cuda", dtype=torch.int32)
+        tok = (torch.arange(m, device="cuda", dtype=torch.int32) * (V // m)).repeat(B)
+        val = torch.randn(B * m, device="cuda")
+        best = math.inf
+        for _ in range(3):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            S.constrain_logits(z, bias=(off, tok, val), out=out)
+            end.record()
+            end.synchronize()
+            best = min(best, begin.elapsed_time(end) * 1e3)
+        return best
+
+    few, all_ = us(V // 16), us(V)
+    assert all_ < 64 * few, (few, all_)
