@@ -60,8 +60,9 @@ typedef struct {
   int32_t history_width;
   const int32_t* history_len;
   const int32_t* prompt_len;
-  /* drafts[b * drafts_ld + j], j < P - 1: position k counts those with j < k as output.  A
-   * token outside [0, V) is left out (ASYMSPEC_DATA_BAD_TOKEN). */
+  /* drafts[b * drafts_ld + j], j < P - 1: position k counts those with j < k as output; so P = 1
+   * counts none, and a loop that drafts a position at a time has the drafts before it in the
+   * history.  A token outside [0, V) is left out (ASYMSPEC_DATA_BAD_TOKEN). */
   const int32_t* drafts;
   int64_t drafts_ld;
   /* penalties [B] (NULL: 1, 0 and 0).  A request with a bad one is not penalised at all
@@ -87,8 +88,9 @@ typedef struct {
   int32_t mask_count;
   const int32_t* mask_rows;
   /* What a masked logit becomes, clamped to the type's finite range: -FLT_MAX gives its
-   * lowest value (which the step and the draft take on rows that stream; -1e4 serves
-   * everywhere). */
+   * lowest value.  The drafter's draw and the step's streaming kernels take that; its staged
+   * and generic kernels answer masks of about -1e30 and lower with ASYMSPEC_DATA_NONFINITE.
+   * -1e4 serves everywhere. */
   float mask_value;
 } asymspec_constraints;
 

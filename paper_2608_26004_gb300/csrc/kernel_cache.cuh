@@ -58,7 +58,7 @@ __device__ __forceinline__ void scan3(int64_t& a, int& b, int& c, int64_t* wa, i
 // numbers each: cheaper than an exchange), then they share the blocks given back, the
 // blocks taken and the slots, each found by a search in the prefix sums, with a barrier
 // between what one part writes and the next reads.  Bound by latency: 64 requests of 8 slots
-// 4.9 us, 256 requests of 115,000 slots in all 17.3 us (8 CTAs; 120 with one).
+// 5.1 us, 256 requests of 115,000 slots in all 17.3 us (8 CTAs; 120 with one).
 template <bool CLUSTER>
 __global__ void __launch_bounds__(kPThreads) cache_plan_kernel(const PlanParams p) {
   extern __shared__ int64_t p_smem[];

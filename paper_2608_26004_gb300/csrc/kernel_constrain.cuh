@@ -25,7 +25,7 @@ struct CParams {
 constexpr int kCThreads = 256;
 constexpr int kCAhead = 2;     // 16-byte loads of the history that a thread has on their way
 constexpr int kCSlots = 12;    // vectors of a thread in a batch of rows at most
-constexpr int kCOrdered = 64;     // requests that are taken in the order of their lengths at most
+constexpr int kCOrdered = 64;  // requests that are taken in the order of their lengths at most: two a lane of a warp
 constexpr int kCStepBits = 8;      // in steps of so many tokens (a power of two)
 constexpr int kCBiases = 256;  // a slice's bias entries that shared memory holds
 constexpr int kCPart = 2 * kCBiases;  // tokens of a part of a slice with more of them: divides every W

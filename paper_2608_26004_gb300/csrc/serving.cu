@@ -72,7 +72,8 @@ constexpr int kThreadVectors = 4;
 // end, take the requests with the longest histories first, so that none of those begins last.
 // us, in the grid's order / with the last CTAs ordered / with all (each waits for the lengths then):
 // 32x9 with histories to 8192 35.0 / 34.7 / 38.0, 32768 40.1 / 38.5 / 39.6, 65536 48.2 / 44.9 / 42.9;
-// 64x8 to 8192 47.8 / 48.7 / 53.9, 16384 49.8 / 49.9 / 55.5, 32768 53.7 / 51.4 / 57.0.
+// 64x8 to 8192 47.8 / 48.7 / 53.9, 16384 49.8 / 49.9 / 55.5, 32768 53.7 / 51.4 / 57.0.  (The host knows
+// how long they may be, not how long they are: short ones with room for long ones pay those 2 %.)
 constexpr int kOrderWidth = 16384;
 constexpr int kOrderCtas = 4;  // on an SM
 template <typename T>

@@ -154,8 +154,11 @@ def constrain_logits(logits, *, history=None, history_len=None, prompt_len=None,
     prompt_len are the prompt); drafts [B, P - 1] int32; repetition, frequency, presence
     [B] float32; bias (offsets [B + 1] int32, tokens int32, values float32); mask [M,
     words] int32, bit v % 32 of word v / 32 set where v is allowed, mask_rows [B, P]
-    int32 (-1: none).  A masked logit becomes mask_value (default: the type's lowest).
-    Returns `out`, which may be `logits` itself."""
+    int32 (-1: none).  A masked logit becomes mask_value (default: the type's lowest, which
+    the draw and the step's streaming kernels take; its staged and generic kernels answer
+    about -1e30 and lower with a data error, and -1e4 serves everywhere).  Position k counts
+    the drafts before it: with P = 1 none, so those belong into the history then.  Returns
+    `out`, which may be `logits` itself."""
     if torch is None:
         _begin()
     dev = logits.get_device()
