@@ -382,7 +382,7 @@ def run(state):
         if "rotary" not in state:  # the frequencies that a model keeps
             state["rotary"] = S.Rotary(case["D"], rotary_dim=case["rot"], base=BASE,
                                        interleaved=case["interleaved"], scaling=_scaling(case))
-        return state["rotary"](x["q"], x["positions"], x["k"], inverse=case["inverse"], q_out=x["q_out"],
+        return state["rotary"](x["q"], x["positions"], x["k"], transpose=case["inverse"], q_out=x["q_out"],
                                k_out=x["k_out"])
     if "cache" not in state:  # the view of the pool that a serving loop keeps
         state["cache"] = S.Cache4(x["key_codes"], x["key_scales"], x["value_codes"], x["value_scales"],
