@@ -99,7 +99,7 @@ def _log_uniform(rng, lo, hi):
 def draw(rng):
     kind = rng.choices(("rotary", "store", "read", "attend"), (3, 2, 1, 4))[0]
     dtype = rng.choices(("bf16", "fp32"), (2, 1))[0]
-    scales = rng.choice((1.0, 0.5, 0.0625)), rng.choice((1.0, 0.25, 0.03))
+    scales = rng.choice((1.0, 0.5, 0.0625)), rng.choice((1.0, 0.25, 0.046875))
     block, layout = rng.choice((8, 16, 24, 32, 64)), rng.choice(("nhd", "hnd"))
     if kind == "rotary":
         kv, G, D = rng.choice((1, 2, 4, 8)), rng.choice((1, 2, 4, 8)), rng.choice((64, 80, 96, 128, 256))
