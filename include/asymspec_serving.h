@@ -223,6 +223,142 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
                           const int64_t* out_strides, float* out_lse, void* workspace,
                           size_t workspace_bytes, uint32_t* out_error_word, void* stream);
 
+/* ---- rotary positions --------------------------------------------------------
+ * A head's first rotary_dim elements are pairs, pair i turned by the token's position p
+ * times the pair's frequency w_i:
+ *
+ *   (a, b) -> (c a - s b, s a + c b),   c = magnitude * cos(p w_i),   s = magnitude * sin(p w_i)
+ *
+ * The pairs are the elements i and i + rotary_dim / 2 (halves), or 2 i and 2 i + 1
+ * (interleaved).  With `transpose` s is -s: the gradient of a call from the gradient of its
+ * outputs and, at a magnitude of 1, the way back.  Elements past rotary_dim and tokens with a
+ * negative position (padding) stay what they are.
+ *
+ * Frequencies are given in turns: steps[i] is w_i / 2 pi of a turn a position, its fraction
+ * as a 64-bit fixed-point number.  A position's phase is then a product of whole numbers, and
+ * as exact at position 2^31 - 1 as at 1.  asymspec_rotary_steps fills rotary_dim / 2 of them on
+ * the host (the caller copies them to the device), from w_i = base^(-2 i / rotary_dim) under a
+ * scaling (NULL or ASYMSPEC_ROTARY_NONE: as they are), or from `frequencies` (radians a position;
+ * no scaling then, base is not read), and *out_magnitude:
+ *
+ *   LINEAR      w / factor
+ *   BASE        base * factor^(rotary_dim / (rotary_dim - 2)) in the place of base: the last
+ *               pair is stretched by `factor`, the first not at all (rotary_dim >= 4)
+ *   RAMP        r w + (1 - r) w / factor, r falling from 1 to 0 along the pairs, from the one
+ *               that turns `fast` times within original_length positions (rounded down) to the one
+ *               that turns `slow` times (up); magnitude 0.1 ln(factor) + 1 (factor > 1).  (YaRN,
+ *               arXiv:2309.00071)
+ *   WAVELENGTH  the same with r = (n - slow) / (fast - slow) cut to [0, 1], n the turns of the pair
+ *               within original_length; magnitude 1
+ *
+ * The magnitude is 1 where nothing else is said.  ASYMSPEC_ERR_INVALID_ARG: a null pointer, an odd
+ * rotary_dim or one < 2, a base that is not finite and > 1, an unknown kind, a factor that is not
+ * finite and >= 1, original_length < 1 or not 0 < slow < fast where they are read, a frequency that is
+ * not finite, a scaling beside frequencies. */
+typedef enum {
+  ASYMSPEC_ROTARY_NONE = 0,
+  ASYMSPEC_ROTARY_LINEAR = 1,
+  ASYMSPEC_ROTARY_BASE = 2,
+  ASYMSPEC_ROTARY_RAMP = 3,
+  ASYMSPEC_ROTARY_WAVELENGTH = 4
+} asymspec_rotary_kind_t;
+
+typedef struct {
+  int32_t kind;             /* asymspec_rotary_kind_t */
+  int32_t original_length;  /* RAMP, WAVELENGTH */
+  double factor, fast, slow;
+} asymspec_rotary_scaling;
+
+int asymspec_rotary_steps(int rotary_dim, double base, const asymspec_rotary_scaling* scaling,
+                          const double* frequencies, uint64_t* out_steps, float* out_magnitude);
+
+/* Heads of T tokens: token t's head h is the head_dim consecutive elements from in + t *
+ * in_strides[0] + h * in_strides[1]; likewise out, which may be `in` with the same strides, or must
+ * not overlap it. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t in_strides[2], out_strides[2];  /* token, head */
+  int32_t heads;
+} asymspec_rotary_heads;
+
+/* Turns queries and keys (k may be NULL) of T tokens at positions [T] int32.  Angles are
+ * fp32 from exact phases, products fp32, each output rounded once.  One launch; any
+ * element-aligned pointers and strides, 16-byte vectors where all of them allow it.  T = 0
+ * is a no-op.
+ * ASYMSPEC_ERR_INVALID_ARG: a null pointer, T < 0, heads < 1, head_dim < 1, rotary_dim odd, < 2 or >
+ * head_dim, a negative stride, a stride of 0 along an axis of an output that is longer than 1, in = out
+ * with other strides, q and k with one output, a magnitude that is not finite.
+ * ASYMSPEC_ERR_UNSUPPORTED: dtype, head_dim > ASYMSPEC_ROTARY_MAX_D.  ASYMSPEC_ERR_MISALIGNED.
+ * ASYMSPEC_ERR_TOO_LARGE: heads > 65536. */
+#define ASYMSPEC_ROTARY_MAX_D 1024
+int asymspec_rotary(const asymspec_rotary_heads* q, const asymspec_rotary_heads* k, int T,
+                    int head_dim, int rotary_dim, int interleaved, int transpose,
+                    const int32_t* positions, const uint64_t* steps, float magnitude, int dtype,
+                    void* stream);
+
+/* ---- a paged cache in 4 bits -----------------------------------------------------
+ * Keys and values as codes of 4 bits, e2m1 (a sign, magnitudes 0, 0.5, 1, 1.5, 2, 3, 4 and 6), each
+ * 16 consecutive elements of a head with a scale of 8 bits, e4m3, and each pool with one number:
+ * element = code * scale * key_scale (value_scale).  4.5 bits an element.  Of block n, token i, kv
+ * head h, head_dim / 2 bytes of codes lie at codes + n * strides[0] + i * strides[1] + h *
+ * strides[2], element 2 j in the low and 2 j + 1 in the high half of byte j, and head_dim / 16
+ * bytes of scales at scales + their own strides; all strides count bytes, and any order of the three
+ * axes in memory is a matter of the strides.  (With a head's tokens next to one another the attention
+ * reads whole sectors of scales.)
+ *
+ * What is written of 16 elements x, each line rounded to fp32 or to the type named, to the nearest
+ * and to the even one of two:
+ *
+ *   m = max |x| * (1 / (6 * key_scale));   s = e4m3(min(m, 448))
+ *   r = 1 / (s * key_scale), or 0 where s = 0;   code = e2m1(min(max(x * r, -6), 6))
+ *
+ * so that |x| up to 2688 * key_scale is kept to half a step of 4 bits, what is beyond that comes
+ * back as 2688 * key_scale at most (infinities too), and groups below 2^-10 * 6 * key_scale as 0: a
+ * pool's number belongs near the magnitude of its elements, a power of two for instance.  A NaN makes
+ * its group's scale, and so all 16 elements, a NaN. */
+typedef struct {
+  void *key_codes, *key_scales, *value_codes, *value_scales;
+  int64_t key_code_strides[3], key_scale_strides[3];      /* block, token, kv head; bytes */
+  int64_t value_code_strides[3], value_scale_strides[3];
+  int32_t num_blocks, block_size, kv_heads, head_dim;
+  float key_scale, value_scale;
+} asymspec_cache4;
+
+/* Every call on such a cache: ASYMSPEC_ERR_INVALID_ARG: a null pointer, a size < 1, a negative stride, a
+ * key_scale or value_scale outside [2^-64, 2^64].  ASYMSPEC_ERR_UNSUPPORTED: head_dim that is no multiple of
+ * 32, or beyond ASYMSPEC_CACHE_MAX_D.  ASYMSPEC_ERR_MISALIGNED: codes and their strides off the 16-byte
+ * boundaries, scales and theirs odd.  ASYMSPEC_ERR_TOO_LARGE: num_blocks * block_size beyond 2^31 - 1,
+ * kv_heads > 65536. */
+
+/* asymspec_cache_write into such a cache: k, v of `dtype`, their strides (token, head) in elements.  Two
+ * tokens with one slot leave codes and scales there that may be of either.  One launch. */
+int asymspec_cache4_write(const asymspec_cache4* cache, const void* k, const void* v, int dtype,
+                          const int64_t* k_strides, const int64_t* v_strides, const int64_t* slots,
+                          int T, uint32_t* out_error_word, void* stream);
+
+/* Reads T tokens back: slot slots[t]'s keys and values into k[t], v[t] (strides: token, head; any
+ * element-aligned), rounded once to `dtype` (code * scale is exact).  A negative slot gives
+ * zeros, one past the pool too (ASYMSPEC_DATA_BAD_INDEX).  One launch.  T = 0 is a no-op.
+ * ASYMSPEC_ERR_INVALID_ARG besides: T < 0, a stride of 0 along an axis that is longer than 1, k = v.
+ * ASYMSPEC_ERR_UNSUPPORTED: dtype. */
+int asymspec_cache4_read(const asymspec_cache4* cache, const int64_t* slots, int T, void* k, void* v,
+                         int dtype, const int64_t* k_strides, const int64_t* v_strides,
+                         uint32_t* out_error_word, void* stream);
+
+/* asymspec_cache_attend over such a cache, with its arguments, checks and answers to bad data; q and
+ * out are of `dtype`.  Keys and values enter exactly; bf16 queries too, fp32 ones in two fp16
+ * pieces (2^-22); weights in one fp16 piece for bf16 (2^-11, an eighth of the output's own rounding), in
+ * two for fp32.  (Elements of a query below 2^-28 of its largest may be less exact.)
+ * ASYMSPEC_ERR_INVALID_ARG besides: scale * key_scale / ln 2 beyond fp32. */
+size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim);
+int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtype,
+                           const int64_t* q_strides, int B, int Q, int heads,
+                           const int32_t* block_tables, int64_t table_ld, int table_width,
+                           const int32_t* lens, float scale, int window, void* out,
+                           const int64_t* out_strides, float* out_lse, void* workspace,
+                           size_t workspace_bytes, uint32_t* out_error_word, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -70,6 +70,12 @@ EXPORTED = (
     "asymspec_cache_write",
     "asymspec_cache_attend_workspace_bytes",
     "asymspec_cache_attend",
+    "asymspec_rotary_steps",
+    "asymspec_rotary",
+    "asymspec_cache4_write",
+    "asymspec_cache4_read",
+    "asymspec_cache4_attend_workspace_bytes",
+    "asymspec_cache4_attend",
 )
 
 

@@ -21,12 +21,13 @@ CUDA_SRC = [os.path.join(CSRC, f) for f in (
     "k_tma_f32_prod.cu", "k_tma_bf16_any_s.cu", "k_tma_f32_any_s.cu", "k_row_bf16.cu",
     "k_row_f32.cu", "k_full_bf16.cu", "k_full_f32.cu", "k_xrow_bf16.cu",
     "k_xrow_f32.cu", "k_draft.cu", "k_xvocab.cu", "serving.cu",
-    "k_attend_bf16.cu", "k_attend_f32.cu")]
+    "k_attend_bf16.cu", "k_attend_f32.cu", "rotary.cu", "cache4.cu", "k_attend4_bf16.cu",
+    "k_attend4_f32.cu")]
 CUDA_HEADERS = [os.path.join(CSRC, f) for f in (
     "device_common.cuh", "kernel_generic.cuh", "kernel_tma.cuh", "kernel_row.cuh",
     "kernel_full.cuh", "kernel_xrow.cuh", "kernel_draft.cuh", "kernel_xvocab.cuh", "kernel_constrain.cuh",
-    "kernel_cache.cuh", "kernel_attend.cuh", "kernels.h", "host_common.h",
-    "k_attend.h")]
+    "kernel_cache.cuh", "kernel_attend.cuh", "kernel_rotary.cuh", "kernel_cache4.cuh",
+    "kernel_attend4.cuh", "kernels.h", "host_common.h", "serving_host.h", "k_attend.h")]
 CUDA_LIB = os.path.join(HERE, "libasymspec.so")
 GENCODE = "arch=compute_103a,code=sm_103a"
 

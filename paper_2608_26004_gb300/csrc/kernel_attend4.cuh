@@ -1,0 +1,712 @@
+// Attention of a few new tokens over a paged cache in 4 bits (asymspec_cache4_attend).
+#pragma once
+
+#include "kernel_attend.cuh"
+#include "kernel_cache4.cuh"
+
+namespace asymspec_impl {
+
+struct Attend4Params {
+  AttendParams a;  // (its keys, values and their strides are not read)
+  const char* codes[2];
+  const char* scales[2];
+  int64_t cs[2][3], ss[2][3];  // bytes
+  float value_scale;
+  bool wide_scales;  // a token's scales of a head are DP / 16 bytes on such boundaries
+};
+
+// 8x8 elements of 16 bits, a row to four lanes, into its columns.
+__device__ __forceinline__ unsigned transposed(unsigned x) {
+  unsigned y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ unsigned pack_f16(float x, float y) {
+  unsigned r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0,
+                                        unsigned b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The bits of x where those of m are set, of y elsewhere.
+__device__ __forceinline__ unsigned select_bits(unsigned m, unsigned x, unsigned y) { return (x & m) | (y & ~m); }
+__device__ __forceinline__ void cp_async16(unsigned smem, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+}
+
+// Dynamic shared memory.  A step of a group: 16 keys' codes, 16 values' codes in rows 16 bytes
+// longer than they are (lanes read the rows 2 t of their own then without meeting a bank twice), and both's
+// scales.  Where an item ends, the group's ring takes its rows' values.
+__host__ __device__ constexpr int attend4_step_bytes(int DP) { return kAKeys * (DP / 2 + DP / 2 + 16 + DP / 8); }
+__host__ __device__ constexpr int attend4_group_bytes(int DP, int rows, int ST) {
+  return ST * attend4_step_bytes(DP) > rows * DP * 4 ? ST * attend4_step_bytes(DP) : rows * DP * 4;
+}
+__host__ __device__ constexpr int attend4_query_pitch(int DP) { return DP * 2 + 16; }
+constexpr size_t attend4_smem_bytes(int DP, int rows, int ST, int pieces) {
+  return static_cast<size_t>(kAGroups) * attend4_group_bytes(DP, rows, ST) +
+         static_cast<size_t>(rows) * (attend4_query_pitch(DP) * pieces + 4) + kAGroups * ST * 4 +
+         static_cast<size_t>(kAGroups) * rows * 8 + kAGroups * 8 * 8 + 32;
+}
+
+// Of 32-bit word N at `p`.
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char* p, unsigned (&w)[N]) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    }
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x, w[1] = v.y;
+  } else {
+    w[0] = *reinterpret_cast<const unsigned*>(p);
+  }
+}
+
+// The keys are split evenly over the CTAs and over a CTA's four groups of warps, as
+// attend_split's are.  A step's products are formed the other way round: keys, then a head's
+// elements, are the rows of the matrix instructions and up to 8 queries their columns, so that one
+// kv head's few queries fill them, and the codes become their operands in the registers
+// that the lanes load them into: two codes of a byte are two neighbouring elements of a key;
+// for the values the bytes of two keys are interleaved first.  e2m1 times e4m3 has 6
+// significant bits and lies between 2^-10 and 2688: fp16 holds it, the keys and values are exact, and
+// so are bf16 queries, each row times a power of two.  The pools' numbers are left to the
+// scores' factors and the end.
+// T: of queries and outputs.  NT: tiles of 8 rows of a warp.
+template <typename T, int DP, int NT, int WR, int ST, int PER_SM>
+__global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(const __grid_constant__ Attend4Params P) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int kPieces = BF ? 1 : 2;
+  constexpr int kThreadsN = kAGroups * WR * 32, kWarpsN = kAGroups * WR;
+  constexpr int kWarpRows = 8 * NT, kRows = kWarpRows * WR;
+  constexpr int kKeyRow = DP / 2, kValueRow = DP / 2 + 16, kScaleRow = DP / 16;
+  constexpr int kValues = kAKeys * kKeyRow, kScales = kValues + kAKeys * kValueRow;
+  constexpr int kStep = attend4_step_bytes(DP), kGroup = attend4_group_bytes(DP, kRows, ST);
+  constexpr int kQPitch = attend4_query_pitch(DP);
+  constexpr int KW = DP / 32;  // words of a lane's part of a key
+  constexpr int VW = DP / 64;  // words of a lane's part of a value
+  constexpr int MT = DP / 16;  // tiles of 16 elements of a head
+  constexpr int kChunks = DP / 32;                     // 16-byte chunks of a key
+  constexpr bool kBoth = kAKeys * kChunks >= 32 * WR;  // a lane loads of keys and of values
+  constexpr int kLaneKeys = kBoth ? kAKeys * kChunks / (32 * WR) : 1;
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  constexpr float kBelow = 7.f, kSlack = 8.f;
+  constexpr bool kQRegs = kPieces * NT * KW * 4 <= 32;
+  static_assert(ST >= 2 && kStep % 16 == 0 && kGroup % 16 == 0, "the ring");
+  extern __shared__ __align__(1024) unsigned char a_smem[];
+  const AttendParams& p = P.a;
+  unsigned char* at_q = a_smem + kAGroups * kGroup;
+  float* s_factor = reinterpret_cast<float*>(at_q + kRows * kQPitch * kPieces);
+  float* s_ml = s_factor + kRows;
+  unsigned* masks0 = reinterpret_cast<unsigned*>(s_ml + kAGroups * kRows * 2);
+  int64_t* s_scan = reinterpret_cast<int64_t*>((reinterpret_cast<uintptr_t>(masks0 + kAGroups * ST) + 7) & ~uintptr_t(7));
+  int64_t* s_find = s_scan + kWarpsN;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  const int group = warp / WR, wr = warp % WR;  // whose keys; which rows
+  unsigned* masks = masks0 + group * ST;
+  unsigned char* ring = a_smem + group * kGroup;
+  const unsigned ring_at = smem_u32(ring);
+  const int c = blockIdx.x, ctas = gridDim.x;
+  const int HR = p.kv_heads * p.row_tiles;
+  unsigned err = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // this CTA's share of the units, and where it begins
+  const int per = (p.B + kThreadsN - 1) / kThreadsN;
+  int64_t mine = 0;
+  for (int b = tid * per; b < min((tid + 1) * per, p.B); ++b) {
+    const int len = attend_len(p, b);
+    if (len != p.lens[b]) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    mine += attend_tiles(p, len) + kAItem;
+  }
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 31) s_scan[warp] = upto;
+  __syncthreads();
+  int64_t total = 0;
+  for (int w = 0; w < kWarpsN; ++w) {
+    if (w < warp) upto += s_scan[w];
+    total += s_scan[w];
+  }
+  total *= HR;
+  const AttendShares shares(total, ctas);
+  int64_t u = shares.start(c);
+  const int64_t u_end = shares.start(c + 1);
+  if (u < u_end && (upto - mine) * HR <= u && u < upto * HR) {
+    int64_t v = u - (upto - mine) * HR;
+    int b = tid * per;
+    for (;; ++b) {
+      const int64_t n = static_cast<int64_t>(attend_tiles(p, attend_len(p, b)) + kAItem) * HR;
+      if (v < n) break;
+      v -= n;
+    }
+    s_find[0] = b;
+    s_find[1] = v;
+  }
+  __syncthreads();
+  AttendInfo* info = reinterpret_cast<AttendInfo*>(p.ws) + c;
+  if (u >= u_end) {
+    if (tid == 0) info->tiles = 0;
+    if (err && p.err) atomicOr(p.err, err);
+    return;
+  }
+  int b = static_cast<int>(s_find[0]);
+  int len = attend_len(p, b), n_tiles = attend_tiles(p, len);
+  int hr = static_cast<int>(div64(s_find[1], n_tiles + kAItem));
+  int at_unit = static_cast<int>(s_find[1] - static_cast<int64_t>(hr) * (n_tiles + kAItem));
+  if (tid == 0) {
+    info->total = total;
+    info->first = u - at_unit;
+    info->b = b;
+    info->hr = hr;
+    info->tiles = at_unit > kAItem ? n_tiles : 0;
+  }
+
+  // what this lane loads of a step: chunk `chunk` of keys load_key + i * kLaneRows (kBoth: and of their
+  // values; else of the keys or of the values), and lanes of the group's first warp the scales of
+  // key lane % 16, or of its value
+  constexpr int kLaneRows = 32 * WR / kChunks;
+  const int lane_id = wr * 32 + lane;
+  const int chunk = lane_id % kChunks, load_key = lane_id / kChunks % kAKeys;
+  const int load_what = lane_id / kChunks / kAKeys;  // (kBoth: 0)
+  const bool chunk_on = chunk * 32 < p.D;
+  const int what = lane >> 4;
+  const int step_blocks = kATile / p.block_size, step_rest = kATile % p.block_size;
+
+  float O[NT][MT][4], m[NT][2], l[NT][2], factor[NT][2];
+  unsigned qf[kQRegs ? kPieces : 1][kQRegs ? NT : 1][kQRegs ? KW : 1][4];
+  int last[NT][2];
+  for (; u < u_end; at_unit = 0) {
+    if (hr == HR) {
+      hr = 0;
+      ++b;
+      len = attend_len(p, b);
+      n_tiles = attend_tiles(p, len);
+    }
+    const int end_unit = static_cast<int>(min(static_cast<int64_t>(n_tiles + kAItem), at_unit + (u_end - u)));
+    const int t0 = max(0, at_unit - kAItem), t1 = end_unit - kAItem;
+    u += end_unit - at_unit;
+    if (t1 <= t0) continue;  // (the item's first tile is the next CTA's)
+    const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * kRows;
+    const int lo = attend_first(p, len);
+    const int rows = min(kRows, p.rows - R0);  // of the item
+    const char* key_codes = P.codes[0] + kh * P.cs[0][2];
+    const char* value_codes = P.codes[1] + kh * P.cs[1][2];
+    const int32_t* table = p.tables + b * p.table_ld;
+    const int k_group = lo + group * kAKeys;  // the group's first key of tile 0
+
+    // the next step to load: its first key, and that key's block and place there
+    int next_key = k_group + t0 * kATile;
+    int next_block = next_key / p.block_size, next_at = next_key % p.block_size;
+    const int end_key = min(len, lo + t1 * kATile);
+    struct Place {
+      int page, at;
+    };
+    auto place = [&](int r) {  // of the next step's key r
+      Place x = {INT_MIN, next_at + r};
+      int block = next_block;
+      if (x.at >= p.block_size) {
+        const int more = static_cast<unsigned>(x.at) / static_cast<unsigned>(p.block_size);
+        block += more;
+        x.at -= more * p.block_size;
+      }
+      if (next_key + r < end_key) x.page = __ldg(table + block);
+      return x;
+    };
+    Place places[kLaneKeys], scale_place;
+    int scale_key;
+    auto find = [&] {  // the next step's blocks
+#pragma unroll
+      for (int i = 0; i < kLaneKeys; ++i) places[i] = place(load_key + i * kLaneRows);
+      if (wr == 0) scale_place = place(lane & 15);
+      scale_key = next_key + (lane & 15);
+      next_key += kATile;
+      next_block += step_blocks;
+      next_at += step_rest;
+      if (next_at >= p.block_size) next_at -= p.block_size, ++next_block;
+    };
+    auto there = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks); };
+    unsigned sc[VW];      // the scales on their way
+    unsigned sc_live = 0;
+    auto issue = [&](int stage) {
+      const unsigned at = ring_at + stage * kStep;
+#pragma unroll
+      for (int i = 0; i < kLaneKeys; ++i) {
+        const int r = load_key + i * kLaneRows;
+        if (!there(places[i].page) || !chunk_on) continue;
+        if (kBoth || load_what == 0)
+          cp_async16(at + r * kKeyRow + chunk * 16, key_codes + chunk * 16 + places[i].page * P.cs[0][0] + places[i].at * P.cs[0][1]);
+        if (kBoth || load_what == 1)
+          cp_async16(at + kValues + r * kValueRow + chunk * 16,
+                     value_codes + chunk * 16 + places[i].page * P.cs[1][0] + places[i].at * P.cs[1][1]);
+      }
+      cp_async_commit();
+      if (wr == 0) {
+        const bool on = there(scale_place.page);
+        sc_live = __ballot_sync(~0u, on) & 0xFFFFu;
+        // (up to 15 keys are before the window of every query: their block may be gone)
+        if (!on && scale_key < end_key && (p.window == 0 || scale_key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
+#pragma unroll
+        for (int i = 0; i < VW; ++i) sc[i] = 0;
+        if (on) {
+          const char* from = P.scales[what] + kh * P.ss[what][2] + scale_place.page * P.ss[what][0] +
+                             scale_place.at * P.ss[what][1];
+          if (P.wide_scales) {
+            load_words<VW>(reinterpret_cast<const unsigned char*>(from), sc);
+          } else {
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+              if (i * 64 < p.D) sc[i] = *reinterpret_cast<const uint16_t*>(from + 4 * i);
+              if (i * 64 + 32 < p.D) sc[i] |= static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(from + 4 * i + 2)) << 16;
+            }
+          }
+        }
+      }
+    };
+    // the scales of the step issued last, into the ring
+    auto settle = [&](int stage) {
+      if (wr == 0) {
+        unsigned char* to = ring + stage * kStep + kScales + what * (kAKeys * kScaleRow) + (lane & 15) * kScaleRow;
+        if constexpr (VW == 4) *reinterpret_cast<uint4*>(to) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
+        else if constexpr (VW == 2) *reinterpret_cast<uint2*>(to) = make_uint2(sc[0], sc[1]);
+        else *reinterpret_cast<unsigned*>(to) = sc[0];
+        if (lane == 0) masks[stage] = sc_live;
+      }
+    };
+    find();
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) {
+      issue(s);
+      if (s < ST - 2) settle(s);
+      find();
+    }
+
+    // the item's queries, each row times the power of two that takes its largest element to 2^13
+    for (int r = warp; r < kRows; r += kWarpsN) {
+      const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+      const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
+      float x[DP / 32];
+      unsigned most = 0;
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const int d = lane + 32 * k;
+        x[k] = r < rows && d < p.D ? to_f32(src[d]) : 0.f;
+        most = max(most, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+      }
+      const unsigned e = min(max(__reduce_max_sync(~0u, most) >> 23, 14u), 254u);
+      const float up = __uint_as_float((267u - e) << 23);  // 2^(13 - (e - 127))
+      __half* to = reinterpret_cast<__half*>(at_q + r * kQPitch);
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const float y = x[k] * up;
+        const __half hi = __float2half_rn(y);
+        to[lane + 32 * k] = hi;
+        if constexpr (!BF) to[kRows * kQPitch / 2 + lane + 32 * k] = __float2half_rn(y - __half2float(hi));
+      }
+      if (lane == 0) s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
+    }
+    // of this thread's rows: the last key seen; of the warp's the least, and the windows'
+    // largest first
+    const int R = R0 + wr * kWarpRows, warp_rows = rows - wr * kWarpRows;  // (may be none)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = n * 8 + 2 * t4 + e;
+        last[n][e] = r < warp_rows ? len - p.Q + (R + r) / p.group : -1;
+        m[n][e] = -INFINITY;
+        l[n][e] = 0.f;
+      }
+    const int least = len - p.Q + R / p.group;
+    const int from = p.window ? len - p.Q + (R + min(warp_rows, kWarpRows) - 1) / p.group - p.window + 1 : 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) O[n][i][e] = 0.f;
+    __syncthreads();
+    const unsigned char* q_lane = at_q + (wr * kWarpRows + g) * kQPitch + t4 * (DP / 2);
+    auto query = [&](int piece, int n, int w, unsigned (&x)[4]) {
+      load_words<4>(q_lane + (piece * kRows + n * 8) * kQPitch + w * 16, x);
+    };
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      factor[n][0] = s_factor[wr * kWarpRows + n * 8 + 2 * t4];
+      factor[n][1] = s_factor[wr * kWarpRows + n * 8 + 2 * t4 + 1];
+      if constexpr (kQRegs) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+          for (int w = 0; w < KW; ++w) query(k, n, w, qf[k][n][w]);
+      }
+    }
+
+    int stage = 0;
+    for (int t = t0; t < t1; ++t) {
+      settle(stage < 2 ? stage + ST - 2 : stage - 2);
+      cp_async_wait<ST - 2>();
+      // the group's warps have loaded the step, and are done with the one before
+      if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
+      else __syncwarp();
+      issue(stage == 0 ? ST - 1 : stage - 1);
+      find();
+      const unsigned char* st = ring + stage * kStep;
+      const unsigned live = masks[stage];
+      const int k0 = k_group + t * kATile;
+      if (live != 0 && warp_rows > 0) {
+        // scores of keys g and g + 8 (rows of the products) and of queries 2 t4 and 2 t4 + 1: a
+        // lane's part of a key are DP / 4 elements in a row
+        float S[NT][4];
+        {
+          unsigned ka[KW], kb[KW], sa[VW], sb[VW];
+          load_words<KW>(st + g * kKeyRow + t4 * (DP / 8), ka);
+          load_words<KW>(st + (g + 8) * kKeyRow + t4 * (DP / 8), kb);
+          const unsigned char* sk = st + kScales + g * kScaleRow + t4 * VW;
+          if constexpr (VW == 1) {
+            const unsigned x = sk[0], y = sk[8 * kScaleRow];
+            sa[0] = e4m3_to_f16(x | x << 8);
+            sb[0] = e4m3_to_f16(y | y << 8);
+          } else {
+#pragma unroll
+            for (int i = 0; i < VW; i += 2) {
+              const unsigned x = e4m3_to_f16(*reinterpret_cast<const uint16_t*>(sk + i));
+              const unsigned y = e4m3_to_f16(*reinterpret_cast<const uint16_t*>(sk + 8 * kScaleRow + i));
+              sa[i] = __byte_perm(x, x, 0x1010), sa[i + 1] = __byte_perm(x, x, 0x3232);
+              sb[i] = __byte_perm(y, y, 0x1010), sb[i + 1] = __byte_perm(y, y, 0x3232);
+            }
+          }
+          float more[BF ? 1 : NT][4], small[BF ? 1 : NT][4];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              S[n][e] = 0.f;
+              if constexpr (!BF) more[n][e] = small[n][e] = 0.f;
+            }
+#pragma unroll
+          for (int w = 0; w < KW; ++w) {
+            unsigned fa[4], fb[4];
+            e2m1_to_f16(ka[w], fa);
+            e2m1_to_f16(kb[w], fb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              fa[i] = mul_f16x2(fa[i], sa[w / 2]);
+              fb[i] = mul_f16x2(fb[i], sb[w / 2]);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              unsigned x[4];
+              if constexpr (kQRegs) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = qf[0][n][w][i];
+              } else {
+                query(0, n, w, x);
+              }
+              mma_f16(S[n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
+              if constexpr (BF) {
+                mma_f16(S[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+              } else {
+                // (the matrix unit's running sums are cut, not rounded: short ones, added up in fp32)
+                mma_f16(more[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                if constexpr (kQRegs) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) x[i] = qf[kPieces - 1][n][w][i];
+                } else {
+                  query(1, n, w, x);
+                }
+                mma_f16(small[n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
+                mma_f16(small[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+              }
+            }
+          }
+          if constexpr (!BF) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) S[n][e] += more[n][e] + small[n][e];
+          }
+        }
+        const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
+        // Weights are 2^(s - m), m kBelow below the largest score at the time; only a score kSlack above
+        // that raises it (the maximum itself, kept, would rescale the values at most steps, for one
+        // of the rows or another).  So weights stay below 2^15, and fp16, whose step is 2^-24 at the
+        // smallest, holds one of 2^-31 of a row's largest.
+        bool above = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float& s = S[n][2 * k + e];
+              s *= factor[n][e];
+              if (!whole) {
+                const int j = k0 + g + 8 * k;
+                const bool seen = ((live >> (g + 8 * k)) & 1u) && j <= last[n][e] && (p.window == 0 || j > last[n][e] - p.window);
+                s = seen ? s : -INFINITY;
+              }
+            }
+            above = above || fmaxf(S[n][e], S[n][2 + e]) > m[n][e] + (kBelow + kSlack);
+          }
+        if (__any_sync(~0u, above)) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float v = fmaxf(S[n][e], S[n][2 + e]);
+              v = fmaxf(v, __shfl_xor_sync(~0u, v, 4));
+              v = fmaxf(v, __shfl_xor_sync(~0u, v, 8));
+              v = fmaxf(v, __shfl_xor_sync(~0u, v, 16));
+              v = fmaxf(m[n][e], v - kBelow);
+              const float f = v == m[n][e] ? 1.f : ex2(m[n][e] - v);
+              m[n][e] = v;
+              l[n][e] *= f;
+#pragma unroll
+              for (int i = 0; i < MT; ++i) {
+                O[n][i][e] *= f;
+                O[n][i][2 + e] *= f;
+              }
+            }
+        }
+        // weights, turned so that queries are the columns of the second products
+        unsigned w0[kPieces][NT], w1[kPieces][NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float ref = m[n][e] == -INFINITY ? 0.f : m[n][e];
+            S[n][e] = ex2(S[n][e] - ref);
+            S[n][2 + e] = ex2(S[n][2 + e] - ref);
+            l[n][e] += S[n][e] + S[n][2 + e];
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const unsigned hi = pack_f16(S[n][2 * k], S[n][2 * k + 1]);
+            (k ? w1 : w0)[0][n] = transposed(hi);
+            if constexpr (!BF) {
+              const float2 x = f16x2_to_f32(hi);
+              (k ? w1 : w0)[kPieces - 1][n] = transposed(pack_f16(S[n][2 * k] - x.x, S[n][2 * k + 1] - x.y));
+            }
+          }
+        }
+        // values: of keys 2 t4, 2 t4 + 1 and those + 8, the lane's DP / 8 elements in a row from g * DP / 8
+        // on; even ones are rows g of the products, odd ones rows g + 8
+        {
+          const unsigned char* sv = st + kValues + 2 * t4 * kValueRow + g * (DP / 16);
+          const unsigned char* ss = st + kScales + kAKeys * kScaleRow + 2 * t4 * kScaleRow + (VW == 1 ? g / 2 : g * (VW / 2));
+          unsigned x[4][VW], s2[2][VW == 4 ? 2 : 1];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) load_words<VW>(sv + ((k & 1) + (k >> 1) * 8) * kValueRow, x[k]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if constexpr (VW == 4) {
+              const unsigned y = *reinterpret_cast<const uint16_t*>(ss + k * 8 * kScaleRow);
+              const unsigned z = *reinterpret_cast<const uint16_t*>(ss + (k * 8 + 1) * kScaleRow);
+              s2[k][0] = e4m3_to_f16(__byte_perm(y, z, 0x0040));
+              s2[k][1] = e4m3_to_f16(__byte_perm(y, z, 0x0051));
+            } else {
+              s2[k][0] = e4m3_to_f16(ss[k * 8 * kScaleRow] | ss[(k * 8 + 1) * kScaleRow] << 8);
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            unsigned f[2][2][4];  // key pair, parity of the element
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const unsigned y = x[2 * k][w], z = x[2 * k + 1][w];
+              e2m1_to_f16(select_bits(0x0F0F0F0Fu, y, z << 4), f[k][0]);
+              e2m1_to_f16(select_bits(0x0F0F0F0Fu, y >> 4, z), f[k][1]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                f[k][0][i] = mul_f16x2(f[k][0][i], s2[k][VW == 4 ? w / 2 : 0]);
+                f[k][1][i] = mul_f16x2(f[k][1][i], s2[k][VW == 4 ? w / 2 : 0]);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                if constexpr (BF) {
+                  mma_f16(O[n][4 * w + i], f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[0][n], w1[0][n]);
+                } else {
+                  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[kPieces - 1][n], w1[kPieces - 1][n]);
+                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[0][n], w1[0][n]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) O[n][4 * w + i][e] += sum[e];
+                }
+              }
+          }
+        }
+      }
+      stage = stage + 1 == ST ? 0 : stage + 1;
+    }
+    cp_async_wait<0>();
+
+    // A NaN (a scale, or a query): a weight of zero times one that its row does not see is a NaN that the
+    // formula does not have.  A warp that ends with any works its keys again, one after another, and
+    // leaves out what a row does not see.
+    float odd = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (n * 8 + 2 * t4 + e < warp_rows) {
+          odd = fmaf(0.f, l[n][e], odd);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) odd = fmaf(0.f, O[n][i][e], fmaf(0.f, O[n][i][2 + e], odd));
+        }
+    if (__any_sync(~0u, odd != 0.f)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          m[n][e] = -INFINITY;
+          l[n][e] = 0.f;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) O[n][i][e] = O[n][i][2 + e] = 0.f;
+        }
+      for (int k = 0; k < (t1 - t0) * kAKeys; ++k) {
+        const int j = k_group + (t0 + k / kAKeys) * kATile + k % kAKeys;
+        if (j >= len) break;
+        const int page = table[j / p.block_size], at = j % p.block_size;
+        if (!there(page)) continue;
+        const unsigned char* code[2];
+        const unsigned char* scale[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          code[w] = reinterpret_cast<const unsigned char*>(P.codes[w]) + kh * P.cs[w][2] + page * P.cs[w][0] + at * P.cs[w][1];
+          scale[w] = reinterpret_cast<const unsigned char*>(P.scales[w]) + kh * P.ss[w][2] + page * P.ss[w][0] + at * P.ss[w][1];
+        }
+        auto pair = [&](int w, int d) {  // elements d and d + 1, d even
+          unsigned f[4];
+          e2m1_to_f16(code[w][d / 2], f);
+          const unsigned s = scale[w][d / 16];
+          return f16x2_to_f32(mul_f16x2(f[0], e4m3_to_f16(s | s << 8)));
+        };
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = R + min(n * 8 + 2 * t4 + e, warp_rows - 1);
+            const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + r / p.group * p.qs[1] +
+                          (kh * p.group + r % p.group) * p.qs[2];
+            float s = 0.f;
+#pragma unroll 1
+            for (int d = 2 * g; d < p.D; d += 16) {
+              const float2 x = pair(0, d);
+              s = fmaf(to_f32(qr[d]), x.x, s);
+              s = fmaf(to_f32(qr[d + 1]), x.y, s);
+            }
+            s += __shfl_xor_sync(~0u, s, 4);
+            s += __shfl_xor_sync(~0u, s, 8);
+            s += __shfl_xor_sync(~0u, s, 16);
+            s *= p.scale2;
+            // (a row that does not see the key takes nothing of it)
+            if (j > last[n][e] || (p.window != 0 && j <= last[n][e] - p.window)) continue;
+            const float old = m[n][e], v = fmaxf(old, s), ref = v == -INFINITY ? 0.f : v;
+            const float f = v == old ? 1.f : ex2(old - v), w = ex2(s - ref);
+            m[n][e] = v;
+            l[n][e] = l[n][e] * f + (g == 0 ? w : 0.f);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              const int d = g * (DP / 8) + 2 * i;
+              const float2 x = d < p.D ? pair(1, d) : make_float2(0.f, 0.f);
+              O[n][i][e] = fmaf(w, x.x, O[n][i][e] * f);
+              O[n][i][2 + e] = fmaf(w, x.y, O[n][i][2 + e] * f);
+            }
+          }
+      }
+    }
+
+    // the groups' parts of the item: each warp leaves its values in its group's ring
+    if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
+    else __syncwarp();
+    auto chunk_at = [](int ch) { return ch ^ ((ch >> 3) & 7); };  // (of 16 bytes, so that lanes g meet few banks twice)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = wr * kWarpRows + n * 8 + 2 * t4 + e;
+        float s = l[n][e];
+        s += __shfl_xor_sync(~0u, s, 4);
+        s += __shfl_xor_sync(~0u, s, 8);
+        s += __shfl_xor_sync(~0u, s, 16);
+        if (g == 0) {
+          s_ml[(group * kRows + r) * 2] = m[n][e];
+          s_ml[(group * kRows + r) * 2 + 1] = s;
+        }
+        float* row = reinterpret_cast<float*>(ring) + r * DP;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int d = g * (DP / 8) + 2 * i;
+          *reinterpret_cast<float2*>(row + chunk_at(d / 4) * 4 + (d & 2)) = make_float2(O[n][i][e], O[n][i][2 + e]);
+        }
+      }
+    __syncthreads();
+    const bool all = t0 == 0 && t1 == n_tiles;
+    const int part = t0 > 0 ? 2 * c : 2 * c + 1;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * kRows * 2;
+    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * kRows * DP;
+    for (int e = tid; e < rows * (DP / 4); e += kThreadsN) {
+      const int r = e / (DP / 4), d = (e % (DP / 4)) * 4;
+      float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kAGroups; ++w) M = fmaxf(M, s_ml[(w * kRows + r) * 2]);
+#pragma unroll
+      for (int w = 0; w < kAGroups; ++w) {
+        const float mw = s_ml[(w * kRows + r) * 2], lw = s_ml[(w * kRows + r) * 2 + 1];
+        const float f = mw == M ? 1.f : ex2(mw - M);
+        const float4 o = *reinterpret_cast<const float4*>(
+            reinterpret_cast<const float*>(a_smem + w * kGroup) + r * DP + chunk_at(d / 4) * 4);
+        L = fmaf(f, lw, L);
+        x[0] = fmaf(f, o.x, x[0]);
+        x[1] = fmaf(f, o.y, x[1]);
+        x[2] = fmaf(f, o.z, x[2]);
+        x[3] = fmaf(f, o.w, x[3]);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] *= P.value_scale;
+      if (all) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+        T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
+        if (d < p.D) {  // (D is a multiple of 4)
+          __align__(16) T y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) put(y + k, x[k] * inv);
+          if (p.out_vec) {
+            if constexpr (BF) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
+            else *reinterpret_cast<float4*>(out) = *reinterpret_cast<const float4*>(y);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] = y[k];
+          }
+        }
+        if (d == 0 && p.lse)
+          p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = lse_of(M, L);
+      } else {
+        *reinterpret_cast<float4*>(ws_o + r * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
+        if (d == 0) *reinterpret_cast<float2*>(ws_ml + r * 2) = make_float2(M, L);
+      }
+    }
+    __syncthreads();
+    ++hr;
+  }
+  if (err && p.err) atomicOr(p.err, err);
+}
+
+}  // namespace asymspec_impl

@@ -10,51 +10,17 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
-#include <mutex>
 
 #include "host_common.h"
 #include "k_attend.h"
 #include "kernel_attend.cuh"
 #include "kernel_cache.cuh"
 #include "kernel_constrain.cuh"
+#include "serving_host.h"
 
 namespace {
 
 using namespace asymspec_impl;
-
-constexpr int64_t kMax32 = INT32_MAX;
-
-bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-
-int elt_size(int dtype) { return dtype == ASYMSPEC_FP32 ? 4 : 2; }
-
-bool known_dtype(int dtype) { return dtype == ASYMSPEC_FP32 || dtype == ASYMSPEC_BF16; }
-
-constexpr int kStaticSmem = 8192;  // what a kernel has beside its dynamic shared memory at most
-
-// Once per kernel and device: room for all the dynamic shared memory that it may ask for.
-struct Prepared {
-  const void* fn;
-  int device;
-};
-std::mutex g_mu;
-Prepared g_prepared[64];
-int g_prepared_count = 0;
-
-cudaError_t prepare(const void* fn, int device, int smem) {
-  if (smem <= 48 * 1024 - kStaticSmem) return cudaSuccess;
-  std::lock_guard<std::mutex> lock(g_mu);
-  for (int i = 0; i < g_prepared_count; ++i)
-    if (g_prepared[i].fn == fn && g_prepared[i].device == device) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - kStaticSmem);
-  if (e == cudaSuccess && g_prepared_count < 64) g_prepared[g_prepared_count++] = {fn, device};
-  return e;
-}
-
-cudaError_t device_sms(int* device, int* sms) {
-  const cudaError_t e = cudaGetDevice(device);
-  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device) : e;
-}
 
 constexpr int kWriteCtas = 1216;  // CTAs of the write at most: eight on each SM
 
@@ -85,19 +51,6 @@ const void* constrain_pick(bool in_place, bool edges) {
 
 AttendKernels attend_kernels(int dtype, int D, int rows) {
   return dtype == ASYMSPEC_FP32 ? attend_kernels_f32(D, rows) : attend_kernels_bf16(D, rows);
-}
-
-int launch(const void* fn, dim3 grid, dim3 block, size_t smem, void* params, void* stream) {
-  cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024 - kStaticSmem) {
-    int device = 0;
-    e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = prepare(fn, device, static_cast<int>(smem));
-    if (e != cudaSuccess) return cuda_fail(e);
-  }
-  void* args[] = {params};
-  e = cudaLaunchKernel(fn, grid, block, args, smem, static_cast<cudaStream_t>(stream));
-  return e == cudaSuccess ? ASYMSPEC_OK : cuda_fail(e);
 }
 
 int check_constraints(const asymspec_constraints& c, int B, int P, int V) {

@@ -2,8 +2,8 @@
 
 Python side of include/asymspec_serving.h, in the same library as the step: logits
 under penalties, biases and grammar masks; block tables and slot maps of a paged
-key-value cache; the writing of new keys and values; attention over the cache.  The
-functions on tensors below extract addresses, sizes and strides, enqueue on the
+key-value cache; the writing of new keys and values; attention over the cache; rotary
+positions; a cache in 4 bits with its writing, reading and attention.  The functions on tensors below extract addresses, sizes and strides, enqueue on the
 current stream and raise ``AsymSpecError`` on a status other than OK; everything is
 computed in the library's CUDA kernels.  Nothing is read back to the host.  All tensors
 of a call lie on the current device.
@@ -25,6 +25,9 @@ DATA_NO_BLOCKS = 0x200
 CONSTRAIN_MAX_P = 256  # positions that constrain_logits takes
 CACHE_MAX_B = 8192     # requests that cache_plan and cache_attend take
 CACHE_MAX_D = 256      # head size that cache_attend takes
+ROTARY_MAX_D = 1024    # head size that rotary takes
+
+ROTARY_KINDS = {"linear": 1, "base": 2, "ramp": 3, "wavelength": 4}
 
 FLT_MAX = 3.4028234663852886e38
 
@@ -51,10 +54,34 @@ class Cache(ctypes.Structure):
                 ("dtype", ctypes.c_int32)]
 
 
+class RotaryScaling(ctypes.Structure):
+    """asymspec_rotary_scaling."""
+    _fields_ = [("kind", ctypes.c_int32), ("original_length", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("fast", ctypes.c_double), ("slow", ctypes.c_double)]
+
+
+class RotaryHeads(ctypes.Structure):
+    """asymspec_rotary_heads, for calls by address through lib()."""
+    _fields_ = [("x", _P), ("out", _P), ("in_strides", _L2), ("out_strides", _L2),
+                ("heads", ctypes.c_int32)]
+
+
+class PackedCache(ctypes.Structure):
+    """asymspec_cache4, for calls by address through lib()."""
+    _fields_ = [("key_codes", _P), ("key_scales", _P), ("value_codes", _P), ("value_scales", _P),
+                ("key_code_strides", _L3), ("key_scale_strides", _L3), ("value_code_strides", _L3),
+                ("value_scale_strides", _L3), ("num_blocks", ctypes.c_int32),
+                ("block_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("key_scale", ctypes.c_float),
+                ("value_scale", ctypes.c_float)]
+
+
 # The same structs as bytes, filled in one step: field by field took a third of a small
 # call's host time.
 _CONSTRAINTS = struct.Struct("@PqixxxxPPPqPPPPPPixxxxPqixxxxPfxxxx")
 _CACHE = struct.Struct("@PP6q5ixxxx")
+_HEADS = struct.Struct("@PP4qixxxx")
+_CACHE4 = struct.Struct("@4P12q4iff")
 _STRIDES2, _STRIDES3 = struct.Struct("@2q"), struct.Struct("@3q")
 
 torch = None  # imported with the first call: the addresses' side needs no PyTorch
@@ -80,12 +107,57 @@ def lib():
         L.asymspec_cache_attend.argtypes = [_P, _P, _P, _I, _I, _I, _P, _L, _I, _P, ctypes.c_float, _I,
                                             _P, _P, _P, _P, ctypes.c_size_t, _P, _P]
         L.asymspec_cache_attend.restype = _I
+        L.asymspec_rotary_steps.argtypes = [_I, ctypes.c_double, _P, _P, _P, _P]
+        L.asymspec_rotary_steps.restype = _I
+        L.asymspec_rotary.argtypes = [_P, _P, _I, _I, _I, _I, _I, _P, _P, ctypes.c_float, _I, _P]
+        L.asymspec_rotary.restype = _I
+        L.asymspec_cache4_write.argtypes = [_P, _P, _P, _I, _P, _P, _P, _I, _P, _P]
+        L.asymspec_cache4_write.restype = _I
+        L.asymspec_cache4_read.argtypes = [_P, _P, _I, _P, _P, _I, _P, _P, _P, _P]
+        L.asymspec_cache4_read.restype = _I
+        L.asymspec_cache4_attend_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
+        L.asymspec_cache4_attend_workspace_bytes.restype = ctypes.c_size_t
+        L.asymspec_cache4_attend.argtypes = [_P, _P, _I, _P, _I, _I, _I, _P, _L, _I, _P, ctypes.c_float, _I,
+                                             _P, _P, _P, _P, ctypes.c_size_t, _P, _P]
+        L.asymspec_cache4_attend.restype = _I
         _lib = L
     return _lib
 
 
 def cache_attend_workspace_bytes(B: int, Q: int, heads: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().asymspec_cache_attend_workspace_bytes(B, Q, heads, kv_heads, head_dim))
+
+
+def cache4_attend_workspace_bytes(B: int, Q: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().asymspec_cache4_attend_workspace_bytes(B, Q, heads, kv_heads, head_dim))
+
+
+def rotary_steps(rotary_dim: int, base: float = 10000.0, scaling=None, frequencies=None):
+    """([turns of each pair a position, as 64-bit fractions], magnitude): what asymspec_rotary takes.
+
+    scaling: None, or a dict of kind ("linear", "base", "ramp", "wavelength"), factor and, for the
+    last two, original_length, fast and slow; frequencies: radians a position of each of the
+    rotary_dim / 2 pairs, in the place of base and scaling."""
+    pairs = max(rotary_dim // 2, 0)
+    given = None
+    if frequencies is not None:
+        if len(frequencies) != pairs:
+            raise ValueError(f"frequencies must be {pairs} numbers")
+        given = (ctypes.c_double * pairs)(*frequencies)
+    s = None
+    if scaling is not None:
+        unknown = set(scaling) - {"kind", "factor", "original_length", "fast", "slow"}
+        if unknown or scaling.get("kind") not in ROTARY_KINDS:
+            raise ValueError(f"scaling must be a dict of kind {tuple(ROTARY_KINDS)}, factor, original_length, "
+                             "fast, slow")
+        s = RotaryScaling(ROTARY_KINDS[scaling["kind"]], _int(scaling.get("original_length", 0)),
+                          scaling.get("factor", 1.0), scaling.get("fast", 0.0), scaling.get("slow", 0.0))
+    steps, magnitude = (ctypes.c_uint64 * max(pairs, 1))(), ctypes.c_float()
+    st = lib().asymspec_rotary_steps(rotary_dim, base, None if s is None else ctypes.byref(s), given, steps,
+                                     ctypes.byref(magnitude))
+    if st != OK:
+        raise AsymSpecError(st, "asymspec_rotary_steps")
+    return list(steps), magnitude.value
 
 
 # ----------------------------------------------------------------- PyTorch
@@ -113,6 +185,14 @@ def _int(n) -> int:
     """n for a C int, which would take the low bits of a larger number: past its range the range's
     largest, below zero -1."""
     return n if -1 <= n <= 0x7FFFFFFF else 0x7FFFFFFF if n > 0 else -1
+
+
+def _tokens_of(x) -> int:
+    """The length of a tensor's first axis, for a C int."""
+    T = x.shape[0] if x.dim() else 0
+    if T > 0x7FFFFFFF:
+        raise ValueError("more than 2^31 - 1 tokens")
+    return T
 
 
 def _flat(name, x, dtype, dev, n):
@@ -379,4 +459,216 @@ class CacheAttend:
             0 if error_word is None else _error_word(error_word, dev), _stream(dev))
         if st != OK:
             raise AsymSpecError(st, "asymspec_cache_attend")
+        return out, lse
+
+
+class Rotary:
+    """Rotary positions: the frequencies of a head's pairs, on the device.
+
+    head_dim, rotary_dim (the elements that are turned, from the first on; default all), base,
+    scaling and frequencies as rotary_steps takes them; interleaved: pairs of neighbours, else of
+    the halves; magnitude: in the place of the scaling's.
+
+    ``__call__`` turns q [T, heads, head_dim] and k [T, kv_heads, head_dim] (or None), float32 or
+    bfloat16, any strides with contiguous heads, by positions [T] int32 (negative: a token that stays
+    as it is), and returns (q, k) in new tensors or in q_out, k_out, which may be q and k themselves or
+    must not overlap them.  transpose: by the opposite angle (times the same magnitude): the gradient of
+    q and k from the gradients of the results.
+    """
+
+    def __init__(self, head_dim: int, *, rotary_dim=None, base: float = 10000.0, interleaved: bool = False,
+                 scaling=None, frequencies=None, magnitude=None, device=None):
+        if torch is None:
+            _begin()
+        self.head_dim, self.rotary_dim = head_dim, head_dim if rotary_dim is None else rotary_dim
+        if not 2 <= self.rotary_dim <= head_dim:
+            raise ValueError("rotary_dim must be 2 to head_dim")
+        self.interleaved = bool(interleaved)
+        steps, own = rotary_steps(self.rotary_dim, base, scaling, frequencies)
+        self.magnitude = own if magnitude is None else float(magnitude)
+        # (as signed numbers of the same bits)
+        self.steps = torch.tensor([s - (s >> 63 << 64) for s in steps], dtype=torch.int64,
+                                  device=torch.device("cuda" if device is None else device))
+        self.device_index = self.steps.get_device()
+
+    def _heads(self, name, x, out, T, kind, dev):
+        shape = x.shape
+        if len(shape) != 3 or shape[0] != T or shape[2] != self.head_dim or x.dtype is not kind \
+                or x.get_device() != dev:
+            raise ValueError(f"{name} must be a [{T}, heads, {self.head_dim}] {kind} tensor on cuda:{dev}")
+        s0, s1, s2 = x.stride()
+        if out is None:
+            out = x.new_empty(shape)
+        elif out.shape != shape or out.dtype is not kind or out.get_device() != dev:
+            raise ValueError(f"{name}_out must have the shape, type and device of {name}")
+        o0, o1, o2 = out.stride()
+        if (s2 != 1 or o2 != 1) and self.head_dim > 1:
+            raise ValueError(f"the heads of {name} must be contiguous")
+        return _HEADS.pack(x.data_ptr(), out.data_ptr(), s0, s1, o0, o1, shape[1]), out
+
+    def __call__(self, q, positions, k=None, *, transpose=False, q_out=None, k_out=None):
+        dev, kind = q.get_device(), q.dtype
+        if dev != self.device_index:
+            raise ValueError("q must be on the frequencies' device")
+        if k is None and k_out is not None:
+            raise ValueError("k_out without k")
+        T = _tokens_of(q)
+        dtype = _dtype(q)
+        q_heads, q_out = self._heads("q", q, q_out, T, kind, dev)
+        k_heads = None
+        if k is not None:
+            k_heads, k_out = self._heads("k", k, k_out, T, kind, dev)
+        st = _lib.asymspec_rotary(
+            q_heads, k_heads, T, self.head_dim, self.rotary_dim, self.interleaved, bool(transpose),
+            _flat("positions", positions, torch.int32, dev, T), self.steps.data_ptr(), self.magnitude, dtype,
+            _stream(dev))
+        if st != OK:
+            raise AsymSpecError(st, "asymspec_rotary")
+        return q_out, k_out
+
+
+class Cache4:
+    """A paged key-value cache in 4 bits: codes and scales of the keys and of the values.
+
+    key_codes, value_codes [blocks, block_size, kv_heads, head_dim / 2] uint8, two codes (e2m1) a
+    byte, and key_scales, value_scales [blocks, block_size, kv_heads, head_dim / 16] uint8 or
+    float8_e4m3fn, a scale for each 16 elements; last axes contiguous, the others in any order in memory;
+    key_scale, value_scale: numbers that all elements are times of.  Holds the tensors, no copies.
+    """
+
+    def __init__(self, key_codes, key_scales, value_codes, value_scales, *, key_scale=1.0, value_scale=1.0):
+        if torch is None:
+            _begin()
+        tensors = (key_codes, key_scales, value_codes, value_scales)
+        dev, shape = key_codes.get_device(), key_codes.shape
+        if dev < 0 or len(shape) != 4 or value_codes.shape != shape or any(
+                x.dtype is not torch.uint8 for x in (key_codes, value_codes)):
+            raise ValueError("codes must be CUDA uint8 tensors of one shape [blocks, block_size, kv_heads, head_dim / 2]")
+        of_scales = (*shape[:3], shape[3] // 8)
+        if any(x.shape != of_scales or x.dtype not in (torch.uint8, torch.float8_e4m3fn)
+               for x in (key_scales, value_scales)):
+            raise ValueError(f"scales must be uint8 or float8_e4m3fn tensors of shape {list(of_scales)}")
+        if any(x.get_device() != dev or (x.stride(3) != 1 and x.shape[3] > 1) for x in tensors):
+            raise ValueError("codes and scales must be on one device, each token's of a head contiguous")
+        self.key_codes, self.key_scales, self.value_codes, self.value_scales = tensors
+        self.key_scale, self.value_scale = float(key_scale), float(value_scale)
+        self.device_index = dev
+        self.kv_heads, self.head_dim = shape[2], shape[3] * 2
+        strides = (s if n > 1 else 0 for x in tensors for s, n in zip(x.stride()[:3], x.shape))
+        self.view = _CACHE4.pack(*(x.data_ptr() for x in tensors), *strides, *shape[:3], self.head_dim,
+                                 self.key_scale, self.value_scale)
+
+    @classmethod
+    def zeros(cls, blocks: int, block_size: int, kv_heads: int, head_dim: int, *, key_scale=1.0, value_scale=1.0,
+              device=None):
+        """A pool of zeros in which a block's tokens of one head lie next to one another."""
+        if torch is None:
+            _begin()
+
+        def part(width):
+            return torch.zeros(blocks, kv_heads, block_size, width, dtype=torch.uint8,
+                               device=torch.device("cuda" if device is None else device)).transpose(1, 2)
+
+        return cls(*(part(head_dim // n) for n in (2, 16, 2, 16)), key_scale=key_scale, value_scale=value_scale)
+
+
+def _tokens(name, x, cache, kind, T):
+    """The strides of `x`: [T, kv_heads, head_dim] like the cache's heads, which are contiguous."""
+    shape = x.shape
+    if x.dtype is not kind or x.get_device() != cache.device_index or shape != (T, cache.kv_heads, cache.head_dim) \
+            or x.stride(2) != 1:
+        raise ValueError(f"{name} must be a [{T}, {cache.kv_heads}, {cache.head_dim}] {kind} tensor like the cache, "
+                         "heads contiguous")
+    s0, s1, _ = x.stride()
+    return _STRIDES2.pack(s0, s1)
+
+
+def cache4_write(k, v, cache, slots, *, error_word=None):
+    """Writes k, v [T, kv_heads, head_dim], float32 or bfloat16, into a cache in 4 bits at slots [T]
+    int64; negative slots are skipped.  (include/asymspec_serving.h says how they are rounded.)"""
+    dev, T, kind = cache.device_index, _tokens_of(k), k.dtype
+    st = _lib.asymspec_cache4_write(
+        cache.view, k.data_ptr(), v.data_ptr(), _dtype(k), _tokens("k", k, cache, kind, T),
+        _tokens("v", v, cache, kind, T), _flat("slots", slots, torch.int64, dev, T), T,
+        0 if error_word is None else _error_word(error_word, dev), _stream(dev))
+    if st != OK:
+        raise AsymSpecError(st, "asymspec_cache4_write")
+
+
+def cache4_read(cache, slots, *, dtype=None, out=None, error_word=None):
+    """(k, v) [T, kv_heads, head_dim] of a cache in 4 bits at slots [T] int64, of `dtype` (float32 or
+    bfloat16, the default) or in the tensors `out`; negative slots give zeros."""
+    dev, T = cache.device_index, _tokens_of(slots)
+    if out is None:
+        shape = (T, cache.kv_heads, cache.head_dim)
+        like = cache.key_codes
+        k, v = (like.new_empty(shape, dtype=torch.bfloat16 if dtype is None else dtype) for _ in range(2))
+    else:
+        k, v = out
+        if dtype is not None and k.dtype is not dtype:
+            raise ValueError(f"out must be of {dtype}")
+    st = _lib.asymspec_cache4_read(
+        cache.view, _flat("slots", slots, torch.int64, dev, T), T, k.data_ptr(), v.data_ptr(), _dtype(k),
+        _tokens("k", k, cache, k.dtype, T), _tokens("v", v, cache, k.dtype, T),
+        0 if error_word is None else _error_word(error_word, dev), _stream(dev))
+    if st != OK:
+        raise AsymSpecError(st, "asymspec_cache4_read")
+    return k, v
+
+
+class Cache4Attend:
+    """CacheAttend over a cache in 4 bits: holds a workspace for up to B_max requests with Q_max
+    queries each.
+
+    ``__call__`` takes q [B, Q, heads, head_dim], float32 or bfloat16, a Cache4, tables [B, width]
+    int32 and lens [B] int32 and returns (out like q, lse [B, Q, heads] float32); everything else as
+    CacheAttend has it.
+    """
+
+    def __init__(self, B_max: int, Q_max: int, heads: int, kv_heads: int, head_dim: int, device=None):
+        if torch is None:
+            _begin()
+        self.B_max, self.Q_max = B_max, Q_max
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.nbytes = cache4_attend_workspace_bytes(B_max, Q_max, heads, kv_heads, head_dim)
+        if self.nbytes == 0:
+            raise ValueError("no attention of this shape")
+        self.workspace = torch.empty(self.nbytes, dtype=torch.uint8,
+                                     device=torch.device("cuda" if device is None else device))
+        self.device_index = self.workspace.get_device()
+        self.scale = 1.0 / math.sqrt(head_dim)
+
+    def __call__(self, q, cache, tables, lens, *, scale=None, window=0, out=None, lse=None, error_word=None):
+        dev = cache.device_index
+        B, Q, heads, dim = shape = q.shape
+        kind = q.dtype
+        if dev != self.device_index:
+            raise ValueError("the cache must be on the workspace's device")
+        if B > self.B_max or Q > self.Q_max or (heads, cache.kv_heads, cache.head_dim) != (
+                self.heads, self.kv_heads, self.head_dim):
+            raise ValueError("batch does not fit this workspace")
+        q0, q1, q2, q3 = q.stride()
+        if q.get_device() != dev or q3 != 1 or dim != self.head_dim:
+            raise ValueError("q must be [B, Q, heads, head_dim] like the cache, heads contiguous")
+        dtype = _dtype(q)
+        if out is None:
+            out = q.new_empty(shape)
+            o0, o1, o2 = Q * heads * dim, heads * dim, dim
+        else:
+            o0, o1, o2, o3 = out.stride()
+            if out.dtype is not kind or out.get_device() != dev or out.shape != shape or o3 != 1:
+                raise ValueError("out must be [B, Q, heads, head_dim] like q, heads contiguous")
+        if lse is None:
+            lse = q.new_empty((B, Q, heads), dtype=torch.float32)
+            l = lse.data_ptr()
+        else:
+            l = _flat("lse", lse, torch.float32, dev, B * Q * heads)
+        t, t_ld, width = _rows("tables", tables, torch.int32, dev, B)
+        st = _lib.asymspec_cache4_attend(
+            cache.view, q.data_ptr(), dtype, _STRIDES3.pack(q0, q1, q2), B, Q, heads, t, t_ld, width,
+            _flat("lens", lens, torch.int32, dev, B), self.scale if scale is None else scale, _int(window),
+            out.data_ptr(), _STRIDES3.pack(o0, o1, o2), l, self.workspace.data_ptr(), self.nbytes,
+            0 if error_word is None else _error_word(error_word, dev), _stream(dev))
+        if st != OK:
+            raise AsymSpecError(st, "asymspec_cache4_attend")
         return out, lse
