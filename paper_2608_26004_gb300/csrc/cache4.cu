@@ -181,13 +181,27 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
   p.err = out_error_word;
   P.codes[0] = static_cast<const char*>(cache->key_codes), P.codes[1] = static_cast<const char*>(cache->value_codes);
   P.scales[0] = static_cast<const char*>(cache->key_scales), P.scales[1] = static_cast<const char*>(cache->value_scales);
+  const int64_t* codes[2] = {cache->key_code_strides, cache->value_code_strides};
+  const int64_t* scales[2] = {cache->key_scale_strides, cache->value_scale_strides};
   const size_t scale_row = k.DP / 16;
-  P.wide_scales = p.D == k.DP && aligned(P.scales[0], scale_row) && aligned(P.scales[1], scale_row);
-  for (int i = 0; i < 3; ++i) {
-    P.cs[0][i] = cache->key_code_strides[i], P.cs[1][i] = cache->value_code_strides[i];
-    P.ss[0][i] = cache->key_scale_strides[i], P.ss[1][i] = cache->value_scale_strides[i];
-    for (int w = 0; w < 2; ++w) P.wide_scales = P.wide_scales && P.ss[w][i] % static_cast<int64_t>(scale_row) == 0;
+  P.wide_scales = P.wide_codes = p.D == k.DP;
+  for (int w = 0; w < 2; ++w) {
+    P.head_codes[w] = codes[w][2], P.head_scales[w] = scales[w][2];
+    for (int i = 0; i < 2; ++i) {
+      if (codes[w][i] > kMax32 || scales[w][i] > kMax32) return ASYMSPEC_ERR_TOO_LARGE;
+      P.codes_of[w][i] = static_cast<unsigned>(codes[w][i]), P.scales_of[w][i] = static_cast<unsigned>(scales[w][i]);
+    }
+    P.wide_scales = P.wide_scales && aligned(P.scales[w], scale_row);
+    P.wide_codes = P.wide_codes && aligned(P.codes[w], 32);
+    for (int i = 0; i < 3; ++i) {
+      P.wide_scales = P.wide_scales && scales[w][i] % static_cast<int64_t>(scale_row) == 0;
+      P.wide_codes = P.wide_codes && codes[w][i] % 32 == 0;
+    }
   }
+  // For keys below 2^30 and a block size n <= 2^s, d = ceil(2^(31 + s) / n) gives key / n = key * d >> (31 + s): d n is
+  // less than n above 2^(31 + s), and key times that less than 2^(31 + s).
+  while ((1ll << P.shift) < p.block_size) ++P.shift;
+  P.divide = static_cast<unsigned>(((1ull << (31 + P.shift)) + p.block_size - 1) / p.block_size);
   P.value_scale = cache->value_scale;
   int device = 0, sms = 0;
   cudaError_t e = device_sms(&device, &sms);

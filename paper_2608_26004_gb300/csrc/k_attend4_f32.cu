@@ -16,16 +16,16 @@ AttendKernels attend4_pick() {
 
 AttendKernels attend4_kernels_f32(int D, int rows) {
   if (D <= 64)
-    return rows <= 8    ? attend4_pick<64, 1, 1, 4, 3>()
-           : rows <= 16 ? attend4_pick<64, 2, 1, 4, 3>()
-           : rows <= 32 ? attend4_pick<64, 2, 2, 4, 2>()
-                        : attend4_pick<64, 2, 4, 4, 1>();
+    return rows <= 8    ? attend4_pick<64, 1, 1, 3, 3>()
+           : rows <= 16 ? attend4_pick<64, 2, 1, 3, 3>()
+           : rows <= 32 ? attend4_pick<64, 2, 2, 3, 2>()
+                        : attend4_pick<64, 2, 4, 3, 1>();
   if (D <= 128)
-    return rows <= 8    ? attend4_pick<128, 1, 1, 4, 3>()
-           : rows <= 16 ? attend4_pick<128, 2, 1, 4, 2>()
-           : rows <= 32 ? attend4_pick<128, 2, 2, 4, 1>()
-                        : attend4_pick<128, 2, 4, 4, 1>();
-  return rows <= 8 ? attend4_pick<256, 1, 1, 4, 2>() : attend4_pick<256, 2, 1, 4, 1>();
+    return rows <= 8    ? attend4_pick<128, 1, 1, 3, 3>()
+           : rows <= 16 ? attend4_pick<128, 2, 1, 3, 2>()
+           : rows <= 32 ? attend4_pick<128, 2, 2, 3, 1>()
+                        : attend4_pick<128, 2, 4, 3, 1>();
+  return rows <= 8 ? attend4_pick<256, 1, 1, 2, 2>() : attend4_pick<256, 2, 1, 3, 1>();
 }
 
 }  // namespace asymspec_impl

@@ -32,7 +32,7 @@ struct AttendParams {
 constexpr int kAGroups = 4;                 // groups of warps, each with keys of its own
 constexpr int kAKeys = 16;                  // keys of a group's step
 constexpr int kATile = kAGroups * kAKeys;   // keys of a CTA's step, the unit of the split
-constexpr int kAMaxCtas = 456;              // CTAs that share the work (up to three on each of 152 SMs)
+constexpr int kAMaxCtas = 608;              // CTAs that share the work (up to four on each of 152 SMs)
 constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each

@@ -10,9 +10,13 @@ struct Attend4Params {
   AttendParams a;  // (its keys, values and their strides are not read)
   const char* codes[2];
   const char* scales[2];
-  int64_t cs[2][3], ss[2][3];  // bytes
+  int64_t head_codes[2], head_scales[2];          // strides in bytes: of heads,
+  unsigned codes_of[2][2], scales_of[2][2];  // and of blocks and tokens
   float value_scale;
+  unsigned divide;  // key / block_size is the high half of 2 key * divide, shifted
+  int shift;
   bool wide_scales;  // a token's scales of a head are DP / 16 bytes on such boundaries
+  bool wide_codes;   // its codes DP / 2 bytes on 32-byte boundaries
 };
 
 // 8x8 elements of 16 bits, a row to four lanes, into its columns.
@@ -28,29 +32,46 @@ __device__ __forceinline__ unsigned pack_f16(float x, float y) {
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0,
                                         unsigned b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// The bits of x where those of m are set, of y elsewhere.
-__device__ __forceinline__ unsigned select_bits(unsigned m, unsigned x, unsigned y) { return (x & m) | (y & ~m); }
+// The bits of x where those of m are set, of y elsewhere (as one instruction, which the compiler did not find).
+__device__ __forceinline__ unsigned select_bits(unsigned m, unsigned x, unsigned y) {
+  unsigned r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xCA;" : "=r"(r) : "r"(m), "r"(x), "r"(y));
+  return r;
+}
+// p + n * size.
+__device__ __forceinline__ const char* stepped(const char* p, int n, unsigned size) {
+  return p + static_cast<uint64_t>(static_cast<unsigned>(n)) * size;
+}
 __device__ __forceinline__ void cp_async16(unsigned smem, const void* gmem) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
 }
+// N = 4, 8 or 16 bytes, or with bytes = 0 zeros (the address is then not read).
+template <int N>
+__device__ __forceinline__ void cp_async_or_zero(unsigned smem, const void* gmem, int bytes) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(bytes) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(smem), "l"(gmem), "n"(N), "r"(bytes) : "memory");
+}
 
-// Dynamic shared memory.  A step of a group: 16 keys' codes, 16 values' codes in rows 16 bytes
-// longer than they are (lanes read the rows 2 t of their own then without meeting a bank twice), and both's
-// scales.  Where an item ends, the group's ring takes its rows' values.
-__host__ __device__ constexpr int attend4_step_bytes(int DP) { return kAKeys * (DP / 2 + DP / 2 + 16 + DP / 8); }
+// Dynamic shared memory.  A group's step is kASubs times 16 keys: their codes, their values' codes in rows
+// 16 bytes longer than they are (lanes read the rows 2 t of their own then without meeting a bank twice), and
+// both's scales, in rows 4 bytes longer where they begin off the boundaries.  Where an item ends, the
+// group's ring takes its rows' values.
+constexpr int kASubs = 2;
+__host__ __device__ constexpr int attend4_sub_bytes(int DP) { return kAKeys * (DP / 2 + DP / 2 + 16 + DP / 8 + 8); }
 __host__ __device__ constexpr int attend4_group_bytes(int DP, int rows, int ST) {
-  return ST * attend4_step_bytes(DP) > rows * DP * 4 ? ST * attend4_step_bytes(DP) : rows * DP * 4;
+  const int ring = ST * kASubs * attend4_sub_bytes(DP);
+  return ring > rows * DP * 4 ? ring : rows * DP * 4;
 }
 __host__ __device__ constexpr int attend4_query_pitch(int DP) { return DP * 2 + 16; }
 constexpr size_t attend4_smem_bytes(int DP, int rows, int ST, int pieces) {
   return static_cast<size_t>(kAGroups) * attend4_group_bytes(DP, rows, ST) +
-         static_cast<size_t>(rows) * (attend4_query_pitch(DP) * pieces + 4) + kAGroups * ST * 4 +
+         static_cast<size_t>(rows) * (attend4_query_pitch(DP) * pieces + 4) + kAGroups * ST * 16 + 16 +
          static_cast<size_t>(kAGroups) * rows * 8 + kAGroups * 8 * 8 + 32;
 }
 
@@ -89,14 +110,15 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
   constexpr int kWarpRows = 8 * NT, kRows = kWarpRows * WR;
   constexpr int kKeyRow = DP / 2, kValueRow = DP / 2 + 16, kScaleRow = DP / 16;
   constexpr int kValues = kAKeys * kKeyRow, kScales = kValues + kAKeys * kValueRow;
-  constexpr int kStep = attend4_step_bytes(DP), kGroup = attend4_group_bytes(DP, kRows, ST);
+  constexpr int kSub = attend4_sub_bytes(DP), kStep = kASubs * kSub, kGroup = attend4_group_bytes(DP, kRows, ST);
   constexpr int kQPitch = attend4_query_pitch(DP);
   constexpr int KW = DP / 32;  // words of a lane's part of a key
   constexpr int VW = DP / 64;  // words of a lane's part of a value
   constexpr int MT = DP / 16;  // tiles of 16 elements of a head
-  constexpr int kChunks = DP / 32;                     // 16-byte chunks of a key
-  constexpr bool kBoth = kAKeys * kChunks >= 32 * WR;  // a lane loads of keys and of values
-  constexpr int kLaneKeys = kBoth ? kAKeys * kChunks / (32 * WR) : 1;
+  constexpr int kChunks = DP / 32;                 // 16-byte chunks of a key
+  constexpr int kLaneRows = 32 * WR / kChunks;     // keys that the group's lanes load at once
+  constexpr int kLoads = kASubs * kAKeys > kLaneRows ? kASubs * kAKeys / kLaneRows : 1;
+  constexpr int U = NT == 1 ? kASubs : 1;          // sixteens of keys that are worked at together
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
   constexpr float kBelow = 7.f, kSlack = 8.f;
   constexpr bool kQRegs = kPieces * NT * KW * 4 <= 32;
@@ -106,12 +128,13 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
   unsigned char* at_q = a_smem + kAGroups * kGroup;
   float* s_factor = reinterpret_cast<float*>(at_q + kRows * kQPitch * kPieces);
   float* s_ml = s_factor + kRows;
-  unsigned* masks0 = reinterpret_cast<unsigned*>(s_ml + kAGroups * kRows * 2);
-  int64_t* s_scan = reinterpret_cast<int64_t*>((reinterpret_cast<uintptr_t>(masks0 + kAGroups * ST) + 7) & ~uintptr_t(7));
+  uint4* masks0 = reinterpret_cast<uint4*>((reinterpret_cast<uintptr_t>(s_ml + kAGroups * kRows * 2) + 15) & ~uintptr_t(15));
+  int64_t* s_scan = reinterpret_cast<int64_t*>(masks0 + kAGroups * ST);
   int64_t* s_find = s_scan + kWarpsN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const int group = warp / WR, wr = warp % WR;  // whose keys; which rows
-  unsigned* masks = masks0 + group * ST;
+  // of a step's sixteens of keys: keys that exist; scales that begin off the 4-byte boundaries
+  unsigned* masks = reinterpret_cast<unsigned*>(masks0 + group * ST);
   unsigned char* ring = a_smem + group * kGroup;
   const unsigned ring_at = smem_u32(ring);
   const int c = blockIdx.x, ctas = gridDim.x;
@@ -174,16 +197,14 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     info->tiles = at_unit > kAItem ? n_tiles : 0;
   }
 
-  // what this lane loads of a step: chunk `chunk` of keys load_key + i * kLaneRows (kBoth: and of their
-  // values; else of the keys or of the values), and lanes of the group's first warp the scales of
-  // key lane % 16, or of its value
-  constexpr int kLaneRows = 32 * WR / kChunks;
+  // what this lane loads of a step: chunk `chunk` of keys load_row + i * kLaneRows and of their values;
+  // and of each sixteen the scales of key lane % 16, or of its value
   const int lane_id = wr * 32 + lane;
-  const int chunk = lane_id % kChunks, load_key = lane_id / kChunks % kAKeys;
-  const int load_what = lane_id / kChunks / kAKeys;  // (kBoth: 0)
-  const bool chunk_on = chunk * 32 < p.D;
+  const int chunk = lane_id % kChunks, load_row = lane_id / kChunks;
+  const bool chunk_on = chunk * 32 < p.D && load_row < kASubs * kAKeys;
   const int what = lane >> 4;
-  const int step_blocks = kATile / p.block_size, step_rest = kATile % p.block_size;
+  const unsigned scales_block = P.scales_of[what][0], scales_token = P.scales_of[what][1];
+  const int scale_row = P.wide_scales ? kScaleRow : kScaleRow + 4;
 
   float O[NT][MT][4], m[NT][2], l[NT][2], factor[NT][2];
   unsigned qf[kQRegs ? kPieces : 1][kQRegs ? NT : 1][kQRegs ? KW : 1][4];
@@ -202,94 +223,83 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * kRows;
     const int lo = attend_first(p, len);
     const int rows = min(kRows, p.rows - R0);  // of the item
-    const char* key_codes = P.codes[0] + kh * P.cs[0][2];
-    const char* value_codes = P.codes[1] + kh * P.cs[1][2];
+    const char* key_codes = P.codes[0] + kh * P.head_codes[0] + chunk * 16;
+    const char* value_codes = P.codes[1] + kh * P.head_codes[1] + chunk * 16;
+    const char* scales = P.scales[what] + kh * P.head_scales[what];
     const int32_t* table = p.tables + b * p.table_ld;
     const int k_group = lo + group * kAKeys;  // the group's first key of tile 0
 
-    // the next step to load: its first key, and that key's block and place there
+    // the next step to load: its first key, and the blocks of the keys that this lane loads of it
     int next_key = k_group + t0 * kATile;
-    int next_block = next_key / p.block_size, next_at = next_key % p.block_size;
     const int end_key = min(len, lo + t1 * kATile);
     struct Place {
       int page, at;
     };
-    auto place = [&](int r) {  // of the next step's key r
-      Place x = {INT_MIN, next_at + r};
-      int block = next_block;
-      if (x.at >= p.block_size) {
-        const int more = static_cast<unsigned>(x.at) / static_cast<unsigned>(p.block_size);
-        block += more;
-        x.at -= more * p.block_size;
-      }
-      if (next_key + r < end_key) x.page = __ldg(table + block);
-      return x;
+    auto place = [&](int key) {
+      const int block = static_cast<int>(__umulhi(2u * static_cast<unsigned>(key), P.divide) >> P.shift);
+      return Place{key < end_key ? __ldg(table + block) : INT_MIN, key - block * p.block_size};
     };
-    Place places[kLaneKeys], scale_place;
-    int scale_key;
-    auto find = [&] {  // the next step's blocks
+    Place places[kLoads], scale_places[kASubs];
+    auto find = [&] {
 #pragma unroll
-      for (int i = 0; i < kLaneKeys; ++i) places[i] = place(load_key + i * kLaneRows);
-      if (wr == 0) scale_place = place(lane & 15);
-      scale_key = next_key + (lane & 15);
-      next_key += kATile;
-      next_block += step_blocks;
-      next_at += step_rest;
-      if (next_at >= p.block_size) next_at -= p.block_size, ++next_block;
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = load_row + i * kLaneRows;
+        places[i] = place(next_key + r % kAKeys + r / kAKeys * kATile);
+      }
+#pragma unroll
+      for (int s = 0; s < kASubs; ++s)
+        if (WR == 1 || wr == s) scale_places[s] = place(next_key + (lane & 15) + s * kATile);
+      next_key += kASubs * kATile;
     };
     auto there = [&](int page) { return static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks); };
-    unsigned sc[VW];      // the scales on their way
-    unsigned sc_live = 0;
     auto issue = [&](int stage) {
       const unsigned at = ring_at + stage * kStep;
 #pragma unroll
-      for (int i = 0; i < kLaneKeys; ++i) {
-        const int r = load_key + i * kLaneRows;
-        if (!there(places[i].page) || !chunk_on) continue;
-        if (kBoth || load_what == 0)
-          cp_async16(at + r * kKeyRow + chunk * 16, key_codes + chunk * 16 + places[i].page * P.cs[0][0] + places[i].at * P.cs[0][1]);
-        if (kBoth || load_what == 1)
-          cp_async16(at + kValues + r * kValueRow + chunk * 16,
-                     value_codes + chunk * 16 + places[i].page * P.cs[1][0] + places[i].at * P.cs[1][1]);
-      }
-      cp_async_commit();
-      if (wr == 0) {
-        const bool on = there(scale_place.page);
-        sc_live = __ballot_sync(~0u, on) & 0xFFFFu;
-        // (up to 15 keys are before the window of every query: their block may be gone)
-        if (!on && scale_key < end_key && (p.window == 0 || scale_key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
-#pragma unroll
-        for (int i = 0; i < VW; ++i) sc[i] = 0;
-        if (on) {
-          const char* from = P.scales[what] + kh * P.ss[what][2] + scale_place.page * P.ss[what][0] +
-                             scale_place.at * P.ss[what][1];
-          if (P.wide_scales) {
-            load_words<VW>(reinterpret_cast<const unsigned char*>(from), sc);
-          } else {
-#pragma unroll
-            for (int i = 0; i < VW; ++i) {
-              if (i * 64 < p.D) sc[i] = *reinterpret_cast<const uint16_t*>(from + 4 * i);
-              if (i * 64 + 32 < p.D) sc[i] |= static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(from + 4 * i + 2)) << 16;
-            }
-          }
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = load_row + i * kLaneRows;
+        const Place x = places[i];
+        if (there(x.page) && chunk_on) {
+          const unsigned to = at + r / kAKeys * kSub + chunk * 16;
+          cp_async16(to + r % kAKeys * kKeyRow,
+                     stepped(stepped(key_codes, x.page, P.codes_of[0][0]), x.at, P.codes_of[0][1]));
+          cp_async16(to + kValues + r % kAKeys * kValueRow,
+                     stepped(stepped(value_codes, x.page, P.codes_of[1][0]), x.at, P.codes_of[1][1]));
         }
       }
-    };
-    // the scales of the step issued last, into the ring
-    auto settle = [&](int stage) {
-      if (wr == 0) {
-        unsigned char* to = ring + stage * kStep + kScales + what * (kAKeys * kScaleRow) + (lane & 15) * kScaleRow;
-        if constexpr (VW == 4) *reinterpret_cast<uint4*>(to) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
-        else if constexpr (VW == 2) *reinterpret_cast<uint2*>(to) = make_uint2(sc[0], sc[1]);
-        else *reinterpret_cast<unsigned*>(to) = sc[0];
-        if (lane == 0) masks[stage] = sc_live;
+#pragma unroll
+      for (int s = 0; s < kASubs; ++s) {
+        if (WR > 1 && wr != s) continue;
+        const Place x = scale_places[s];
+        const bool on = there(x.page);
+        const unsigned live = __ballot_sync(~0u, on) & 0xFFFFu;
+        // (up to 15 keys are before the window of every query: their block may be gone)
+        if (!on) {
+          const int key = next_key - kASubs * kATile + (lane & 15) + s * kATile;
+          if (key < end_key && (p.window == 0 || key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
+        }
+        // zeros for a key that does not exist: its codes are what the memory held, finite in any case
+        const char* from = scales;
+        if (on) from = stepped(stepped(from, x.page, scales_block), x.at, scales_token);
+        const unsigned to = at + s * kSub + kScales + lane * scale_row;  // (row lane: values' after the keys')
+        if (P.wide_scales) {
+          cp_async_or_zero<kScaleRow>(to, from, on ? kScaleRow : 0);
+        } else {
+          const int off = static_cast<int>(reinterpret_cast<uintptr_t>(from) & 2);
+          from -= off;
+#pragma unroll
+          for (int i = 0; i <= VW; ++i)  // (words that hold some of them)
+            if (4 * i < off + p.D / 16) cp_async_or_zero<4>(to + 4 * i, from + 4 * i, on ? 4 : 0);
+          const unsigned odd = __ballot_sync(~0u, off != 0);
+          if (lane == 0) masks[4 * stage + 2 + s] = odd;
+        }
+        if (lane == 0) masks[4 * stage + s] = live;
       }
+      cp_async_commit();
     };
     find();
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) {
       issue(s);
-      if (s < ST - 2) settle(s);
       find();
     }
 
@@ -355,118 +365,146 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     }
 
     int stage = 0;
-    for (int t = t0; t < t1; ++t) {
-      settle(stage < 2 ? stage + ST - 2 : stage - 2);
+    for (int t = t0; t < t1; t += kASubs) {
       cp_async_wait<ST - 2>();
       // the group's warps have loaded the step, and are done with the one before
       if constexpr (WR > 1) group_barrier(1 + group, WR * 32);
       else __syncwarp();
       issue(stage == 0 ? ST - 1 : stage - 1);
       find();
-      const unsigned char* st = ring + stage * kStep;
-      const unsigned live = masks[stage];
-      const int k0 = k_group + t * kATile;
-      if (live != 0 && warp_rows > 0) {
+#pragma unroll 1
+      for (int s0 = 0; s0 < kASubs; s0 += U) {
+        const unsigned char* st = ring + stage * kStep + s0 * kSub;
+        unsigned live[U], any = 0;
+#pragma unroll
+        for (int u2 = 0; u2 < U; ++u2) any |= live[u2] = masks[4 * stage + s0 + u2];
+        const int k0 = k_group + (t + s0) * kATile;  // (and kATile further for the second)
+        if (any == 0 || warp_rows <= 0) continue;
         // scores of keys g and g + 8 (rows of the products) and of queries 2 t4 and 2 t4 + 1: a
         // lane's part of a key are DP / 4 elements in a row
-        float S[NT][4];
+        float S[U][NT][4];
         {
-          unsigned ka[KW], kb[KW], sa[VW], sb[VW];
-          load_words<KW>(st + g * kKeyRow + t4 * (DP / 8), ka);
-          load_words<KW>(st + (g + 8) * kKeyRow + t4 * (DP / 8), kb);
-          const unsigned char* sk = st + kScales + g * kScaleRow + t4 * VW;
-          if constexpr (VW == 1) {
-            const unsigned x = sk[0], y = sk[8 * kScaleRow];
-            sa[0] = e4m3_to_f16(x | x << 8);
-            sb[0] = e4m3_to_f16(y | y << 8);
-          } else {
+          unsigned ka[U][KW], kb[U][KW], sa[U][VW], sb[U][VW];
 #pragma unroll
-            for (int i = 0; i < VW; i += 2) {
-              const unsigned x = e4m3_to_f16(*reinterpret_cast<const uint16_t*>(sk + i));
-              const unsigned y = e4m3_to_f16(*reinterpret_cast<const uint16_t*>(sk + 8 * kScaleRow + i));
-              sa[i] = __byte_perm(x, x, 0x1010), sa[i + 1] = __byte_perm(x, x, 0x3232);
-              sb[i] = __byte_perm(y, y, 0x1010), sb[i + 1] = __byte_perm(y, y, 0x3232);
+          for (int y = 0; y < U; ++y) {
+            const unsigned char* sub = st + y * kSub;
+            load_words<KW>(sub + g * kKeyRow + t4 * (DP / 8), ka[y]);
+            load_words<KW>(sub + (g + 8) * kKeyRow + t4 * (DP / 8), kb[y]);
+            const unsigned char* sk = sub + kScales + g * scale_row + t4 * VW;
+            const unsigned char* sl = sk + 8 * scale_row;
+            if (!P.wide_scales) {
+              const unsigned odd = masks[4 * stage + 2 + s0 + y];
+              sk += (odd >> g & 1u) * 2;
+              sl += (odd >> (g + 8) & 1u) * 2;
             }
-          }
-          float more[BF ? 1 : NT][4], small[BF ? 1 : NT][4];
+            if constexpr (VW == 1) {
+              const unsigned v = t4 * 16 < p.D ? sk[0] : 0u, w = t4 * 16 < p.D ? sl[0] : 0u;
+              sa[y][0] = e4m3_to_f16(v | v << 8);
+              sb[y][0] = e4m3_to_f16(w | w << 8);
+            } else {
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              S[n][e] = 0.f;
-              if constexpr (!BF) more[n][e] = small[n][e] = 0.f;
-            }
-#pragma unroll
-          for (int w = 0; w < KW; ++w) {
-            unsigned fa[4], fb[4];
-            e2m1_to_f16(ka[w], fa);
-            e2m1_to_f16(kb[w], fb);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              fa[i] = mul_f16x2(fa[i], sa[w / 2]);
-              fb[i] = mul_f16x2(fb[i], sb[w / 2]);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              unsigned x[4];
-              if constexpr (kQRegs) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = qf[0][n][w][i];
-              } else {
-                query(0, n, w, x);
-              }
-              mma_f16(S[n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
-              if constexpr (BF) {
-                mma_f16(S[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
-              } else {
-                // (the matrix unit's running sums are cut, not rounded: short ones, added up in fp32)
-                mma_f16(more[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
-                if constexpr (kQRegs) {
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) x[i] = qf[kPieces - 1][n][w][i];
-                } else {
-                  query(1, n, w, x);
-                }
-                mma_f16(small[n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
-                mma_f16(small[n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+              for (int i = 0; i < VW; i += 2) {
+                // (a lane's part of a key, or its half, is of the head or past it)
+                const bool on = P.wide_scales || t4 * (DP / 4) + i * 16 < p.D;
+                const unsigned v = e4m3_to_f16(on ? *reinterpret_cast<const uint16_t*>(sk + i) : 0u);
+                const unsigned w = e4m3_to_f16(on ? *reinterpret_cast<const uint16_t*>(sl + i) : 0u);
+                sa[y][i] = __byte_perm(v, v, 0x1010), sa[y][i + 1] = __byte_perm(v, v, 0x3232);
+                sb[y][i] = __byte_perm(w, w, 0x1010), sb[y][i + 1] = __byte_perm(w, w, 0x3232);
               }
             }
           }
-          if constexpr (!BF) {
+          float more[BF ? 1 : U][NT][4], small[BF ? 1 : U][NT][4];
+#pragma unroll
+          for (int y = 0; y < U; ++y)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) S[n][e] += more[n][e] + small[n][e];
+              for (int e = 0; e < 4; ++e) {
+                S[y][n][e] = 0.f;
+                if constexpr (!BF) more[y][n][e] = small[y][n][e] = 0.f;
+              }
+#pragma unroll
+          for (int w = 0; w < KW; ++w)
+#pragma unroll
+            for (int y = 0; y < U; ++y) {
+              unsigned fa[4], fb[4];
+              e2m1_to_f16(ka[y][w], fa);
+              e2m1_to_f16(kb[y][w], fb);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                fa[i] = mul_f16x2(fa[i], sa[y][w / 2]);
+                fb[i] = mul_f16x2(fb[i], sb[y][w / 2]);
+              }
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                unsigned x[4];
+                if constexpr (kQRegs) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) x[i] = qf[0][n][w][i];
+                } else {
+                  query(0, n, w, x);
+                }
+                mma_f16(S[y][n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
+                if constexpr (BF) {
+                  mma_f16(S[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                } else {
+                  // (the matrix unit's running sums are cut, not rounded: short ones, added up in fp32)
+                  mma_f16(more[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                  if constexpr (kQRegs) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = qf[kPieces - 1][n][w][i];
+                  } else {
+                    query(1, n, w, x);
+                  }
+                  mma_f16(small[y][n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
+                  mma_f16(small[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                }
+              }
+            }
+          if constexpr (!BF) {
+#pragma unroll
+            for (int y = 0; y < U; ++y)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[y][n][e] += more[y][n][e] + small[y][n][e];
           }
         }
-        const bool whole = live == 0xFFFFu && k0 + kAKeys - 1 <= least && k0 >= from;
+        bool whole = k0 + (U - 1) * kATile + kAKeys - 1 <= least && k0 >= from;
+#pragma unroll
+        for (int y = 0; y < U; ++y) whole = whole && live[y] == 0xFFFFu;
         // Weights are 2^(s - m), m kBelow below the largest score at the time; only a score kSlack above
         // that raises it (the maximum itself, kept, would rescale the values at most steps, for one
         // of the rows or another).  So weights stay below 2^15, and fp16, whose step is 2^-24 at the
         // smallest, holds one of 2^-31 of a row's largest.
         bool above = false;
+        float top[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+            top[n][e] = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float& s = S[n][2 * k + e];
-              s *= factor[n][e];
-              if (!whole) {
-                const int j = k0 + g + 8 * k;
-                const bool seen = ((live >> (g + 8 * k)) & 1u) && j <= last[n][e] && (p.window == 0 || j > last[n][e] - p.window);
-                s = seen ? s : -INFINITY;
+            for (int y = 0; y < U; ++y)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                float& s = S[y][n][2 * k + e];
+                s *= factor[n][e];
+                if (!whole) {
+                  const int j = k0 + y * kATile + g + 8 * k;
+                  const bool seen = ((live[y] >> (g + 8 * k)) & 1u) && j <= last[n][e] && (p.window == 0 || j > last[n][e] - p.window);
+                  s = seen ? s : -INFINITY;
+                }
+                top[n][e] = fmaxf(top[n][e], s);
               }
-            }
-            above = above || fmaxf(S[n][e], S[n][2 + e]) > m[n][e] + (kBelow + kSlack);
+            above = above || top[n][e] > m[n][e] + (kBelow + kSlack);
           }
         if (__any_sync(~0u, above)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float v = fmaxf(S[n][e], S[n][2 + e]);
+              float v = top[n][e];
               v = fmaxf(v, __shfl_xor_sync(~0u, v, 4));
               v = fmaxf(v, __shfl_xor_sync(~0u, v, 8));
               v = fmaxf(v, __shfl_xor_sync(~0u, v, 16));
@@ -482,43 +520,58 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
             }
         }
         // weights, turned so that queries are the columns of the second products
-        unsigned w0[kPieces][NT], w1[kPieces][NT];
+        unsigned wt[U][kPieces][NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float ref = m[n][e] == -INFINITY ? 0.f : m[n][e];
-            S[n][e] = ex2(S[n][e] - ref);
-            S[n][2 + e] = ex2(S[n][2 + e] - ref);
-            l[n][e] += S[n][e] + S[n][2 + e];
-          }
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const unsigned hi = pack_f16(S[n][2 * k], S[n][2 * k + 1]);
-            (k ? w1 : w0)[0][n] = transposed(hi);
-            if constexpr (!BF) {
-              const float2 x = f16x2_to_f32(hi);
-              (k ? w1 : w0)[kPieces - 1][n] = transposed(pack_f16(S[n][2 * k] - x.x, S[n][2 * k + 1] - x.y));
+            for (int y = 0; y < U; ++y) {
+              S[y][n][e] = ex2(S[y][n][e] - ref);
+              S[y][n][2 + e] = ex2(S[y][n][2 + e] - ref);
+              l[n][e] += S[y][n][e] + S[y][n][2 + e];
             }
           }
+#pragma unroll
+          for (int y = 0; y < U; ++y)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const unsigned hi = pack_f16(S[y][n][2 * k], S[y][n][2 * k + 1]);
+              wt[y][0][n][k] = transposed(hi);
+              if constexpr (!BF) {
+                const float2 x = f16x2_to_f32(hi);
+                wt[y][kPieces - 1][n][k] = transposed(pack_f16(S[y][n][2 * k] - x.x, S[y][n][2 * k + 1] - x.y));
+              }
+            }
         }
         // values: of keys 2 t4, 2 t4 + 1 and those + 8, the lane's DP / 8 elements in a row from g * DP / 8
         // on; even ones are rows g of the products, odd ones rows g + 8
-        {
-          const unsigned char* sv = st + kValues + 2 * t4 * kValueRow + g * (DP / 16);
-          const unsigned char* ss = st + kScales + kAKeys * kScaleRow + 2 * t4 * kScaleRow + (VW == 1 ? g / 2 : g * (VW / 2));
+        const int group_at = VW == 1 ? g / 2 : g * (VW / 2);  // the lane's first group of 16 elements
+        const bool head = P.wide_scales || group_at * 16 < p.D;
+#pragma unroll
+        for (int y = 0; y < U; ++y) {
+          const unsigned char* sv = st + y * kSub + kValues + 2 * t4 * kValueRow + g * (DP / 16);
+          const unsigned char* ss = st + y * kSub + kScales + (kAKeys + 2 * t4) * scale_row + group_at;
+          const unsigned odd = P.wide_scales ? 0u : masks[4 * stage + 2 + s0 + y] >> (16 + 2 * t4);
           unsigned x[4][VW], s2[2][VW == 4 ? 2 : 1];
 #pragma unroll
           for (int k = 0; k < 4; ++k) load_words<VW>(sv + ((k & 1) + (k >> 1) * 8) * kValueRow, x[k]);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
+            const unsigned char* s0p = ss + k * 8 * scale_row;
+            const unsigned char* s1p = s0p + scale_row;
+            if (!P.wide_scales) {
+              s0p += (odd >> (k * 8) & 1u) * 2;
+              s1p += (odd >> (k * 8 + 1) & 1u) * 2;
+            }
             if constexpr (VW == 4) {
-              const unsigned y = *reinterpret_cast<const uint16_t*>(ss + k * 8 * kScaleRow);
-              const unsigned z = *reinterpret_cast<const uint16_t*>(ss + (k * 8 + 1) * kScaleRow);
-              s2[k][0] = e4m3_to_f16(__byte_perm(y, z, 0x0040));
-              s2[k][1] = e4m3_to_f16(__byte_perm(y, z, 0x0051));
+              const unsigned v = head ? *reinterpret_cast<const uint16_t*>(s0p) : 0u;
+              const unsigned z = head ? *reinterpret_cast<const uint16_t*>(s1p) : 0u;
+              s2[k][0] = e4m3_to_f16(__byte_perm(v, z, 0x0040));
+              s2[k][1] = e4m3_to_f16(__byte_perm(v, z, 0x0051));
             } else {
-              s2[k][0] = e4m3_to_f16(ss[k * 8 * kScaleRow] | ss[(k * 8 + 1) * kScaleRow] << 8);
+              s2[k][0] = e4m3_to_f16(head ? *s0p | *s1p << 8 : 0);
             }
           }
 #pragma unroll
@@ -526,9 +579,9 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
             unsigned f[2][2][4];  // key pair, parity of the element
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const unsigned y = x[2 * k][w], z = x[2 * k + 1][w];
-              e2m1_to_f16(select_bits(0x0F0F0F0Fu, y, z << 4), f[k][0]);
-              e2m1_to_f16(select_bits(0x0F0F0F0Fu, y >> 4, z), f[k][1]);
+              const unsigned v = x[2 * k][w], z = x[2 * k + 1][w];
+              e2m1_to_f16(select_bits(0x0F0F0F0Fu, v, z << 4), f[k][0]);
+              e2m1_to_f16(select_bits(0x0F0F0F0Fu, v >> 4, z), f[k][1]);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 f[k][0][i] = mul_f16x2(f[k][0][i], s2[k][VW == 4 ? w / 2 : 0]);
@@ -540,11 +593,12 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 if constexpr (BF) {
-                  mma_f16(O[n][4 * w + i], f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[0][n], w1[0][n]);
+                  mma_f16(O[n][4 * w + i], f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][0][n][0], wt[y][0][n][1]);
                 } else {
                   float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[kPieces - 1][n], w1[kPieces - 1][n]);
-                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], w0[0][n], w1[0][n]);
+                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][kPieces - 1][n][0],
+                          wt[y][kPieces - 1][n][1]);
+                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][0][n][0], wt[y][0][n][1]);
 #pragma unroll
                   for (int e = 0; e < 4; ++e) O[n][4 * w + i][e] += sum[e];
                 }
@@ -588,8 +642,10 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
         const unsigned char* scale[2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          code[w] = reinterpret_cast<const unsigned char*>(P.codes[w]) + kh * P.cs[w][2] + page * P.cs[w][0] + at * P.cs[w][1];
-          scale[w] = reinterpret_cast<const unsigned char*>(P.scales[w]) + kh * P.ss[w][2] + page * P.ss[w][0] + at * P.ss[w][1];
+          code[w] = reinterpret_cast<const unsigned char*>(P.codes[w]) + kh * P.head_codes[w] +
+                    static_cast<uint64_t>(page) * P.codes_of[w][0] + static_cast<uint64_t>(at) * P.codes_of[w][1];
+          scale[w] = reinterpret_cast<const unsigned char*>(P.scales[w]) + kh * P.head_scales[w] +
+                     static_cast<uint64_t>(page) * P.scales_of[w][0] + static_cast<uint64_t>(at) * P.scales_of[w][1];
         }
         auto pair = [&](int w, int d) {  // elements d and d + 1, d even
           unsigned f[4];

@@ -1,0 +1,552 @@
+// Attention of a few new tokens over a paged cache in 4 bits on the tensor cores' own memory
+// (asymspec_cache4_attend, bf16 queries).
+#pragma once
+
+#include "kernel_attend4.cuh"
+
+namespace asymspec_impl {
+
+constexpr int kTThreads = 128;
+constexpr int kTKeys = 128;  // keys of a step, one a thread: the unit of the split
+constexpr unsigned long long kTWaitNs = 200000000ull;
+
+__device__ __forceinline__ int tensor_tiles(const AttendParams& p, int len) {
+  return max(1, (len - attend_first(p, len) + kTKeys - 1) / kTKeys);
+}
+
+// ----------------------------------------------------------- tcgen05
+
+template <int COLS>
+__device__ __forceinline__ void tmem_alloc(unsigned smem) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem), "n"(COLS) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_free(unsigned at) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "n"(COLS));
+}
+__device__ __forceinline__ void tmem_load8(unsigned at, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "r"(at));
+}
+__device__ __forceinline__ void tmem_store8(unsigned at, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"f"(r[0]), "f"(r[1]),
+               "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_store16(unsigned at, const unsigned (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// All products issued before arrive at `bar` when they are done.
+__device__ __forceinline__ void tensor_commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// D (+)= A B, fp16 products and fp32 sums: A in tensor memory, or in shared memory.
+__device__ __forceinline__ void tensor_mma_t(unsigned d, unsigned a, uint64_t b, unsigned form, bool add) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(form),
+      "r"(static_cast<unsigned>(add))
+      : "memory");
+}
+__device__ __forceinline__ void tensor_mma_s(unsigned d, uint64_t a, uint64_t b, unsigned form, bool add) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(form),
+      "r"(static_cast<unsigned>(add))
+      : "memory");
+}
+// Of operands in shared memory in rows of 128 bytes whose 16-byte chunk c lies at c ^ (row % 8): the
+// distances of 64-element blocks (`lead`, where rows run along the sum) and of eights of rows (`stride`).
+__device__ __forceinline__ uint64_t tensor_operand(unsigned at, unsigned lead, unsigned stride) {
+  return static_cast<uint64_t>((at & 0x3FFFF) >> 4) | static_cast<uint64_t>(lead >> 4) << 16 |
+         static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp16 operands, fp32 result, M = 128; A's rows along the sum, or (across) along M.
+__host__ __device__ constexpr unsigned tensor_form(int n, bool across) {
+  return 1u << 4 | (across ? 1u << 15 : 0u) | static_cast<unsigned>(n / 8) << 17 | 8u << 24;
+}
+
+// 32 bytes.
+__device__ __forceinline__ void load32(unsigned* r, const char* p) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p));
+}
+__device__ __forceinline__ void load16(unsigned* r, const char* p) {
+  asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+}
+template <int N>
+__device__ __forceinline__ void load_scales(unsigned (&r)[N], const char* p) {
+  if constexpr (N == 4) load16(r, p);
+  else if constexpr (N == 2) asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+  else asm volatile("ld.global.b32 %0, [%1];" : "=r"(r[0]) : "l"(p));
+}
+
+__host__ __device__ constexpr int tensor_blocks(int DP) { return (DP + 127) / 128; }  // 128s of a head's elements
+__host__ __device__ constexpr int tensor_columns(int DP, int NR) {
+  const int n = DP / 2 + NR + tensor_blocks(DP) * NR;
+  return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
+}
+constexpr size_t tensor_smem_bytes(int DP, int NR) {
+  return static_cast<size_t>(tensor_blocks(DP)) * 32768 + static_cast<size_t>(NR) * (256 + (DP > 64 ? DP * 2 : 128)) +
+         static_cast<size_t>(NR) * 4 * 8 + 1024;
+}
+
+// The keys are split evenly over the CTAs as attend_split's are, in steps of 128, one a thread.  Of a step,
+// both products have the keys' side as their 128 rows and the queries of the kv head as their
+// columns:
+//
+//   S = K Q^T   K, 128 keys: codes times scales as fp16 (exact), straight from the registers into tensor memory
+//   O += V^T P^T  V^T, 128 elements of a head: the same in shared memory, a key a row; the weights P beside it
+//
+// so a few queries cost what one does: a thread turns its key and its value into fp16, which takes most of
+// its instructions, and has one row of scores, a number for each query.  While the tensor core multiplies by
+// the keys the threads turn the values, and while it multiplies by those the next keys; their codes
+// come from memory a step ahead.  O stays in tensor memory, and is touched only when a score rises
+// far above its row's reference.
+template <int DP, int NR, int PER_SM>
+__global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid_constant__ Attend4Params P) {
+  using T = __nv_bfloat16;
+  constexpr int MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
+  constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
+  constexpr int QA = DP > 64 ? DP / 64 : 1;  // 64s of a query's elements
+  constexpr int kPWords = NR * 256;          // bytes of the weights
+  constexpr size_t kMlBytes = attend_ml_bytes(NR);
+  constexpr float kBelow = 7.f, kSlack = 8.f;
+  extern __shared__ __align__(1024) unsigned char a_smem[];
+  const AttendParams& p = P.a;
+  unsigned char* const s_v = a_smem + (-smem_u32(a_smem) & 1023u);  // (the operands' rows are 1024-byte patterns)
+  unsigned char* const s_p = s_v + MB * 32768;
+  unsigned char* const s_q = s_p + kPWords;
+  float* const s_m = reinterpret_cast<float*>(s_q + NR * QA * 128);  // references, factors, and what an item's
+  float* const s_factor = s_m + NR;                              // rows need beside
+  int* const s_last = reinterpret_cast<int*>(s_factor + NR);
+  float* const s_red = reinterpret_cast<float*>(s_last + NR);        // [4][NR]
+  float* const s_rescale = s_red + 4 * NR;
+  __shared__ __align__(8) unsigned long long s_bar[2];
+  __shared__ unsigned s_tmem;
+  __shared__ int64_t s_scan[kTThreads / 32], s_find[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int c = blockIdx.x, ctas = gridDim.x;
+  const int HR = p.kv_heads * p.row_tiles;
+  unsigned err = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    mbar_init(&s_bar[0], 1);
+    mbar_init(&s_bar[1], 1);
+    fence_mbar_init();
+  }
+  if (warp == 0) tmem_alloc<kCols>(smem_u32(&s_tmem));
+
+  // this CTA's share of the units, and where it begins
+  const int per = (p.B + kTThreads - 1) / kTThreads;
+  int64_t mine = 0;
+  for (int b = tid * per; b < min((tid + 1) * per, p.B); ++b) {
+    const int len = attend_len(p, b);
+    if (len != p.lens[b]) err |= ASYMSPEC_DATA_BAD_LENGTH;
+    mine += tensor_tiles(p, len) + kAItem;
+  }
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t o = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 31) s_scan[warp] = upto;
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  const unsigned tm_k = s_tmem, tm_s = tm_k + DP / 2, tm_o = tm_s + NR;
+  const unsigned tm_warp = static_cast<unsigned>(warp * 32) << 16;  // this warp's lanes
+  int64_t total = 0;
+  for (int w = 0; w < kTThreads / 32; ++w) {
+    if (w < warp) upto += s_scan[w];
+    total += s_scan[w];
+  }
+  total *= HR;
+  const AttendShares shares(total, ctas);
+  int64_t u = shares.start(c);
+  const int64_t u_end = shares.start(c + 1);
+  if (u < u_end && (upto - mine) * HR <= u && u < upto * HR) {
+    int64_t v = u - (upto - mine) * HR;
+    int b = tid * per;
+    for (;; ++b) {
+      const int64_t n = static_cast<int64_t>(tensor_tiles(p, attend_len(p, b)) + kAItem) * HR;
+      if (v < n) break;
+      v -= n;
+    }
+    s_find[0] = b;
+    s_find[1] = v;
+  }
+  __syncthreads();
+  AttendInfo* info = reinterpret_cast<AttendInfo*>(p.ws) + c;
+  int b = 0, len = 0, n_tiles = 0, hr = 0, at_unit = 0;
+  if (u >= u_end) {
+    if (tid == 0) info->tiles = 0;
+  } else {
+    b = static_cast<int>(s_find[0]);
+    len = attend_len(p, b), n_tiles = tensor_tiles(p, len);
+    hr = static_cast<int>(div64(s_find[1], n_tiles + kAItem));
+    at_unit = static_cast<int>(s_find[1] - static_cast<int64_t>(hr) * (n_tiles + kAItem));
+    if (tid == 0) {
+      info->total = total;
+      info->first = u - at_unit;
+      info->b = b;
+      info->hr = hr;
+      info->tiles = at_unit > kAItem ? n_tiles : 0;
+    }
+  }
+
+  unsigned parity_s = 0, parity_o = 0;
+  auto wait = [&](int which, unsigned parity) {
+    if (!(err & ASYMSPEC_DATA_TIMEOUT) && !mbar_wait_bounded(&s_bar[which], parity, kTWaitNs)) err |= ASYMSPEC_DATA_TIMEOUT;
+    tensor_fence_after();
+  };
+  const unsigned swizzle = (tid & 7) << 4;
+  unsigned char* const v_row = s_v + (tid >> 3) * 1024 + (tid & 7) * 128;  // this thread's value in a 64 of elements
+  unsigned char* const p_at = s_p + (tid >> 6) * (NR * 128);
+  const unsigned p_byte = (tid & 63) * 2;
+
+  for (; u < u_end; at_unit = 0) {
+    if (hr == HR) {
+      hr = 0;
+      ++b;
+      len = attend_len(p, b);
+      n_tiles = tensor_tiles(p, len);
+    }
+    const int end_unit = static_cast<int>(min(static_cast<int64_t>(n_tiles + kAItem), at_unit + (u_end - u)));
+    const int t0 = max(0, at_unit - kAItem), t1 = end_unit - kAItem;
+    u += end_unit - at_unit;
+    if (t1 <= t0) continue;  // (the item's first tile is the next CTA's)
+    const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * NR;
+    const int lo = attend_first(p, len);
+    const int rows = min(NR, p.rows - R0);  // of the item
+    const char* codes[2];
+    const char* scales[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      codes[w] = P.codes[w] + kh * P.head_codes[w];
+      scales[w] = P.scales[w] + kh * P.head_scales[w];
+    }
+    const int32_t* table = p.tables + b * p.table_ld;
+    const int end_key = min(len, lo + t1 * kTKeys);
+
+    // this thread's key of a step: its block, a step further ahead than its codes
+    int next_key = lo + t0 * kTKeys + tid, next_page, next_at;
+    auto find = [&] {
+      const int block = static_cast<int>(__umulhi(2u * static_cast<unsigned>(next_key), P.divide) >> P.shift);
+      next_at = next_key - block * p.block_size;
+      next_page = next_key < end_key ? __ldg(table + block) : INT_MIN;
+    };
+    unsigned kc[CW], ks[SW], vc[CW], vs[SW];
+    int page = INT_MIN, at = 0;
+    bool there = false, live = false;
+    auto load = [&](int w, unsigned (&code)[CW], unsigned (&scale)[SW]) {
+      if (there) {
+        const char* from = stepped(stepped(codes[w], page, P.codes_of[w][0]), at, P.codes_of[w][1]);
+        if (P.wide_codes) {
+#pragma unroll
+          for (int i = 0; i < CW; i += 8) load32(code + i, from + 4 * i);
+        } else {
+#pragma unroll
+          for (int i = 0; i < CW; i += 4) {
+            if (i * 8 < p.D) load16(code + i, from + 4 * i);
+            else code[i] = code[i + 1] = code[i + 2] = code[i + 3] = 0;
+          }
+        }
+        from = stepped(stepped(scales[w], page, P.scales_of[w][0]), at, P.scales_of[w][1]);
+        if (P.wide_scales) {
+          load_scales<SW>(scale, from);
+        } else {
+#pragma unroll
+          for (int i = 0; i < SW; ++i) {
+            scale[i] = 0;
+            if (i * 64 < p.D) scale[i] = *reinterpret_cast<const uint16_t*>(from + 4 * i);
+            if (i * 64 + 32 < p.D) scale[i] |= static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(from + 4 * i + 2)) << 16;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < CW; ++i) code[i] = 0;
+#pragma unroll
+        for (int i = 0; i < SW; ++i) scale[i] = 0;
+      }
+    };
+    auto take = [&] {  // the next step becomes the one whose codes are loaded
+      page = next_page, at = next_at;
+      there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
+      // (up to 15 keys are before the window of every query: their block may be gone)
+      if (!there && next_key < end_key && (p.window == 0 || next_key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
+      next_key += kTKeys;
+      find();
+    };
+    find();
+    take();
+    load(0, kc, ks);
+    load(1, vc, vs);
+
+    // the item's queries, each row times the power of two that takes its largest element to 2^13
+    for (int r = warp; r < rows; r += kTThreads / 32) {
+      const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+      const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
+      float x[DP / 32];
+      unsigned most = 0;
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const int d = lane + 32 * k;
+        x[k] = d < p.D ? to_f32(src[d]) : 0.f;
+        most = max(most, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+      }
+      const unsigned e = min(max(__reduce_max_sync(~0u, most) >> 23, 14u), 254u);
+      const float up = __uint_as_float((267u - e) << 23);  // 2^(13 - (e - 127))
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const int d = lane + 32 * k;
+        *reinterpret_cast<__half*>(s_q + (d >> 6) * (NR * 128) + r * 128 + (((d & 63) * 2) ^ ((r & 7) << 4))) =
+            __float2half_rn(x[k] * up);
+      }
+      if (lane == 0) {
+        s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
+        s_m[r] = -INFINITY;
+        s_last[r] = len - p.Q + i;
+      }
+    }
+    const int least = len - p.Q + R0 / p.group;
+    const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
+    float l[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) l[n] = 0.f;
+    bool bad_values = false, pending = false;  // a value with a NaN; products of values on their way
+    fence_to_async();
+
+    for (int t = t0; t < t1; ++t) {
+      const int k0 = lo + t * kTKeys;
+      live = there;
+      // keys
+#pragma unroll
+      for (int i = 0; i < CW; i += 4) {
+        unsigned f[16];
+        const unsigned s2 = e4m3_to_f16(ks[i / 8] >> (i % 8 ? 16 : 0));
+        const unsigned sa = __byte_perm(s2, s2, 0x1010), sb = __byte_perm(s2, s2, 0x3232);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          unsigned x[4];
+          e2m1_to_f16(kc[i + w], x);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) f[4 * w + k] = mul_f16x2(x[k], w < 2 ? sa : sb);
+        }
+        tmem_store16(tm_k + tm_warp + 4 * i, f);
+      }
+      tmem_wait_store();
+      take();
+      load(0, kc, ks);
+      tensor_fence_before();
+      __syncthreads();
+      if (tid == 0) {
+        tensor_fence_after();
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          tensor_mma_t(tm_s, tm_k + k * 8,
+                       tensor_operand(smem_u32(s_q) + (k >> 2) * (NR * 128) + (k & 3) * 32, 16, 1024),
+                       tensor_form(NR, false), k > 0);
+        tensor_commit(&s_bar[0]);
+      }
+      // values, when those of the step before have been multiplied
+      if (pending) {
+        wait(1, parity_o);
+        parity_o ^= 1;
+      }
+#pragma unroll
+      for (int i = 0; i < SW; ++i) {
+        const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        if (nan) {
+          vs[i] &= ~((nan >> 7) * 0xFFu);
+          bad_values = true;
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < CW; ++w) {
+        const unsigned s2 = e4m3_to_f16(vs[w / 8] >> (w % 8 >= 4 ? 16 : 0));
+        const unsigned s = __byte_perm(s2, s2, w % 4 < 2 ? 0x1010 : 0x3232);
+        unsigned x[4];
+        e2m1_to_f16(vc[w], x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
+        *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      load(1, vc, vs);
+      // scores: this thread's key with each query
+      wait(0, parity_s);
+      parity_s ^= 1;
+      float S[NR];
+#pragma unroll
+      for (int n = 0; n < NR; n += 8)
+        if (n < rows) tmem_load8(tm_s + tm_warp + n, S + n);
+      tmem_wait_load();
+      const int j = k0 + tid;
+      const bool whole = __all_sync(~0u, live) && k0 + kTKeys - 1 <= least && k0 >= from;
+      bool above = false;
+#pragma unroll
+      for (int n = 0; n < NR; n += 4) {
+        if (n >= rows) continue;
+        const float4 f = *reinterpret_cast<const float4*>(s_factor + n), m = *reinterpret_cast<const float4*>(s_m + n);
+        const float fs[4] = {f.x, f.y, f.z, f.w}, ms[4] = {m.x, m.y, m.z, m.w};
+        int4 last = make_int4(0, 0, 0, 0);
+        if (!whole) last = *reinterpret_cast<const int4*>(s_last + n);
+        const int lasts[4] = {last.x, last.y, last.z, last.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float s = S[n + e] * fs[e];
+          if (!whole) s = live && j <= lasts[e] && (p.window == 0 || j > lasts[e] - p.window) ? s : -INFINITY;
+          S[n + e] = s;
+          above = above || (n + e < rows && s > ms[e] + (kBelow + kSlack));
+        }
+      }
+      if (__syncthreads_or(above)) {
+        // references rise: each row's to kBelow under its largest score, and what has been summed goes down
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          if (n >= rows) continue;
+          float v = S[n];
+#pragma unroll
+          for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, d));
+          if (lane == 0) s_red[warp * NR + n] = v;
+        }
+        __syncthreads();
+        for (int n = tid; n < rows; n += kTThreads) {
+          const float v = fmaxf(fmaxf(s_red[n], s_red[NR + n]), fmaxf(s_red[2 * NR + n], s_red[3 * NR + n]));
+          const float old = s_m[n], now = fmaxf(old, v - kBelow);
+          s_rescale[n] = now == old ? 1.f : ex2(old - now);
+          s_m[n] = now;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+          if (n < rows) l[n] *= s_rescale[n];
+        if (t > t0) {
+#pragma unroll 1
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll 1
+            for (int n = 0; n < rows; n += 8) {
+              float o[8];
+              tmem_load8(tm_o + mb * NR + tm_warp + n, o);
+              tmem_wait_load();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_rescale[n + e] : 1.f;
+              tmem_store8(tm_o + mb * NR + tm_warp + n, o);
+            }
+          tmem_wait_store();
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NR; n += 4) {
+        if (n >= rows) continue;
+        const float4 m = *reinterpret_cast<const float4*>(s_m + n);
+        const float ms[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = ex2(S[n + e] - (ms[e] == -INFINITY ? 0.f : ms[e]));
+          l[n + e] += w;
+          const int r = n + e;
+          *reinterpret_cast<__half*>(p_at + (r >> 3) * 1024 + (r & 7) * 128 + (p_byte ^ ((r & 7) << 4))) = __float2half_rn(w);
+        }
+      }
+      fence_to_async();
+      tensor_fence_before();
+      __syncthreads();
+      if (tid == 0) {
+        tensor_fence_after();
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int k = 0; k < kTKeys / 16; ++k)
+            tensor_mma_s(tm_o + mb * NR, tensor_operand(smem_u32(s_v) + mb * 32768 + k * 2048, 16384, 1024),
+                         tensor_operand(smem_u32(s_p) + (k >> 2) * (NR * 128) + (k & 3) * 32, 16, 1024),
+                         tensor_form(NR, true), t > t0 || k > 0);
+        tensor_commit(&s_bar[1]);
+      }
+      pending = true;
+    }
+    wait(1, parity_o);
+    parity_o ^= 1;
+
+    // the rows' sums over the threads
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      if (n >= rows) continue;
+      float v = l[n];
+#pragma unroll
+      for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+      if (lane == 0) s_red[warp * NR + n] = v;
+    }
+    // A value's NaN was left out of the products, where a weight of zero would make it one in rows that do not
+    // see it: those that do have it here.
+    uint64_t hit[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) hit[mb] = 0;
+    if (__syncthreads_or(bad_values)) {
+      for (int j = lo + t0 * kTKeys; j < end_key; ++j) {
+        const int block = j / p.block_size, pg = table[block];
+        if (static_cast<unsigned>(pg) >= static_cast<unsigned>(p.num_blocks)) continue;
+        const char* sc = stepped(stepped(scales[1], pg, P.scales_of[1][0]), j - block * p.block_size, P.scales_of[1][1]);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          const int d = mb * 128 + tid;
+          if (d < p.D && (sc[d / 16] & 0x7F) == 0x7F)
+            for (int n = 0; n < rows; ++n)
+              if (j <= s_last[n] && (p.window == 0 || j > s_last[n] - p.window)) hit[mb] |= 1ull << n;
+        }
+      }
+    }
+    const bool all = t0 == 0 && t1 == n_tiles;
+    const int part = t0 > 0 ? 2 * c : 2 * c + 1;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * NR * 2;
+    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * NR * DP;
+#pragma unroll 1
+    for (int n0 = 0; n0 < rows; n0 += 8) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        float o[8];
+        tmem_load8(tm_o + mb * NR + tm_warp + n0, o);
+        tmem_wait_load();
+        const int d = mb * 128 + tid;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int n = n0 + e;
+          if (n >= rows) continue;
+          const float L = s_red[n] + s_red[NR + n] + s_red[2 * NR + n] + s_red[3 * NR + n];
+          const float x = hit[mb] >> n & 1 ? NAN : o[e] * P.value_scale;
+          const int i = (R0 + n) / p.group, h = kh * p.group + (R0 + n) % p.group;
+          if (all) {
+            if (d < p.D)
+              put(static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d, L == 0.f ? 0.f : x * (1.f / L));
+            if (d == 0 && p.lse) p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = lse_of(s_m[n], L);
+          } else {
+            if (d < DP) ws_o[n * DP + d] = x;
+            if (d == 0) *reinterpret_cast<float2*>(ws_ml + n * 2) = make_float2(s_m[n], L);
+          }
+        }
+      }
+    }
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    ++hr;
+  }
+  if (err && p.err) atomicOr(p.err, err);
+  __syncthreads();
+  if (warp == 0) tmem_free<kCols>(tm_k);
+}
+
+}  // namespace asymspec_impl
