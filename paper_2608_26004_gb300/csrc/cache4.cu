@@ -20,8 +20,8 @@ using namespace asymspec_impl;
 
 constexpr int kMoveCtas = 1216;  // CTAs of a write or read at most: eight on each SM
 
-AttendKernels attend4_kernels(int dtype, int D, int rows) {
-  return dtype == ASYMSPEC_FP32 ? attend4_kernels_f32(D, rows) : attend4_kernels_bf16(D, rows);
+AttendKernels attend4_kernels(int dtype, int D, int rows, bool fast) {
+  return dtype == ASYMSPEC_FP32 ? attend4_kernels_f32(D, rows, fast) : attend4_kernels_bf16(D, rows, fast);
 }
 
 int check_cache4(const asymspec_cache4* c) {
@@ -120,7 +120,7 @@ size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_he
     return 0;
   // (any number of queries up to Q: the row tiles only grow with them)
   const int rows = Q * (heads / kv_heads);
-  const AttendKernels a = attend4_kernels_bf16(head_dim, rows), b = attend4_kernels_f32(head_dim, rows);
+  const AttendKernels a = attend4_kernels_bf16(head_dim, rows, true), b = attend4_kernels_f32(head_dim, rows, true);
   return std::max(attend_ws_bytes(a.rows, a.DP), attend_ws_bytes(b.rows, b.DP));
 }
 
@@ -172,7 +172,7 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
   p.window = attend_window(window, table_width, cache->block_size);
   p.group = heads / cache->kv_heads;
   p.rows = Q * p.group;
-  const AttendKernels k = attend4_kernels(dtype, p.D, p.rows);
+  AttendKernels k = attend4_kernels(dtype, p.D, p.rows, true);
   p.row_tiles = (p.rows + k.rows - 1) / k.rows;
   p.scale2 = static_cast<float>(scale2);
   p.out_vec = aligned(out, 4 * elt);
@@ -202,6 +202,7 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
   // less than n above 2^(31 + s), and key times that less than 2^(31 + s).
   while ((1ll << P.shift) < p.block_size) ++P.shift;
   P.divide = static_cast<unsigned>(((1ull << (31 + P.shift)) + p.block_size - 1) / p.block_size);
+  if (!P.wide_scales || !P.wide_codes) k = attend4_kernels(dtype, p.D, p.rows, false);
   P.value_scale = cache->value_scale;
   int device = 0, sms = 0;
   cudaError_t e = device_sms(&device, &sms);

@@ -14,7 +14,7 @@ AttendKernels attend4_pick() {
           reinterpret_cast<const void*>(&attend_join<float, DP, rows>), DP, rows, 128 * WR, smem, PER_SM};
 }
 
-AttendKernels attend4_kernels_f32(int D, int rows) {
+AttendKernels attend4_kernels_f32(int D, int rows, bool) {
   if (D <= 64)
     return rows <= 8    ? attend4_pick<64, 1, 1, 3, 3>()
            : rows <= 16 ? attend4_pick<64, 2, 1, 3, 3>()

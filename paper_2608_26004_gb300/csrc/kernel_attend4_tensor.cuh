@@ -77,6 +77,21 @@ __host__ __device__ constexpr unsigned tensor_form(int n, bool across) {
   return 1u << 4 | (across ? 1u << 15 : 0u) | static_cast<unsigned>(n / 8) << 17 | 8u << 24;
 }
 
+// The largest of a warp's numbers; a NaN where all are.
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ bool elected() {
+  unsigned r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
+}
+// One warp waits for all, the others go on.
+__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, 128;" ::"r"(id) : "memory"); }
+
 // 32 bytes.
 __device__ __forceinline__ void load32(unsigned* r, const char* p) {
   asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -95,45 +110,47 @@ __device__ __forceinline__ void load_scales(unsigned (&r)[N], const char* p) {
 
 __host__ __device__ constexpr int tensor_blocks(int DP) { return (DP + 127) / 128; }  // 128s of a head's elements
 __host__ __device__ constexpr int tensor_columns(int DP, int NR) {
-  const int n = DP / 2 + NR + tensor_blocks(DP) * NR;
+  const int n = DP / 2 + NR + tensor_blocks(DP) * NR;  // keys, scores, what is summed
   return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
 }
+__host__ __device__ constexpr int tensor_rows(int rows) { return rows < 16 ? 16 : rows; }
+__host__ __device__ constexpr int tensor_query_blocks(int DP) { return DP > 64 ? DP / 64 : 1; }  // 64s of elements
 constexpr size_t tensor_smem_bytes(int DP, int NR) {
-  return static_cast<size_t>(tensor_blocks(DP)) * 32768 + static_cast<size_t>(NR) * (256 + (DP > 64 ? DP * 2 : 128)) +
-         static_cast<size_t>(NR) * 4 * 8 + 1024;
+  return static_cast<size_t>(tensor_blocks(DP)) * 32768 + static_cast<size_t>(NR) * (256 + tensor_query_blocks(DP) * 128) +
+         static_cast<size_t>(NR) * 4 * 9 + 1024;
 }
 
-// The keys are split evenly over the CTAs as attend_split's are, in steps of 128, one a thread.  Of a step,
-// both products have the keys' side as their 128 rows and the queries of the kv head as their
-// columns:
+// The keys are split evenly over the CTAs as attend_split's are, in steps of 128, one a thread.  Of a step, both
+// products have the keys' side as their 128 rows and the queries of the kv head as their columns, so a few
+// queries cost what one does:
 //
-//   S = K Q^T   K, 128 keys: codes times scales as fp16 (exact), straight from the registers into tensor memory
+//   S = K Q^T     K, 128 keys: codes times scales as fp16 (exact), from the registers into tensor memory
 //   O += V^T P^T  V^T, 128 elements of a head: the same in shared memory, a key a row; the weights P beside it
 //
-// so a few queries cost what one does: a thread turns its key and its value into fp16, which takes most of
-// its instructions, and has one row of scores, a number for each query.  While the tensor core multiplies by
-// the keys the threads turn the values, and while it multiplies by those the next keys; their codes
-// come from memory a step ahead.  O stays in tensor memory, and is touched only when a score rises
-// far above its row's reference.
-template <int DP, int NR, int PER_SM>
+// A thread turns its key and its value into fp16 and has the key's scores, a number for each query.  S of a
+// step is formed a step ahead, while the threads turn the values of the step and make its weights, and O is
+// while they turn the next keys; codes come from memory a step ahead of that.  O stays in tensor memory, and is
+// touched only when a score rises far above its row's reference.
+// RR: rows that an item has at most (NR columns of the products, 16 at least).  FAST: codes and scales lie on
+// the vectors' boundaries, D = DP.
+template <int DP, int RR, int PER_SM, bool FAST>
 __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid_constant__ Attend4Params P) {
   using T = __nv_bfloat16;
-  constexpr int MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
+  constexpr int NR = tensor_rows(RR), MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
-  constexpr int QA = DP > 64 ? DP / 64 : 1;  // 64s of a query's elements
-  constexpr int kPWords = NR * 256;          // bytes of the weights
-  constexpr size_t kMlBytes = attend_ml_bytes(NR);
-  constexpr float kBelow = 7.f, kSlack = 8.f;
+  constexpr size_t kMlBytes = attend_ml_bytes(RR);
+  constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -4.f, kLow = -8.f;
   extern __shared__ __align__(1024) unsigned char a_smem[];
   const AttendParams& p = P.a;
   unsigned char* const s_v = a_smem + (-smem_u32(a_smem) & 1023u);  // (the operands' rows are 1024-byte patterns)
   unsigned char* const s_p = s_v + MB * 32768;
-  unsigned char* const s_q = s_p + kPWords;
-  float* const s_m = reinterpret_cast<float*>(s_q + NR * QA * 128);  // references, factors, and what an item's
-  float* const s_factor = s_m + NR;                              // rows need beside
+  unsigned char* const s_q = s_p + NR * 256;
+  float* const s_m = reinterpret_cast<float*>(s_q + NR * tensor_query_blocks(DP) * 128);
+  float* const s_factor = s_m + NR;  // (an item's references, factors and last keys, and what its rows need beside)
   int* const s_last = reinterpret_cast<int*>(s_factor + NR);
-  float* const s_red = reinterpret_cast<float*>(s_last + NR);        // [4][NR]
-  float* const s_rescale = s_red + 4 * NR;
+  float* const s_red = reinterpret_cast<float*>(s_last + NR);  // [4][NR]
+  float* const s_up = s_red + 4 * NR;
+  float* const s_sub = s_up + NR;  // what scores are taken less: the reference, or 0 where there is none yet
   __shared__ __align__(8) unsigned long long s_bar[2];
   __shared__ unsigned s_tmem;
   __shared__ int64_t s_scan[kTThreads / 32], s_find[2];
@@ -209,16 +226,19 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   }
 
   unsigned parity_s = 0, parity_o = 0;
-  auto wait = [&](int which, unsigned parity) {
+  auto wait = [&](int which, unsigned& parity) {
     if (!(err & ASYMSPEC_DATA_TIMEOUT) && !mbar_wait_bounded(&s_bar[which], parity, kTWaitNs)) err |= ASYMSPEC_DATA_TIMEOUT;
+    parity ^= 1;
     tensor_fence_after();
   };
   const unsigned swizzle = (tid & 7) << 4;
   unsigned char* const v_row = s_v + (tid >> 3) * 1024 + (tid & 7) * 128;  // this thread's value in a 64 of elements
   unsigned char* const p_at = s_p + (tid >> 6) * (NR * 128);
   const unsigned p_byte = (tid & 63) * 2;
+  const uint64_t q_operand = tensor_operand(smem_u32(s_q), 16, 1024), p_operand = tensor_operand(smem_u32(s_p), 16, 1024);
+  const uint64_t v_operand = tensor_operand(smem_u32(s_v), 16384, 1024);
 
-  for (; u < u_end; at_unit = 0) {
+  for (; u < u_end; at_unit = 0, ++hr) {
     if (hr == HR) {
       hr = 0;
       ++b;
@@ -229,20 +249,14 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     const int t0 = max(0, at_unit - kAItem), t1 = end_unit - kAItem;
     u += end_unit - at_unit;
     if (t1 <= t0) continue;  // (the item's first tile is the next CTA's)
-    const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * NR;
+    const int kh = hr / p.row_tiles, R0 = (hr % p.row_tiles) * RR;
     const int lo = attend_first(p, len);
-    const int rows = min(NR, p.rows - R0);  // of the item
-    const char* codes[2];
-    const char* scales[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      codes[w] = P.codes[w] + kh * P.head_codes[w];
-      scales[w] = P.scales[w] + kh * P.head_scales[w];
-    }
-    const int32_t* table = p.tables + b * p.table_ld;
+    const int rows = min(RR, p.rows - R0);  // of the item
     const int end_key = min(len, lo + t1 * kTKeys);
+    const int32_t* table = p.tables + b * p.table_ld;
 
-    // this thread's key of a step: its block, a step further ahead than its codes
+    // this thread's key of a step: where it is (key), and whether it is there.  Looked up two steps ahead of
+    // the one whose keys are turned, loaded one step ahead; values go a step after the keys.
     int next_key = lo + t0 * kTKeys + tid, next_page, next_at;
     auto find = [&] {
       const int block = static_cast<int>(__umulhi(2u * static_cast<unsigned>(next_key), P.divide) >> P.shift);
@@ -250,55 +264,98 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       next_page = next_key < end_key ? __ldg(table + block) : INT_MIN;
     };
     unsigned kc[CW], ks[SW], vc[CW], vs[SW];
-    int page = INT_MIN, at = 0;
-    bool there = false, live = false;
-    auto load = [&](int w, unsigned (&code)[CW], unsigned (&scale)[SW]) {
-      if (there) {
-        const char* from = stepped(stepped(codes[w], page, P.codes_of[w][0]), at, P.codes_of[w][1]);
-        if (P.wide_codes) {
+    int page = 0, at = 0, page_v = 0, at_v = 0;
+    bool there = false, there_v = false;
+    const char* codes[2];
+    const char* scales[2];
 #pragma unroll
-          for (int i = 0; i < CW; i += 8) load32(code + i, from + 4 * i);
-        } else {
-#pragma unroll
-          for (int i = 0; i < CW; i += 4) {
-            if (i * 8 < p.D) load16(code + i, from + 4 * i);
-            else code[i] = code[i + 1] = code[i + 2] = code[i + 3] = 0;
-          }
-        }
-        from = stepped(stepped(scales[w], page, P.scales_of[w][0]), at, P.scales_of[w][1]);
-        if (P.wide_scales) {
-          load_scales<SW>(scale, from);
-        } else {
-#pragma unroll
-          for (int i = 0; i < SW; ++i) {
-            scale[i] = 0;
-            if (i * 64 < p.D) scale[i] = *reinterpret_cast<const uint16_t*>(from + 4 * i);
-            if (i * 64 + 32 < p.D) scale[i] |= static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(from + 4 * i + 2)) << 16;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < CW; ++i) code[i] = 0;
-#pragma unroll
-        for (int i = 0; i < SW; ++i) scale[i] = 0;
-      }
-    };
-    auto take = [&] {  // the next step becomes the one whose codes are loaded
-      page = next_page, at = next_at;
-      there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_blocks);
+    for (int w = 0; w < 2; ++w) {
+      codes[w] = P.codes[w] + kh * P.head_codes[w];
+      scales[w] = P.scales[w] + kh * P.head_scales[w];
+    }
+    auto take = [&] {  // the step that was looked up becomes the one whose keys are loaded
+      there = static_cast<unsigned>(next_page) < static_cast<unsigned>(p.num_blocks);
       // (up to 15 keys are before the window of every query: their block may be gone)
       if (!there && next_key < end_key && (p.window == 0 || next_key > len - p.Q - p.window)) err |= ASYMSPEC_DATA_BAD_INDEX;
+      // (for a key that does not exist some codes of block 0, finite in any case, and zeros for scales)
+      page = there ? next_page : 0, at = there ? next_at : 0;
       next_key += kTKeys;
       find();
     };
+    auto load = [&](int w, int page_of, int at_of, unsigned (&code)[CW], unsigned (&scale)[SW]) {
+      const char* from = stepped(stepped(codes[w], page_of, P.codes_of[w][0]), at_of, P.codes_of[w][1]);
+      const char* scales_at = stepped(stepped(scales[w], page_of, P.scales_of[w][0]), at_of, P.scales_of[w][1]);
+      if constexpr (FAST) {
+#pragma unroll
+        for (int i = 0; i < CW; i += 8) load32(code + i, from + 4 * i);
+        load_scales<SW>(scale, scales_at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < CW; i += 4) {
+          if (i * 8 < p.D) load16(code + i, from + 4 * i);
+          else code[i] = code[i + 1] = code[i + 2] = code[i + 3] = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < SW; ++i) {
+          scale[i] = 0;
+          if (i * 64 < p.D) scale[i] = *reinterpret_cast<const uint16_t*>(scales_at + 4 * i);
+          if (i * 64 + 32 < p.D) scale[i] |= static_cast<unsigned>(*reinterpret_cast<const uint16_t*>(scales_at + 4 * i + 2)) << 16;
+        }
+      }
+    };
+    auto turn_keys = [&] {  // into tensor memory, and the next step's are loaded
+#pragma unroll
+      for (int i = 0; i < SW; ++i) ks[i] = there ? ks[i] : 0u;
+#pragma unroll
+      for (int i = 0; i < CW; i += 4) {
+        unsigned f[16];
+        const unsigned s2 = e4m3_to_f16(ks[i / 8] >> (i % 8 ? 16 : 0));
+        const unsigned sa = __byte_perm(s2, s2, 0x1010), sb = __byte_perm(s2, s2, 0x3232);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          unsigned x[4];
+          e2m1_to_f16(kc[i + w], x);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) f[4 * w + k] = mul_f16x2(x[k], w < 2 ? sa : sb);
+        }
+        tmem_store16(tm_k + tm_warp + 4 * i, f);
+      }
+      there_v = there, page_v = page, at_v = at;
+      take();
+      load(0, page, at, kc, ks);
+      tmem_wait_store();
+    };
+    auto start_scores = [&] {  // one warp waits for the others and starts the products, the others go on
+      tensor_fence_before();
+      if (warp == 0) {
+        barrier_sync(1);
+        if (elected()) {
+          tensor_fence_after();
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+            tensor_mma_t(tm_s, tm_k + k * 8, q_operand + ((k >> 2) * (NR * 128) + (k & 3) * 32) / 16, tensor_form(NR, false),
+                         k > 0);
+          tensor_commit(&s_bar[0]);
+        }
+        __syncwarp();
+      } else {
+        barrier_arrive(1);
+      }
+    };
     find();
     take();
-    load(0, kc, ks);
-    load(1, vc, vs);
+    load(0, page, at, kc, ks);
+    load(1, page, at, vc, vs);
 
     // the item's queries, each row times the power of two that takes its largest element to 2^13
+    const int least = len - p.Q + R0 / p.group;
+    const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
+    // A first reference: if every row sees all keys of the first step, 2^kGuess is close enough to most
+    // scores (in [2^-12, 2^11]) and saves looking for the largest; a row that has none of its warp's within
+    // that range, or one above, raises the references all the same.
+    const bool guess = lo + (t0 + 1) * kTKeys - 1 <= least && lo + t0 * kTKeys >= from && lo + (t0 + 1) * kTKeys <= end_key;
     for (int r = warp; r < rows; r += kTThreads / 32) {
-      const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
+      const int i = (R0 + r) / p.group, h = kh * p.group + R0 + r - i * p.group;
       const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
       float x[DP / 32];
       unsigned most = 0;
@@ -318,57 +375,39 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       }
       if (lane == 0) {
         s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
-        s_m[r] = -INFINITY;
+        s_m[r] = guess ? kGuess : -INFINITY;
+        s_sub[r] = guess ? kGuess : 0.f;
         s_last[r] = len - p.Q + i;
       }
     }
-    const int least = len - p.Q + R0 / p.group;
-    const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
-    float l[NR];
+    if (tid >= rows && tid < RR) s_factor[tid] = s_sub[tid] = 0.f;  // (scores beyond `rows` are 0 or NaN)
+    float l[RR];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) l[n] = 0.f;
-    bool bad_values = false, pending = false;  // a value with a NaN; products of values on their way
+    for (int n = 0; n < RR; ++n) l[n] = 0.f;
+    bool bad_values = false;  // a value with a NaN
+    bool fresh = !guess;      // a row without a reference
     fence_to_async();
+    turn_keys();
+    start_scores();
 
     for (int t = t0; t < t1; ++t) {
-      const int k0 = lo + t * kTKeys;
-      live = there;
-      // keys
+      const int j = lo + t * kTKeys + tid;  // this thread's key
+      const bool live = there_v;
+      wait(0, parity_s);
+      float S[RR];
 #pragma unroll
-      for (int i = 0; i < CW; i += 4) {
-        unsigned f[16];
-        const unsigned s2 = e4m3_to_f16(ks[i / 8] >> (i % 8 ? 16 : 0));
-        const unsigned sa = __byte_perm(s2, s2, 0x1010), sb = __byte_perm(s2, s2, 0x3232);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          unsigned x[4];
-          e2m1_to_f16(kc[i + w], x);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) f[4 * w + k] = mul_f16x2(x[k], w < 2 ? sa : sb);
-        }
-        tmem_store16(tm_k + tm_warp + 4 * i, f);
-      }
-      tmem_wait_store();
-      take();
-      load(0, kc, ks);
-      tensor_fence_before();
-      __syncthreads();
-      if (tid == 0) {
-        tensor_fence_after();
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          tensor_mma_t(tm_s, tm_k + k * 8,
-                       tensor_operand(smem_u32(s_q) + (k >> 2) * (NR * 128) + (k & 3) * 32, 16, 1024),
-                       tensor_form(NR, false), k > 0);
-        tensor_commit(&s_bar[0]);
-      }
-      // values, when those of the step before have been multiplied
-      if (pending) {
-        wait(1, parity_o);
-        parity_o ^= 1;
-      }
+      for (int n = 0; n < RR; n += 8)
+        if (n < rows) tmem_load8(tm_s + tm_warp + n, S + n);
+      // the next step's keys, while the scores come
+      if (t + 1 < t1) turn_keys();
+      tmem_wait_load();
+      if (t + 1 < t1) start_scores();
+      // values, when those of the step before have been multiplied.  A NaN is left out of the products, where a
+      // weight of zero would make it one in rows that do not see it.
+      if (t > t0) wait(1, parity_o);
 #pragma unroll
       for (int i = 0; i < SW; ++i) {
+        vs[i] = live ? vs[i] : 0u;
         const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
         if (nan) {
           vs[i] &= ~((nan >> 7) * 0xFFu);
@@ -385,55 +424,76 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
         *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
       }
-      load(1, vc, vs);
-      // scores: this thread's key with each query
-      wait(0, parity_s);
-      parity_s ^= 1;
-      float S[NR];
+      if (t + 1 < t1) load(1, page_v, at_v, vc, vs);
+      // scores less their references
+      auto less = [&] {
 #pragma unroll
-      for (int n = 0; n < NR; n += 8)
-        if (n < rows) tmem_load8(tm_s + tm_warp + n, S + n);
-      tmem_wait_load();
-      const int j = k0 + tid;
-      const bool whole = __all_sync(~0u, live) && k0 + kTKeys - 1 <= least && k0 >= from;
-      bool above = false;
-#pragma unroll
-      for (int n = 0; n < NR; n += 4) {
-        if (n >= rows) continue;
-        const float4 f = *reinterpret_cast<const float4*>(s_factor + n), m = *reinterpret_cast<const float4*>(s_m + n);
-        const float fs[4] = {f.x, f.y, f.z, f.w}, ms[4] = {m.x, m.y, m.z, m.w};
-        int4 last = make_int4(0, 0, 0, 0);
-        if (!whole) last = *reinterpret_cast<const int4*>(s_last + n);
-        const int lasts[4] = {last.x, last.y, last.z, last.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float s = S[n + e] * fs[e];
-          if (!whole) s = live && j <= lasts[e] && (p.window == 0 || j > lasts[e] - p.window) ? s : -INFINITY;
-          S[n + e] = s;
-          above = above || (n + e < rows && s > ms[e] + (kBelow + kSlack));
+        for (int n = 0; n < RR; n += 4) {
+          if (n >= rows) continue;
+          const float4 f = *reinterpret_cast<const float4*>(s_factor + n), m = *reinterpret_cast<const float4*>(s_sub + n);
+          S[n] = fmaf(S[n], f.x, -m.x);
+          S[n + 1] = fmaf(S[n + 1], f.y, -m.y);
+          S[n + 2] = fmaf(S[n + 2], f.z, -m.z);
+          S[n + 3] = fmaf(S[n + 3], f.w, -m.w);
         }
+      };
+      const int k0 = lo + t * kTKeys;
+      const bool whole = __all_sync(~0u, live) && k0 + kTKeys - 1 <= least && k0 >= from;
+      auto hide = [&] {  // what a row does not see
+#pragma unroll
+        for (int n = 0; n < RR; ++n) {
+          if (n >= rows) continue;
+          const int last = s_last[n];
+          if (!live || j > last || (p.window != 0 && j <= last - p.window)) S[n] = -INFINITY;
+        }
+      };
+      less();
+      if (!whole) hide();
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < RR; n += 4)
+        if (n < rows) top = fmaxf(fmaxf(top, fmaxf(S[n], S[n + 1])), fmaxf(S[n + 2], S[n + 3]));
+      bool raise = top > kBelow + kSlack;
+      if (fresh) {
+#pragma unroll
+        for (int n = 0; n < RR; ++n)
+          if (n < rows) raise = raise || (S[n] > -INFINITY && s_m[n] == -INFINITY);
+      } else if (t == t0) {
+#pragma unroll
+        for (int n = 0; n < RR; ++n)
+          if (n < rows) {
+            const bool low = !(warp_max(S[n]) >= kLow);  // (all lanes take part)
+            raise = raise || low;
+          }
       }
-      if (__syncthreads_or(above)) {
+      if (__syncthreads_or(raise)) {
         // references rise: each row's to kBelow under its largest score, and what has been summed goes down
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
+        for (int n = 0; n < RR; ++n) {
           if (n >= rows) continue;
-          float v = S[n];
-#pragma unroll
-          for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, d));
+          const float v = warp_max(S[n]);
           if (lane == 0) s_red[warp * NR + n] = v;
         }
         __syncthreads();
         for (int n = tid; n < rows; n += kTThreads) {
           const float v = fmaxf(fmaxf(s_red[n], s_red[NR + n]), fmaxf(s_red[2 * NR + n], s_red[3 * NR + n]));
-          const float old = s_m[n], now = fmaxf(old, v - kBelow);
-          s_rescale[n] = now == old ? 1.f : ex2(old - now);
-          s_m[n] = now;
+          // (a row that has nothing summed yet: to wherever its scores are, if there are any)
+          const bool empty = t == t0 || s_m[n] == -INFINITY, none = empty && !(v > -INFINITY);
+          const float up = none ? 0.f : empty ? v - kBelow : fmaxf(v - kBelow, 0.f);
+          s_m[n] = none ? -INFINITY : s_sub[n] + up;
+          s_sub[n] = none ? 0.f : s_sub[n] + up;
+          s_up[n] = up;
+          s_red[n] = empty || up == 0.f ? 1.f : ex2(-up);
         }
         __syncthreads();
+        fresh = false;
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-          if (n < rows) l[n] *= s_rescale[n];
+        for (int n = 0; n < RR; ++n)
+          if (n < rows) {
+            l[n] *= s_red[n];
+            S[n] -= s_up[n];
+            fresh = fresh || s_m[n] == -INFINITY;
+          }
         if (t > t0) {
 #pragma unroll 1
           for (int mb = 0; mb < MB; ++mb)
@@ -443,55 +503,56 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
               tmem_load8(tm_o + mb * NR + tm_warp + n, o);
               tmem_wait_load();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_rescale[n + e] : 1.f;
+              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_red[n + e] : 1.f;
               tmem_store8(tm_o + mb * NR + tm_warp + n, o);
             }
           tmem_wait_store();
         }
       }
 #pragma unroll
-      for (int n = 0; n < NR; n += 4) {
+      for (int n = 0; n < RR; n += 4) {
         if (n >= rows) continue;
-        const float4 m = *reinterpret_cast<const float4*>(s_m + n);
-        const float ms[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = ex2(S[n + e] - (ms[e] == -INFINITY ? 0.f : ms[e]));
-          l[n + e] += w;
-          const int r = n + e;
-          *reinterpret_cast<__half*>(p_at + (r >> 3) * 1024 + (r & 7) * 128 + (p_byte ^ ((r & 7) << 4))) = __float2half_rn(w);
+        for (int r = n; r < n + 4; r += 2) {
+          const float w0 = ex2(S[r]), w1 = ex2(S[r + 1]);
+          l[r] += w0;
+          l[r + 1] += w1;
+          const unsigned w = pack_f16(w0, w1);
+          unsigned char* to = p_at + (r >> 3) * 1024 + (r & 7) * 128;
+          *reinterpret_cast<uint16_t*>(to + (p_byte ^ ((r & 7) << 4))) = static_cast<uint16_t>(w);
+          *reinterpret_cast<uint16_t*>(to + 128 + (p_byte ^ (((r & 7) + 1) << 4))) = static_cast<uint16_t>(w >> 16);
         }
       }
       fence_to_async();
       tensor_fence_before();
-      __syncthreads();
-      if (tid == 0) {
-        tensor_fence_after();
+      if (warp == 1) {
+        barrier_sync(2);
+        if (elected()) {
+          tensor_fence_after();
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
+          for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int k = 0; k < kTKeys / 16; ++k)
-            tensor_mma_s(tm_o + mb * NR, tensor_operand(smem_u32(s_v) + mb * 32768 + k * 2048, 16384, 1024),
-                         tensor_operand(smem_u32(s_p) + (k >> 2) * (NR * 128) + (k & 3) * 32, 16, 1024),
-                         tensor_form(NR, true), t > t0 || k > 0);
-        tensor_commit(&s_bar[1]);
+            for (int k = 0; k < kTKeys / 16; ++k)
+              tensor_mma_s(tm_o + mb * NR, v_operand + (mb * 32768 + k * 2048) / 16,
+                           p_operand + ((k >> 2) * (NR * 128) + (k & 3) * 32) / 16, tensor_form(NR, true), t > t0 || k > 0);
+          tensor_commit(&s_bar[1]);
+        }
+        __syncwarp();
+      } else {
+        barrier_arrive(2);
       }
-      pending = true;
     }
-    wait(1, parity_o);
-    parity_o ^= 1;
 
     // the rows' sums over the threads
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
+    for (int n = 0; n < RR; ++n) {
       if (n >= rows) continue;
       float v = l[n];
 #pragma unroll
       for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
       if (lane == 0) s_red[warp * NR + n] = v;
     }
-    // A value's NaN was left out of the products, where a weight of zero would make it one in rows that do not
-    // see it: those that do have it here.
+    // a value's NaN that was left out, in the rows that see it
     uint64_t hit[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) hit[mb] = 0;
@@ -511,38 +572,40 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     }
     const bool all = t0 == 0 && t1 == n_tiles;
     const int part = t0 > 0 ? 2 * c : 2 * c + 1;
-    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * NR * 2;
-    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * NR * DP;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * RR * 2;
+    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * RR * DP;
+    int i = R0 / p.group, h = R0 - i * p.group;  // the row's query and head, of the kv head's
+    wait(1, parity_o);
 #pragma unroll 1
     for (int n0 = 0; n0 < rows; n0 += 8) {
+      float o[MB][8];
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        float o[8];
-        tmem_load8(tm_o + mb * NR + tm_warp + n0, o);
-        tmem_wait_load();
-        const int d = mb * 128 + tid;
+      for (int mb = 0; mb < MB; ++mb) tmem_load8(tm_o + mb * NR + tm_warp + n0, o[mb]);
+      tmem_wait_load();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int n = n0 + e;
-          if (n >= rows) continue;
-          const float L = s_red[n] + s_red[NR + n] + s_red[2 * NR + n] + s_red[3 * NR + n];
-          const float x = hit[mb] >> n & 1 ? NAN : o[e] * P.value_scale;
-          const int i = (R0 + n) / p.group, h = kh * p.group + (R0 + n) % p.group;
-          if (all) {
-            if (d < p.D)
-              put(static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d, L == 0.f ? 0.f : x * (1.f / L));
-            if (d == 0 && p.lse) p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = lse_of(s_m[n], L);
-          } else {
-            if (d < DP) ws_o[n * DP + d] = x;
-            if (d == 0) *reinterpret_cast<float2*>(ws_ml + n * 2) = make_float2(s_m[n], L);
-          }
+      for (int e = 0; e < 8; ++e) {
+        const int n = n0 + e;
+        if (n >= rows) continue;
+        const float L = s_red[n] + s_red[NR + n] + s_red[2 * NR + n] + s_red[3 * NR + n];
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + (kh * p.group + h) * p.os[2];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          const int d = mb * 128 + tid;
+          const float x = hit[mb] >> n & 1 ? NAN : o[mb][e] * P.value_scale;
+          if (all && d < p.D) put(out + d, L == 0.f ? 0.f : x * inv);
+          if (!all && d < DP) ws_o[n * DP + d] = x;
         }
+        if (tid == 0) {
+          if (!all) *reinterpret_cast<float2*>(ws_ml + n * 2) = make_float2(s_m[n], L);
+          else if (p.lse) p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + kh * p.group + h] = lse_of(s_m[n], L);
+        }
+        if (++h == p.group) h = 0, ++i;
       }
     }
     tensor_fence_before();
     __syncthreads();
     tensor_fence_after();
-    ++hr;
   }
   if (err && p.err) atomicOr(p.err, err);
   __syncthreads();
