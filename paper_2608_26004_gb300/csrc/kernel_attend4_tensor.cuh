@@ -386,6 +386,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     for (int n = 0; n < RR; ++n) l[n] = 0.f;
     bool bad_values = false;  // a value with a NaN
     bool fresh = !guess;      // a row without a reference
+    const bool few = RR == 8 && rows <= RR / 2;
     fence_to_async();
     turn_keys();
     start_scores();
@@ -396,8 +397,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       wait(0, parity_s);
       float S[RR];
 #pragma unroll
-      for (int n = 0; n < RR; n += 8)
-        if (n < rows) tmem_load8(tm_s + tm_warp + n, S + n);
+      for (int n = 0; n < RR; n += 8) tmem_load8(tm_s + tm_warp + n, S + n);
       // the next step's keys, while the scores come
       if (t + 1 < t1) turn_keys();
       tmem_wait_load();
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       auto less = [&] {
 #pragma unroll
         for (int n = 0; n < RR; n += 4) {
-          if (n >= rows) continue;
+          if (few && n >= RR / 2) continue;
           const float4 f = *reinterpret_cast<const float4*>(s_factor + n), m = *reinterpret_cast<const float4*>(s_sub + n);
           S[n] = fmaf(S[n], f.x, -m.x);
           S[n + 1] = fmaf(S[n + 1], f.y, -m.y);
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       float top = -INFINITY;
 #pragma unroll
       for (int n = 0; n < RR; n += 4)
-        if (n < rows) top = fmaxf(fmaxf(top, fmaxf(S[n], S[n + 1])), fmaxf(S[n + 2], S[n + 3]));
+        if (!few || n < RR / 2) top = fmaxf(fmaxf(top, fmaxf(S[n], S[n + 1])), fmaxf(S[n + 2], S[n + 3]));
       bool raise = top > kBelow + kSlack;
       if (fresh) {
 #pragma unroll
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       }
 #pragma unroll
       for (int n = 0; n < RR; n += 4) {
-        if (n >= rows) continue;
+        if (few && n >= RR / 2) continue;
 #pragma unroll
         for (int r = n; r < n + 4; r += 2) {
           const float w0 = ex2(S[r]), w1 = ex2(S[r + 1]);
@@ -552,55 +552,80 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
       if (lane == 0) s_red[warp * NR + n] = v;
     }
-    // a value's NaN that was left out, in the rows that see it
-    uint64_t hit[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) hit[mb] = 0;
-    if (__syncthreads_or(bad_values)) {
-      for (int j = lo + t0 * kTKeys; j < end_key; ++j) {
-        const int block = j / p.block_size, pg = table[block];
-        if (static_cast<unsigned>(pg) >= static_cast<unsigned>(p.num_blocks)) continue;
-        const char* sc = stepped(stepped(scales[1], pg, P.scales_of[1][0]), j - block * p.block_size, P.scales_of[1][1]);
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          const int d = mb * 128 + tid;
-          if (d < p.D && (sc[d / 16] & 0x7F) == 0x7F)
-            for (int n = 0; n < rows; ++n)
-              if (j <= s_last[n] && (p.window == 0 || j > s_last[n] - p.window)) hit[mb] |= 1ull << n;
-        }
-      }
-    }
+    const bool nans = __syncthreads_or(bad_values);
     const bool all = t0 == 0 && t1 == n_tiles;
     const int part = t0 > 0 ? 2 * c : 2 * c + 1;
     float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * RR * 2;
     float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * RR * DP;
-    int i = R0 / p.group, h = R0 - i * p.group;  // the row's query and head, of the kv head's
+    // a row's sum, and what its values are taken times
+    if (tid < rows) {
+      const int n = tid;
+      const float L = s_red[n] + s_red[NR + n] + s_red[2 * NR + n] + s_red[3 * NR + n];
+      s_up[n] = !all ? P.value_scale : L == 0.f ? 0.f : P.value_scale / L;
+      if (!all) {
+        *reinterpret_cast<float2*>(ws_ml + n * 2) = make_float2(s_m[n], L);
+      } else if (p.lse) {
+        const int i = (R0 + n) / p.group, h = kh * p.group + R0 + n - i * p.group;
+        p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + h] = lse_of(s_m[n], L);
+      }
+    }
     wait(1, parity_o);
+    if (nans) {
+      // a value's NaN that was left out of the products, in the rows that see it
+#pragma unroll 1
+      for (int mb = 0; mb < MB; ++mb) {
+        const int d = mb * 128 + tid;
+        uint64_t hit = 0;
+        for (int j = lo + t0 * kTKeys; j < end_key; ++j) {
+          const int block = j / p.block_size, pg = table[block];
+          if (static_cast<unsigned>(pg) >= static_cast<unsigned>(p.num_blocks) || d >= p.D) continue;
+          const char* sc = stepped(stepped(scales[1], pg, P.scales_of[1][0]), j - block * p.block_size, P.scales_of[1][1]);
+          if ((sc[d / 16] & 0x7F) == 0x7F)
+            for (int n = 0; n < rows; ++n)
+              if (j <= s_last[n] && (p.window == 0 || j > s_last[n] - p.window)) hit |= 1ull << n;
+        }
+#pragma unroll 1
+        for (int n = 0; n < rows; n += 8) {
+          __syncwarp();
+          float o[8];
+          tmem_load8(tm_o + mb * NR + tm_warp + n, o);
+          tmem_wait_load();
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = hit >> (n + e) & 1 ? NAN : o[e];
+          tmem_store8(tm_o + mb * NR + tm_warp + n, o);
+        }
+      }
+      tmem_wait_store();
+    }
+    __syncthreads();
+    int h = R0 % p.group;  // the row's head, of the kv head's, and its output
+    T* out = static_cast<T*>(p.out) + b * p.os[0] + R0 / p.group * p.os[1] + (kh * p.group + h) * p.os[2] + tid;
+    const int64_t next_query = p.os[1] - (p.group - 1) * p.os[2];
 #pragma unroll 1
     for (int n0 = 0; n0 < rows; n0 += 8) {
       float o[MB][8];
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) tmem_load8(tm_o + mb * NR + tm_warp + n0, o[mb]);
       tmem_wait_load();
+      if (!all) {
+        // (the rows past the item's last one have room there too)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int n = n0 + e;
-        if (n >= rows) continue;
-        const float L = s_red[n] + s_red[NR + n] + s_red[2 * NR + n] + s_red[3 * NR + n];
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + (kh * p.group + h) * p.os[2];
+        for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          const int d = mb * 128 + tid;
-          const float x = hit[mb] >> n & 1 ? NAN : o[mb][e] * P.value_scale;
-          if (all && d < p.D) put(out + d, L == 0.f ? 0.f : x * inv);
-          if (!all && d < DP) ws_o[n * DP + d] = x;
+          for (int mb = 0; mb < MB; ++mb)
+            if (DP >= 128 || tid < DP) ws_o[(n0 + e) * DP + mb * 128 + tid] = o[mb][e] * P.value_scale;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (n0 + e >= rows) continue;
+          const float f = s_up[n0 + e];
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+            if (mb * 128 + tid < p.D) put(out + mb * 128, f == 0.f ? 0.f : o[mb][e] * f);
+          const bool turn = ++h == p.group;
+          out += turn ? next_query : p.os[2];
+          if (turn) h = 0;
         }
-        if (tid == 0) {
-          if (!all) *reinterpret_cast<float2*>(ws_ml + n * 2) = make_float2(s_m[n], L);
-          else if (p.lse) p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + kh * p.group + h] = lse_of(s_m[n], L);
-        }
-        if (++h == p.group) h = 0, ++i;
       }
     }
     tensor_fence_before();
