@@ -3,7 +3,7 @@
 //
 //   cache4_write_kernel, cache4_read_kernel  (kernel_cache4.cuh)
 //   attend4_split  (kernel_attend4.cuh) attention over it, the keys split evenly over the chip;
-//                  attend_join (kernel_attend.cuh) joins the parts of a request's keys
+//                  attend4_join joins the parts of a request's keys
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -43,6 +43,14 @@ int check_cache4(const asymspec_cache4* c) {
     return ASYMSPEC_ERR_MISALIGNED;
   if (static_cast<int64_t>(c->num_blocks) * c->block_size > kMax32 || c->kv_heads > 65536) return ASYMSPEC_ERR_TOO_LARGE;
   return ASYMSPEC_OK;
+}
+
+// For numbers k below 2^30 and n <= 2^s, d = ceil(2^(31 + s) / n) gives k / n = k * d >> (31 + s): d n is less than n
+// above 2^(31 + s), and k times that less than 2^(31 + s).
+void divide_by(int n, unsigned* d, int* s) {
+  *s = 0;
+  while ((1ll << *s) < n) ++*s;
+  *d = static_cast<unsigned>(((1ull << (31 + *s)) + n - 1) / n);
 }
 
 // What a write and a read have in common.
@@ -198,17 +206,17 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
       P.wide_codes = P.wide_codes && codes[w][i] % 32 == 0;
     }
   }
-  // For keys below 2^30 and a block size n <= 2^s, d = ceil(2^(31 + s) / n) gives key / n = key * d >> (31 + s): d n is
-  // less than n above 2^(31 + s), and key times that less than 2^(31 + s).
-  while ((1ll << P.shift) < p.block_size) ++P.shift;
-  P.divide = static_cast<unsigned>(((1ull << (31 + P.shift)) + p.block_size - 1) / p.block_size);
+  divide_by(p.block_size, &P.divide, &P.shift);
+  divide_by(p.group, &P.divide_rows, &P.shift_rows);
   if (!P.wide_scales || !P.wide_codes) k = attend4_kernels(dtype, p.D, p.rows, false);
   P.value_scale = cache->value_scale;
   int device = 0, sms = 0;
   cudaError_t e = device_sms(&device, &sms);
   if (e == cudaSuccess) e = prepare(k.split, device, k.smem);
   if (e != cudaSuccess) return cuda_fail(e);
-  int ctas = std::min(kAMaxCtas, sms * k.ctas_per_sm);
+  // as many CTAs as fit on the chip, but no more than there may be units of work (see attend_tiles)
+  const int64_t most = static_cast<int64_t>(table_width) * p.block_size / k.tile + 1 + kAItem;
+  int ctas = static_cast<int>(std::min<int64_t>(std::min(kAMaxCtas, sms * k.ctas_per_sm), B * most * p.kv_heads * p.row_tiles));
   const cudaStream_t st_ = static_cast<cudaStream_t>(stream);
   void* args[] = {&P};
   e = cudaLaunchKernel(k.split, dim3(ctas), dim3(k.threads), args, k.smem, st_);
@@ -218,7 +226,8 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(ctas - 1, std::min(p.rows, k.rows));
+  const int join_rows = std::min(p.rows, k.rows);
+  cfg.gridDim = join_rows <= 16 ? dim3(ctas - 1, join_rows) : dim3(std::min(4 * sms, (ctas - 1) * join_rows));
   cfg.blockDim = dim3(kAJoinThreads);
   cfg.stream = st_;
   cfg.attrs = attr;

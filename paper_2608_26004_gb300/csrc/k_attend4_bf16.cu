@@ -13,7 +13,7 @@ AttendKernels tensor_pick(bool fast) {
   static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
   return {fast ? reinterpret_cast<const void*>(&attend4_tensor<DP, RR, PER_SM, true>)
                : reinterpret_cast<const void*>(&attend4_tensor<DP, RR, PER_SM, false>),
-          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, RR>), DP, RR, kTThreads, smem, PER_SM};
+          reinterpret_cast<const void*>(&attend4_join<__nv_bfloat16, DP, RR>), DP, RR, kTThreads, smem, PER_SM, kTKeys};
 }
 
 AttendKernels attend4_kernels_bf16(int D, int rows, bool fast) {

@@ -11,7 +11,7 @@ AttendKernels attend4_pick() {
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
   static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
   return {reinterpret_cast<const void*>(&attend4_split<float, DP, NT, WR, ST, PER_SM>),
-          reinterpret_cast<const void*>(&attend_join<float, DP, rows>), DP, rows, 128 * WR, smem, PER_SM};
+          reinterpret_cast<const void*>(&attend4_join<float, DP, rows>), DP, rows, 128 * WR, smem, PER_SM, kATile};
 }
 
 AttendKernels attend4_kernels_f32(int D, int rows, bool) {

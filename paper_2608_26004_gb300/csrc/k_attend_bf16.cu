@@ -10,7 +10,7 @@ AttendKernels attend_pick() {
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
   static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
   return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, WR, ST, PER_SM, kH>),
-          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM};
+          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM, kATile};
 }
 
 // One, two or four warps for the rows of a group: as many as the rows fill.  us, 8 requests of

@@ -15,6 +15,8 @@ struct Attend4Params {
   float value_scale;
   unsigned divide;  // key / block_size is the high half of 2 key * divide, shifted
   int shift;
+  unsigned divide_rows;  // the same for row / group
+  int shift_rows;
   bool wide_scales;  // a token's scales of a head are DP / 16 bytes on such boundaries
   bool wide_codes;   // its codes DP / 2 bytes on 32-byte boundaries
 };
@@ -194,7 +196,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     info->first = u - at_unit;
     info->b = b;
     info->hr = hr;
-    info->tiles = at_unit > kAItem ? n_tiles : 0;
+    // (the first CTA that goes on with an item: the one before has its first tile)
+    info->tiles = at_unit > kAItem && shares.start(c - 1) <= u - at_unit + kAItem ? n_tiles : 0;
   }
 
   // what this lane loads of a step: chunk `chunk` of keys load_row + i * kLaneRows and of their values;
@@ -763,6 +766,109 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     ++hr;
   }
   if (err && p.err) atomicOr(p.err, err);
+}
+
+// The items whose keys lie in several CTAs' shares; the parts join in the order of the CTAs.  Up to 16 rows
+// (grid.y > 1 of them, or one) a CTA takes a row of the first CTA that went on with an item, if its CTA was one.  With
+// more rows most of so many CTAs would end at once (8 kv heads of 32 rows, 608 CTAs: 19,000 of them, 8 us):
+// each then looks for those CTAs among all, a few hundred numbers, and takes its turn of their rows.
+template <typename T, int DP, int kRows>
+__global__ void __launch_bounds__(kAJoinThreads) attend4_join(const __grid_constant__ AttendParams p, int ctas) {
+  constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_red[kAWarps];
+  __shared__ __align__(16) float s_x[kAJoinThreads * 4];
+  __shared__ uint16_t s_list[kAMaxCtas];
+  __shared__ int s_count[kAWarps];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const AttendInfo* info = reinterpret_cast<const AttendInfo*>(p.ws);
+  const float* ml = reinterpret_cast<const float*>(p.ws + kAInfoBytes);
+  const float* os = reinterpret_cast<const float*>(p.ws + kAInfoBytes + kMlBytes);
+  int count = 0;
+  const bool direct = gridDim.y > 1 || p.rows == 1;
+  if (direct && info[blockIdx.x + 1].tiles == 0) return;
+  for (int c0 = 0; c0 < (direct ? 0 : ctas); c0 += kAJoinThreads) {
+    const int c = c0 + tid;
+    const bool on = c < ctas && info[c].tiles != 0;
+    const unsigned which = __ballot_sync(~0u, on);
+    if (lane == 0) s_count[warp] = __popc(which);
+    __syncthreads();
+    int at = count;
+#pragma unroll
+    for (int w = 0; w < kAWarps; ++w) {
+      if (w < warp) at += s_count[w];
+      count += s_count[w];
+    }
+    if (on) s_list[at + __popc(which & ((1u << lane) - 1u))] = static_cast<uint16_t>(c);
+    __syncthreads();
+  }
+  const int rows_most = min(p.rows, kRows);
+  for (int w = direct ? 0 : blockIdx.x; w < (direct ? 1 : count * rows_most); w += gridDim.x) {
+    const int c = direct ? blockIdx.x + 1 : s_list[w / rows_most], r = direct ? blockIdx.y : w % rows_most;
+    const AttendInfo in = info[c];
+    const int R0 = (in.hr % p.row_tiles) * kRows, kh = in.hr / p.row_tiles;
+    if (R0 + r >= p.rows) continue;
+    const AttendShares shares(in.total, ctas);
+    const int c0 = c - 1, c1 = shares.owner(in.first + kAItem + in.tiles - 1);
+    const int parts = c1 - c0 + 1;
+    auto part_of = [&](int k) { return k == 0 ? 2 * c0 + 1 : 2 * (c0 + k); };
+    float M = -INFINITY;
+    for (int k = tid; k < parts; k += kAJoinThreads) {
+      const float2 x = *reinterpret_cast<const float2*>(ml + (static_cast<size_t>(part_of(k)) * kRows + r) * 2);
+      s_w[k] = x.x;
+      s_l[k] = x.y;
+      M = fmaxf(M, x.x);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
+    if (lane == 0) s_red[warp] = M;
+    __syncthreads();
+    M = s_red[0];
+#pragma unroll
+    for (int k = 1; k < kAWarps; ++k) M = fmaxf(M, s_red[k]);
+    const int col = tid % kCols, way = tid / kCols;
+    float x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+#pragma unroll 8
+    for (int k = way; k < parts; k += kWays) {
+      const float f = s_w[k] == M ? 1.f : ex2(s_w[k] - M);
+      const float4 o = *reinterpret_cast<const float4*>(os + (static_cast<size_t>(part_of(k)) * kRows + r) * DP + col * 4);
+      L = fmaf(f, s_l[k], L);
+      x[0] = fmaf(f, o.x, x[0]);
+      x[1] = fmaf(f, o.y, x[1]);
+      x[2] = fmaf(f, o.z, x[2]);
+      x[3] = fmaf(f, o.w, x[3]);
+    }
+    __syncthreads();
+    *reinterpret_cast<float4*>(s_x + tid * 4) = make_float4(x[0], x[1], x[2], x[3]);
+    if (col == 0) s_w[way] = L;
+    __syncthreads();
+    if (way == 0) {
+      L = s_w[0];
+      for (int k = 1; k < kWays; ++k) {
+        L += s_w[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += s_x[(k * kCols + col) * 4 + e];
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group, d = col * 4;
+      T* out = static_cast<T*>(p.out) + in.b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
+      if (d < p.D) {
+        __align__(16) T y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) put(y + k, x[k] * inv);
+        if (p.out_vec) {
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
+          else *reinterpret_cast<float4*>(out) = *reinterpret_cast<const float4*>(y);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) out[k] = y[k];
+        }
+      }
+      if (d == 0 && p.lse) p.lse[(static_cast<int64_t>(in.b) * p.Q + i) * p.heads + h] = lse_of(M, L);
+    }
+    __syncthreads();  // (before the next row's numbers)
+  }
 }
 
 }  // namespace asymspec_impl

@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   constexpr int NR = tensor_rows(RR), MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
   constexpr size_t kMlBytes = attend_ml_bytes(RR);
+  constexpr bool kValuesFirst = RR <= 8;  // values are turned before a step's weights are made
   constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -4.f, kLow = -8.f;
   extern __shared__ __align__(1024) unsigned char a_smem[];
   const AttendParams& p = P.a;
@@ -221,7 +222,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       info->first = u - at_unit;
       info->b = b;
       info->hr = hr;
-      info->tiles = at_unit > kAItem ? n_tiles : 0;
+      // (the first CTA that goes on with an item: the one before has its first tile)
+      info->tiles = at_unit > kAItem && shares.start(c - 1) <= u - at_unit + kAItem ? n_tiles : 0;
     }
   }
 
@@ -325,22 +327,24 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       load(0, page, at, kc, ks);
       tmem_wait_store();
     };
-    auto start_scores = [&] {  // one warp waits for the others and starts the products, the others go on
+    // Warps 1 to 3 say that their keys are turned and go on; warp 0 looks for that later, when it need not wait,
+    // and starts the products.
+    auto keys_turned = [&] {
       tensor_fence_before();
-      if (warp == 0) {
-        barrier_sync(1);
-        if (elected()) {
-          tensor_fence_after();
+      if (warp != 0) barrier_arrive(1);
+    };
+    auto start_scores = [&] {
+      if (warp != 0) return;
+      barrier_sync(1);
+      if (elected()) {
+        tensor_fence_after();
 #pragma unroll
-          for (int k = 0; k < DP / 16; ++k)
-            tensor_mma_t(tm_s, tm_k + k * 8, q_operand + ((k >> 2) * (NR * 128) + (k & 3) * 32) / 16, tensor_form(NR, false),
-                         k > 0);
-          tensor_commit(&s_bar[0]);
-        }
-        __syncwarp();
-      } else {
-        barrier_arrive(1);
+        for (int k = 0; k < DP / 16; ++k)
+          tensor_mma_t(tm_s, tm_k + k * 8, q_operand + ((k >> 2) * (NR * 128) + (k & 3) * 32) / 16, tensor_form(NR, false),
+                       k > 0);
+        tensor_commit(&s_bar[0]);
       }
+      __syncwarp();
     };
     find();
     take();
@@ -354,31 +358,43 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     // scores (in [2^-12, 2^11]) and saves looking for the largest; a row that has none of its warp's within
     // that range, or one above, raises the references all the same.
     const bool guess = lo + (t0 + 1) * kTKeys - 1 <= least && lo + t0 * kTKeys >= from && lo + (t0 + 1) * kTKeys <= end_key;
-    for (int r = warp; r < rows; r += kTThreads / 32) {
-      const int i = (R0 + r) / p.group, h = kh * p.group + R0 + r - i * p.group;
-      const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
-      float x[DP / 32];
-      unsigned most = 0;
+    constexpr int kBatch = RR / 4 < 4 ? RR / 4 : 4;  // rows of a warp that are on their way together
+#pragma unroll 1
+    for (int r0 = warp; r0 < rows; r0 += 4 * kBatch) {
+      uint16_t y[kBatch][DP / 32];
 #pragma unroll
-      for (int k = 0; k < DP / 32; ++k) {
-        const int d = lane + 32 * k;
-        x[k] = d < p.D ? to_f32(src[d]) : 0.f;
-        most = max(most, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-      }
-      const unsigned e = min(max(__reduce_max_sync(~0u, most) >> 23, 14u), 254u);
-      const float up = __uint_as_float((267u - e) << 23);  // 2^(13 - (e - 127))
+      for (int k = 0; k < kBatch; ++k) {
+        const int R = R0 + min(r0 + 4 * k, rows - 1);
+        const int i = static_cast<int>(__umulhi(2u * static_cast<unsigned>(R), P.divide_rows) >> P.shift_rows);
+        const uint16_t* src = static_cast<const uint16_t*>(p.q) + b * p.qs[0] + i * p.qs[1] +
+                              (kh * p.group + R - i * p.group) * p.qs[2] + lane;
 #pragma unroll
-      for (int k = 0; k < DP / 32; ++k) {
-        const int d = lane + 32 * k;
-        *reinterpret_cast<__half*>(s_q + (d >> 6) * (NR * 128) + r * 128 + (((d & 63) * 2) ^ ((r & 7) << 4))) =
-            __float2half_rn(x[k] * up);
+        for (int d = 0; d < DP; d += 32) y[k][d / 32] = lane + d < p.D ? src[d] : uint16_t(0);
       }
-      if (lane == 0) {
-        s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
-        s_m[r] = guess ? kGuess : -INFINITY;
-        s_sub[r] = guess ? kGuess : 0.f;
-        s_last[r] = len - p.Q + i;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int r = r0 + 4 * k;
+        if (r >= rows) continue;
+        float x[DP / 32];
+        unsigned most = 0;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+          x[d] = __uint_as_float(static_cast<unsigned>(y[k][d]) << 16);
+          most = max(most, __float_as_uint(x[d]) & 0x7FFFFFFFu);
+        }
+        const unsigned e = min(max(__reduce_max_sync(~0u, most) >> 23, 14u), 254u);
+        const float up = __uint_as_float((267u - e) << 23);  // 2^(13 - (e - 127))
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+          *reinterpret_cast<__half*>(s_q + (d >> 1) * (NR * 128) + r * 128 +
+                                     (((lane + 32 * (d & 1)) * 2) ^ ((r & 7) << 4))) = __float2half_rn(x[d] * up);
+        if (lane == 0) s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
       }
+    }
+    if (tid < rows) {
+      s_m[tid] = guess ? kGuess : -INFINITY;
+      s_sub[tid] = guess ? kGuess : 0.f;
+      s_last[tid] = len - p.Q + (R0 + tid) / p.group;
     }
     if (tid >= rows && tid < RR) s_factor[tid] = s_sub[tid] = 0.f;  // (scores beyond `rows` are 0 or NaN)
     float l[RR];
@@ -389,6 +405,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     const bool few = RR == 8 && rows <= RR / 2;
     fence_to_async();
     turn_keys();
+    keys_turned();
     start_scores();
 
     for (int t = t0; t < t1; ++t) {
@@ -401,30 +418,36 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       // the next step's keys, while the scores come
       if (t + 1 < t1) turn_keys();
       tmem_wait_load();
-      if (t + 1 < t1) start_scores();
-      // values, when those of the step before have been multiplied.  A NaN is left out of the products, where a
-      // weight of zero would make it one in rows that do not see it.
-      if (t > t0) wait(1, parity_o);
+      if (t + 1 < t1) keys_turned();
+      if (t > t0) wait(1, parity_o);  // (O of the step before: its weights and values have been read)
+      auto turn_values = [&] {
+        // Values.  A NaN is left out of the products, where a weight of zero would make it one in rows that do not
+        // see it.
 #pragma unroll
-      for (int i = 0; i < SW; ++i) {
-        vs[i] = live ? vs[i] : 0u;
-        const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-        if (nan) {
-          vs[i] &= ~((nan >> 7) * 0xFFu);
-          bad_values = true;
+        for (int i = 0; i < SW; ++i) {
+          vs[i] = live ? vs[i] : 0u;
+          const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+          if (nan) {
+            vs[i] &= ~((nan >> 7) * 0xFFu);
+            bad_values = true;
+          }
         }
-      }
 #pragma unroll
-      for (int w = 0; w < CW; ++w) {
-        const unsigned s2 = e4m3_to_f16(vs[w / 8] >> (w % 8 >= 4 ? 16 : 0));
-        const unsigned s = __byte_perm(s2, s2, w % 4 < 2 ? 0x1010 : 0x3232);
-        unsigned x[4];
-        e2m1_to_f16(vc[w], x);
+        for (int w = 0; w < CW; ++w) {
+          const unsigned s2 = e4m3_to_f16(vs[w / 8] >> (w % 8 >= 4 ? 16 : 0));
+          const unsigned s = __byte_perm(s2, s2, w % 4 < 2 ? 0x1010 : 0x3232);
+          unsigned x[4];
+          e2m1_to_f16(vc[w], x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
-        *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
+          for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
+          *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        if (t + 1 < t1) load(1, page_v, at_v, vc, vs);
+      };
+      if constexpr (kValuesFirst) {
+        turn_values();
+        if (t + 1 < t1) start_scores();
       }
-      if (t + 1 < t1) load(1, page_v, at_v, vc, vs);
       // scores less their references
       auto less = [&] {
 #pragma unroll
@@ -522,6 +545,10 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
           *reinterpret_cast<uint16_t*>(to + (p_byte ^ ((r & 7) << 4))) = static_cast<uint16_t>(w);
           *reinterpret_cast<uint16_t*>(to + 128 + (p_byte ^ (((r & 7) + 1) << 4))) = static_cast<uint16_t>(w >> 16);
         }
+      }
+      if constexpr (!kValuesFirst) {
+        if (t + 1 < t1) start_scores();
+        turn_values();
       }
       fence_to_async();
       tensor_fence_before();
