@@ -12,7 +12,10 @@ weights over a paged key-value cache of its own.  A round of every request:
   draft_tokens       the drafter's draw
   FuseVerify         the accepted drafts and the next token
 
-    python examples/serving_round.py [--requests 8] [--drafts 4] [--rounds 16]
+With --rotary, queries and keys are turned by their positions before that (Rotary); with
+--four-bits the caches are held in 4 bits (Cache4, cache4_write, Cache4Attend).
+
+    python examples/serving_round.py [--requests 8] [--drafts 4] [--rounds 16] [--rotary] [--four-bits]
 """
 from __future__ import annotations
 
@@ -52,19 +55,24 @@ class Context:
     """A model on one context of every request, of `tokens` tokens at most: its paged cache and the state
     of its plan."""
 
-    def __init__(self, model, B, most_new, tokens, block_size=16):
+    def __init__(self, model, B, most_new, tokens, block_size=16, rotary=None, four_bits=False):
         i32 = dict(dtype=torch.int32, device="cuda")
         width = -(-tokens // block_size)
         blocks = B * width
         shape = (blocks, block_size, model.kv_heads, model.dim)
         self.model, self.B, self.block_size = model, B, block_size
-        self.keys = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
-        self.values = torch.empty_like(self.keys)
+        self.rotary, self.four_bits = rotary, four_bits
+        if four_bits:
+            self.cache = S.Cache4.zeros(*shape)
+        else:
+            self.keys = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+            self.values = torch.empty_like(self.keys)
         self.tables = torch.full((B, width), -1, **i32)
         self.free = torch.randperm(blocks, device="cuda").to(torch.int32)
         self.state = dict(start=torch.zeros(B, **i32), held=torch.zeros(B, **i32),
                           free_count=torch.tensor([blocks], **i32))
-        self.attend = S.CacheAttend(B, most_new, model.heads, model.kv_heads, model.dim)
+        self.attend = (S.Cache4Attend if four_bits else S.CacheAttend)(B, most_new, model.heads, model.kv_heads,
+                                                                       model.dim)
         self.error = torch.zeros(1, **i32)
 
     def plan(self, grow, accepted=None, capacity=None):
@@ -80,12 +88,29 @@ class Context:
         return x, q.unflatten(-1, (m.heads, m.dim)), k.unflatten(-1, (m.kv_heads, m.dim)), \
             v.unflatten(-1, (m.kv_heads, m.dim))
 
+    def placed(self, q, k, positions):
+        """q [B, n, heads, dim] (or None) and k [B, n, kv_heads, dim] turned by the tokens' positions [B * n]."""
+        if self.rotary is None:
+            return q, k
+        turned, _ = self.rotary(k.flatten(0, 1), positions)
+        if q is not None:
+            q = self.rotary(q.flatten(0, 1), positions)[0].view(q.shape)
+        return q, turned.view(k.shape)
+
+    def write(self, k, v, slots):
+        k, v = k.flatten(0, 1), v.flatten(0, 1)
+        if self.four_bits:
+            S.cache4_write(k, v, self.cache, slots, error_word=self.error)
+        else:
+            S.cache_write(k, v, self.keys, self.values, slots, error_word=self.error)
+
     def prefill(self, prompts, lengths):
         """prompts: [tokens of all requests, one after another].  (One layer: its keys and values
         are all that later tokens need of a prompt.)"""
         self.plan(lengths, capacity=prompts.numel())
         _, _, k, v = self.project(prompts)
-        S.cache_write(k, v, self.keys, self.values, self.state["slots"], error_word=self.error)
+        _, k = self.placed(None, k[None], self.state["positions"])
+        self.write(k, v[None], self.state["slots"])
         # the next plan keeps what was just written, but for the last token: that is the first
         # round's first, which writes it again, at its place
         self.state = dict(self.state, start=(self.state["len"] - 1).clamp(min=0))
@@ -94,17 +119,20 @@ class Context:
         """[B, n, V] after each of the round's tokens first .. first + n - 1."""
         B, n = tokens.shape
         x, q, k, v = self.project(tokens)
-        slots = self.state["slots"].view(B, -1)[:, first:first + n].contiguous().view(-1)
-        S.cache_write(k.flatten(0, 1), v.flatten(0, 1), self.keys, self.values, slots, error_word=self.error)
+        slots, positions = (self.state[name].view(B, -1)[:, first:first + n].contiguous().view(-1)
+                            for name in ("slots", "positions"))
+        q, k = self.placed(q, k, positions)
+        self.write(k, v, slots)
         # (no more than its blocks hold: where the pool had none for a request, the table's entries
         # from there on are another's)
         seen = torch.minimum(self.state["start"] + (first + n), self.state["len"])
-        o, _ = self.attend(q, self.keys, self.values, self.tables, seen, error_word=self.error)
+        cache = (self.cache,) if self.four_bits else (self.keys, self.values)
+        o, _ = self.attend(q, *cache, self.tables, seen, error_word=self.error)
         return self.model.logits(x, o.flatten(2))
 
 
 class Loop:
-    def __init__(self, B=8, K=4, V=4096, prompt=(40, 200), rounds=16, seed=1):
+    def __init__(self, B=8, K=4, V=4096, prompt=(40, 200), rounds=16, seed=1, rotary=False, four_bits=False):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         i32 = dict(dtype=torch.int32, device="cuda")
         self.B, self.K, self.V = B, K, V
@@ -112,9 +140,10 @@ class Loop:
         verifier = Model(V, gen, near=drafter)
         full, short = prompt[1], prompt[0]  # tokens of a full context, and of a compressed one
         tokens = full + (K + 1) * (rounds + 1)
-        self.drafter_full = Context(drafter, B, 1, tokens)
-        self.drafter_comp = Context(drafter, B, K + 1, tokens)
-        self.verifier = Context(verifier, B, K + 1, tokens)
+        how = dict(rotary=S.Rotary(drafter.dim) if rotary else None, four_bits=four_bits)
+        self.drafter_full = Context(drafter, B, 1, tokens, **how)
+        self.drafter_comp = Context(drafter, B, K + 1, tokens, **how)
+        self.verifier = Context(verifier, B, K + 1, tokens, **how)
         self.contexts = (self.drafter_full, self.drafter_comp, self.verifier)
         lengths = torch.randint(short // 2, short + 1, (B,), generator=gen, **i32)
         prompts = torch.randint(0, V, (B, full), generator=gen, **i32)
@@ -206,8 +235,10 @@ def main():
     ap.add_argument("--requests", type=int, default=8)
     ap.add_argument("--drafts", type=int, default=4)
     ap.add_argument("--rounds", type=int, default=16)
+    ap.add_argument("--rotary", action="store_true", help="turn queries and keys by their positions")
+    ap.add_argument("--four-bits", action="store_true", help="hold the caches in 4 bits")
     a = ap.parse_args()
-    loop = Loop(B=a.requests, K=a.drafts, rounds=a.rounds)
+    loop = Loop(B=a.requests, K=a.drafts, rounds=a.rounds, rotary=a.rotary, four_bits=a.four_bits)
     step = torch.zeros(1, dtype=torch.int32, device="cuda")
     for _ in range(a.rounds):
         step |= loop.round()

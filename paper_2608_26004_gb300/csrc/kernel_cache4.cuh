@@ -52,108 +52,149 @@ struct Cache4Params {
   void* x[2];  // keys and values outside the cache
   int64_t xs[2][2];
   const int64_t* slots;
-  int T, num_blocks, block_size, kv_heads, groups;  // groups: of a head
-  int per_token;                                    // groups of a token's keys and values
+  int T, num_blocks, block_size, kv_heads;
+  int pairs;       // pairs of groups of 16 elements, of a head
+  int per_token;   // and of a token's keys and values
+  int log_lanes;   // 2^log_lanes threads take a token
   uint32_t* err;
 };
 
 constexpr int k4Threads = 256;
 
-// Copies, bound by their bytes: a thread takes 16 elements with one scale, neighbours those of a
-// head, then of the token's heads, then of its values.  WIDE: the elements lie on 16-byte boundaries.
+// Where a thread's pair of groups lies: of keys or values, the head, the pair.
+struct Cache4Place {
+  int which, h, pair;
+};
+__device__ __forceinline__ Cache4Place cache4_place(const Cache4Params& p, int e) {
+  const unsigned head_of = static_cast<unsigned>(e) / static_cast<unsigned>(p.pairs);
+  const int which = head_of >= static_cast<unsigned>(p.kv_heads);
+  return {which, static_cast<int>(head_of) - (which ? p.kv_heads : 0), e - static_cast<int>(head_of) * p.pairs};
+}
+__device__ __forceinline__ void load_wide(unsigned (&r)[8], const void* p) {
+  asm("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+}
+__device__ __forceinline__ void store_wide(void* p, const unsigned (&r)[8]) {
+  asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "l"(p) : "memory");
+}
+
+// Copies, bound by their bytes: a thread takes 32 elements with two scales, neighbours those of a head, then
+// of the token's heads, then of its values.  WIDE: the elements lie on 32-byte boundaries.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(k4Threads) cache4_write_kernel(const __grid_constant__ Cache4Params p) {
-  const int64_t total = static_cast<int64_t>(p.T) * p.per_token;
   const unsigned slots = static_cast<unsigned>(p.num_blocks) * static_cast<unsigned>(p.block_size);
-  for (int64_t w = static_cast<int64_t>(blockIdx.x) * k4Threads + threadIdx.x; w < total;
-       w += static_cast<int64_t>(gridDim.x) * k4Threads) {
-    const int64_t t = w / p.per_token;
-    const int e = static_cast<int>(w - t * p.per_token);
+  const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * (k4Threads >> p.log_lanes);
+  for (int64_t t = (static_cast<int64_t>(blockIdx.x) * k4Threads + threadIdx.x) >> p.log_lanes; t < p.T; t += stride) {
     const int64_t slot = p.slots[t];
     if (slot < 0) continue;
     if (slot >= slots) {
-      if (e == 0 && p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
+      if (lane == 0 && p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
       continue;
     }
     const unsigned block = static_cast<unsigned>(slot) / static_cast<unsigned>(p.block_size);
     const unsigned at = static_cast<unsigned>(slot) - block * static_cast<unsigned>(p.block_size);
-    const int head_of = e / p.groups, group = e - head_of * p.groups;
-    const int which = head_of >= p.kv_heads, h = head_of - (which ? p.kv_heads : 0);
-    const Cache4Part& c = p.part[which];
-    const T* x = static_cast<const T*>(p.x[which]) + t * p.xs[which][0] + h * p.xs[which][1] + group * 16;
-    float y[16];
-    if constexpr (WIDE) {
-      constexpr int N = 16 / sizeof(T);
-      uint4 v[16 / N];
+    for (int e = lane; e < p.per_token; e += lanes) {
+      const Cache4Place c = cache4_place(p, e);
+      const Cache4Part& part = p.part[c.which];
+      const T* x = static_cast<const T*>(p.x[c.which]) + t * p.xs[c.which][0] + c.h * p.xs[c.which][1] + c.pair * 32;
+      float y[32];
+      if constexpr (WIDE) {
+        constexpr int N = 32 / sizeof(T);
+        unsigned v[32 / N][8];
 #pragma unroll
-      for (int i = 0; i < 16 / N; ++i) v[i] = reinterpret_cast<const uint4*>(x)[i];
+        for (int i = 0; i < 32 / N; ++i) load_wide(v[i], x + i * N);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = to_f32(reinterpret_cast<const T*>(v)[i]);
-    } else {
+        for (int i = 0; i < 32; ++i) {
+          if constexpr (sizeof(T) == 4) y[i] = __uint_as_float(v[i / 8][i % 8]);
+          else y[i] = __uint_as_float(i % 2 ? v[i / 16][i / 2 % 8] & 0xFFFF0000u : v[i / 16][i / 2 % 8] << 16);
+        }
+      } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = to_f32(x[i]);
+        for (int i = 0; i < 32; ++i) y[i] = to_f32(x[i]);
+      }
+      unsigned code[4] = {0, 0, 0, 0}, scales = 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        // (as whole numbers: a NaN is above every magnitude)
+        unsigned most = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(y[16 * k + i]) & 0x7FFFFFFFu);
+        const unsigned s = e4m3_byte(__fmul_rn(__uint_as_float(most), part.to_units));
+        const float step = __fmul_rn(f16x2_to_f32(e4m3_to_f16(s)).x, part.scale);
+        const float r = step > 0.f ? __frcp_rn(step) : 0.f;
+        scales |= s << (8 * k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          code[2 * k + (i >> 2)] |= e2m1_pair(__fmul_rn(y[16 * k + 2 * i], r), __fmul_rn(y[16 * k + 2 * i + 1], r)) << (8 * (i & 3));
+      }
+      *reinterpret_cast<uint4*>(part.codes + block * part.cs[0] + at * part.cs[1] + c.h * part.cs[2] + c.pair * 16) =
+          make_uint4(code[0], code[1], code[2], code[3]);
+      *reinterpret_cast<uint16_t*>(part.scales + block * part.ss[0] + at * part.ss[1] + c.h * part.ss[2] + c.pair * 2) =
+          static_cast<uint16_t>(scales);
     }
-    // (as whole numbers: a NaN is above every magnitude)
-    unsigned most = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-    const unsigned s = e4m3_byte(__fmul_rn(__uint_as_float(most), c.to_units));
-    const float step = __fmul_rn(f16x2_to_f32(e4m3_to_f16(s)).x, c.scale);
-    const float r = step > 0.f ? __frcp_rn(step) : 0.f;
-    unsigned code[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      code[i >> 2] |= e2m1_pair(__fmul_rn(y[2 * i], r), __fmul_rn(y[2 * i + 1], r)) << (8 * (i & 3));
-    *reinterpret_cast<uint2*>(c.codes + block * c.cs[0] + at * c.cs[1] + h * c.cs[2] + group * 8) =
-        make_uint2(code[0], code[1]);
-    c.scales[block * c.ss[0] + at * c.ss[1] + h * c.ss[2] + group] = static_cast<char>(s);
   }
 }
 
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(k4Threads) cache4_read_kernel(const __grid_constant__ Cache4Params p) {
-  const int64_t total = static_cast<int64_t>(p.T) * p.per_token;
   const unsigned slots = static_cast<unsigned>(p.num_blocks) * static_cast<unsigned>(p.block_size);
-  for (int64_t w = static_cast<int64_t>(blockIdx.x) * k4Threads + threadIdx.x; w < total;
-       w += static_cast<int64_t>(gridDim.x) * k4Threads) {
-    const int64_t t = w / p.per_token;
-    const int e = static_cast<int>(w - t * p.per_token);
+  const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * (k4Threads >> p.log_lanes);
+  for (int64_t t = (static_cast<int64_t>(blockIdx.x) * k4Threads + threadIdx.x) >> p.log_lanes; t < p.T; t += stride) {
     const int64_t slot = p.slots[t];
     const bool there = slot >= 0 && slot < slots;
-    if (slot >= slots && e == 0 && p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
-    const int head_of = e / p.groups, group = e - head_of * p.groups;
-    const int which = head_of >= p.kv_heads, h = head_of - (which ? p.kv_heads : 0);
-    const Cache4Part& c = p.part[which];
-    unsigned code[2] = {0, 0}, s = 0;
-    if (there) {
-      const unsigned block = static_cast<unsigned>(slot) / static_cast<unsigned>(p.block_size);
-      const unsigned at = static_cast<unsigned>(slot) - block * static_cast<unsigned>(p.block_size);
-      const uint2 v = *reinterpret_cast<const uint2*>(c.codes + block * c.cs[0] + at * c.cs[1] + h * c.cs[2] + group * 8);
-      code[0] = v.x, code[1] = v.y;
-      s = static_cast<unsigned char>(c.scales[block * c.ss[0] + at * c.ss[1] + h * c.ss[2] + group]);
-    }
-    const unsigned s2 = e4m3_to_f16(s | s << 8);
-    T* x = static_cast<T*>(p.x[which]) + t * p.xs[which][0] + h * p.xs[which][1] + group * 16;
-    __align__(16) T y[16];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      unsigned f[4];
-      e2m1_to_f16(code[k], f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 v = f16x2_to_f32(mul_f16x2(f[i], s2));  // exact
-        const float a = __fmul_rn(v.x, c.scale), b = __fmul_rn(v.y, c.scale);
-        if constexpr (sizeof(T) == 4) y[8 * k + 2 * i] = a, y[8 * k + 2 * i + 1] = b;
-        else y[8 * k + 2 * i] = __float2bfloat16_rn(a), y[8 * k + 2 * i + 1] = __float2bfloat16_rn(b);
+    if (slot >= slots && lane == 0 && p.err) atomicOr(p.err, ASYMSPEC_DATA_BAD_INDEX);
+    const unsigned of = there ? static_cast<unsigned>(slot) : 0;
+    const unsigned block = of / static_cast<unsigned>(p.block_size), at = of - block * static_cast<unsigned>(p.block_size);
+    for (int e = lane; e < p.per_token; e += lanes) {
+      const Cache4Place c = cache4_place(p, e);
+      const Cache4Part& part = p.part[c.which];
+      uint4 code = make_uint4(0, 0, 0, 0);
+      unsigned scales = 0;
+      if (there) {
+        code = *reinterpret_cast<const uint4*>(part.codes + block * part.cs[0] + at * part.cs[1] + c.h * part.cs[2] + c.pair * 16);
+        scales = *reinterpret_cast<const uint16_t*>(part.scales + block * part.ss[0] + at * part.ss[1] + c.h * part.ss[2] + c.pair * 2);
       }
-    }
-    if constexpr (WIDE) {
+      const unsigned both = e4m3_to_f16(scales);
+      T* x = static_cast<T*>(p.x[c.which]) + t * p.xs[c.which][0] + c.h * p.xs[c.which][1] + c.pair * 32;
+      const unsigned words[4] = {code.x, code.y, code.z, code.w};
 #pragma unroll
-      for (int i = 0; i < static_cast<int>(sizeof(T)); ++i)
-        reinterpret_cast<uint4*>(x)[i] = reinterpret_cast<const uint4*>(y)[i];
-    } else {
+      for (int k = 0; k < 2; ++k) {
+        const unsigned s2 = __byte_perm(both, both, k ? 0x3232 : 0x1010);
+        float y[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = y[i];
+        for (int w = 0; w < 2; ++w) {
+          unsigned f[4];
+          e2m1_to_f16(words[2 * k + w], f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = f16x2_to_f32(mul_f16x2(f[i], s2));  // exact
+            y[8 * w + 2 * i] = __fmul_rn(v.x, part.scale);
+            y[8 * w + 2 * i + 1] = __fmul_rn(v.y, part.scale);
+          }
+        }
+        if constexpr (WIDE) {
+          constexpr int N = 32 / sizeof(T);
+#pragma unroll
+          for (int i = 0; i < 16 / N; ++i) {
+            unsigned v[8];
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+              if constexpr (sizeof(T) == 4) v[d] = __float_as_uint(y[8 * i + d]);
+              else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[d]) : "f"(y[2 * d + 1]), "f"(y[2 * d]));
+            }
+            store_wide(x + 16 * k + i * N, v);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if constexpr (sizeof(T) == 4) x[16 * k + i] = y[i];
+            else x[16 * k + i] = __float2bfloat16_rn(y[i]);
+          }
+        }
+      }
     }
   }
 }

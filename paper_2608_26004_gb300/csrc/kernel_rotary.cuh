@@ -26,7 +26,7 @@ struct RotaryParams {
 };
 
 constexpr int kRThreads = 256;
-constexpr int kRBatch = 4;       // units that a thread has on their way together
+constexpr int kRBatch = 3;       // units that a thread has on their way together
 constexpr int kRTable = 2048;    // cosines and sines of a CTA's tokens at most
 constexpr int kRTokens = 256;    // tokens of a CTA at most
 
