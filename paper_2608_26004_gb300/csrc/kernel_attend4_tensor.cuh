@@ -47,8 +47,10 @@ __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// All products issued before arrive at `bar` when they are done.
+// All products issued before arrive at `bar` when they are done; and this thread does, so that who waits there
+// sees what this thread has seen.
 __device__ __forceinline__ void tensor_commit(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // D (+)= A B, fp16 products and fp32 sums: A in tensor memory, or in shared memory.
@@ -117,7 +119,7 @@ __host__ __device__ constexpr int tensor_rows(int rows) { return rows < 16 ? 16 
 __host__ __device__ constexpr int tensor_query_blocks(int DP) { return DP > 64 ? DP / 64 : 1; }  // 64s of elements
 constexpr size_t tensor_smem_bytes(int DP, int NR) {
   return static_cast<size_t>(tensor_blocks(DP)) * 32768 + static_cast<size_t>(NR) * (256 + tensor_query_blocks(DP) * 128) +
-         static_cast<size_t>(NR) * 4 * 9 + 1024;
+         static_cast<size_t>(NR) * 4 * 10 + 1024;
 }
 
 // The keys are split evenly over the CTAs as attend_split's are, in steps of 128, one a thread.  Of a step, both
@@ -151,7 +153,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   int* const s_last = reinterpret_cast<int*>(s_factor + NR);
   float* const s_red = reinterpret_cast<float*>(s_last + NR);  // [4][NR]
   float* const s_up = s_red + 4 * NR;
-  float* const s_sub = s_up + NR;  // what scores are taken less: the reference, or 0 where there is none yet
+  float* const s_fall = s_up + NR;
+  float* const s_sub = s_fall + NR;  // what scores are taken less: the reference, or 0 where there is none yet
   __shared__ __align__(8) unsigned long long s_bar[2];
   __shared__ unsigned s_tmem;
   __shared__ int64_t s_scan[kTThreads / 32], s_find[2];
@@ -161,8 +164,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   unsigned err = 0;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
-    mbar_init(&s_bar[0], 1);
-    mbar_init(&s_bar[1], 1);
+    mbar_init(&s_bar[0], 2);
+    mbar_init(&s_bar[1], 2);
     fence_mbar_init();
   }
   if (warp == 0) tmem_alloc<kCols>(smem_u32(&s_tmem));
@@ -506,14 +509,14 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
           s_m[n] = none ? -INFINITY : s_sub[n] + up;
           s_sub[n] = none ? 0.f : s_sub[n] + up;
           s_up[n] = up;
-          s_red[n] = empty || up == 0.f ? 1.f : ex2(-up);
+          s_fall[n] = empty || up == 0.f ? 1.f : ex2(-up);
         }
         __syncthreads();
         fresh = false;
 #pragma unroll
         for (int n = 0; n < RR; ++n)
           if (n < rows) {
-            l[n] *= s_red[n];
+            l[n] *= s_fall[n];
             S[n] -= s_up[n];
             fresh = fresh || s_m[n] == -INFINITY;
           }
@@ -526,7 +529,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
               tmem_load8(tm_o + mb * NR + tm_warp + n, o);
               tmem_wait_load();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_red[n + e] : 1.f;
+              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_fall[n + e] : 1.f;
               tmem_store8(tm_o + mb * NR + tm_warp + n, o);
             }
           tmem_wait_store();
