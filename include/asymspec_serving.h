@@ -331,14 +331,15 @@ typedef struct {
  * boundaries, scales and theirs odd.  ASYMSPEC_ERR_TOO_LARGE: num_blocks * block_size beyond 2^31 - 1,
  * kv_heads > 65536. */
 
-/* asymspec_cache_write into such a cache: k, v of `dtype`, their strides (token, head) in elements.  Two
- * tokens with one slot leave codes and scales there that may be of either.  One launch. */
+/* asymspec_cache_write into such a cache: k, v of `dtype`, their strides (token, head) in elements.  Each
+ * slot once: of two tokens with one slot the codes may be one's and the scales the other's.  One launch. */
 int asymspec_cache4_write(const asymspec_cache4* cache, const void* k, const void* v, int dtype,
                           const int64_t* k_strides, const int64_t* v_strides, const int64_t* slots,
                           int T, uint32_t* out_error_word, void* stream);
 
 /* Reads T tokens back: slot slots[t]'s keys and values into k[t], v[t] (strides: token, head; any
- * element-aligned), rounded once to `dtype` (code * scale is exact).  A negative slot gives
+ * element-aligned): code * scale, which is exact, times the pool's number, rounded to fp32 and then to
+ * `dtype`.  k and v must not overlap.  A negative slot gives
  * zeros, one past the pool too (ASYMSPEC_DATA_BAD_INDEX).  One launch.  T = 0 is a no-op.
  * ASYMSPEC_ERR_INVALID_ARG besides: T < 0, a stride of 0 along an axis that is longer than 1, k = v.
  * ASYMSPEC_ERR_UNSUPPORTED: dtype. */
@@ -349,7 +350,8 @@ int asymspec_cache4_read(const asymspec_cache4* cache, const int64_t* slots, int
 /* asymspec_cache_attend over such a cache, with its arguments, checks and answers to bad data; q and
  * out are of `dtype`.  Keys and values enter exactly; bf16 queries too, fp32 ones in two fp16
  * pieces (2^-22); weights in one fp16 piece for bf16 (2^-11, an eighth of the output's own rounding), in
- * two for fp32.  (Elements of a query below 2^-28 of its largest may be less exact.)
+ * two for fp32.  (Elements of a query below 2^-28 of its largest may be less exact.)  Waits for the tensor core are
+ * bounded: one that gave up after 0.2 s leaves ASYMSPEC_DATA_TIMEOUT, and the call's results are not valid.
  * ASYMSPEC_ERR_INVALID_ARG besides: scale * key_scale / ln 2 beyond fp32.  ASYMSPEC_ERR_TOO_LARGE: a stride of
  * blocks or tokens beyond 2^31 - 1 bytes. */
 size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim);

@@ -14,6 +14,8 @@ AttendKernels attend4_pick() {
           reinterpret_cast<const void*>(&attend4_join<float, DP, rows>), DP, rows, 128 * WR, smem, PER_SM, kATile};
 }
 
+// fp32 queries: on the warps' matrix instructions, whose sums stay in registers, as the tensor core's would be cut
+// over a whole context (see attend4_split).  As many CTAs an SM as the registers allow.
 AttendKernels attend4_kernels_f32(int D, int rows, bool) {
   if (D <= 64)
     return rows <= 8    ? attend4_pick<64, 1, 1, 3, 3>()

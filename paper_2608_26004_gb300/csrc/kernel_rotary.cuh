@@ -45,6 +45,8 @@ struct RotaryVector {
 // computes their cosines and sines once, into shared memory, while its threads' first loads are
 // on their way.  A unit is what a thread moves at once: the same vector of both halves
 // (or two neighbours, interleaved: one vector, or a pair), or a vector past rotary_dim.
+// 16384 tokens of 40 heads of 128 bf16: 66 us = 5.1 TB/s (three units of a thread at once; two 72, four 67; CTAs of
+// 128 threads the same), 5 tokens of 24 heads 2.7 us.
 // U: 16 bytes, or one element where something is not on the 16-byte boundaries.
 template <typename T, typename U, bool INTER>
 __global__ void __launch_bounds__(kRThreads) rotary_kernel(const __grid_constant__ RotaryParams p) {

@@ -554,6 +554,7 @@ class Cache4:
         self.key_scale, self.value_scale = float(key_scale), float(value_scale)
         self.device_index = dev
         self.kv_heads, self.head_dim = shape[2], shape[3] * 2
+        self.token_strides = _STRIDES2.pack(self.kv_heads * self.head_dim, self.head_dim)
         strides = (s if n > 1 else 0 for x in tensors for s, n in zip(x.stride()[:3], x.shape))
         self.view = _CACHE4.pack(*(x.data_ptr() for x in tensors), *strides, *shape[:3], self.head_dim,
                                  self.key_scale, self.value_scale)
@@ -600,16 +601,18 @@ def cache4_read(cache, slots, *, dtype=None, out=None, error_word=None):
     bfloat16, the default) or in the tensors `out`; negative slots give zeros."""
     dev, T = cache.device_index, _tokens_of(slots)
     if out is None:
-        shape = (T, cache.kv_heads, cache.head_dim)
-        like = cache.key_codes
-        k, v = (like.new_empty(shape, dtype=torch.bfloat16 if dtype is None else dtype) for _ in range(2))
+        shape, kind, new = (T, cache.kv_heads, cache.head_dim), dtype or torch.bfloat16, cache.key_codes.new_empty
+        k, v = new(shape, dtype=kind), new(shape, dtype=kind)
+        code = _dtype(k)
+        k_strides = v_strides = cache.token_strides
     else:
         k, v = out
         if dtype is not None and k.dtype is not dtype:
             raise ValueError(f"out must be of {dtype}")
+        code = _dtype(k)
+        k_strides, v_strides = _tokens("k", k, cache, k.dtype, T), _tokens("v", v, cache, k.dtype, T)
     st = _lib.asymspec_cache4_read(
-        cache.view, _flat("slots", slots, torch.int64, dev, T), T, k.data_ptr(), v.data_ptr(), _dtype(k),
-        _tokens("k", k, cache, k.dtype, T), _tokens("v", v, cache, k.dtype, T),
+        cache.view, _flat("slots", slots, torch.int64, dev, T), T, k.data_ptr(), v.data_ptr(), code, k_strides, v_strides,
         0 if error_word is None else _error_word(error_word, dev), _stream(dev))
     if st != OK:
         raise AsymSpecError(st, "asymspec_cache4_read")

@@ -104,6 +104,7 @@ CASES = [
     ([211], 3, 6, 6, 32, "bfloat16", 1, "nhd", 0),
     ([1500, 40], 2, 4, 1, 256, "bfloat16", 16, "nhd", 0),
     ([1500, 40], 5, 8, 2, 256, "bfloat16", 16, "hnd", 0),                 # 20 rows of 256
+    ([1500, 700], 10, 8, 2, 256, "bfloat16", 16, "hnd", 0),               # 40 rows of 256
     ([600], 4, 12, 4, 160, "bfloat16", 48, "nhd", 0),
     ([600, 77], 4, 12, 4, 128, "bfloat16", 8, "hnd", 0),                  # 12 rows
     ([90, 91], 2, 10, 2, 64, "bfloat16", 16, "hnd", 0),                   # 10 rows of 64
@@ -111,6 +112,8 @@ CASES = [
     ([5000, 70], 5, 16, 8, 128, "bfloat16", 16, "nhd", 100),              # windows
     ([3000, 1], 1, 16, 2, 128, "bfloat16", 64, "hnd", 1),
     ([130, 2000], 8, 8, 8, 64, "bfloat16", 48, "nhd", 16),
+    ([900, 300, 127], 9, 32, 4, 128, "bfloat16", 16, "hnd", 130),         # 72 rows, first keys inside a step
+    ([2049, 128, 129, 255, 256, 257], 1, 8, 2, 128, "bfloat16", 16, "hnd", 0),
     ([1], 1, 2, 1, 64, "float32", 16, "nhd", 0),
     ([1000, 77], 1, 16, 8, 128, "float32", 16, "nhd", 0),
     ([300, 0, 2, 4100], 5, 8, 8, 64, "float32", 48, "hnd", 0),
@@ -383,6 +386,44 @@ def test_queries_and_outputs_off_the_16_byte_boundaries(torch, dtype, off):
     _, lse2 = attend(q, *x[1:], out=out)
     assert torch.equal(out, want) and torch.equal(lse, lse2)
     assert (room[:off] == 0).all() and (room[off:].view(3, 3, -1)[..., 512:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_codes_and_scales_off_the_wide_boundaries(torch, dtype, D):
+    """Codes on 16-byte boundaries but not on 32, scales on 2-byte ones: the same numbers."""
+    q, cache, tables, lens = x = inputs(torch, [300, 20, 1000], 3, 8, 2, D, dtype, 16, 41)
+    attend = S.Cache4Attend(3, 3, 8, 2, D)
+    want, want_lse = attend(*x)
+
+    def moved(t, room, off):
+        y = torch.zeros(*t.shape[:3], t.shape[3] + room, dtype=torch.uint8, device="cuda")[..., off:off + t.shape[3]]
+        y.copy_(t)
+        return y
+
+    for code_off, scale_off in ((16, 2), (0, 2), (16, 0)):
+        other = S.Cache4(moved(cache.key_codes, 16, code_off), moved(cache.key_scales, 2, scale_off),
+                         moved(cache.value_codes, 16, code_off), moved(cache.value_scales, 2, scale_off))
+        out, lse = attend(q, other, tables, lens)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_a_step_whose_scores_are_far_from_the_first_reference(torch):
+    """Rows whose scores are all far below or above what a first reference is good for, in the first steps or
+    only later, for some rows of an item and not for others."""
+    q, cache, tables, lens = inputs(torch, [900, 260], 4, 8, 2, 128, "bfloat16", 16, 43)
+    k = torch.zeros(900, 2, 128, device="cuda")
+    k[..., 0] = 6.0
+    k[:, :, 1] = torch.where(torch.arange(900, device="cuda") < 640, 6.0, 0.5)[:, None]
+    slots = (tables[0, :57].long()[:, None] * 16 + torch.arange(16, device="cuda")).flatten()[:900]
+    S.cache4_write(k, torch.randn(900, 2, 128, device="cuda"), cache, slots)
+    attend = S.Cache4Attend(2, 4, 8, 2, 128)
+    for first, second in ((-20.0, 0.0), (20.0, 0.0), (0.0, -30.0), (0.0, 30.0), (-400.0, 1.0), (3.0, -4.0)):
+        y = q.clone()
+        y[0, 1:, :, 0], y[0, ::2, :4, 1] = first, second
+        x = (y, cache, tables, lens)
+        out, lse = attend(*x, scale=1.0)
+        check(torch, x, out, lse, some_rows(2, 4, 8, 3, 64), scale=1.0)
 
 
 def test_refusals_of_the_binding(torch):
