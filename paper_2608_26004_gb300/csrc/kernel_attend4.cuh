@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
   constexpr int kLoads = kASubs * kAKeys > kLaneRows ? kASubs * kAKeys / kLaneRows : 1;
   constexpr int U = NT == 1 ? kASubs : 1;          // sixteens of keys that are worked at together
   constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  constexpr float kBelow = 7.f, kSlack = 8.f;
+  constexpr float kBelow = BF ? 7.f : 12.f, kSlack = 15.f - kBelow;
   constexpr bool kQRegs = kPieces * NT * KW * 4 <= 32;
   static_assert(ST >= 2 && kStep % 16 == 0 && kGroup % 16 == 0, "the ring");
   extern __shared__ __align__(1024) unsigned char a_smem[];
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
         // Weights are 2^(s - m), m kBelow below the largest score at the time; only a score kSlack above
         // that raises it (the maximum itself, kept, would rescale the values at most steps, for one
         // of the rows or another).  So weights stay below 2^15, and fp16, whose step is 2^-24 at the
-        // smallest, holds one of 2^-31 of a row's largest.
+        // smallest, holds one of 2^-31 (fp32: 2^-36) of a row's largest.
         bool above = false;
         float top[NT][2];
 #pragma unroll

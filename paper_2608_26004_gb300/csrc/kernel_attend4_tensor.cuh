@@ -9,6 +9,11 @@ namespace asymspec_impl {
 constexpr int kTThreads = 128;
 constexpr int kTKeys = 128;  // keys of a step, one a thread: the unit of the split
 constexpr unsigned long long kTWaitNs = 200000000ull;
+#ifdef ASYMSPEC_TEST_LATE_PRODUCTS  // (a test's build: every wait, once it has ended, counts as one that gave up)
+constexpr bool kTestLate = true;
+#else
+constexpr bool kTestLate = false;
+#endif
 
 __device__ __forceinline__ int tensor_tiles(const AttendParams& p, int len) {
   return max(1, (len - attend_first(p, len) + kTKeys - 1) / kTKeys);
@@ -150,7 +155,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
   constexpr size_t kMlBytes = attend_ml_bytes(RR);
   constexpr bool kValuesFirst = RR <= 8;  // values are turned before a step's weights are made
-  constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -4.f, kLow = -8.f;
+  constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -7.f, kLow = 7.f;
   extern __shared__ __align__(1024) unsigned char a_smem[];
   const AttendParams& p = P.a;
   unsigned char* const s_v = a_smem + (-smem_u32(a_smem) & 1023u);  // (the operands' rows are 1024-byte patterns)
@@ -163,7 +168,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   float* const s_up = s_red + 4 * NR;
   float* const s_fall = s_up + NR;
   float* const s_sub = s_fall + NR;  // what scores are taken less: the reference, or 0 where there is none yet
-  __shared__ __align__(8) unsigned long long s_bar[2];
+  __shared__ __align__(8) unsigned long long s_bar[3];  // scores, what is summed; all, after a wait that gave up
   __shared__ unsigned s_tmem;
   __shared__ int64_t s_scan[kTThreads / 32], s_find[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -174,6 +179,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   if (tid == 0) {
     mbar_init(&s_bar[0], 2);
     mbar_init(&s_bar[1], 2);
+    mbar_init(&s_bar[2], 4);
     fence_mbar_init();
   }
   if (warp == 0) tmem_alloc<kCols>(smem_u32(&s_tmem));
@@ -239,8 +245,10 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   }
 
   unsigned parity_s = 0, parity_o = 0;
+  // (a thread that gave up waits no more, and starts no products)
+  auto gave_up = [&] { return (err & ASYMSPEC_DATA_TIMEOUT) != 0; };
   auto wait = [&](int which, unsigned& parity) {
-    if (!(err & ASYMSPEC_DATA_TIMEOUT) && !mbar_wait_bounded(&s_bar[which], parity, kTWaitNs)) err |= ASYMSPEC_DATA_TIMEOUT;
+    if (!gave_up() && (!mbar_wait_bounded(&s_bar[which], parity, kTWaitNs) || kTestLate)) err |= ASYMSPEC_DATA_TIMEOUT;
     parity ^= 1;
     tensor_fence_after();
   };
@@ -347,7 +355,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     auto start_scores = [&] {
       if (warp != 0) return;
       barrier_sync(1);
-      if (elected()) {
+      if (elected() && !gave_up()) {
         tensor_fence_after();
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
@@ -365,9 +373,10 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     // the item's queries, each row times the power of two that takes its largest element to 2^13
     const int least = len - p.Q + R0 / p.group;
     const int from = p.window ? len - p.Q + (R0 + rows - 1) / p.group - p.window + 1 : 0;
-    // A first reference: if every row sees all keys of the first step, 2^kGuess is close enough to most
-    // scores (in [2^-12, 2^11]) and saves looking for the largest; a row that has none of its warp's within
-    // that range, or one above, raises the references all the same.
+    // A first reference: if every row sees all keys of the first step, kGuess is close enough to most rows'
+    // largest scores (0 to 8) and saves looking for them; a row whose largest of a warp's 32 is below that, or that
+    // has one above, raises the references all the same.  So a row's largest weight is never below 2^kBelow: fp16
+    // loses 2^-25 at most of each small one, which many keys may have.
     const bool guess = lo + (t0 + 1) * kTKeys - 1 <= least && lo + t0 * kTKeys >= from && lo + (t0 + 1) * kTKeys <= end_key;
     constexpr int kBatch = RR / 4 < 4 ? RR / 4 : 4;  // rows of a warp that are on their way together
 #pragma unroll 1
@@ -565,7 +574,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       tensor_fence_before();
       if (warp == 1) {
         barrier_sync(2);
-        if (elected()) {
+        if (elected() && !gave_up()) {
           tensor_fence_after();
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb)
@@ -671,7 +680,12 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     tensor_fence_after();
   }
   if (err && p.err) atomicOr(p.err, err);
-  __syncthreads();
+  if (__syncthreads_or(gave_up())) {
+    // products may be under way, of what is freed here
+    if (warp < 2 && elected()) tensor_commit(&s_bar[2]);
+    mbar_wait_bounded(&s_bar[2], 0, kTWaitNs);
+    __syncthreads();
+  }
   if (warp == 0) tmem_free<kCols>(tm_k);
 }
 

@@ -426,6 +426,28 @@ def test_a_step_whose_scores_are_far_from_the_first_reference(torch):
         check(torch, x, out, lse, some_rows(2, 4, 8, 3, 64), scale=1.0)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_keys_far_below_a_few(torch, dtype):
+    """Four keys of the first step, one of each warp's, and 32,764 whose weights are 2^-18.1 of theirs each: a
+    30th of the result together, and of the only values that are not zero.  80 requests share the pages, so that a
+    CTA takes most of an item's keys by itself."""
+    n, B = 32768, 80
+    q, cache, tables, _ = inputs(torch, [n], 1, 8, 8, 64, dtype, 16, 47)
+    k, v = torch.zeros(2, n, 8, 64, device="cuda")
+    few = torch.zeros(n, device="cuda", dtype=torch.bool)
+    few[:128:32] = True
+    k[..., 0] = 6.0
+    k[~few, :, 1] = 6.0
+    v[~few] = 6.0
+    slots = (tables[0, :n // 16].long()[:, None] * 16 + torch.arange(16, device="cuda")).flatten()
+    S.cache4_write(k, v, cache, slots)
+    y = torch.zeros_like(q)
+    y[..., 0], y[..., 1] = (-11.5 / 6 * math.log(2.0), -18.1 / 6 * math.log(2.0))
+    x = (y.repeat(B, 1, 1, 1), cache, tables.repeat(B, 1), torch.full((B,), n, device="cuda", dtype=torch.int32))
+    out, lse = S.Cache4Attend(B, 1, 8, 8, 64)(*x, scale=1.0)
+    check(torch, x, out, lse, [(0, 0, 0), (41, 0, 3), (79, 0, 7)], scale=1.0)
+
+
 def test_refusals_of_the_binding(torch):
     q, cache, tables, lens = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.Cache4Attend(2, 2, 4, 2, 64)
