@@ -288,7 +288,7 @@ typedef struct {
  * is a no-op.
  * ASYMSPEC_ERR_INVALID_ARG: a null pointer, T < 0, heads < 1, head_dim < 1, rotary_dim odd, < 2 or >
  * head_dim, a negative stride, a stride of 0 along an axis of an output that is longer than 1, in = out
- * with other strides, q and k with one output, a magnitude that is not finite.
+ * with other strides, q and k with one output or one's output the other's input, a magnitude that is not finite.
  * ASYMSPEC_ERR_UNSUPPORTED: dtype, head_dim > ASYMSPEC_ROTARY_MAX_D.  ASYMSPEC_ERR_MISALIGNED.
  * ASYMSPEC_ERR_TOO_LARGE: heads > 65536. */
 #define ASYMSPEC_ROTARY_MAX_D 1024

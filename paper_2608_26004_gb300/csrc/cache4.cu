@@ -49,14 +49,6 @@ int check_cache4(const asymspec_cache4* c) {
   return ASYMSPEC_OK;
 }
 
-// For numbers k below 2^30 and n <= 2^s, d = ceil(2^(31 + s) / n) gives k / n = k * d >> (31 + s): d n is less than n
-// above 2^(31 + s), and k times that less than 2^(31 + s).
-void divide_by(int n, unsigned* d, int* s) {
-  *s = 0;
-  while ((1ll << *s) < n) ++*s;
-  *d = static_cast<unsigned>(((1ull << (31 + *s)) + n - 1) / n);
-}
-
 // What a write and a read have in common.
 int move(const asymspec_cache4* c, const void* k, const void* v, int dtype, const int64_t* k_strides,
          const int64_t* v_strides, const int64_t* slots, int T, uint32_t* err, bool read, void* stream) {

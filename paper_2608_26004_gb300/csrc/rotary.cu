@@ -105,7 +105,8 @@ int asymspec_rotary(const asymspec_rotary_heads* q, const asymspec_rotary_heads*
   if (!positions || !steps) return ASYMSPEC_ERR_INVALID_ARG;
   for (const asymspec_rotary_heads* x : both)
     if (x && (!x->in || !x->out)) return ASYMSPEC_ERR_INVALID_ARG;
-  if (k && q->out == k->out) return ASYMSPEC_ERR_INVALID_ARG;
+  // (a swap in place, too: one's outputs would be the other's inputs)
+  if (k && (q->out == k->out || q->out == k->in || k->out == q->in)) return ASYMSPEC_ERR_INVALID_ARG;
   const int elt = elt_size(dtype), per = 16 / elt;
   if (!aligned(positions, 4) || !aligned(steps, 8)) return ASYMSPEC_ERR_MISALIGNED;
   bool wide = (interleaved ? rotary_dim : rotary_dim / 2) % per == 0 && head_dim % per == 0;
@@ -134,10 +135,11 @@ int asymspec_rotary(const asymspec_rotary_heads* q, const asymspec_rotary_heads*
     for (int s = 0; s < 2; ++s) y.is[s] = x->in_strides[s], y.os[s] = x->out_strides[s];
     y.heads = x->heads;
     y.units = p.turning + (x->in == x->out ? 0 : (head_dim - rotary_dim) / (wide ? per : 1));
+    divide_by(y.units, &y.divide, &y.shift);
     units += static_cast<int64_t>(y.heads) * y.units;
   }
-  if (units > kMax32) return ASYMSPEC_ERR_TOO_LARGE;
-  p.all_units = static_cast<int>(units);
+  p.all_units = static_cast<int>(units);  // (2^27 at most)
+  divide_by(p.all_units, &p.divide, &p.shift);
   int device = 0, sms = 0;
   const cudaError_t e = device_sms(&device, &sms);
   if (e != cudaSuccess) return cuda_fail(e);

@@ -40,6 +40,14 @@ inline cudaError_t prepare(const void* fn, int device, int smem) {
   return e;
 }
 
+// For numbers k below 2^30 and n <= 2^s, d = ceil(2^(31 + s) / n) gives k / n = k * d >> (31 + s): d n is less than n
+// above 2^(31 + s), and k times that less than 2^(31 + s).
+inline void divide_by(int n, unsigned* d, int* s) {
+  *s = 0;
+  while ((1ll << *s) < n) ++*s;
+  *d = static_cast<unsigned>(((1ull << (31 + *s)) + n - 1) / n);
+}
+
 inline cudaError_t device_sms(int* device, int* sms) {
   const cudaError_t e = cudaGetDevice(device);
   return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device) : e;

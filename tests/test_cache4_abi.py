@@ -40,7 +40,10 @@ def test_rotary_validation_codes(lib):
                 dict(q=heads(in_strides=(-1, 64))), dict(q=heads(out_strides=(256, -64))),
                 dict(q=heads(out_strides=(0, 64))), dict(q=heads(out_strides=(256, 0))),
                 dict(q=heads(out=FAKE, out_strides=(512, 64))), dict(k=heads(n=-1)),
-                dict(k=heads())):                                        # both into one output
+                dict(k=heads()),                                         # both into one output
+                dict(q=heads(x=FAKE, out=2 * FAKE), k=heads(x=3 * FAKE, out=FAKE)),  # one's output the other's input
+                dict(q=heads(x=FAKE, out=2 * FAKE), k=heads(x=2 * FAKE, out=3 * FAKE)),
+                dict(q=heads(x=FAKE, out=2 * FAKE), k=heads(x=2 * FAKE, out=FAKE))):
         assert f(**bad) == A.ERR_INVALID_ARG, bad
     assert f(q=heads(n=65537)) == A.ERR_TOO_LARGE
     for bad in (dict(positions=FAKE + 2), dict(steps=FAKE + 4), dict(q=heads(x=FAKE + 1)), dict(q=heads(out=FAKE + 1)),
