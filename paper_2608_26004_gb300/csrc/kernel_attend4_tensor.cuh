@@ -80,9 +80,17 @@ __device__ __forceinline__ uint64_t tensor_operand(unsigned at, unsigned lead, u
   return static_cast<uint64_t>((at & 0x3FFFF) >> 4) | static_cast<uint64_t>(lead >> 4) << 16 |
          static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-// fp16 operands, fp32 result, M = 128; A's rows along the sum, or (across) along M.
+// The same of rows of `row` = 32, 64 or 128 bytes along N, the 16-byte chunk c of row r at c ^ weights_turn(row, r).
+__device__ __forceinline__ uint64_t tensor_operand_across(unsigned at, int row) {
+  const uint64_t kind = row == 128 ? 2 : row == 64 ? 4 : 6;
+  return static_cast<uint64_t>((at & 0x3FFFF) >> 4) | 1ull << 16 | static_cast<uint64_t>(row / 2) << 32 | 1ull << 46 | kind << 61;
+}
+__device__ __forceinline__ int weights_turn(int row, int r) {
+  return row == 128 ? r & 7 : row == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+}
+// fp16 operands, fp32 result, M = 128; both operands' rows along the sum, or (across) along M and N.
 __host__ __device__ constexpr unsigned tensor_form(int n, bool across) {
-  return 1u << 4 | (across ? 1u << 15 : 0u) | static_cast<unsigned>(n / 8) << 17 | 8u << 24;
+  return 1u << 4 | (across ? 3u << 15 : 0u) | static_cast<unsigned>(n / 8) << 17 | 8u << 24;
 }
 
 // The largest of a warp's numbers; a NaN where all are.
@@ -133,14 +141,14 @@ constexpr size_t tensor_smem_bytes(int DP, int NR) {
 // queries cost what one does:
 //
 //   S = K Q^T     K, 128 keys: codes times scales as fp16 (exact), from the registers into tensor memory
-//   O += V^T P^T  V^T, 128 elements of a head: the same in shared memory, a key a row; the weights P beside it
+//   O += V^T P^T  V^T, 128 elements of a head: the same in shared memory, a key a row, and the weights P beside it
 //
 // A thread turns its key and its value into fp16 and has the key's scores, a number for each query.  S of a
 // step is formed a step ahead, while the threads turn the values of the step and make its weights, and O is
 // while they turn the next keys; codes come from memory a step ahead of that.  O stays in tensor memory, and is
 // touched only when a score rises far above its row's reference.
-// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 261 us, the bytes 106, issue
-// 46 %, DRAM 45 %, the tensor core a quarter: nothing is full, a step's chain of dependent parts (keys turned, scores
+// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 249 us, the bytes 106, issue
+// 45 %, DRAM 47 %, the tensor core a quarter: nothing is full, a step's chain of dependent parts (keys turned, scores
 // read, references compared by all threads, weights, values turned) and its barriers are not hidden by the two other
 // CTAs of the SM.  64 requests of 64 to 8192 tokens, 4 rows: 43 us, the bytes 18; a step costs 0.55 us an SM (its bytes
 // 0.41), an item about three, the launch, the first loads and the join 13 us together.  The same products on the
@@ -254,9 +262,9 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   };
   const unsigned swizzle = (tid & 7) << 4;
   unsigned char* const v_row = s_v + (tid >> 3) * 1024 + (tid & 7) * 128;  // this thread's value in a 64 of elements
-  unsigned char* const p_at = s_p + (tid >> 6) * (NR * 128);
-  const unsigned p_byte = (tid & 63) * 2;
-  const uint64_t q_operand = tensor_operand(smem_u32(s_q), 16, 1024), p_operand = tensor_operand(smem_u32(s_p), 16, 1024);
+  unsigned char* const p_row = s_p + tid * (NR * 2);  // this thread's weights
+  const int p_turn = weights_turn(NR * 2, tid);
+  const uint64_t q_operand = tensor_operand(smem_u32(s_q), 16, 1024), p_operand = tensor_operand_across(smem_u32(s_p), NR * 2);
   const uint64_t v_operand = tensor_operand(smem_u32(s_v), 16384, 1024);
 
   for (; u < u_end; at_unit = 0, ++hr) {
@@ -553,18 +561,18 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         }
       }
 #pragma unroll
-      for (int n = 0; n < RR; n += 4) {
-        if (few && n >= RR / 2) continue;
+      for (int n = 0; n < RR; n += 8) {
+        unsigned w[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int r = n; r < n + 4; r += 2) {
-          const float w0 = ex2(S[r]), w1 = ex2(S[r + 1]);
-          l[r] += w0;
-          l[r + 1] += w1;
-          const unsigned w = pack_f16(w0, w1);
-          unsigned char* to = p_at + (r >> 3) * 1024 + (r & 7) * 128;
-          *reinterpret_cast<uint16_t*>(to + (p_byte ^ ((r & 7) << 4))) = static_cast<uint16_t>(w);
-          *reinterpret_cast<uint16_t*>(to + 128 + (p_byte ^ (((r & 7) + 1) << 4))) = static_cast<uint16_t>(w >> 16);
+        for (int e = 0; e < 8; e += 2) {
+          if (few && n + e >= RR / 2) continue;
+          const float w0 = ex2(S[n + e]), w1 = ex2(S[n + e + 1]);
+          l[n + e] += w0;
+          l[n + e + 1] += w1;
+          w[e / 2] = pack_f16(w0, w1);
         }
+        // (a key a row, as the values: one store for 8 queries; a query a row took 16-bit stores, 261 us for 249)
+        *reinterpret_cast<uint4*>(p_row + ((n / 8) ^ p_turn) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
       }
       if constexpr (!kValuesFirst) {
         if (t + 1 < t1) start_scores();
@@ -581,7 +589,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
 #pragma unroll
             for (int k = 0; k < kTKeys / 16; ++k)
               tensor_mma_s(tm_o + mb * NR, v_operand + (mb * 32768 + k * 2048) / 16,
-                           p_operand + ((k >> 2) * (NR * 128) + (k & 3) * 32) / 16, tensor_form(NR, true), t > t0 || k > 0);
+                           p_operand + k * (NR * 32) / 16, tensor_form(NR, true), t > t0 || k > 0);
           tensor_commit(&s_bar[1]);
         }
         __syncwarp();
