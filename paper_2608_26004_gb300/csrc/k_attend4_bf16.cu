@@ -19,10 +19,7 @@ AttendKernels tensor_pick(bool fast) {
 // Rows of an item: the products' columns come in sixteens, but a thread's scores and sums are registers, so up to
 // 8 rows have a kernel of their own.  CTAs an SM: as many as tensor memory and shared memory have room for (four
 // of 128 columns), three where 32 rows need more registers.  us with one CTA less: 64 requests of 64 to 8192
-// tokens, 4 rows 42.8 / 48.1 with three.  256 threads for 16 rows and more, half of them for the values and each
-// half with half of the rows, was faster for 16 (52 against 58 us, 8 requests of 4096 to 32768), 32 (71, 77) and 64
-// rows (110, 128), the same for 16 requests of 32 rows to 131072 (260) and slower up to 8 rows (46 against 43): not
-// worth a second kernel.
+// tokens, 4 rows 42.7 / 48.1 with three, 8 of 4096 to 32768, 16 rows 52 / 54.
 AttendKernels attend4_kernels_bf16(int D, int rows, bool fast) {
   if (D <= 64)
     return rows <= 8    ? tensor_pick<64, 8, 4>(fast)

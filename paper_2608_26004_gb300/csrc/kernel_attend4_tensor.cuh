@@ -162,7 +162,9 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   constexpr int NR = tensor_rows(RR), MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
   constexpr size_t kMlBytes = attend_ml_bytes(RR);
-  constexpr bool kValuesFirst = RR <= 8;  // values are turned before a step's weights are made
+  // Values are turned before a step's weights are made, unless the scores, kept meanwhile, take too many registers: 8
+  // requests of 4096 to 32768 tokens, 16 rows 52 us (after 58), 64 rows 120 (125); 32 rows 77 (75).
+  constexpr bool kValuesFirst = RR != 32;
   constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -7.f, kLow = 7.f;
   extern __shared__ __align__(1024) unsigned char a_smem[];
   const AttendParams& p = P.a;
