@@ -29,9 +29,9 @@ struct RotaryParams {
   const uint64_t* steps;
 };
 
-constexpr int kRThreads = 256;
+constexpr int kRThreads = 128;
 constexpr int kRBatch = 3;       // units that a thread has on their way together
-constexpr int kRTable = 2048;    // cosines and sines of a CTA's tokens at most
+constexpr int kRTable = 1024;    // cosines and sines of a CTA's tokens at most
 constexpr int kRTokens = 256;    // tokens of a CTA at most
 
 __device__ __forceinline__ float2 turned(float2 cs, float a, float b) {
@@ -55,11 +55,12 @@ __device__ __forceinline__ unsigned divided(int n, unsigned divide, int shift) {
 // on their way.  A unit is what a thread moves at once: the same vector of both halves
 // (or two neighbours, interleaved: one vector, or a pair), or a vector past rotary_dim.
 // A vector's pairs lie in the table two by two (chunks of 16 bytes), the same two of all vectors next to one another, so
-// that lanes meet no bank twice.  16384 tokens of 40 heads of 128 bf16: 53 us = 6.3 TB/s (one after another in the
-// table, 64-bit reads that met banks four times, divisions: 66), 5 tokens of 24 heads 2.7 us.
+// that lanes meet no bank twice.  16384 tokens of 40 heads of 128 bf16 take 52 us = 6.4 TB/s (one after another in the
+// table, 64-bit reads that met banks four times, divisions: 66), 4099 of 40 heads of 64 9.3 us, 5 of 24 heads 2.4.
+// CTAs of 256 threads: 53 and 10.2 us; of two units a thread, six an SM, 53.5 and 9.1.
 // U: 16 bytes, or one element where something is not on the 16-byte boundaries.
 template <typename T, typename U, bool INTER>
-__global__ void __launch_bounds__(kRThreads) rotary_kernel(const __grid_constant__ RotaryParams p) {
+__global__ void __launch_bounds__(kRThreads, 8) rotary_kernel(const __grid_constant__ RotaryParams p) {
   constexpr int N = sizeof(U) / sizeof(T);
   constexpr bool kOne = INTER && N > 1;  // a turning unit is one vector
   constexpr int kPairs = kOne ? N / 2 : N;  // of a unit
@@ -108,7 +109,8 @@ __global__ void __launch_bounds__(kRThreads) rotary_kernel(const __grid_constant
     const float y = p.magnitude * (quarter & 1 ? c : s), x = p.magnitude * (quarter & 1 ? -s : c);
     const bool back = quarter & 2;
     const int u = pair / kPairs, k = pair % kPairs;
-    s_turn[kPairs == 1 ? i : t * half + (k / 2 * p.turning + u) * 2 + (k & 1)] = make_float2(back ? -x : x, back != p.transpose ? -y : y);
+    s_turn[kPairs == 1 ? i : t * half + (k / 2 * p.turning + u) * 2 + (k & 1)] =
+        make_float2(back ? -x : x, back != p.transpose ? -y : y);
   }
   __syncthreads();
   for (int first = tid;;) {
