@@ -18,10 +18,10 @@ namespace {
 
 using namespace asymspec_impl;
 
-// CTAs of a write at most, eight on each SM, and of a read: 16384 tokens written and read of 8 heads of 128 bf16 33.7 us
-// with 1216, 36.2 with 12160 for both; 100,003 tokens read 112 and 98 (and no fewer with a token's slot looked up
-// a token ahead, 114).
-constexpr int kWriteCtas = 1216;
+// CTAs of a write at most, the five that an SM has room for, and of a read: 16384 tokens written and read of 8 heads of
+// 128 bf16 31.9 us with 760, 32.8 with twice that (four an SM: 32.9 with 608, 34.1 with 1216); 100,003
+// tokens read 112 with 1216, 98 with a token's threads to each (and no fewer with a slot looked up a token ahead, 114).
+constexpr int kWriteCtas = 760;
 constexpr int kReadCtas = 1 << 20;
 
 AttendKernels attend4_kernels(int dtype, int D, int rows, bool fast) {

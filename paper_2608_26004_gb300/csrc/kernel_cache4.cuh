@@ -81,9 +81,9 @@ __device__ __forceinline__ void store_wide(void* p, const unsigned (&r)[8]) {
 
 // Copies, bound by their bytes: a thread takes 32 elements with two scales, neighbours those of a head, then
 // of the token's heads, then of its values.  WIDE: the elements lie on 32-byte boundaries.  16384 tokens of 8 heads of
-// 128 bf16 written and read 34 us (a thread per 16 elements, 64-bit divisions: 46), the bytes 25; 100,003 read 98 = 5.4 TB/s.
+// 128 bf16 written and read 32 us (a thread per 16 elements, 64-bit divisions: 46), the bytes 25; 100,003 read 98 = 5.4 TB/s.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(k4Threads) cache4_write_kernel(const __grid_constant__ Cache4Params p) {
+__global__ void __launch_bounds__(k4Threads, 5) cache4_write_kernel(const __grid_constant__ Cache4Params p) {
   const unsigned slots = static_cast<unsigned>(p.num_blocks) * static_cast<unsigned>(p.block_size);
   const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);
   const int64_t stride = static_cast<int64_t>(gridDim.x) * (k4Threads >> p.log_lanes);
