@@ -356,15 +356,17 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       load(0, page, at, kc, ks);
       tmem_wait_store();
     };
-    // Warps 1 to 3 say that their keys are turned and go on; warp 0 looks for that later, when it need not wait,
-    // and starts the products.
-    auto keys_turned = [&] {
+    // Warps 1 to 3 say that a step's keys are turned and go on; warp 0 looks for that later, when it need not wait,
+    // and starts the products.  Neighbouring steps have a barrier each: without the wait for the scores (after one
+    // that gave up) a warp may be a step ahead of warp 0, but no more, as each step has a barrier of the CTA; with
+    // one for all steps its second arrival would stand in for another's.
+    auto keys_turned = [&](int step) {
       tensor_fence_before();
-      if (warp != 0) barrier_arrive(1);
+      if (warp != 0) barrier_arrive(1 + (step & 1));
     };
-    auto start_scores = [&] {
+    auto start_scores = [&](int step) {
       if (warp != 0) return;
-      barrier_sync(1);
+      barrier_sync(1 + (step & 1));
       if (elected() && !gave_up()) {
         tensor_fence_after();
 #pragma unroll
@@ -435,8 +437,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     const bool few = RR == 8 && rows <= RR / 2;
     fence_to_async();
     turn_keys();
-    keys_turned();
-    start_scores();
+    keys_turned(t0);
+    start_scores(t0);
 
     for (int t = t0; t < t1; ++t) {
       const int j = lo + t * kTKeys + tid;  // this thread's key
@@ -448,7 +450,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       // the next step's keys, while the scores come
       if (t + 1 < t1) turn_keys();
       tmem_wait_load();
-      if (t + 1 < t1) keys_turned();
+      if (t + 1 < t1) keys_turned(t + 1);
       if (t > t0) wait(1, parity_o);  // (O of the step before: its weights and values have been read)
       auto turn_values = [&] {
         // Values.  A NaN is left out of the products, where a weight of zero would make it one in rows that do not
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       };
       if constexpr (kValuesFirst) {
         turn_values();
-        if (t + 1 < t1) start_scores();
+        if (t + 1 < t1) start_scores(t + 1);
       }
       // scores less their references
       auto less = [&] {
@@ -577,13 +579,13 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         *reinterpret_cast<uint4*>(p_row + ((n / 8) ^ p_turn) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
       }
       if constexpr (!kValuesFirst) {
-        if (t + 1 < t1) start_scores();
+        if (t + 1 < t1) start_scores(t + 1);
         turn_values();
       }
       fence_to_async();
       tensor_fence_before();
       if (warp == 1) {
-        barrier_sync(2);
+        barrier_sync(3);
         if (elected() && !gave_up()) {
           tensor_fence_after();
 #pragma unroll
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         }
         __syncwarp();
       } else {
-        barrier_arrive(2);
+        barrier_arrive(3);
       }
     }
 
