@@ -105,8 +105,10 @@ __device__ __forceinline__ bool elected() {
   return r != 0;
 }
 // One warp waits for all, the others go on.
-__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, 128;" ::"r"(id) : "memory"); }
+template <int ID>
+__device__ __forceinline__ void barrier_sync() { asm volatile("bar.sync %0, 128;" ::"n"(ID) : "memory"); }
+template <int ID>
+__device__ __forceinline__ void barrier_arrive() { asm volatile("bar.arrive %0, 128;" ::"n"(ID) : "memory"); }
 
 // 32 bytes.
 __device__ __forceinline__ void load32(unsigned* r, const char* p) {
@@ -362,11 +364,12 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     // one for all steps its second arrival would stand in for another's.
     auto keys_turned = [&](int step) {
       tensor_fence_before();
-      if (warp != 0) barrier_arrive(1 + (step & 1));
+      if (warp == 0) return;
+      step & 1 ? barrier_arrive<2>() : barrier_arrive<1>();
     };
     auto start_scores = [&](int step) {
       if (warp != 0) return;
-      barrier_sync(1 + (step & 1));
+      step & 1 ? barrier_sync<2>() : barrier_sync<1>();
       if (elected() && !gave_up()) {
         tensor_fence_after();
 #pragma unroll
@@ -585,7 +588,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       fence_to_async();
       tensor_fence_before();
       if (warp == 1) {
-        barrier_sync(3);
+        barrier_sync<3>();
         if (elected() && !gave_up()) {
           tensor_fence_after();
 #pragma unroll
@@ -598,7 +601,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         }
         __syncwarp();
       } else {
-        barrier_arrive(3);
+        barrier_arrive<3>();
       }
     }
 
