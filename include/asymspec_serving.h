@@ -351,7 +351,8 @@ int asymspec_cache4_read(const asymspec_cache4* cache, const int64_t* slots, int
  * out are of `dtype`.  Keys and values enter exactly; bf16 queries too, fp32 ones in two fp16
  * pieces (2^-22); weights in one fp16 piece for bf16 (2^-11, an eighth of the output's own rounding), in
  * two for fp32.  (Elements of a query below 2^-28 of its largest may be less exact.)  Waits for the tensor core are
- * bounded: one that gave up after 0.2 s leaves ASYMSPEC_DATA_TIMEOUT, and the call's results are not valid.
+ * bounded: where one gave up after 0.2 s, out and lse are NaN in all rows of the requests' kv heads that its CTA
+ * had a part of (rows without keys too), and the error word has ASYMSPEC_DATA_TIMEOUT.
  * ASYMSPEC_ERR_INVALID_ARG besides: scale * key_scale / ln 2 beyond fp32.  ASYMSPEC_ERR_TOO_LARGE: a stride of
  * blocks or tokens beyond 2^31 - 1 bytes. */
 size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_heads, int head_dim);

@@ -260,7 +260,9 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   // (a thread that gave up waits no more, and starts no products)
   auto gave_up = [&] { return (err & ASYMSPEC_DATA_TIMEOUT) != 0; };
   auto wait = [&](int which, unsigned& parity) {
-    if (!gave_up() && (!mbar_wait_bounded(&s_bar[which], parity, kTWaitNs) || kTestLate)) err |= ASYMSPEC_DATA_TIMEOUT;
+    // (looked at once more when the time is over: it may have passed while nothing here ran)
+    if (!gave_up() && ((!mbar_wait_bounded(&s_bar[which], parity, kTWaitNs) && !mbar_try_wait(&s_bar[which], parity)) || kTestLate))
+      err |= ASYMSPEC_DATA_TIMEOUT;
     parity ^= 1;
     tensor_fence_after();
   };
@@ -659,7 +661,18 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       }
       tmem_wait_store();
     }
-    __syncthreads();
+    // A CTA in which a thread gave up: nothing of the item is right, nor of a later one.  NaN, which the join carries.
+    const bool late = __syncthreads_or(gave_up());
+    if (late && tid < rows) {
+      s_up[tid] = NAN;
+      if (!all) {
+        ws_ml[tid * 2 + 1] = NAN;
+      } else if (p.lse) {
+        const int i = (R0 + tid) / p.group;
+        p.lse[(static_cast<int64_t>(b) * p.Q + i) * p.heads + kh * p.group + R0 + tid - i * p.group] = NAN;
+      }
+    }
+    if (late) __syncthreads();
     int h = R0 % p.group;  // the row's head, of the kv head's, and its output
     T* out = static_cast<T*>(p.out) + b * p.os[0] + R0 / p.group * p.os[1] + (kh * p.group + h) * p.os[2] + tid;
     const int64_t next_query = p.os[1] - (p.group - 1) * p.os[2];
@@ -675,7 +688,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb)
-            if (DP >= 128 || tid < DP) ws_o[(n0 + e) * DP + mb * 128 + tid] = o[mb][e] * P.value_scale;
+            if (DP >= 128 || tid < DP) ws_o[(n0 + e) * DP + mb * 128 + tid] = late ? NAN : o[mb][e] * P.value_scale;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

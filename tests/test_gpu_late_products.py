@@ -52,3 +52,30 @@ def test_a_call_that_gave_up_says_so_and_the_next_one_is_right(torch, late, monk
         out, lse = attend(*x, error_word=err)
         assert int(err) == 0
         check(torch, x, out, lse, some_rows(B, Q, heads, seed))
+
+
+@pytest.mark.parametrize("lens,Q,heads,kv,D", [
+    *CASES,
+    ([500, 9000, 40, 129] * 30, 8, 32, 8, 128),  # several items a CTA, 32 rows
+    ([300, 1, 2000] * 40, 8, 16, 4, 64),         # 32 rows of 64
+    ([400, 700] * 30, 4, 32, 4, 256),            # 32 rows of 256
+    ([200, 64] * 200, 1, 16, 4, 128),            # 4 rows
+])
+def test_results_of_a_call_that_gave_up_are_nan(torch, late, monkeypatch, lens, Q, heads, kv, D):
+    """Without an error word, too: no number is left that could be taken for a result."""
+    B = len(lens)
+    x = inputs(torch, lens, Q, heads, kv, D, "bfloat16", 16, 3)
+    attend = S.Cache4Attend(B, Q, heads, kv, D)
+    out, lse = torch.zeros_like(x[0]), torch.zeros(B, Q, heads, device="cuda")
+    with monkeypatch.context() as m:
+        m.setattr(A, "LIB_PATH", late)
+        for module in (A, S):
+            m.setattr(module, "_lib", None)
+        S.lib()
+        attend(*x, out=out, lse=lse)
+        torch.cuda.synchronize()
+    assert out.isnan().all() and lse.isnan().all()
+    err = torch.zeros(1, device="cuda", dtype=torch.int32)
+    out, lse = attend(*x, error_word=err)
+    assert int(err) == 0
+    check(torch, x, out, lse, some_rows(B, Q, heads, 3))
