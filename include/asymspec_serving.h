@@ -349,8 +349,9 @@ int asymspec_cache4_read(const asymspec_cache4* cache, const int64_t* slots, int
 
 /* asymspec_cache_attend over such a cache, with its arguments, checks and answers to bad data; q and
  * out are of `dtype`.  Keys and values enter exactly; bf16 queries too, fp32 ones in two fp16
- * pieces (2^-22); weights in one fp16 piece for bf16 (2^-11, an eighth of the output's own rounding), in
- * two for fp32.  (Elements of a query below 2^-28 of its largest may be less exact.)  Waits for the tensor core are
+ * pieces (2^-22 of each element down to 2^-27 of its row's largest, smaller ones 2^-49 of that); weights in one fp16 piece for bf16 (2^-11, an eighth of the output's own rounding), in
+ * two for fp32.  (bf16 elements below 2^-28 of their row's largest enter
+ * to 2^-38 of that.)  Waits for the tensor core are
  * bounded: where one gave up after 0.2 s, out and lse are NaN in all rows of the requests' kv heads that its CTA
  * had a part of (rows without keys too), and the error word has ASYMSPEC_DATA_TIMEOUT.
  * ASYMSPEC_ERR_INVALID_ARG besides: scale * key_scale / ln 2 beyond fp32.  ASYMSPEC_ERR_TOO_LARGE: a stride of

@@ -101,7 +101,7 @@ __device__ __forceinline__ void load_words(const unsigned char* p, unsigned (&w)
 // in the registers that the lanes load them into: two codes of a byte are two neighbouring elements of a key;
 // for the values the bytes of two keys are interleaved first.  e2m1 times e4m3 has 6 significant bits and lies
 // between 2^-10 and 2688: fp16 holds it, keys and values are exact; queries, each row times a power of two, are
-// two fp16 pieces (2^-22), and so are the weights.  The pools' numbers are left to the scores' factors and
+// two fp16 pieces (2^-22 of an element down to 2^-27 of its row's largest), and so are the weights.  The pools' numbers are left to the scores' factors and
 // the end.  The conversion of two codes and its product with their scale take a warp 0.78 cycles of an SM; codes
 // that were whole numbers, taken out by masks, took 1.34.
 // Bound by latency at few CTAs: 32 requests of 5 queries, a window of 2000, 8 heads of 64 25 us (bf16 keys and
@@ -309,7 +309,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
       find();
     }
 
-    // the item's queries, each row times the power of two that takes its largest element to 2^13
+    // the item's queries, each row times the power of two that takes its largest element to 2^13; what is left of an
+    // element is taken times 2^11, or fp16's smallest step would show in those below 2^-16 of the largest
     for (int r = warp; r < kRows; r += kWarpsN) {
       const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
       const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
         const float y = x[k] * up;
         const __half hi = __float2half_rn(y);
         to[lane + 32 * k] = hi;
-        if constexpr (!BF) to[kRows * kQPitch / 2 + lane + 32 * k] = __float2half_rn(y - __half2float(hi));
+        if constexpr (!BF) to[kRows * kQPitch / 2 + lane + 32 * k] = __float2half_rn((y - __half2float(hi)) * 0x1p11f);
       }
       if (lane == 0) s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
     }
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[y][n][e] += more[y][n][e] + small[y][n][e];
+                for (int e = 0; e < 4; ++e) S[y][n][e] += fmaf(small[y][n][e], 0x1p-11f, more[y][n][e]);
           }
         }
         bool whole = k0 + (U - 1) * kATile + kAKeys - 1 <= least && k0 >= from;

@@ -448,6 +448,22 @@ def test_many_keys_far_below_a_few(torch, dtype):
     check(torch, x, out, lse, [(0, 0, 0), (41, 0, 3), (79, 0, 7)], scale=1.0)
 
 
+def test_fp32_queries_with_elements_far_below_another(torch):
+    """An element 2^26 times the others' size where the keys are zero: the score is the others' alone, and what is
+    allowed of it (see check) goes by them.  Each request has one or two keys: lse is the score itself."""
+    lens = [1, 2] * 24
+    for D in (64, 128, 256):
+        q, cache, tables, n = inputs(torch, lens, 2, 8, 2, D, "float32", 16, 51)
+        k = torch.randn(cache.key_codes.shape[0] * 16, 2, D, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+        k[..., 5] = 0.0
+        S.cache4_write(k, torch.randn_like(k), cache, torch.arange(k.shape[0], device="cuda"))
+        q = q.clone()
+        q[..., 5] = 2.0 ** 26
+        x = (q, cache, tables, n)
+        out, lse = S.Cache4Attend(len(lens), 2, 8, 2, D)(*x)
+        check(torch, x, out, lse, some_rows(len(lens), 2, 8, D, 80))
+
+
 def test_refusals_of_the_binding(torch):
     q, cache, tables, lens = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.Cache4Attend(2, 2, 4, 2, 64)
