@@ -9,6 +9,10 @@ namespace asymspec_impl {
 constexpr int kTThreads = 128;
 constexpr int kTKeys = 128;  // keys of a step, one a thread: the unit of the split
 constexpr unsigned long long kTWaitNs = 200000000ull;
+// Steps whose products are summed in tensor memory (a power of two).  The tensor core cuts its running sums and does not
+// round them, by 2^-23 at most each 16 keys and always one way: a million keys in one CTA came out 0.2 % short.  So every
+// 8192 keys, 2^-14, the sums go to the workspace, where they are added up with rounding.
+constexpr int kTSteps = 64;
 #ifdef ASYMSPEC_TEST_LATE_PRODUCTS  // (a test's build: every wait, once it has ended, counts as one that gave up)
 constexpr bool kTestLate = true;
 #else
@@ -148,11 +152,12 @@ constexpr size_t tensor_smem_bytes(int DP, int NR) {
 // A thread turns its key and its value into fp16 and has the key's scores, a number for each query.  S of a
 // step is formed a step ahead, while the threads turn the values of the step and make its weights, and O is
 // while they turn the next keys; codes come from memory a step ahead of that.  O stays in tensor memory, and is
-// touched only when a score rises far above its row's reference.
-// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 249 us, the bytes 106, issue
+// touched only when a score rises far above its row's reference, and every 64 steps.  The weights are one fp16 piece,
+// 2^-11: an eighth of the output's own rounding to bf16; a second piece would double the second product and its stores.
+// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 257 us, the bytes 106, issue
 // 45 %, DRAM 47 %, the tensor core a quarter: nothing is full, a step's chain of dependent parts (keys turned, scores
 // read, references compared by all threads, weights, values turned) and its barriers are not hidden by the two other
-// CTAs of the SM.  64 requests of 64 to 8192 tokens, 4 rows: 43 us, the bytes 18; a step costs 0.55 us an SM (its bytes
+// CTAs of the SM.  64 requests of 64 to 8192 tokens, 4 rows: 43.6 us, the bytes 18; a step costs 0.55 us an SM (its bytes
 // 0.41), an item about three, the launch, the first loads and the join 13 us together.  The same products on the
 // warps' matrix instructions (as attend4_split's) took 449 and 56 us; with warps of their own for loading, weighing and
 // starting the products, one CTA less an SM or two, 482 and 60.
@@ -440,6 +445,10 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     bool bad_values = false;  // a value with a NaN
     bool fresh = !guess;      // a row without a reference
     const bool few = RR == 8 && rows <= RR / 2;
+    // The item's part in the workspace: its sums, each element of a head its thread's.  (An item that is all this CTA's
+    // has the place of the one that the next CTA goes on with, which is the CTA's last.)
+    auto part = [&] { return static_cast<size_t>(t0 > 0 ? 2 * c : 2 * c + 1); };
+    auto sums_at = [&] { return reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + part() * RR * DP + tid; };
     fence_to_async();
     turn_keys();
     keys_turned(t0);
@@ -526,7 +535,9 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
             raise = raise || low;
           }
       }
-      if (__syncthreads_or(raise)) {
+      // (sums go to the workspace now, and the products' begin anew)
+      const bool put_by = t > t0 && ((t - t0) & (kTSteps - 1)) == 0;
+      if (__syncthreads_or(raise || put_by)) {
         // references rise: each row's to kBelow under its largest score, and what has been summed goes down
 #pragma unroll
         for (int n = 0; n < RR; ++n) {
@@ -555,6 +566,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
             fresh = fresh || s_m[n] == -INFINITY;
           }
         if (t > t0) {
+          const bool kept = t - t0 > kTSteps;
+          float* const ws_o = sums_at();
 #pragma unroll 1
           for (int mb = 0; mb < MB; ++mb)
 #pragma unroll 1
@@ -563,7 +576,15 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
               tmem_load8(tm_o + mb * NR + tm_warp + n, o);
               tmem_wait_load();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] *= n + e < rows ? s_fall[n + e] : 1.f;
+              for (int e = 0; e < 8; ++e) {
+                const float fall = n + e < rows ? s_fall[n + e] : 1.f;
+                o[e] *= fall;
+                if ((DP >= 128 || tid < DP) && (kept || put_by)) {
+                  float* const sum = ws_o + (n + e) * DP + mb * 128;
+                  const float old = kept ? *sum * fall : 0.f;
+                  *sum = put_by ? old + o[e] : old;
+                }
+              }
               tmem_store8(tm_o + mb * NR + tm_warp + n, o);
             }
           tmem_wait_store();
@@ -598,7 +619,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
 #pragma unroll
             for (int k = 0; k < kTKeys / 16; ++k)
               tensor_mma_s(tm_o + mb * NR, v_operand + (mb * 32768 + k * 2048) / 16,
-                           p_operand + k * (NR * 32) / 16, tensor_form(NR, true), t > t0 || k > 0);
+                           p_operand + k * (NR * 32) / 16, tensor_form(NR, true), (t > t0 && !put_by) || k > 0);
           tensor_commit(&s_bar[1]);
         }
         __syncwarp();
@@ -618,9 +639,8 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     }
     const bool nans = __syncthreads_or(bad_values);
     const bool all = t0 == 0 && t1 == n_tiles;
-    const int part = t0 > 0 ? 2 * c : 2 * c + 1;
-    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * RR * 2;
-    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * RR * DP;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + part() * RR * 2;
+    float* const ws_o = sums_at();
     // a row's sum, and what its values are taken times
     if (tid < rows) {
       const int n = tid;
@@ -682,13 +702,20 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) tmem_load8(tm_o + mb * NR + tm_warp + n0, o[mb]);
       tmem_wait_load();
+      if (t1 - t0 > kTSteps) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+            if (DP >= 128 || tid < DP) o[mb][e] += ws_o[(n0 + e) * DP + mb * 128];
+      }
       if (!all) {
         // (the rows past the item's last one have room there too)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb)
-            if (DP >= 128 || tid < DP) ws_o[(n0 + e) * DP + mb * 128 + tid] = late ? NAN : o[mb][e] * P.value_scale;
+            if (DP >= 128 || tid < DP) ws_o[(n0 + e) * DP + mb * 128] = late ? NAN : o[mb][e] * P.value_scale;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

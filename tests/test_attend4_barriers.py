@@ -21,7 +21,7 @@ def the_kernels_order():
     assert ways[0] == ways[1] and len(ways[0]) <= 2  # of odd steps and of even ones, or of all
     step = re.search(r"for \(int t = t0; t < t1; \+\+t\) \{(.*?)// the rows' sums over the threads", text, re.S).group(1)
     events, when = [], None
-    for m in re.finditer(r"if constexpr \((!?)kValuesFirst\)|keys_turned\(|start_scores\(|__syncthreads_or\(raise\)|"
+    for m in re.finditer(r"if constexpr \((!?)kValuesFirst\)|keys_turned\(|start_scores\(|__syncthreads_or\(raise|"
                          r"barrier_sync<(.*?)>\(\);", step):
         word = m.group(0)
         if word.startswith("if"):

@@ -464,6 +464,32 @@ def test_fp32_queries_with_elements_far_below_another(torch):
         check(torch, x, out, lse, some_rows(len(lens), 2, 8, D, 80))
 
 
+@pytest.mark.parametrize("heads,D", [(1, 64), (32, 128)])
+def test_sums_over_a_million_keys(torch, heads, D):
+    """Each request's 2^20 keys in one CTA's hands, with equal weights and positive values: what the tensor core cuts
+    off its running sums all goes one way.  Tolerance: sums run over 8192 keys, 16 at a time, each cut by 2^-23 of the
+    sum at most, 2^-14 in all; 128 such are added up with rounding, 2^-17; a key's weight is 2^7, exactly; two products
+    at the end, 2^-22.  In all below 2^-13; the output is rounded once."""
+    n, bs, B = 2 ** 20, 64, 608
+    g = torch.Generator(device="cuda").manual_seed(17)
+    cache = S.Cache4.zeros(n // bs, bs, 1, D)
+    slots = torch.arange(n, device="cuda")
+    for part in slots.split(2 ** 17):
+        v = torch.rand(part.numel(), 1, D, generator=g, device="cuda") * torch.rand(part.numel(), 1, 1, generator=g, device="cuda").exp2()
+        S.cache4_write(torch.zeros_like(v), v, cache, part)
+    tables = torch.arange(n // bs, device="cuda", dtype=torch.int32).repeat(B, 1)
+    q = torch.zeros(B, 1, heads, D, device="cuda", dtype=torch.bfloat16)
+    attend = S.Cache4Attend(B, 1, heads, 1, D)
+    out, lse = attend(q, cache, tables, torch.full((B,), n, device="cuda", dtype=torch.int32))
+    total = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for part in slots.split(2 ** 17):
+        total += S.cache4_read(cache, part, dtype=torch.float32)[1][:, 0].double().sum(0)
+    mean = total / n
+    least, most = ((mean * (1 + e)).bfloat16() for e in (-(2.0 ** -13), 2.0 ** -13))
+    assert ((least <= out) & (out <= most)).all(), ((out.double() / mean - 1).mean(), (out.double() / mean - 1).abs().max())
+    assert ((lse.double() - math.log(n)).abs() <= 2.0 ** -20 * 15).all()
+
+
 def test_refusals_of_the_binding(torch):
     q, cache, tables, lens = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.Cache4Attend(2, 2, 4, 2, 64)
