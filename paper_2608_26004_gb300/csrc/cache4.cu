@@ -123,10 +123,15 @@ size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_he
   if (B < 1 || Q < 1 || heads < 1 || kv_heads < 1 || head_dim < 1 || heads % kv_heads != 0 || head_dim % 32 != 0 ||
       head_dim > ASYMSPEC_CACHE_MAX_D || B > ASYMSPEC_CACHE_MAX_B || static_cast<int64_t>(Q) * heads > (1 << 20))
     return 0;
-  // (any number of queries up to Q: the row tiles only grow with them)
+  // any number of queries up to Q: fewer rows may have more CTAs
+  size_t most = 0;
   const int rows = Q * (heads / kv_heads);
-  const AttendKernels a = attend4_kernels_bf16(head_dim, rows, true), b = attend4_kernels_f32(head_dim, rows, true);
-  return std::max(attend_ws_bytes(a.rows, a.DP), attend_ws_bytes(b.rows, b.DP));
+  for (const int r : {rows, 32, 16, 8}) {
+    if (r > rows) continue;
+    for (const AttendKernels& k : {attend4_kernels_bf16(head_dim, r, true), attend4_kernels_f32(head_dim, r, true)})
+      most = std::max(most, attend_ws_bytes(k.rows, k.DP, k.most_ctas));
+  }
+  return most;
 }
 
 int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtype, const int64_t* q_strides,
@@ -213,7 +218,7 @@ int asymspec_cache4_attend(const asymspec_cache4* cache, const void* q, int dtyp
   if (e != cudaSuccess) return cuda_fail(e);
   // as many CTAs as fit on the chip, but no more than there may be units of work (see attend_tiles)
   const int64_t most = static_cast<int64_t>(table_width) * p.block_size / k.tile + 1 + kAItem;
-  int ctas = static_cast<int>(std::min<int64_t>(std::min(kAMaxCtas, sms * k.ctas_per_sm), B * most * p.kv_heads * p.row_tiles));
+  int ctas = static_cast<int>(std::min<int64_t>(std::min(k.most_ctas, sms * k.ctas_per_sm), B * most * p.kv_heads * p.row_tiles));
   const cudaStream_t st_ = static_cast<cudaStream_t>(stream);
   void* args[] = {&P};
   e = cudaLaunchKernel(k.split, dim3(ctas), dim3(k.threads), args, k.smem, st_);

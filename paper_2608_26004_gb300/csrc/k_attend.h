@@ -16,7 +16,8 @@ inline int attend_window(int window, int table_width, int block_size) {
 struct AttendKernels {
   const void *split, *join;
   int DP, rows, threads, smem, ctas_per_sm;
-  int tile;  // keys of a unit of work
+  int most_ctas;  // that the workspace has room for
+  int tile;       // keys of a unit of work
 };
 
 // The kernels for heads of D elements and `rows` queries a kv head (k_attend_bf16.cu,

@@ -10,10 +10,10 @@ AttendKernels tensor_pick(bool fast) {
   constexpr int NR = tensor_rows(RR), smem = static_cast<int>(tensor_smem_bytes(DP, NR));
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 2048) <= 228 * 1024, "the operands fit");
   static_assert(PER_SM * tensor_columns(DP, NR) <= 512, "and the tensor memory");
-  static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
   return {fast ? reinterpret_cast<const void*>(&attend4_tensor<DP, RR, PER_SM, true>)
                : reinterpret_cast<const void*>(&attend4_tensor<DP, RR, PER_SM, false>),
-          reinterpret_cast<const void*>(&attend4_join<__nv_bfloat16, DP, RR>), DP, RR, kTThreads, smem, PER_SM, kTKeys};
+          reinterpret_cast<const void*>(&attend4_join<__nv_bfloat16, DP, RR, PER_SM * kASms>), DP, RR, kTThreads, smem, PER_SM,
+          PER_SM * kASms, kTKeys};
 }
 
 // Rows of an item: the products' columns come in sixteens, but a thread's scores and sums are registers, so up to

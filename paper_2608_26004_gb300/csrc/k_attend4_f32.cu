@@ -9,9 +9,9 @@ AttendKernels attend4_pick() {
   constexpr int rows = 8 * NT * WR;
   constexpr int smem = static_cast<int>(attend4_smem_bytes(DP, rows, ST, 2));
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
-  static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
   return {reinterpret_cast<const void*>(&attend4_split<float, DP, NT, WR, ST, PER_SM>),
-          reinterpret_cast<const void*>(&attend4_join<float, DP, rows>), DP, rows, 128 * WR, smem, PER_SM, kATile};
+          reinterpret_cast<const void*>(&attend4_join<float, DP, rows, PER_SM * kASms>), DP, rows, 128 * WR, smem, PER_SM,
+          PER_SM * kASms, kATile};
 }
 
 // fp32 queries: on the warps' matrix instructions, whose sums stay in registers, as the tensor core's would be cut

@@ -8,9 +8,9 @@ template <int DP, int WR, int ST, int PER_SM, int kH = 2>
 AttendKernels attend_pick() {
   constexpr int smem = static_cast<int>(attend_smem_bytes<__nv_bfloat16>(DP, WR, ST));
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
-  static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
+  static_assert(PER_SM * kASms <= kAMaxCtas, "the workspace has room");
   return {reinterpret_cast<const void*>(&attend_split<__nv_bfloat16, DP, WR, ST, PER_SM, kH>),
-          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM, kATile};
+          reinterpret_cast<const void*>(&attend_join<__nv_bfloat16, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM, kAMaxCtas, kATile};
 }
 
 // One, two or four warps for the rows of a group: as many as the rows fill.  us, 8 requests of

@@ -8,9 +8,9 @@ template <int DP, int WR, int ST, int PER_SM, int kH = 2>
 AttendKernels attend_pick() {
   constexpr int smem = static_cast<int>(attend_smem_bytes<float>(DP, WR, ST));
   static_assert(smem <= kMaxSmem - 8192 && PER_SM * (smem + 1024) <= 228 * 1024, "the rings fit");
-  static_assert(PER_SM * 152 <= kAMaxCtas, "the workspace has room");
+  static_assert(PER_SM * kASms <= kAMaxCtas, "the workspace has room");
   return {reinterpret_cast<const void*>(&attend_split<float, DP, WR, ST, PER_SM, kH>),
-          reinterpret_cast<const void*>(&attend_join<float, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM, kATile};
+          reinterpret_cast<const void*>(&attend_join<float, DP, 16 * WR>), DP, 16 * WR, 128 * WR, smem, PER_SM, kAMaxCtas, kATile};
 }
 
 // As for bf16 (three CTAs an SM instead of two at 16 rows of 64: a window of 2000, 32 requests

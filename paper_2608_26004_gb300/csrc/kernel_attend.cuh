@@ -32,7 +32,8 @@ struct AttendParams {
 constexpr int kAGroups = 4;                 // groups of warps, each with keys of its own
 constexpr int kAKeys = 16;                  // keys of a group's step
 constexpr int kATile = kAGroups * kAKeys;   // keys of a CTA's step, the unit of the split
-constexpr int kAMaxCtas = 608;              // CTAs that share the work (up to four on each of 152 SMs)
+constexpr int kASms = 152;
+constexpr int kAMaxCtas = 3 * kASms;        // CTAs that share the work
 constexpr int kAJoinThreads = 128;
 
 // The work is split by units: an item (a request, kv head and row tile) has one for each
@@ -50,13 +51,16 @@ struct AttendInfo {
 // Workspace: an AttendInfo per CTA; then, for two parts a CTA (one of an item that an
 // earlier CTA began, one of an item that a later CTA goes on with), each row's maximum
 // and sum, and each row's weighted values.
-constexpr size_t kAInfoBytes = (kAMaxCtas * sizeof(AttendInfo) + 255) / 256 * 256;
-__host__ __device__ constexpr size_t attend_ml_bytes(int rows) {
-  return (static_cast<size_t>(2 * kAMaxCtas) * rows * 2 * sizeof(float) + 255) / 256 * 256;
+__host__ __device__ constexpr size_t attend_info_bytes(int ctas) {
+  return (ctas * sizeof(AttendInfo) + 255) / 256 * 256;
 }
-constexpr size_t attend_ws_bytes(int rows, int DP) {
-  return kAInfoBytes + attend_ml_bytes(rows) + static_cast<size_t>(2 * kAMaxCtas) * rows * DP * sizeof(float);
+__host__ __device__ constexpr size_t attend_ml_bytes(int rows, int ctas) {
+  return (static_cast<size_t>(2 * ctas) * rows * 2 * sizeof(float) + 255) / 256 * 256;
 }
+constexpr size_t attend_ws_bytes(int rows, int DP, int ctas) {
+  return attend_info_bytes(ctas) + attend_ml_bytes(rows, ctas) + static_cast<size_t>(2 * ctas) * rows * DP * sizeof(float);
+}
+constexpr size_t kAInfoBytes = attend_info_bytes(kAMaxCtas);
 
 // Whether rows of keys, values and queries lie in shared memory 16 bytes further apart than they
 // are long, so that the eight rows that ldmatrix reads meet no bank twice and all addresses are
@@ -201,7 +205,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
   constexpr int kRows = 16 * WR;
   constexpr int NT = DP / 8;
   constexpr int kLoads = kChunks / 2 / WR;   // vectors that a lane loads of a step's keys
-  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows, kAMaxCtas);
   constexpr float kSlack = 8.f;
   constexpr bool kQRegs = BF && DP <= 128 && WR == 1;
   static_assert(kLoads >= 1 && (BF ? 1 : 2) * ST >= WR, "a warp loads, and the parts fit in the rings");
@@ -768,7 +772,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend_split(const
 template <typename T, int DP, int kRows>
 __global__ void __launch_bounds__(kAJoinThreads) attend_join(const AttendParams p, int ctas) {
   constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
-  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  constexpr size_t kMlBytes = attend_ml_bytes(kRows, kAMaxCtas);
   __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_red[kAWarps];
   __shared__ __align__(16) float s_x[kAJoinThreads * 4];
   asm volatile("griddepcontrol.wait;" ::: "memory");

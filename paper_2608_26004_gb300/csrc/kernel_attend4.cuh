@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
   constexpr int kLaneRows = 32 * WR / kChunks;     // keys that the group's lanes load at once
   constexpr int kLoads = kASubs * kAKeys > kLaneRows ? kASubs * kAKeys / kLaneRows : 1;
   constexpr int U = NT == 1 ? kASubs : 1;          // sixteens of keys that are worked at together
-  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
+  constexpr size_t kInfoBytes = attend_info_bytes(PER_SM * kASms), kMlBytes = attend_ml_bytes(kRows, PER_SM * kASms);
   constexpr float kBelow = BF ? 7.f : 12.f, kSlack = 15.f - kBelow;
   constexpr bool kQRegs = kPieces * NT * KW * 4 <= 32;
   static_assert(ST >= 2 && kStep % 16 == 0 && kGroup % 16 == 0, "the ring");
@@ -722,8 +722,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     __syncthreads();
     const bool all = t0 == 0 && t1 == n_tiles;
     const int part = t0 > 0 ? 2 * c : 2 * c + 1;
-    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + static_cast<size_t>(part) * kRows * 2;
-    float* ws_o = reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + static_cast<size_t>(part) * kRows * DP;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kInfoBytes) + static_cast<size_t>(part) * kRows * 2;
+    float* ws_o = reinterpret_cast<float*>(p.ws + kInfoBytes + kMlBytes) + static_cast<size_t>(part) * kRows * DP;
     for (int e = tid; e < rows * (DP / 4); e += kThreadsN) {
       const int r = e / (DP / 4), d = (e % (DP / 4)) * 4;
       float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -776,19 +776,20 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
 // (grid.y > 1 of them, or one) a CTA takes a row of the first CTA that went on with an item, if its CTA was one.  With
 // more rows most of so many CTAs would end at once (8 kv heads of 32 rows, 608 CTAs: 19,000 of them, 8 us):
 // each then looks for those CTAs among all, a few hundred numbers, and takes its turn of their rows.
-template <typename T, int DP, int kRows>
+// CTAS: of the split at most.
+template <typename T, int DP, int kRows, int CTAS>
 __global__ void __launch_bounds__(kAJoinThreads) attend4_join(const __grid_constant__ AttendParams p, int ctas) {
   constexpr int kCols = DP / 4, kWays = kAJoinThreads / kCols, kAWarps = kAJoinThreads / 32;
-  constexpr size_t kMlBytes = attend_ml_bytes(kRows);
-  __shared__ float s_w[kAMaxCtas], s_l[kAMaxCtas], s_red[kAWarps];
+  constexpr size_t kInfoBytes = attend_info_bytes(CTAS), kMlBytes = attend_ml_bytes(kRows, CTAS);
+  __shared__ float s_w[CTAS], s_l[CTAS], s_red[kAWarps];
   __shared__ __align__(16) float s_x[kAJoinThreads * 4];
-  __shared__ uint16_t s_list[kAMaxCtas];
+  __shared__ uint16_t s_list[CTAS];
   __shared__ int s_count[kAWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const AttendInfo* info = reinterpret_cast<const AttendInfo*>(p.ws);
-  const float* ml = reinterpret_cast<const float*>(p.ws + kAInfoBytes);
-  const float* os = reinterpret_cast<const float*>(p.ws + kAInfoBytes + kMlBytes);
+  const float* ml = reinterpret_cast<const float*>(p.ws + kInfoBytes);
+  const float* os = reinterpret_cast<const float*>(p.ws + kInfoBytes + kMlBytes);
   int count = 0;
   const bool direct = gridDim.y > 1 || p.rows == 1;
   if (direct && info[blockIdx.x + 1].tiles == 0) return;

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   using T = __nv_bfloat16;
   constexpr int NR = tensor_rows(RR), MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
-  constexpr size_t kMlBytes = attend_ml_bytes(RR);
+  constexpr size_t kInfoBytes = attend_info_bytes(PER_SM * kASms), kMlBytes = attend_ml_bytes(RR, PER_SM * kASms);
   // Values are turned before a step's weights are made, unless the scores, kept meanwhile, take too many registers: 8
   // requests of 4096 to 32768 tokens, 16 rows 52 us (after 58), 64 rows 120 (125); 32 rows 77 (75).
   constexpr bool kValuesFirst = RR != 32;
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     // The item's part in the workspace: its sums, each element of a head its thread's.  (An item that is all this CTA's
     // has the place of the one that the next CTA goes on with, which is the CTA's last.)
     auto part = [&] { return static_cast<size_t>(t0 > 0 ? 2 * c : 2 * c + 1); };
-    auto sums_at = [&] { return reinterpret_cast<float*>(p.ws + kAInfoBytes + kMlBytes) + part() * RR * DP + tid; };
+    auto sums_at = [&] { return reinterpret_cast<float*>(p.ws + kInfoBytes + kMlBytes) + part() * RR * DP + tid; };
     fence_to_async();
     turn_keys();
     keys_turned(t0);
@@ -639,7 +639,7 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
     }
     const bool nans = __syncthreads_or(bad_values);
     const bool all = t0 == 0 && t1 == n_tiles;
-    float* ws_ml = reinterpret_cast<float*>(p.ws + kAInfoBytes) + part() * RR * 2;
+    float* ws_ml = reinterpret_cast<float*>(p.ws + kInfoBytes) + part() * RR * 2;
     float* const ws_o = sums_at();
     // a row's sum, and what its values are taken times
     if (tid < rows) {

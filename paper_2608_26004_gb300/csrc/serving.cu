@@ -254,7 +254,7 @@ size_t asymspec_cache_attend_workspace_bytes(int B, int Q, int heads, int kv_hea
     return 0;
   const int rows = Q * (heads / kv_heads);
   const AttendKernels a = attend_kernels_bf16(head_dim, rows), b = attend_kernels_f32(head_dim, rows);
-  return std::max(attend_ws_bytes(a.rows, a.DP), attend_ws_bytes(b.rows, b.DP));
+  return std::max(attend_ws_bytes(a.rows, a.DP, a.most_ctas), attend_ws_bytes(b.rows, b.DP, b.most_ctas));
 }
 
 int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int64_t* q_strides,

@@ -144,6 +144,24 @@ def test_workspace_bytes(lib):
     assert sizes == sorted(sizes) and sizes[0] > 0                       # one for more queries serves fewer
 
 
+def test_workspaces_have_room_for_the_ctas_that_there_are(lib):
+    """32 bytes a CTA, and for two parts of each a row's 2 numbers and its values: 456 CTAs for attention over the
+    16-bit and 32-bit cache, whose callers may have laid out that; over the 4-bit one as many as its kernels have."""
+    def nbytes(ctas, rows, D):
+        whole = lambda n: -(-n // 256) * 256  # noqa: E731
+        return whole(32 * ctas) + whole(2 * ctas * rows * 2 * 4) + 2 * ctas * rows * D * 4
+
+    f, g = S.cache_attend_workspace_bytes, S.cache4_attend_workspace_bytes
+    assert f(8, 8, 64, 8, 128) == nbytes(456, 64, 128) == 30365952
+    assert f(64, 1, 32, 8, 128) == nbytes(456, 16, 128) and f(1, 4, 32, 8, 64) == nbytes(456, 16, 64)
+    assert g(64, 1, 32, 8, 128) == nbytes(608, 8, 128)
+    assert g(8, 8, 64, 8, 128) == nbytes(304, 64, 128)
+    assert g(8, 8, 64, 8, 256) == max(nbytes(152, 64, 256), nbytes(304, 32, 256))  # (for up to 64 rows, or up to 32)
+    for D in (32, 64, 96, 128, 160, 256):
+        sizes = [g(4, Q, 8, 8, D) for Q in range(1, 200)]
+        assert sizes == sorted(sizes)                                    # one for more queries serves fewer
+
+
 # ---------------------------------------------------------------- the binding
 
 torch = pytest.importorskip("torch")
