@@ -85,6 +85,7 @@ _CACHE4 = struct.Struct("@4P12q4iff")
 _STRIDES2, _STRIDES3 = struct.Struct("@2q"), struct.Struct("@3q")
 
 torch = None  # imported with the first call: the addresses' side needs no PyTorch
+_Turned = None  # what autograd keeps of a Rotary call, likewise
 
 
 _lib = None
@@ -167,11 +168,33 @@ _DTYPES = {}
 
 def _begin():
     """The library and PyTorch, at the first call on tensors."""
-    global torch
+    global torch, _Turned
     import torch as t
     lib()
     _DTYPES.update({t.float32: FP32, t.bfloat16: BF16})
     torch = t
+
+    class Turned(t.autograd.Function):
+        @staticmethod
+        def forward(ctx, rotary, transpose, positions, q, k):
+            ctx.rotary, ctx.transpose = rotary, transpose
+            ctx.save_for_backward(positions)
+            ctx.set_materialize_grads(False)
+            return rotary._turn(q, positions, k, transpose, None, None)
+
+        @staticmethod
+        def backward(ctx, q_grad, k_grad):
+            positions, = ctx.saved_tensors
+            # (a sum's gradient is one number for all elements)
+            given = [g if g is None or g.stride(-1) == 1 else g.contiguous() for g in (q_grad, k_grad)]
+            turned = [None, None]
+            if given[0] is not None:
+                turned = ctx.rotary(given[0], positions, given[1], transpose=not ctx.transpose)
+            elif given[1] is not None:
+                turned[1], _ = ctx.rotary(given[1], positions, transpose=not ctx.transpose)
+            return None, None, None, *turned
+
+    _Turned = Turned
 
 
 def _dtype(x) -> int:
@@ -473,7 +496,8 @@ class Rotary:
     bfloat16, any strides with contiguous heads, by positions [T] int32 (negative: a token that stays
     as it is), and returns (q, k) in new tensors or in q_out, k_out, which may be q and k themselves or
     must not overlap them.  transpose: by the opposite angle (times the same magnitude): the gradient of
-    q and k from the gradients of the results.
+    q and k from the gradients of the results.  Where q or k requires a gradient, autograd takes that as its
+    backward pass; such a call has no q_out or k_out.
     """
 
     def __init__(self, head_dim: int, *, rotary_dim=None, base: float = 10000.0, interleaved: bool = False,
@@ -507,6 +531,15 @@ class Rotary:
         return _HEADS.pack(x.data_ptr(), out.data_ptr(), s0, s1, o0, o1, shape[1]), out
 
     def __call__(self, q, positions, k=None, *, transpose=False, q_out=None, k_out=None):
+        if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)
+                                        or (q_out is not None and q_out.requires_grad)
+                                        or (k_out is not None and k_out.requires_grad)):
+            if q_out is not None or k_out is not None:
+                raise ValueError("q_out and k_out are for calls without gradients")
+            return _Turned.apply(self, bool(transpose), positions, q, k)
+        return self._turn(q, positions, k, transpose, q_out, k_out)
+
+    def _turn(self, q, positions, k, transpose, q_out, k_out):
         dev, kind = q.get_device(), q.dtype
         if dev != self.device_index:
             raise ValueError("q must be on the frequencies' device")

@@ -291,3 +291,22 @@ def test_refusals_of_the_binding(library):
         with pytest.raises(ValueError):
             rotary_(**bad)
     assert not library.calls
+
+
+def test_rotary_of_tensors_that_require_a_gradient(library):
+    """Results that autograd knows, or a refusal; without gradients as ever."""
+    turn = S.Rotary.__new__(S.Rotary)
+    turn.head_dim, turn.rotary_dim, turn.interleaved, turn.magnitude = 64, 32, False, 1.0
+    turn.steps, turn.device_index = placed(16, dtype=torch.int64), 0
+    q, k, pos = placed(4, 2, 64), placed(4, 1, 64), placed(4, dtype=torch.int32)
+    q.requires_grad_()
+    for out in (turn(q, pos)[0], *turn(q, pos, k), *turn(k, pos, q)):
+        assert out.requires_grad and out.grad_fn is not None
+    for more in (dict(q_out=placed(4, 2, 64)), dict(k=k, k_out=placed(4, 1, 64)), dict(q_out=q)):
+        n = len(library.calls)
+        with pytest.raises(ValueError, match="without gradients"):
+            turn(q, pos, **more)
+        assert len(library.calls) == n
+    with torch.no_grad():
+        assert not turn(q, pos, q_out=placed(4, 2, 64))[0].requires_grad
+    assert turn(k, pos)[0].grad_fn is None

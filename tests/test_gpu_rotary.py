@@ -161,6 +161,76 @@ def test_gradient(torch):
                 assert abs(slope - float(got[t, head, d])) <= 2.0 ** -20 * size
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_autograd(torch, dtype, transpose):
+    """Autograd's gradients are the other direction's results, bit for bit: of both, of one alone, of one number for
+    all elements, of the gradient itself, and in a graph."""
+    T, h, hk, D = 37, 6, 2, 96
+    kind = getattr(torch, dtype)
+    q, k, p = inputs(torch, T, h, hk, D, dtype, 21)
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    gq, gk = (torch.randn(x.shape, device="cuda", generator=gen).to(kind) for x in (q, k))
+    rotary = S.Rotary(D, rotary_dim=64, scaling=dict(kind="ramp", factor=4.0, original_length=64, fast=4.0, slow=0.5))
+    plain = rotary(q, p, k, transpose=transpose)
+    want = rotary(gq, p, gk, transpose=not transpose)
+    a, b = q.clone().requires_grad_(), k.clone().requires_grad_()
+    y, z = rotary(a, p, b, transpose=transpose)
+    assert torch.equal(y, plain[0]) and torch.equal(z, plain[1])
+    got = torch.autograd.grad((y, z), (a, b), (gq, gk), retain_graph=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(torch.autograd.grad(z, b, gk, retain_graph=True)[0], want[1])
+    assert torch.equal(torch.autograd.grad(y, a, gq, retain_graph=True)[0], want[0])
+    one, = torch.autograd.grad(y.sum(), a)
+    assert torch.equal(one, rotary(torch.ones_like(q), p, transpose=not transpose)[0])
+    y, none = rotary(a, p, transpose=transpose)
+    assert none is None and torch.equal(torch.autograd.grad(y, a, gq)[0], want[0])
+    y, z = rotary(a, p, k, transpose=transpose)          # k needs none
+    assert torch.equal(torch.autograd.grad((y, z), a, (gq, gk))[0], want[0])
+    # the gradient is linear in what it is given: its own gradient turns again
+    c = gq.clone().requires_grad_()
+    y, _ = rotary(a, p, transpose=transpose)
+    first, = torch.autograd.grad(y, a, c, create_graph=True)
+    assert torch.equal(torch.autograd.grad(first, c, q)[0], plain[0])
+    # through a projection, leaves accumulate
+    w = torch.randn(D, D, device="cuda", generator=gen).to(kind).requires_grad_()
+    (rotary((q @ w).contiguous(), p, transpose=transpose)[0] * gq).sum().backward()
+    back = (q.flatten(0, 1).mT.double() @ want[0].flatten(0, 1).double())
+    size = q.flatten(0, 1).mT.double().abs() @ want[0].flatten(0, 1).double().abs()
+    # sums of T * h products, in 32 bits, and one rounding
+    assert ((w.grad.double() - back).abs() <= size * (T * h * 2.0 ** -24) + back.abs() * torch.finfo(kind).eps).all()
+    with torch.no_grad():
+        assert rotary(a, p)[0].grad_fn is None
+    with pytest.raises(ValueError):
+        rotary(a, p, q_out=torch.empty_like(q))
+    p2 = p.clone()
+    y, _ = rotary(a, p2, transpose=transpose)
+    p2.add_(1)                                          # what the backward pass needs has changed
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y, a, gq)
+
+
+def test_autograd_in_a_graph_and_on_a_stream(torch):
+    q, k, p = inputs(torch, 40, 8, 2, 128, "bfloat16", 23)
+    rotary = S.Rotary(128)
+    gq = torch.ones_like(q).mul_(0.5)
+    want, _ = rotary(gq, p, transpose=True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a = q.clone().requires_grad_()
+        got, = torch.autograd.grad(rotary(a, p)[0], a, gq)
+        s.synchronize()
+        assert torch.equal(got, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            got, = torch.autograd.grad(rotary(a, p)[0], a, gq)
+    p.add_(5)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, rotary(gq, p, transpose=True)[0])
+
+
 def test_there_and_back_and_moved(torch):
     """Turned by p and back is the input but for two results' roundings; turned by p, then by r, it is turned by
     p + r."""
