@@ -27,7 +27,8 @@ CUDA_HEADERS = [os.path.join(CSRC, f) for f in (
     "device_common.cuh", "kernel_generic.cuh", "kernel_tma.cuh", "kernel_row.cuh",
     "kernel_full.cuh", "kernel_xrow.cuh", "kernel_draft.cuh", "kernel_xvocab.cuh", "kernel_constrain.cuh",
     "kernel_cache.cuh", "kernel_attend.cuh", "kernel_rotary.cuh", "kernel_cache4.cuh",
-    "kernel_attend4.cuh", "kernel_attend4_tensor.cuh", "kernels.h", "host_common.h", "serving_host.h", "k_attend.h")]
+    "kernel_attend4.cuh", "kernel_attend4_tensor.cuh", "kernels.h", "host_common.h", "serving_host.h", "prepared.h",
+    "k_attend.h")]
 CUDA_LIB = os.path.join(HERE, "libasymspec.so")
 GENCODE = "arch=compute_103a,code=sm_103a"
 

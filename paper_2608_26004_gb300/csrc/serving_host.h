@@ -3,11 +3,11 @@
 
 #include <climits>
 #include <cstdint>
-#include <mutex>
 
 #include "asymspec_serving.h"
 #include "device_common.cuh"
 #include "host_common.h"
+#include "prepared.h"
 
 namespace asymspec_impl {
 
@@ -21,23 +21,14 @@ inline bool known_dtype(int dtype) { return dtype == ASYMSPEC_FP32 || dtype == A
 
 constexpr int kStaticSmem = 8192;  // what a kernel has beside its dynamic shared memory at most
 
-// Once per kernel and device: room for all the dynamic shared memory that it may ask for.
-struct Prepared {
-  const void* fn;
-  int device;
-};
-inline std::mutex g_mu;
-inline Prepared g_prepared[64];
-inline int g_prepared_count = 0;
+inline Prepared g_prepared;
 
+// Once per kernel and device: room for all the dynamic shared memory that it may ask for.
 inline cudaError_t prepare(const void* fn, int device, int smem) {
   if (smem <= 48 * 1024 - kStaticSmem) return cudaSuccess;
-  std::lock_guard<std::mutex> lock(g_mu);
-  for (int i = 0; i < g_prepared_count; ++i)
-    if (g_prepared[i].fn == fn && g_prepared[i].device == device) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - kStaticSmem);
-  if (e == cudaSuccess && g_prepared_count < 64) g_prepared[g_prepared_count++] = {fn, device};
-  return e;
+  return static_cast<cudaError_t>(g_prepared.once(fn, device, [fn] {
+    return static_cast<int>(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - kStaticSmem));
+  }));
 }
 
 // For numbers k below 2^30 and n <= 2^s, d = ceil(2^(31 + s) / n) gives k / n = k * d >> (31 + s): d n is less than n
