@@ -18,10 +18,9 @@ namespace {
 
 using namespace asymspec_impl;
 
-// CTAs of a write at most, the five that an SM has room for, and of a read: 16384 tokens written and read of 8 heads of
-// 128 bf16 31.9 us with 760, 32.8 with twice that (four an SM: 32.9 with 608, 34.1 with 1216); 100,003
-// tokens read 112 with 1216, 98 with a token's threads to each (and no fewer with a slot looked up a token ahead, 114).
-constexpr int kWriteCtas = 760;
+// CTAs of a read at most: 100,003 tokens 98 us with a token's threads to each, 112 with 1216 (and no fewer with a
+// slot looked up a token ahead, 114).  A write takes what an SM has room for on each of 152: 16384 tokens written and
+// read of 8 heads of 128 bf16 31.9 us with 760, 32.8 with twice that.
 constexpr int kReadCtas = 1 << 20;
 
 AttendKernels attend4_kernels(int dtype, int D, int rows, bool fast) {
@@ -47,6 +46,12 @@ int check_cache4(const asymspec_cache4* c) {
     return ASYMSPEC_ERR_MISALIGNED;
   if (static_cast<int64_t>(c->num_blocks) * c->block_size > kMax32 || c->kv_heads > 65536) return ASYMSPEC_ERR_TOO_LARGE;
   return ASYMSPEC_OK;
+}
+
+template <typename T, bool WIDE>
+const void* write_pick(int* most_ctas) {
+  *most_ctas = cache4_write_ctas<T, WIDE>() * kASms;
+  return reinterpret_cast<const void*>(&cache4_write_kernel<T, WIDE>);
 }
 
 // What a write and a read have in common.
@@ -89,18 +94,18 @@ int move(const asymspec_cache4* c, const void* k, const void* v, int dtype, cons
   p.err = err;
   using B = __nv_bfloat16;
   const void* fn;
+  int most = kReadCtas;
   if (read)
     fn = elt == 4 ? (wide ? reinterpret_cast<const void*>(&cache4_read_kernel<float, true>)
                           : reinterpret_cast<const void*>(&cache4_read_kernel<float, false>))
                   : (wide ? reinterpret_cast<const void*>(&cache4_read_kernel<B, true>)
                           : reinterpret_cast<const void*>(&cache4_read_kernel<B, false>));
+  else if (elt == 4)
+    fn = wide ? write_pick<float, true>(&most) : write_pick<float, false>(&most);
   else
-    fn = elt == 4 ? (wide ? reinterpret_cast<const void*>(&cache4_write_kernel<float, true>)
-                          : reinterpret_cast<const void*>(&cache4_write_kernel<float, false>))
-                  : (wide ? reinterpret_cast<const void*>(&cache4_write_kernel<B, true>)
-                          : reinterpret_cast<const void*>(&cache4_write_kernel<B, false>));
+    fn = wide ? write_pick<B, true>(&most) : write_pick<B, false>(&most);
   const int64_t ctas = (static_cast<int64_t>(T) + (k4Threads >> p.log_lanes) - 1) / (k4Threads >> p.log_lanes);
-  return launch(fn, dim3(static_cast<unsigned>(std::min<int64_t>(ctas, read ? kReadCtas : kWriteCtas))), dim3(k4Threads), 0, &p, stream);
+  return launch(fn, dim3(static_cast<unsigned>(std::min<int64_t>(ctas, most))), dim3(k4Threads), 0, &p, stream);
 }
 
 }  // namespace

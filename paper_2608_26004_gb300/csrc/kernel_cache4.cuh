@@ -82,8 +82,14 @@ __device__ __forceinline__ void store_wide(void* p, const unsigned (&r)[8]) {
 // Copies, bound by their bytes: a thread takes 32 elements with two scales, neighbours those of a head, then
 // of the token's heads, then of its values.  WIDE: the elements lie on 32-byte boundaries.  16384 tokens of 8 heads of
 // 128 bf16 written and read 32 us (a thread per 16 elements, 64-bit divisions: 46), the bytes 25; 100,003 read 98 = 5.4 TB/s.
+// A write has five CTAs an SM where 48 registers hold 32 elements, as vectors of bf16, else four.  us of 16384 tokens
+// written, with five and with four: fp32 32.0 and 30.8 (the bytes 22.6), off the boundaries bf16 65.7 and 62.8, fp32 121
+// and 118 (with five 28 to 32 bytes a thread are spilled); vectors of bf16 18.4 with five.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(k4Threads, 5) cache4_write_kernel(const __grid_constant__ Cache4Params p) {
+constexpr int cache4_write_ctas() { return sizeof(T) == 2 && WIDE ? 5 : 4; }
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(k4Threads, (cache4_write_ctas<T, WIDE>())) cache4_write_kernel(const __grid_constant__ Cache4Params p) {
   const unsigned slots = static_cast<unsigned>(p.num_blocks) * static_cast<unsigned>(p.block_size);
   const int lanes = 1 << p.log_lanes, lane = threadIdx.x & (lanes - 1);
   const int64_t stride = static_cast<int64_t>(gridDim.x) * (k4Threads >> p.log_lanes);
