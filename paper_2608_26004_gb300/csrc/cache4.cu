@@ -24,7 +24,7 @@ using namespace asymspec_impl;
 constexpr int kReadCtas = 1 << 20;
 
 AttendKernels attend4_kernels(int dtype, int D, int rows, bool fast) {
-  return dtype == ASYMSPEC_FP32 ? attend4_kernels_f32(D, rows, fast) : attend4_kernels_bf16(D, rows, fast);
+  return dtype == ASYMSPEC_FP32 ? attend4_kernels_f32(D, rows) : attend4_kernels_bf16(D, rows, fast);
 }
 
 int check_cache4(const asymspec_cache4* c) {
@@ -133,7 +133,7 @@ size_t asymspec_cache4_attend_workspace_bytes(int B, int Q, int heads, int kv_he
   const int rows = Q * (heads / kv_heads);
   for (const int r : {rows, 32, 16, 8}) {
     if (r > rows) continue;
-    for (const AttendKernels& k : {attend4_kernels_bf16(head_dim, r, true), attend4_kernels_f32(head_dim, r, true)})
+    for (const AttendKernels& k : {attend4_kernels_bf16(head_dim, r, true), attend4_kernels_f32(head_dim, r)})
       most = std::max(most, attend_ws_bytes(k.rows, k.DP, k.most_ctas));
   }
   return most;

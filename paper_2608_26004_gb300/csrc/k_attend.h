@@ -24,9 +24,9 @@ struct AttendKernels {
 // k_attend_f32.cu).
 AttendKernels attend_kernels_bf16(int D, int rows);
 AttendKernels attend_kernels_f32(int D, int rows);
-// The same over a cache in 4 bits (k_attend4_bf16.cu, k_attend4_f32.cu); fast: a token's codes and scales of a
-// head lie on boundaries of 32 and of DP / 16 bytes, and D is DP.
+// The same over a cache in 4 bits (k_attend4_bf16.cu, k_attend4_f32.cu: one kernel for all boundaries); fast: a
+// token's codes and scales of a head lie on boundaries of 32 and of DP / 16 bytes, and D is DP.
 AttendKernels attend4_kernels_bf16(int D, int rows, bool fast);
-AttendKernels attend4_kernels_f32(int D, int rows, bool fast);
+AttendKernels attend4_kernels_f32(int D, int rows);
 
 }  // namespace asymspec_impl

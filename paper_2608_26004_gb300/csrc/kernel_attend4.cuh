@@ -107,10 +107,9 @@ __device__ __forceinline__ void load_words(const unsigned char* p, unsigned (&w)
 // Bound by latency at few CTAs: 32 requests of 5 queries, a window of 2000, 8 heads of 64 25 us (bf16 keys and
 // values, attend_split: 39 in fp32), 3.4 of them the bytes; 64 requests of 64 to 8192 tokens, 32 heads on 8 of 128 70.
 // NT: tiles of 8 rows of a warp.
-template <typename T, int DP, int NT, int WR, int ST, int PER_SM>
+template <int DP, int NT, int WR, int ST, int PER_SM>
 __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(const __grid_constant__ Attend4Params P) {
-  constexpr bool BF = sizeof(T) == 2;
-  constexpr int kPieces = BF ? 1 : 2;
+  constexpr int kPieces = 2;
   constexpr int kThreadsN = kAGroups * WR * 32, kWarpsN = kAGroups * WR;
   constexpr int kWarpRows = 8 * NT, kRows = kWarpRows * WR;
   constexpr int kKeyRow = DP / 2, kValueRow = DP / 2 + 16, kScaleRow = DP / 16;
@@ -125,7 +124,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
   constexpr int kLoads = kASubs * kAKeys > kLaneRows ? kASubs * kAKeys / kLaneRows : 1;
   constexpr int U = NT == 1 ? kASubs : 1;          // sixteens of keys that are worked at together
   constexpr size_t kInfoBytes = attend_info_bytes(PER_SM * kASms), kMlBytes = attend_ml_bytes(kRows, PER_SM * kASms);
-  constexpr float kBelow = BF ? 7.f : 12.f, kSlack = 15.f - kBelow;
+  constexpr float kBelow = 12.f, kSlack = 15.f - kBelow;
   constexpr bool kQRegs = kPieces * NT * KW * 4 <= 32;
   static_assert(ST >= 2 && kStep % 16 == 0 && kGroup % 16 == 0, "the ring");
   extern __shared__ __align__(1024) unsigned char a_smem[];
@@ -313,13 +312,13 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
     // element is taken times 2^11, or fp16's smallest step would show in those below 2^-16 of the largest
     for (int r = warp; r < kRows; r += kWarpsN) {
       const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
-      const T* src = static_cast<const T*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
+      const float* src = static_cast<const float*>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
       float x[DP / 32];
       unsigned most = 0;
 #pragma unroll
       for (int k = 0; k < DP / 32; ++k) {
         const int d = lane + 32 * k;
-        x[k] = r < rows && d < p.D ? to_f32(src[d]) : 0.f;
+        x[k] = r < rows && d < p.D ? src[d] : 0.f;
         most = max(most, __float_as_uint(x[k]) & 0x7FFFFFFFu);
       }
       const unsigned e = min(max(__reduce_max_sync(~0u, most) >> 23, 14u), 254u);
@@ -330,7 +329,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
         const float y = x[k] * up;
         const __half hi = __float2half_rn(y);
         to[lane + 32 * k] = hi;
-        if constexpr (!BF) to[kRows * kQPitch / 2 + lane + 32 * k] = __float2half_rn((y - __half2float(hi)) * 0x1p11f);
+        to[kRows * kQPitch / 2 + lane + 32 * k] = __float2half_rn((y - __half2float(hi)) * 0x1p11f);
       }
       if (lane == 0) s_factor[r] = p.scale2 * __uint_as_float((e - 13u) << 23);
     }
@@ -420,15 +419,14 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
               }
             }
           }
-          float more[BF ? 1 : U][NT][4], small[BF ? 1 : U][NT][4];
+          float more[U][NT][4], small[U][NT][4];
 #pragma unroll
           for (int y = 0; y < U; ++y)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                S[y][n][e] = 0.f;
-                if constexpr (!BF) more[y][n][e] = small[y][n][e] = 0.f;
+                S[y][n][e] = more[y][n][e] = small[y][n][e] = 0.f;
               }
 #pragma unroll
           for (int w = 0; w < KW; ++w)
@@ -452,30 +450,24 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
                   query(0, n, w, x);
                 }
                 mma_f16(S[y][n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
-                if constexpr (BF) {
-                  mma_f16(S[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
-                } else {
-                  // (the matrix unit's running sums are cut, not rounded: short ones, added up in fp32)
-                  mma_f16(more[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
-                  if constexpr (kQRegs) {
+                // (the matrix unit's running sums are cut, not rounded: short ones, added up in fp32)
+                mma_f16(more[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                if constexpr (kQRegs) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = qf[kPieces - 1][n][w][i];
-                  } else {
-                    query(1, n, w, x);
-                  }
-                  mma_f16(small[y][n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
-                  mma_f16(small[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
+                  for (int i = 0; i < 4; ++i) x[i] = qf[kPieces - 1][n][w][i];
+                } else {
+                  query(1, n, w, x);
                 }
+                mma_f16(small[y][n], fa[0], fb[0], fa[1], fb[1], x[0], x[1]);
+                mma_f16(small[y][n], fa[2], fb[2], fa[3], fb[3], x[2], x[3]);
               }
             }
-          if constexpr (!BF) {
 #pragma unroll
-            for (int y = 0; y < U; ++y)
+          for (int y = 0; y < U; ++y)
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[y][n][e] += fmaf(small[y][n][e], 0x1p-11f, more[y][n][e]);
-          }
+              for (int e = 0; e < 4; ++e) S[y][n][e] += fmaf(small[y][n][e], 0x1p-11f, more[y][n][e]);
         }
         bool whole = k0 + (U - 1) * kATile + kAKeys - 1 <= least && k0 >= from;
 #pragma unroll
@@ -483,7 +475,7 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
         // Weights are 2^(s - m), m kBelow below the largest score at the time; only a score kSlack above
         // that raises it (the maximum itself, kept, would rescale the values at most steps, for one
         // of the rows or another).  So weights stay below 2^15, and fp16, whose step is 2^-24 at the
-        // smallest, holds one of 2^-31 (fp32: 2^-36) of a row's largest.
+        // smallest, holds one of 2^-36 of a row's largest.
         bool above = false;
         float top[NT][2];
 #pragma unroll
@@ -546,10 +538,8 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
             for (int k = 0; k < 2; ++k) {
               const unsigned hi = pack_f16(S[y][n][2 * k], S[y][n][2 * k + 1]);
               wt[y][0][n][k] = transposed(hi);
-              if constexpr (!BF) {
-                const float2 x = f16x2_to_f32(hi);
-                wt[y][kPieces - 1][n][k] = transposed(pack_f16(S[y][n][2 * k] - x.x, S[y][n][2 * k + 1] - x.y));
-              }
+              const float2 x = f16x2_to_f32(hi);
+              wt[y][kPieces - 1][n][k] = transposed(pack_f16(S[y][n][2 * k] - x.x, S[y][n][2 * k + 1] - x.y));
             }
         }
         // values: of keys 2 t4, 2 t4 + 1 and those + 8, the lane's DP / 8 elements in a row from g * DP / 8
@@ -599,16 +589,12 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                if constexpr (BF) {
-                  mma_f16(O[n][4 * w + i], f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][0][n][0], wt[y][0][n][1]);
-                } else {
-                  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][kPieces - 1][n][0],
-                          wt[y][kPieces - 1][n][1]);
-                  mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][0][n][0], wt[y][0][n][1]);
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][kPieces - 1][n][0],
+                        wt[y][kPieces - 1][n][1]);
+                mma_f16(sum, f[0][0][i], f[0][1][i], f[1][0][i], f[1][1][i], wt[y][0][n][0], wt[y][0][n][1]);
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) O[n][4 * w + i][e] += sum[e];
-                }
+                for (int e = 0; e < 4; ++e) O[n][4 * w + i][e] += sum[e];
               }
           }
         }
@@ -665,14 +651,14 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int r = R + min(n * 8 + 2 * t4 + e, warp_rows - 1);
-            const T* qr = static_cast<const T*>(p.q) + b * p.qs[0] + r / p.group * p.qs[1] +
-                          (kh * p.group + r % p.group) * p.qs[2];
+            const float* qr = static_cast<const float*>(p.q) + b * p.qs[0] + r / p.group * p.qs[1] +
+                              (kh * p.group + r % p.group) * p.qs[2];
             float s = 0.f;
 #pragma unroll 1
             for (int d = 2 * g; d < p.D; d += 16) {
               const float2 x = pair(0, d);
-              s = fmaf(to_f32(qr[d]), x.x, s);
-              s = fmaf(to_f32(qr[d + 1]), x.y, s);
+              s = fmaf(qr[d], x.x, s);
+              s = fmaf(qr[d + 1], x.y, s);
             }
             s += __shfl_xor_sync(~0u, s, 4);
             s += __shfl_xor_sync(~0u, s, 8);
@@ -746,17 +732,13 @@ __global__ void __launch_bounds__(kAGroups * WR * 32, PER_SM) attend4_split(cons
       if (all) {
         const float inv = L == 0.f ? 0.f : 1.f / L;
         const int i = (R0 + r) / p.group, h = kh * p.group + (R0 + r) % p.group;
-        T* out = static_cast<T*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
+        float* out = static_cast<float*>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2] + d;
         if (d < p.D) {  // (D is a multiple of 4)
-          __align__(16) T y[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) put(y + k, x[k] * inv);
           if (p.out_vec) {
-            if constexpr (BF) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
-            else *reinterpret_cast<float4*>(out) = *reinterpret_cast<const float4*>(y);
+            *reinterpret_cast<float4*>(out) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
           } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) out[k] = y[k];
+            for (int k = 0; k < 4; ++k) out[k] = x[k] * inv;
           }
         }
         if (d == 0 && p.lse)
