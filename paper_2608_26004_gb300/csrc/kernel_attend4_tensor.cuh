@@ -169,9 +169,6 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
   constexpr int NR = tensor_rows(RR), MB = tensor_blocks(DP), kCols = tensor_columns(DP, NR);
   constexpr int CW = DP / 8, SW = DP / 64;  // words of a key's codes, and of its scales
   constexpr size_t kInfoBytes = attend_info_bytes(PER_SM * kASms), kMlBytes = attend_ml_bytes(RR, PER_SM * kASms);
-  // Values are turned before a step's weights are made, unless the scores, kept meanwhile, take too many registers: 8
-  // requests of 4096 to 32768 tokens, 16 rows 52 us (after 58), 64 rows 120 (125); 32 rows 77 (75).
-  constexpr bool kValuesFirst = RR != 32;
   constexpr float kBelow = 7.f, kSlack = 8.f, kGuess = -7.f, kLow = 7.f;
   extern __shared__ __align__(1024) unsigned char a_smem[];
   const AttendParams& p = P.a;
@@ -466,33 +463,32 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
       tmem_wait_load();
       if (t + 1 < t1) keys_turned(t + 1);
       if (t > t0) wait(1, parity_o);  // (O of the step before: its weights and values have been read)
-      auto turn_values = [&] {
-        // Values.  A NaN is left out of the products, where a weight of zero would make it one in rows that do not
-        // see it.
+      // Values, while the scores wait in registers (after the weights, us of 8 requests of 4096 to 32768 tokens, 64 heads
+      // on 8 or fewer: heads of 128 at 8, 16, 32 and 64 rows 42.5, 52.6, 73.9, 124 as it is and 44.2, 54.6, 76.8, 129
+      // after; of 64 33.7, 45.8, 68.6, 110 and 36.2, 45.6, 71.3, 114; of 256 82.8, 88.3, 113, 241 and 83.7, 97.1, 119,
+      // 239).  A NaN is left out of the products, where a weight of zero would make it one in rows that do not see it.
 #pragma unroll
-        for (int i = 0; i < SW; ++i) {
-          vs[i] = live ? vs[i] : 0u;
-          const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-          if (nan) {
-            vs[i] &= ~((nan >> 7) * 0xFFu);
-            bad_values = true;
-          }
+      for (int i = 0; i < SW; ++i) {
+        vs[i] = live ? vs[i] : 0u;
+        const unsigned nan = ((vs[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        if (nan) {
+          vs[i] &= ~((nan >> 7) * 0xFFu);
+          bad_values = true;
         }
+      }
 #pragma unroll
-        for (int w = 0; w < CW; ++w) {
-          const unsigned s2 = e4m3_to_f16(vs[w / 8] >> (w % 8 >= 4 ? 16 : 0));
-          const unsigned s = __byte_perm(s2, s2, w % 4 < 2 ? 0x1010 : 0x3232);
-          unsigned x[4];
-          e2m1_to_f16(vc[w], x);
+      for (int w = 0; w < CW; ++w) {
+        const unsigned s2 = e4m3_to_f16(vs[w / 8] >> (w % 8 >= 4 ? 16 : 0));
+        const unsigned s = __byte_perm(s2, s2, w % 4 < 2 ? 0x1010 : 0x3232);
+        unsigned x[4];
+        e2m1_to_f16(vc[w], x);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
-          *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
-        }
-        if (t + 1 < t1) load(1, page_v, at_v, vc, vs);
-      };
-      if constexpr (kValuesFirst) {
-        turn_values();
-        if (t + 1 < t1) start_scores(t + 1);
+        for (int k = 0; k < 4; ++k) x[k] = mul_f16x2(x[k], s);
+        *reinterpret_cast<uint4*>(v_row + (w / 8) * 16384 + (((w % 8) * 16) ^ swizzle)) = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      if (t + 1 < t1) {
+        load(1, page_v, at_v, vc, vs);
+        start_scores(t + 1);
       }
       // scores less their references
       auto less = [&] {
@@ -603,10 +599,6 @@ __global__ void __launch_bounds__(kTThreads, PER_SM) attend4_tensor(const __grid
         }
         // (a key a row, as the values: one store for 8 queries; a query a row took 16-bit stores, 261 us for 249)
         *reinterpret_cast<uint4*>(p_row + ((n / 8) ^ p_turn) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-      if constexpr (!kValuesFirst) {
-        if (t + 1 < t1) start_scores(t + 1);
-        turn_values();
       }
       fence_to_async();
       tensor_fence_before();
