@@ -490,6 +490,57 @@ def test_sums_over_a_million_keys(torch, heads, D):
     assert ((lse.double() - math.log(n)).abs() <= 2.0 ** -20 * 15).all()
 
 
+@pytest.mark.parametrize("Q,heads,D", [(1, 8, 64), (8, 8, 128), (3, 4, 256)])
+def test_references_that_rise_after_sums_were_put_by(torch, Q, heads, D):
+    """Items of 157 steps in a CTA's hands whose scores rise all the way, slowly or by what raises a reference at most
+    steps; and a NaN in a value that the last of them see, which makes those elements NaN and nothing else."""
+    n, B = 20000, 400
+    q, cache, tables, _ = inputs(torch, [n], Q, heads, 2, D, "bfloat16", 16, 53)
+    slots = (tables[0, :n // 16].long()[:, None] * 16 + torch.arange(16, device="cuda")).flatten()
+    k = torch.zeros(n, 2, D, device="cuda")
+    k[..., 0] = torch.linspace(0, 6, n, device="cuda")[:, None]
+    k[..., 1] = 6.0 * (torch.arange(n, device="cuda") % 3000 == 2999)[:, None]
+    g = torch.Generator(device="cuda").manual_seed(54)
+    S.cache4_write(k, torch.randn(n, 2, D, device="cuda", generator=g), cache, slots)
+    attend = S.Cache4Attend(B, Q, heads, 2, D)
+    tables, lens = tables.repeat(B, 1), torch.full((B,), n, device="cuda", dtype=torch.int32)
+    for first, second in ((0.1, 0.0), (4.0, 0.0), (20.0, 2.0), (-3.0, 5.0)):
+        y = torch.zeros_like(q)
+        y[..., 0], y[..., 1] = first, second
+        x = (y.repeat(B, 1, 1, 1), cache, tables, lens)
+        out, lse = attend(*x, scale=1.0)
+        check(torch, x, out, lse, [(0, 0, 0), (B // 2, Q - 1, heads - 1), (B - 1, Q // 2, 1)], scale=1.0)
+    page = int(tables[0, (n - 1) // 16])
+    cache.value_scales[page, (n - 1) % 16, 0, 1] = 0x7F
+    bad, lse2 = attend(*x, scale=1.0)
+    want = torch.zeros_like(bad, dtype=torch.bool)
+    want[:, Q - 1, :heads // 2, 16:32] = True
+    assert torch.equal(bad.isnan(), want) and torch.equal(lse, lse2)
+    assert torch.equal(bad[~want], out[~want])
+
+
+def test_calls_at_once_on_two_streams(torch):
+    """Attention of other tiles at the same time, a workspace each: their CTAs meet on the SMs and share tensor
+    memory."""
+    calls = []
+    for i, (lens, Q, heads, kv, D) in enumerate((([9000] * 12, 1, 32, 8, 128), ([7000, 30] * 8, 8, 32, 8, 128),
+                                                 ([5000] * 20, 8, 8, 1, 256), ([3000] * 40, 4, 16, 4, 64))):
+        x = inputs(torch, lens, Q, heads, kv, D, "bfloat16", 16, 60 + i)
+        calls.append((S.Cache4Attend(len(lens), Q, heads, kv, D), x))
+    want = [attend(*x) for attend, x in calls]
+    torch.cuda.synchronize()
+    streams, got, errs = [torch.cuda.Stream() for _ in calls], [[] for _ in calls], []
+    for _ in range(6):
+        for i, (s, (attend, x)) in enumerate(zip(streams, calls)):
+            with torch.cuda.stream(s):
+                errs.append(torch.zeros(1, device="cuda", dtype=torch.int32))
+                got[i].append(attend(*x, error_word=errs[-1]))
+    torch.cuda.synchronize()
+    assert not any(int(e) for e in errs)
+    for (out, lse), each in zip(want, got):
+        assert all(torch.equal(a, out) and torch.equal(b, lse) for a, b in each)
+
+
 def test_refusals_of_the_binding(torch):
     q, cache, tables, lens = inputs(torch, [100, 60], 2, 4, 2, 64, "bfloat16", 16, 4)
     attend = S.Cache4Attend(2, 2, 4, 2, 64)
