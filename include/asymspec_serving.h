@@ -235,8 +235,9 @@ int asymspec_cache_attend(const asymspec_cache* cache, const void* q, const int6
  * negative position (padding) stay what they are.
  *
  * Frequencies are given in turns: steps[i] is w_i / 2 pi of a turn a position, its fraction
- * as a 64-bit fixed-point number.  A position's phase is then a product of whole numbers, and
- * as exact at position 2^31 - 1 as at 1.  asymspec_rotary_steps fills rotary_dim / 2 of them on
+ * as a 64-bit fixed-point number.  A position's phase is then a product of whole numbers, exact modulo
+ * a turn; the step itself comes from a w_i of 53 bits, which is all that far positions lose: at 2^31 - 1 up to
+ * 2^-24 of a turn for pairs near one radian a position, at 10^6 2^-35.  asymspec_rotary_steps fills rotary_dim / 2 of them on
  * the host (the caller copies them to the device), from w_i = base^(-2 i / rotary_dim) under a
  * scaling (NULL or ASYMSPEC_ROTARY_NONE: as they are), or from `frequencies` (radians a position;
  * no scaling then, base is not read), and *out_magnitude:

@@ -18,8 +18,9 @@ AttendKernels tensor_pick(bool fast) {
 
 // Rows of an item: the products' columns come in sixteens, but a thread's scores and sums are registers, so up to
 // 8 rows have a kernel of their own.  CTAs an SM: as many as tensor memory and shared memory have room for (four
-// of 128 columns), three where 32 rows need more registers.  us with one CTA less: 64 requests of 64 to 8192
-// tokens, 4 rows 42.7 / 48.1 with three, 8 of 4096 to 32768, 16 rows 52 / 54.
+// of 128 columns), three where 32 rows need more registers.  us, and with one CTA less: 64 requests of 64 to 8192
+// tokens, 4 rows 44.4 / 47.3, heads of 64 36.2 / 39.5; 8 of 4096 to 32768, 16 rows 52.6 / 53.5, 32 rows 73.9 / 76.6 (with
+// four 94.7), 64 rows 124 / 160.
 AttendKernels attend4_kernels_bf16(int D, int rows, bool fast) {
   if (D <= 64)
     return rows <= 8    ? tensor_pick<64, 8, 4>(fast)

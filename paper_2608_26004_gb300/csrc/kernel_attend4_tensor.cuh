@@ -154,10 +154,10 @@ constexpr size_t tensor_smem_bytes(int DP, int NR) {
 // while they turn the next keys; codes come from memory a step ahead of that.  O stays in tensor memory, and is
 // touched only when a score rises far above its row's reference, and every 64 steps.  The weights are one fp16 piece,
 // 2^-11: an eighth of the output's own rounding to bf16; a second piece would double the second product and its stores.
-// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 257 us, the bytes 106, issue
-// 45 %, DRAM 47 %, the tensor core a quarter: nothing is full, a step's chain of dependent parts (keys turned, scores
+// What it takes, of 16 requests of 4096 to 131072 tokens with 32 rows a kv head (8 of 128): 247 us, the bytes 106, issue
+// 48 %, DRAM 48 %, the tensor core a quarter: nothing is full, a step's chain of dependent parts (keys turned, scores
 // read, references compared by all threads, weights, values turned) and its barriers are not hidden by the two other
-// CTAs of the SM.  64 requests of 64 to 8192 tokens, 4 rows: 43.6 us, the bytes 18; a step costs 0.55 us an SM (its bytes
+// CTAs of the SM.  64 requests of 64 to 8192 tokens, 4 rows: 44 us, the bytes 18; a step costs 0.55 us an SM (its bytes
 // 0.41), an item about three, the launch, the first loads and the join 13 us together.  The same products on the
 // warps' matrix instructions (as attend4_split's) took 449 and 56 us; with warps of their own for loading, weighing and
 // starting the products, one CTA less an SM or two, 482 and 60.
